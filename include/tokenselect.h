@@ -315,6 +315,69 @@ int32_t ts_chunk_soft_vote(const ts_problem* p, const void* q, const float* row_
  * problem.  q [device] [B][C][H][D] bf16; q_mean [device] [B][1][H][D] bf16.  fp32: TS_ERR_UNSUPPORTED. */
 int32_t ts_chunk_mean_query(const ts_problem* p, const void* q, void* q_mean, void* stream);
 
+/* ---- The cache itself: filling, attending and moving it.  New tokens are counted by seq_lens already, as a chunk's are:
+ * the n_b new tokens of sequence b are its last ones, logical tokens N_b - n_b .. N_b - 1.  They come as rows, packed one sequence after
+ * the other: q_indptr [device] int32 [B+1], ascending, says that rows q_indptr[b] .. q_indptr[b+1] - 1 belong to sequence b (n_b may
+ * be 0); NULL means chunk rows each, [B][C].  num_rows = q_indptr[B] (B * C with NULL) is known to the host; 0 is fine and launches
+ * nothing.  Entries of q_indptr are clamped into [0, num_rows].  p->chunk is an upper bound on n_b that the choice of a kernel goes
+ * by; a sequence with more is computed all the same. */
+
+/* Attention of the new tokens over their whole sequence (dense: no selection, no index list), both dtypes:
+ *   out[r][h][:] = sum_t softmax_t( <q[r][h], K[slot(b, t)][h/G]> * sm_scale ) * V[slot(b, t)][h/G]
+ * for new token c = r - q_indptr[b] at place x = N_b - n_b + c over t in [max(0, x - window + 1), x]; window 0 = from 0 on (every
+ * cached token and the chunk's own up to x).  Float accumulation, out rounded to p->dtype; bf16: where a sequence's rows
+ * n_b * G are more than 32, the weights that multiply V are rounded to bf16 (matrix-core operand; their sum is not).
+ * q, out [device] [num_rows][H][D], 16-byte aligned, not overlapping; lse [device] float [num_rows][H] or NULL.
+ * A row that sees no token (N_b < n_b: its place is negative) gets out = 0, lse = -inf.  Rows outside q_indptr[0] ..
+ * q_indptr[B] are left as they are.  num_initial / num_local do not matter: every token is attended.
+ * The work is cut into equal shares on the device, by the lengths themselves: max_seq_len may be a loose bound.  The same call gives
+ * the same bits; the order of the sums, and with it the last bits, depends on the other sequences of the batch.
+ * ws: ts_paged_attn_workspace_bytes() bytes, 256-byte aligned, contents irrelevant on entry and exit; one for num_rows, chunk, batch and max_seq_len
+ * serves every call with fewer or smaller ones and the same heads and dtype.  sm_scale finite, window >= 0. */
+int32_t ts_paged_attn_workspace_bytes(const ts_problem* p, int32_t num_rows, size_t* bytes);
+int32_t ts_paged_attn(const ts_problem* p, const void* q, const int32_t* q_indptr, int32_t num_rows, int32_t window,
+                      float sm_scale, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Rotary positions with one to four axes (a text's place; time, height and width of a video's patches), and the new
+ * tokens' K and V rows written into the pages: one launch.
+ * Pair i of a head (i < rotary_dim / 2) is the elements (i, i + rotary_dim / 2), or (2 i, 2 i + 1) with `adjacent`, and turns by
+ *   angle = positions[pair_axis[i]][r] * inv_freq[i]:   (x, y) -> scale * (x cos - y sin, x sin + y cos)
+ * (the angle and its reduction in double: any int32 position; sine, cosine and the products in float, rounded once to p->dtype).
+ * Elements from rotary_dim on pass through unchanged. */
+#define TS_ROPE_MAX_AXES 4
+typedef struct ts_rope {
+  const float* inv_freq;  /* [device] [rotary_dim / 2]                                                */
+  int32_t rotary_dim;     /* even, in [0, D]; 0 = nothing is turned                                   */
+  int32_t num_axes;       /* 1 .. TS_ROPE_MAX_AXES                                                    */
+  int32_t adjacent;       /* 0: halves, 1: neighbours                                                 */
+  float scale;            /* factor on cos and sin (1 for none)                                       */
+  uint8_t pair_axis[64];  /* axis of each pair, below num_axes (the first rotary_dim / 2 entries)     */
+} ts_rope;
+/* q [num_rows][H][D] -> q_out (packed); k, v [num_rows][H_kv][D] -> the slots of the new tokens in p->k_pool / p->v_pool, which are
+ * written (k turned, v as it is; v_pool must not be NULL).  All [device] in p->dtype, 16-byte aligned; rows q_stride, k_stride, v_stride elements
+ * apart (0 = packed; a multiple of 16 bytes, at least a row: parts of a fused projection's output).  q and q_out
+ * may be NULL together (append only), k and v too (turn only).  q_out may be q itself if q is packed; any other overlap is an error
+ * where the library can see it.  r NULL: nothing is turned.  positions [device] int32 [num_axes][num_rows], or NULL: on every
+ * axis a token's place N_b - n_b + c.  Rows that belong to no sequence, and rows whose place is negative or beyond max_seq_len, write nothing into the pages, and
+ * the former no q_out either.  Two sequences that share the page of a new token overwrite each other: give the second a page of its own first. */
+int32_t ts_rope_append(const ts_problem* p, const ts_rope* r, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                       const void* v, int64_t v_stride, const int32_t* q_indptr, int32_t num_rows, const int32_t* positions,
+                       void* q_out, void* stream);
+
+/* Copies pages: K and V (V only if v_pool is not NULL) of page src[i] to page dst[i], i < n.  src, dst [device] int32 [n]; a pair with a page outside
+ * [0, num_pages) is skipped (-1: padding).  No page may be in dst twice, or in both lists with different partners (the copies have no
+ * order among them).  Uses k_pool, v_pool, page_size, num_kv_heads, head_dim and dtype of p, pools 16-byte aligned.  n = 0 launches nothing. */
+int32_t ts_pages_copy(const ts_problem* p, const int32_t* src, const int32_t* dst, int32_t n, int32_t num_pages, void* stream);
+
+/* Cuts sequences down to what ts_sparse_paged_attn (decode) attends: tokens [0, lo_b), the count[b] tokens of idx[b], tokens
+ * [hi_b, N_b) (lo_b, hi_b of ts_problem) are copied in that order, one after the other, into the pages to_indices[to_indptr[b] ..
+ * to_indptr[b+1] - 1]; to_lens[b] = their number, or what the pages hold if that is less (the rest is dropped).  The pages of a table row are not read
+ * behind that number.  idx [device] int32 [B][idx_stride], count [device] int32 [B] as ts_topk leaves them (read as defensively as by
+ * ts_sparse_paged_attn); to_* [device]; skip[b] != 0 leaves a sequence alone, to_lens[b] too.  The new pages must not
+ * be pages that the call reads (of any sequence), nor belong to two sequences.  Keys keep the positions that they were turned by.  chunk must be 1. */
+int32_t ts_cache_compact(const ts_problem* p, const int32_t* idx, int32_t idx_stride, const int32_t* count, const uint8_t* skip,
+                         const int32_t* to_indptr, const int32_t* to_indices, int32_t* to_lens, void* stream);
+
 /* ======================================================================================================
  * Everything below is for benchmarks and tests, not for serving code: process-wide tuning knobs and timing
  * helpers.  They are not thread-safe and must not be changed while a call on another thread is between

@@ -42,6 +42,11 @@ class _CSelcache(ctypes.Structure):
                 ("first_next", ctypes.c_void_p), ("reuse", ctypes.c_void_p), ("theta", ctypes.c_float)]
 
 
+class _CRope(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("rotary_dim", ctypes.c_int32), ("num_axes", ctypes.c_int32),
+                ("adjacent", ctypes.c_int32), ("scale", ctypes.c_float), ("pair_axis", ctypes.c_uint8 * 64)]
+
+
 _lib = None
 
 
@@ -64,7 +69,7 @@ def load():
             raise FileNotFoundError("%s is missing: run `python -m paper_2411_02886_amd.build` (no CPU fallback exists)"
                                     % _LIB_PATH)
         L = ctypes.CDLL(_LIB_PATH)
-        vp, i32, f32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float, ctypes.c_size_t
+        vp, i32, i64, f32, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
         pp = ctypes.POINTER(_CProblem)
         L.ts_version.restype = i32
         L.ts_strerror.restype = ctypes.c_char_p
@@ -89,6 +94,11 @@ def load():
         L.ts_sum_vote.argtypes = [pp, vp, vp, vp, vp]
         L.ts_head_vote_scratch_bytes.argtypes = [pp, ctypes.POINTER(sz)]
         L.ts_head_vote.argtypes = [pp, vp, i32, vp, vp, vp, sz, vp]
+        L.ts_paged_attn_workspace_bytes.argtypes = [pp, i32, ctypes.POINTER(sz)]
+        L.ts_paged_attn.argtypes = [pp, vp, vp, i32, i32, f32, vp, vp, vp, sz, vp]
+        L.ts_rope_append.argtypes = [pp, ctypes.POINTER(_CRope), vp, i64, vp, i64, vp, i64, vp, i32, vp, vp, vp]
+        L.ts_pages_copy.argtypes = [pp, vp, vp, i32, i32, vp]
+        L.ts_cache_compact.argtypes = [pp, vp, i32, vp, vp, vp, vp, vp, vp]
         L.ts_debug_set_score_variant.argtypes = [i32, i32, i32]
         L.ts_debug_set_topk_path.argtypes = [i32]
         L.ts_debug_set_codes_path.argtypes = [i32, i32]
@@ -102,7 +112,8 @@ def load():
                      "ts_head_vote", "ts_debug_set_topk_path", "ts_debug_event_create", "ts_debug_event_destroy",
                      "ts_debug_event_elapsed_ms", "ts_debug_set_score_timing_events", "ts_paged_qk_codes",
                      "ts_soft_vote_bounds", "ts_topk_exact", "ts_debug_set_codes_path", "ts_topk_noalloc",
-                     "ts_paged_qk_scores_checked", "ts_paged_qk_codes_checked", "ts_soft_vote_ranked"):
+                     "ts_paged_qk_scores_checked", "ts_paged_qk_codes_checked", "ts_soft_vote_ranked",
+                     "ts_paged_attn_workspace_bytes", "ts_paged_attn", "ts_rope_append", "ts_pages_copy", "ts_cache_compact"):
             getattr(L, name).restype = i32
         _lib = L
     return _lib
@@ -153,6 +164,39 @@ class Problem:
 
     def ref(self):
         return ctypes.byref(self.c)
+
+
+class Rope:
+    """ts_rope plus a reference that keeps the frequencies alive.  pair_axis: the position axis of each pair (rotary_dim / 2
+    numbers), or None: every pair turns with the first axis.  inv_freq: float tensor on the GPU, one per pair."""
+
+    def __init__(self, *, inv_freq, pair_axis=None, num_axes=1, adjacent=False, scale=1.0):
+        n = int(inv_freq.numel())
+        axes = [0] * n if pair_axis is None else [int(i) for i in pair_axis]
+        if len(axes) != n or n > 64 or any(not 0 <= i < 256 for i in axes):
+            raise ValueError("pair_axis: one axis for each of the %d pairs (at most 64)" % n)
+        if str(inv_freq.dtype) != "torch.float32" or not inv_freq.is_contiguous():
+            raise ValueError("inv_freq: a contiguous float32 tensor")
+        self._keep = inv_freq
+        self.c = _CRope(_ptr(inv_freq), 2 * n, int(num_axes), int(bool(adjacent)), float(scale), (ctypes.c_uint8 * 64)(*axes))
+
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+def rope_axes(sections, dealt=False):
+    """Axis of each pair for position axes that get sections[a] pairs each: the first axis' pairs, then the next one's; dealt:
+    in turn, axis after axis, as long as an axis has pairs left."""
+    sections = [int(n) for n in sections]
+    if not dealt:
+        return [a for a, n in enumerate(sections) for _ in range(n)]
+    left, axes = list(sections), []
+    while any(left):
+        for a in range(len(left)):
+            if left[a]:
+                left[a] -= 1
+                axes.append(a)
+    return axes
 
 
 def ts_version() -> int:
@@ -312,3 +356,49 @@ def ts_sparse_paged_attn(p: Problem, q, idx, idx_stride: int, count, sm_scale: f
                                     _ptr(out), _ptr(lse), _ptr(ws),
                                     ws.numel() * ws.element_size() if ws is not None else 0, _stream(stream)),
         "ts_sparse_paged_attn")
+
+
+def ts_paged_attn_workspace_bytes(p: Problem, num_rows: int) -> int:
+    out = ctypes.c_size_t(0)
+    _ok(load().ts_paged_attn_workspace_bytes(p.ref(), int(num_rows), ctypes.byref(out)), "ts_paged_attn_workspace_bytes")
+    return int(out.value)
+
+
+def ts_paged_attn(p: Problem, q, q_indptr, num_rows: int, window: int, sm_scale: float, out, lse, ws, stream=None) -> None:
+    _ok(load().ts_paged_attn(p.ref(), _ptr(q), _ptr(q_indptr), int(num_rows), int(window), float(sm_scale), _ptr(out), _ptr(lse),
+                             _ptr(ws), _nbytes(ws), _stream(stream)), "ts_paged_attn")
+
+
+def _row_stride(t, row: int, name: str) -> int:
+    """Elements between the rows of a [rows][...] tensor whose rows are packed; row: elements of one."""
+    if t is None:
+        return 0
+    want = 1
+    for n, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if n > 1 and stride != want:
+            raise ValueError("%s: the elements of a row must follow each other" % name)
+        want *= n
+    if want != row:
+        raise ValueError("%s: rows of %d elements, the problem's have %d" % (name, want, row))
+    return int(t.stride(0)) if t.shape[0] > 1 else 0
+
+
+def ts_rope_append(p: Problem, rope, q, k, v, q_indptr, num_rows: int, positions, q_out, stream=None) -> None:
+    """q, k, v: [rows][heads][D] or [rows][heads * D], rows any multiple of 16 bytes apart; q and q_out, or k and v, may be None."""
+    D = p.c.head_dim
+    strides = [_row_stride(t, heads * D, name) for t, heads, name in ((q, p.c.num_q_heads, "q"), (k, p.c.num_kv_heads, "k"),
+                                                                      (v, p.c.num_kv_heads, "v"))]
+    if q_out is not None and not q_out.is_contiguous():
+        raise ValueError("q_out: rows must follow each other")
+    _ok(load().ts_rope_append(p.ref(), None if rope is None else rope.ref(), _ptr(q), strides[0], _ptr(k), strides[1], _ptr(v),
+                              strides[2], _ptr(q_indptr), int(num_rows), _ptr(positions), _ptr(q_out), _stream(stream)),
+        "ts_rope_append")
+
+
+def ts_pages_copy(p: Problem, src, dst, n: int, num_pages: int, stream=None) -> None:
+    _ok(load().ts_pages_copy(p.ref(), _ptr(src), _ptr(dst), int(n), int(num_pages), _stream(stream)), "ts_pages_copy")
+
+
+def ts_cache_compact(p: Problem, idx, idx_stride: int, count, skip, to_indptr, to_indices, to_lens, stream=None) -> None:
+    _ok(load().ts_cache_compact(p.ref(), _ptr(idx), int(idx_stride), _ptr(count), _ptr(skip), _ptr(to_indptr), _ptr(to_indices),
+                                _ptr(to_lens), _stream(stream)), "ts_cache_compact")

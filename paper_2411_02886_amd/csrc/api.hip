@@ -57,7 +57,7 @@ static int score_workgroups(const ts_problem* p) {
 static bool is_pow2(int x) { return x > 0 && (x & (x - 1)) == 0; }
 
 // shape checks shared by all calls; returns TS_OK or an error
-static int32_t check_problem(const ts_problem* p) {
+int32_t check_problem(const ts_problem* p) {
   if (p == nullptr) return TS_ERR_INVALID_ARG;
   if (p->batch < 1 || p->chunk < 1 || p->num_q_heads < 1 || p->num_kv_heads < 1 || p->head_dim < 1 ||
       p->page_size < 1 || p->max_seq_len < 1)
@@ -111,7 +111,7 @@ using namespace ts;
 
 extern "C" {
 
-int32_t ts_version(void) { return 300; }   // 0.3.0: the checked score calls and the ranked vote joined (0.2.0: the compact form, ts_topk_noalloc)
+int32_t ts_version(void) { return 400; }   // 0.4.0: dense attention, rotation + append, page copies and compaction joined (0.3.0: the checked score calls and the ranked vote)
 
 const char* ts_strerror(int32_t status) {
   switch (status) {

@@ -210,6 +210,70 @@ hipError_t launch_selcache(const SelcacheArgs& a, int B, hipStream_t s);
 hipError_t launch_sparse_attn_decode(int dtype, int D, int G, const AttnArgs& a, int B, hipStream_t s);
 // the streaming form (bf16): a.span list entries per split, a multiple of kStreamTile
 hipError_t launch_sparse_attn_stream(int D, int G, const AttnArgs& a, int B, hipStream_t s);
+// the cache itself (cache_api.hip): dense attention of new tokens, rotation + append, page copies, compaction
+struct PagedAttnArgs {
+  const uint8_t* q;            // [T][H][D]
+  const uint8_t* k_pool;
+  const uint8_t* v_pool;
+  const int32_t* page_indptr;
+  const int32_t* page_indices;
+  const int32_t* seq_lens;
+  const int32_t* q_indptr;     // [B+1] or null: C rows each
+  uint8_t* out;                // [T][H][D]
+  float* lse;                  // [T][H] or null
+  int B, C, T, H, H_kv, P, p_shift, max_seq_len, window;
+  float sm_scale;
+};
+hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, hipStream_t s);
+
+struct RopeAppendArgs {
+  const uint8_t* q;            // null: append only
+  const uint8_t* k;            // null: turn only
+  const uint8_t* v;
+  uint8_t* q_out;
+  uint8_t* k_pool;
+  uint8_t* v_pool;
+  const int32_t* page_indptr;
+  const int32_t* page_indices;
+  const int32_t* seq_lens;
+  const int32_t* q_indptr;
+  const int32_t* positions;    // [axes][T] or null
+  const float* inv_freq;
+  int64_t q_stride, k_stride, v_stride;   // bytes between rows
+  int B, C, T, H, H_kv, D, P, p_shift, max_seq_len, rotary, adjacent;
+  float scale;
+  uint8_t pair_axis[64];
+};
+hipError_t launch_rope_append(int dtype, const RopeAppendArgs& a, hipStream_t s);
+
+struct PagesCopyArgs {
+  const int32_t* src;
+  const int32_t* dst;
+  uint8_t* k_pool;
+  uint8_t* v_pool;             // null: K only
+  int n, num_pages;
+  int64_t page_bytes;
+};
+hipError_t launch_pages_copy(const PagesCopyArgs& a, hipStream_t s);
+
+struct CompactArgs {
+  uint8_t* k_pool;
+  uint8_t* v_pool;
+  const int32_t* page_indptr;
+  const int32_t* page_indices;
+  const int32_t* seq_lens;
+  const int32_t* idx;
+  const int32_t* count;
+  const uint8_t* skip;
+  const int32_t* to_indptr;
+  const int32_t* to_indices;
+  int32_t* to_lens;
+  int idx_stride, n_init, n_local, max_seq_len, p_shift, row_bytes;
+};
+hipError_t launch_cache_compact(const CompactArgs& a, int B, hipStream_t s);
+
+int32_t check_problem(const ts_problem* p);   // the shape and pointer checks that every call begins with (api.hip)
+
 hipError_t launch_chunk_mean_query(const void* q, void* out, int B, int C, int n, hipStream_t s);
 hipError_t launch_sum_vote(const VoteArgs& a, int B, hipStream_t s);
 hipError_t launch_transpose_scores(const VoteArgs& a, float* st, int B, hipStream_t s);

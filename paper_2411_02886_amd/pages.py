@@ -1,0 +1,143 @@
+"""Which pages of a paged KV pool belong to which sequence: taking, sharing, copying on write, moving together and giving back.
+
+The table lives on the host, where a server decides what runs next; the pages' contents are moved by ts_pages_copy, once per
+layer, with the (source, destination) lists that the methods here return.  Nothing here touches a page.
+"""
+from __future__ import annotations
+
+import heapq
+
+import numpy as np
+
+
+class PagePool:
+    """Pages 0 .. num_pages - 1 of `page_size` tokens.  A page may belong to several sequences (fork); the lowest free page is
+    taken first, so that a pool that empties stays dense at its low end.  Sequences go by any hashable name.  A call that
+    cannot be served raises and changes nothing."""
+
+    def __init__(self, num_pages: int, page_size: int):
+        if num_pages < 1 or page_size < 1:
+            raise ValueError("a pool has at least one page of at least one token")
+        self.num_pages, self.page_size = int(num_pages), int(page_size)
+        self.refs = np.zeros(self.num_pages, dtype=np.int32)      # sequences that hold the page
+        self._free = list(range(self.num_pages))                  # a heap
+        self._pages, self._lens = {}, {}
+
+    def __contains__(self, seq):
+        return seq in self._pages
+
+    def __len__(self):
+        return len(self._pages)
+
+    @property
+    def free_pages(self) -> int:
+        return len(self._free)
+
+    def length(self, seq) -> int:
+        return self._lens[seq]
+
+    def pages(self, seq):
+        return list(self._pages[seq])
+
+    def _take(self, n: int):
+        got = [heapq.heappop(self._free) for _ in range(n)]
+        self.refs[got] += 1
+        return got
+
+    def _release(self, pages):
+        for page in pages:
+            self.refs[page] -= 1
+            if self.refs[page] == 0:
+                heapq.heappush(self._free, page)
+
+    def add(self, seq, tokens: int = 0) -> None:
+        """A new sequence of `tokens` tokens."""
+        if seq in self._pages:
+            raise KeyError("sequence %r is there already" % (seq,))
+        if tokens < 0:
+            raise ValueError("tokens < 0")
+        need = -(-tokens // self.page_size)
+        if need > len(self._free):
+            raise MemoryError("%d pages wanted, %d free" % (need, len(self._free)))
+        self._pages[seq], self._lens[seq] = self._take(need), int(tokens)
+
+    def grow(self, seq, tokens: int = 1):
+        """Room for `tokens` more tokens.  Returns the page copies, [(src, dst)], to be made before the new tokens are written: a
+        last page that is partly filled and shared is replaced by a copy of its own."""
+        if tokens < 0:
+            raise ValueError("tokens < 0")
+        pages, n = self._pages[seq], self._lens[seq]
+        need = -(-(n + tokens) // self.page_size) - len(pages)
+        own = tokens > 0 and n % self.page_size != 0 and self.refs[pages[-1]] > 1
+        if need + own > len(self._free):
+            raise MemoryError("%d pages wanted, %d free" % (need + own, len(self._free)))
+        copies = []
+        if own:
+            page = self._take(1)[0]
+            copies.append((pages[-1], page))
+            self.refs[pages[-1]] -= 1           # another sequence holds it: it does not become free
+            pages[-1] = page
+        pages += self._take(max(need, 0))
+        self._lens[seq] = n + int(tokens)
+        return copies
+
+    def fork(self, seq, child) -> None:
+        """`child` begins as `seq` is now and shares its pages."""
+        if child in self._pages:
+            raise KeyError("sequence %r is there already" % (child,))
+        pages = self._pages[seq]
+        self.refs[pages] += 1
+        self._pages[child], self._lens[child] = list(pages), self._lens[seq]
+
+    def free(self, seq) -> None:
+        """Gives the sequence's pages back; those that another one holds stay."""
+        self._release(self._pages.pop(seq))
+        del self._lens[seq]
+
+    def spare(self, tokens: int):
+        """Pages for `tokens` tokens that belong to no sequence yet: where a compaction writes (see replace, give_back)."""
+        need = -(-int(tokens) // self.page_size)
+        if need > len(self._free):
+            raise MemoryError("%d pages wanted, %d free" % (need, len(self._free)))
+        return self._take(need)
+
+    def give_back(self, pages) -> None:
+        """Returns spare pages that were not used."""
+        self._release(pages)
+
+    def replace(self, seq, pages, tokens: int) -> None:
+        """The sequence now is the first `tokens` tokens of the spare `pages` (what a compaction wrote); its old pages and
+        those that the tokens do not reach are given back."""
+        need = -(-int(tokens) // self.page_size)
+        if tokens < 0 or need > len(pages):
+            raise ValueError("%d tokens do not fit %d pages" % (tokens, len(pages)))
+        old = self._pages[seq]
+        self._pages[seq], self._lens[seq] = list(pages[:need]), int(tokens)
+        self._release(old)
+        self._release(pages[need:])
+
+    def gather(self):
+        """Moves the pages in use to the low end of the pool.  Returns the page copies, [(src, dst)], to be made before the next
+        page is written; no page is in both columns."""
+        used = np.flatnonzero(self.refs)
+        high = used[used >= used.size]
+        low = np.flatnonzero(self.refs[:used.size] == 0)
+        to = np.arange(self.num_pages)
+        to[high] = low
+        moved = [(int(a), int(b)) for a, b in zip(high, low)]
+        for pages in self._pages.values():
+            pages[:] = [int(to[page]) for page in pages]
+        self.refs[low] = self.refs[high]
+        self.refs[high] = 0
+        self._free = [int(page) for page in np.flatnonzero(self.refs == 0)]     # ascending: a heap
+        return moved
+
+    def table(self, seqs, room: int = 0):
+        """(page_indptr [B+1], page_indices, seq_lens [B]) of the sequences, int32, as ts_problem wants them.  room: empty
+        places in page_indices behind each sequence's pages, for pages it will get."""
+        rows = [self._pages[s] + [0] * room for s in seqs]
+        indptr = np.cumsum([0] + [len(r) for r in rows], dtype=np.int64)
+        if indptr[-1] > np.iinfo(np.int32).max:
+            raise ValueError("more pages than an int32 counts")
+        return (indptr.astype(np.int32), np.array([page for r in rows for page in r] or [0], dtype=np.int32),
+                np.array([self._lens[s] for s in seqs], dtype=np.int32))

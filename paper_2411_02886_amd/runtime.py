@@ -24,7 +24,35 @@ def to_host(t: torch.Tensor, bits16: bool = False) -> np.ndarray:
     return a.view(np.uint16) if bits16 else a
 
 
-class DecodeLayer:
+def copy_pages(problem, copies, num_pages, device="cuda:0"):
+    """Makes the page copies [(src, dst)] that a PagePool asks for, in the pools of `problem` (one call per layer)."""
+    if copies:
+        pairs = torch.tensor(copies, dtype=torch.int32, device=device).t().contiguous()
+        ts.ts_pages_copy(problem, pairs[0], pairs[1], len(copies), num_pages)
+
+
+class _NewTokens:
+    """The calls on new tokens that both layers have.  seq_lens count them; they are rows [B * C] without q_indptr, any
+    number per sequence with it."""
+
+    def append(self, k, v, q=None, q_out=None, rope=None, positions=None, q_indptr=None):
+        """Writes the new tokens' K and V rows into their pages, keys turned by `rope`, and the turned queries into q_out."""
+        ts.ts_rope_append(self.problem, rope, q, k, v, q_indptr, k.shape[0], positions, q_out)
+
+    def attend_all(self, q, sm_scale=None, window=0, q_indptr=None, out=None, lse=None):
+        """Attention of the new tokens over their whole sequence: no selection.  Without q_indptr q is the step's or chunk's
+        query and the result is in self.out / self.lse; packed rows bring their own `out` (and `lse`)."""
+        sm = sm_scale if sm_scale is not None else 1.0 / float(np.sqrt(self.D))
+        rows = self.B * self.problem.c.chunk if q_indptr is None else q.shape[0]
+        if q_indptr is None:
+            out, lse = self.out if out is None else out, self.lse if lse is None else lse
+        nbytes = ts.ts_paged_attn_workspace_bytes(self.problem, rows)
+        if getattr(self, "_all_ws", None) is None or self._all_ws.numel() * 4 < nbytes:
+            self._all_ws = torch.empty((nbytes + 255) // 256 * 64, dtype=torch.int32, device=self.k_pool.device)
+        ts.ts_paged_attn(self.problem, q, q_indptr, rows, window, sm, out, lse, self._all_ws)
+
+
+class DecodeLayer(_NewTokens):
     """Paged KV pool of B sequences on the GPU plus every buffer the decode step needs."""
 
     def __init__(self, *, dtype, H, H_kv, D, P, k, k_pool, v_pool, page_indptr, page_indices, seq_lens,
@@ -141,6 +169,11 @@ class DecodeLayer:
     def attend(self, q, sm_scale):
         ts.ts_sparse_paged_attn(self.problem, q, self.idx, self.k, self.count, sm_scale, self.out, self.lse, self.ws)
 
+    def compact(self, to_indptr, to_indices, to_lens, skip=None):
+        """Copies what attend() reads of every sequence (initial block, selection, recent block) densely into other pages;
+        to_lens gets the new lengths.  Attending all of the new pages then gives what attend() gives."""
+        ts.ts_cache_compact(self.problem, self.idx, self.k, self.count, skip, to_indptr, to_indices, to_lens)
+
     def compact_form_pays(self) -> bool:
         """Which form of the Eq. 5 selection compact=None takes: compact, which never writes the fp32 score matrix, where the
         matrices of the batch are larger than 24 MiB together, and for one sequence of up to 32 heads from 20 MiB on (us on MI355X,
@@ -178,7 +211,7 @@ class DecodeLayer:
         self.attend(q, sm)
 
 
-class ChunkSelector:
+class ChunkSelector(_NewTokens):
     """Chunked-prefill selection for one layer: the C queries of a chunk are the last C tokens of
     their sequences; two MFMA sweeps give the votes, ts_topk the shared index set."""
 
