@@ -23,7 +23,7 @@ int32_t ts_paged_attn_workspace_bytes(const ts_problem* p, int32_t num_rows, siz
   if (bytes == nullptr || num_rows < 0) return TS_ERR_INVALID_ARG;
   const int32_t st = check_problem(p);
   if (st != TS_OK) return st;
-  *bytes = 256;
+  *bytes = paged_attn_workspace(p->dtype, p->head_dim, p->num_q_heads / p->num_kv_heads, p->chunk);
   return TS_OK;
 }
 
@@ -49,7 +49,7 @@ int32_t ts_paged_attn(const ts_problem* p, const void* q, const int32_t* q_indpt
   a.B = p->batch; a.C = p->chunk; a.T = num_rows; a.H = p->num_q_heads; a.H_kv = p->num_kv_heads;
   a.P = p->page_size; a.p_shift = ilog2(p->page_size); a.max_seq_len = p->max_seq_len; a.window = window;
   a.sm_scale = sm_scale;
-  return launch_paged_attn(p->dtype, p->head_dim, a, (hipStream_t)stream) == hipSuccess ? TS_OK : TS_ERR_HIP;
+  return launch_paged_attn(p->dtype, p->head_dim, a, ws, (hipStream_t)stream) == hipSuccess ? TS_OK : TS_ERR_HIP;
 }
 
 int32_t ts_rope_append(const ts_problem* p, const ts_rope* r, const void* q, int64_t q_stride, const void* k, int64_t k_stride,

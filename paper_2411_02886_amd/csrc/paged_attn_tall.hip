@@ -1,0 +1,428 @@
+// Dense attention of new tokens, bf16, many rows per tile: chunks of prompts and whole ones, on the matrix cores.
+//
+// A tile is 256 rows (256 / G tokens times the G heads of a KV head).  Four waves, one per SIMD, own 64 rows each and walk the same
+// 64-key tiles, which arrive in LDS directly, two tiles ahead; every fragment read from LDS serves 64 rows.  In one piece of
+// straight-line code a wave forms the weights of one block of 32 keys on the vector ALU while the matrix cores form the
+// scores of the next and add the output of the last one:
+//   * A wave issues in order, so the vector instructions are shared out behind every single product (two of those in a row make
+//     what follows wait until the first has left the matrix cores).  Four of them fit a product: fma, exp, the weight's sum
+//     and half a conversion.
+//   * The softmax's reference is not a running maximum: it is raised, with what has been added up so far, when a packed weight has
+//     a bit that only numbers of 2 and more have, which the first visible key of a row does.
+//   * Tiles that every row sees in full take a copy of the code without masks.
+// Weights are rounded to bf16 for the product with V (half a step, 2^-8); their sum is of the floats before that rounding, so that the log-sum-exp
+// keeps 24 bits.
+#include "paged_shares.h"
+#include <limits.h>
+#include <type_traits>
+
+namespace ts {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
+typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+typedef __attribute__((ext_vector_type(16))) float f32x16_t;
+
+constexpr int kPtTile = 64;                   // keys per tile
+constexpr int kPtRows = 256;                  // rows per tile of the share
+constexpr int kPtRing = 4;                    // tiles whose page ids are in LDS
+constexpr float kPtUnset = -3.40282347e38f;   // reference exponent of a row that has seen no key: no finite logit lies below it
+constexpr uint32_t kPtTwo = 0x40004000u;      // bits that only bf16 numbers of 2 and more have (and infinities and NaN)
+constexpr float kPtHead = 8.f;                // a raised reference lies this far above the largest exponent so far
+constexpr float kPtBig = 1048576.f;           // references beyond this: the logits are rounded before it is taken off them
+
+// place of a row's 16-byte pieces in LDS: 16 rows x one piece (K fragments) and 4 rows x 4 pieces (V^T) each fall on all banks
+template <int D> __device__ __forceinline__ int pt_swz(int key) {
+  return D == 128 ? (((key & 3) << 2) | ((key >> 2) & 3)) : ((((key >> 1) & 1) << 2) | (((key >> 2) & 1) << 1) | ((key >> 3) & 1));
+}
+
+template <int D>
+__global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, ShareArgs sh) {
+  constexpr int KS = D / 16;                  // k-steps of Q K^T
+  constexpr int NBO = D / 32;                 // 32-row blocks of the transposed output
+  constexpr int RB = D * 2, PPR = RB / 16;    // bytes and 16-byte pieces of a K/V row
+  constexpr int KPI = 64 / PPR;               // keys per wave load
+  constexpr int WK = kPtTile / 4;             // keys of a tile that a wave stages
+  constexpr int NLD = WK / KPI;               // loads per wave, tile and pool
+  constexpr int TILE_B = kPtTile * RB;
+  constexpr int VH = D == 128 ? 32 : 16;      // what eight keys more flip of a piece's place
+  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];   // [buffer][K tile, V tile], page ids [wave][ring][64], the share's ends
+  // (nothing else is in LDS: places of pieces are flipped in the address, so the tiles have to begin at a multiple of a row)
+  SharePlace* s_place = reinterpret_cast<SharePlace*>(smem + 4 * TILE_B + 4 * kPtRing * 256);
+  long* s_scan = reinterpret_cast<long*>(s_place + 2);
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int half = lane >> 5, col = lane & 31;
+  const int H = a.H, G = a.H / a.H_kv;
+  const int wg = share_of(blockIdx.x, sh.wgs);
+  SharePlace from, to;
+  find_share<kPtTile, 256>(a, sh, G, wg, s_place, s_scan, &from, &to);
+  int32_t* desc = sh.desc + (size_t)wg * 8;
+  if (!sh.whole && threadIdx.x == 0) { desc[3] = kPieceNone; desc[7] = kPieceNone; }
+
+  float c2 = a.sm_scale * 1.44269504088896340736f;
+  if (c2 == 0.f) c2 = 1e-37f;                                   // the same weights (all 1), and a hidden key still gets 0
+  const float hidden = c2 > 0.f ? -INFINITY : INFINITY;         // c2 * hidden = -inf
+
+  typedef const __attribute__((address_space(3))) bf16x8_t lds_bf16x8;
+  typedef __attribute__((address_space(3))) s16x4_t lds_s16x4;
+  const uint32_t lds_base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)smem;
+  // K fragment ks of key block kb: row 32 * kb + col, piece (2 * ks + half) ^ swz(col) -- ks flips bits of the address only
+  const uint32_t ka0 = lds_base + (uint32_t)(col * RB + ((half ^ pt_swz<D>(col)) * 16));
+  // V^T: 16 lanes read 4 keys x 16 columns; lane i of them reads key i / 4, columns 4 * (i % 4) ..; the output block nb and
+  // the upper eight keys of a k-step flip bits of the piece
+  const int vt_key = 4 * half + ((lane & 15) >> 2), vt_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+  const uint32_t va0 = lds_base + (uint32_t)(vt_key * RB + (((vt_col >> 3) ^ pt_swz<D>(vt_key)) * 16) + (vt_col & 7) * 2);
+  // staging: this wave's 16 keys of a tile, load i covering keys 16 * wave + i * KPI + lane / PPR
+  const int st_key = lane / PPR, st_pos = lane % PPR;
+  const uint32_t lds_st = __builtin_amdgcn_readfirstlane(lds_base + (uint32_t)(wave * WK * RB));
+  const uint32_t look = __builtin_amdgcn_readfirstlane(lds_base + (uint32_t)(4 * TILE_B + wave * kPtRing * 256));
+  const int row_shift = 31 - __builtin_clz((uint32_t)(a.H_kv * RB));   // H_kv is a power of two
+
+  walk_share<kPtTile>(a, sh, G, from, to, [&](int kvh, const SeqShape& sq, int r, const TileKeys& keys, int ua, int ub) __attribute__((always_inline)) {
+    const int c0 = r * sh.tpt, ntok = min(sh.tpt, sq.n - c0), nrows = ntok * G;
+    const int row0 = sq.row0 + c0, x0 = sq.N - sq.n + c0, x1 = x0 + ntok - 1;   // first row; places of the first and last token
+    const bool whole = ua == 0 && ub == keys.units;
+    const int tmax = keys.end - 1;
+    auto out_row = [&](int j) -> size_t { return (size_t)(row0 + j / G) * H + kvh * G + j % G; };
+    if (keys.end <= keys.first) {                                  // no row sees a token (one unit: the tile is not cut)
+      for (int i = threadIdx.x; i < nrows * D; i += 256) {
+        const size_t o = out_row(i / D) * D + i % D;
+        reinterpret_cast<uint16_t*>(a.out)[o] = 0;
+        if (i % D == 0 && a.lse != nullptr) a.lse[o / D] = -INFINITY;
+      }
+      return;
+    }
+    const int slot = ua > 0 ? 0 : 1;
+    if (!whole && threadIdx.x == 0) {
+      int32_t* d = desc + slot * 4;
+      d[0] = row0; d[1] = kvh; d[2] = ntok; d[3] = ub == keys.units ? kPieceEnds : kPieceGoesOn;
+    }
+    const int32_t* pages = a.page_indices + a.page_indptr[sq.b];
+    const int key0 = (keys.u0 + ua) * kPtTile, nt = ub - ua;       // first key and number of tiles
+    // tiles [f0, f1) are seen in full by every row
+    const int f0 = a.window > 0 ? max((x1 - a.window + 1 - key0 + kPtTile - 1) / kPtTile, 0) : 0;
+    int f1 = x0 >= key0 ? min((x0 + 1 - key0) / kPtTile, nt) : 0;       // (INT_MIN once the logits are rounded before the reference is taken off)
+    const bool idle = wave * 64 >= nrows;                          // no row of this wave's: it stages keys for the others
+
+    // ---- query fragments (B operand of K Q^T): of the wave's two blocks of 32 rows, lane holds row = col, k = 16 * ks + 8 * half .. + 8
+    int vis[2], low[2];                                            // last and first key that the row sees
+    bf16x8_t qfrag[2][KS];
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb) {
+      const int j = wave * 64 + rb * 32 + col;
+      vis[rb] = j < nrows ? x0 + j / G : x1;
+      low[rb] = a.window > 0 ? vis[rb] - a.window + 1 : INT_MIN;
+      const uint8_t* qp = a.q + (out_row(min(j, nrows - 1)) * D + 8 * half) * 2;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (j < nrows) v = *reinterpret_cast<const uint4*>(qp + ks * 32);
+        qfrag[rb][ks] = __builtin_bit_cast(bf16x8_t, v);
+      }
+    }
+    float ref[2] = {kPtUnset, kPtUnset};                           // the rows' reference exponents
+    float lsum[2] = {0.f, 0.f};                                    // this lane's keys' weights
+    float factor = c2;                                             // 1 once the logits are rounded first
+    f32x16_t oacc[2][NBO];                                         // O^T: d = 32 * nb + 8 * (e / 4) + 4 * half + e % 4
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+      for (int nb = 0; nb < NBO; ++nb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) oacc[rb][nb][e] = 0.f;
+
+    // ---- Memory to LDS, 16 bytes per lane: the wave's 64 lanes fill 1 KiB from the (uniform) LDS address.  Written in assembly because the
+    // compiler, which cannot tell the buffers apart, makes every later LDS read wait for the builtin form; completion is
+    // awaited by the vmcnt(0) before a tile's barrier.  Page ids come the same way, one tile earlier.
+    auto fetch_look = [&](int it) __attribute__((always_inline)) {
+      const int t = min(key0 + it * kPtTile + wave * WK + (lane & (WK - 1)), tmax);
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(look + (it & (kPtRing - 1)) * 256), "v"(pages + (t >> a.p_shift)) : "memory", "m0");
+    };
+    uint32_t at_k[NLD], at_v[NLD];                                 // rows of the K tile and of the V tile that are requested next
+    auto rows_of = [&](int it) __attribute__((always_inline)) {    // past the end: the last key again
+#pragma unroll
+      for (int i = 0; i < NLD; ++i) {
+        const int key = i * KPI + st_key, t = min(key0 + it * kPtTile + wave * WK + key, tmax);
+        const int page = *(const volatile __attribute__((address_space(3))) int*)(look + (uint32_t)((it & (kPtRing - 1)) * 256 + key * 4));
+        at_v[i] = at_k[i];
+        at_k[i] = ((uint32_t)page << a.p_shift) + (uint32_t)(t & (a.P - 1));
+      }
+    };
+    auto load_row = [&](const uint8_t* pool, uint32_t at, int i, int tile_slot) __attribute__((always_inline)) {
+      const uint64_t off = ((uint64_t)at << row_shift) + (uint32_t)(kvh * RB + ((st_pos ^ pt_swz<D>((wave * WK + i * KPI + st_key) & 15)) * 16));
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds_st + (uint32_t)(tile_slot * TILE_B + i * 1024)), "v"(pool + off) : "memory", "m0");
+    };
+    auto k_slot = [&](int buf) { return buf * 2; };                // tile slots of the LDS: [buffer][K, V]
+
+    // ---- blocks of 32 keys, two to a tile.  While the vector ALU forms the weights of block j, the matrix cores form the scores of
+    // block j + 1 and add the output of block j - 1.
+    f32x16_t s[2][2];                                              // [block parity][row block] S^T: key 8 * (e / 4) + 4 * half + e % 4
+    uint32_t pk[2][2][8];                                          // the weights, rounded to bf16
+    auto round_logits = [&](f32x16_t (&x)[2]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[rb][e] *= c2;
+    };
+    constexpr int AHEAD = 3;
+    bf16x8_t carry[AHEAD];
+    auto body = [&](auto half_c, int it, auto with_scores, auto with_output, auto with_loads, auto masked_c) __attribute__((always_inline)) {
+      constexpr int CUR = decltype(half_c)::value, NXT = 1 - CUR;  // this block is half CUR of tile `it`
+      constexpr bool SC = decltype(with_scores)::value, OUT = decltype(with_output)::value, LD = decltype(with_loads)::value;
+      constexpr bool MASKED = decltype(masked_c)::value;
+      f32x16_t (&x)[2] = s[CUR];
+      const int j0 = key0 + it * kPtTile + CUR * 32 + 4 * half;    // key of element 0
+      if constexpr (MASKED) {
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int key = j0 + 8 * (e >> 2) + (e & 3);
+            x[rb][e] = key <= vis[rb] && key >= low[rb] ? x[rb][e] : hidden;
+          }
+        if (__builtin_expect(f1 == INT_MIN, 0)) round_logits(x);
+      }
+      const uint32_t kt = ka0 + (uint32_t)(k_slot((it + CUR) & 1) * TILE_B + NXT * 32 * RB);
+      const uint32_t vt = va0 + (uint32_t)((k_slot((it + CUR + 1) & 1) + 1) * TILE_B + NXT * 32 * RB);
+      constexpr int NS = KS + 2 * NBO, T0 = SC ? 0 : KS, T1 = OUT ? NS : KS; // steps: scores, then output; two products each
+      constexpr int PPS = 16 / NS;                                 // pairs of weights per step
+      constexpr bool CIN = CUR == 0 && OUT;                        // this block's first fragments were read at the end of the one before
+      bf16x8_t frag[NS];                                           // of step t: K rows of the next block (t < KS), V^T of the last one
+      auto fetch = [&](int t) __attribute__((always_inline)) {
+        if (t < KS) { frag[t] = *(lds_bf16x8*)(kt ^ (uint32_t)(t * 32)); return; }
+        const int k2 = (t - KS) / NBO, nb = (t - KS) % NBO;        // k-step k2 takes keys 16 * k2 + 4 * half + {0..3, 8..11}, the keys of x[8 * k2 ..]
+        s16x4_t v[2];
+#pragma unroll
+        for (int h8 = 0; h8 < 2; ++h8)
+          v[h8] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((vt ^ (uint32_t)(nb * 64 + h8 * VH)) + (uint32_t)((k2 * 16 + h8 * 8) * RB)));
+        const uint2 v0 = __builtin_bit_cast(uint2, v[0]), v1 = __builtin_bit_cast(uint2, v[1]);
+        frag[t] = __builtin_bit_cast(bf16x8_t, make_uint4(v0.x, v0.y, v1.x, v1.y));
+      };
+      auto weights_of = [&](int rb, int k2) __attribute__((always_inline)) -> bf16x8_t {
+        const uint32_t (&pw)[8] = pk[NXT][rb];
+        return __builtin_bit_cast(bf16x8_t, make_uint4(pw[4 * k2], pw[4 * k2 + 1], pw[4 * k2 + 2], pw[4 * k2 + 3]));
+      };
+      uint32_t any = 0u;
+      float y[16][2], w[16][2], sum[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
+      // pair i of the 16 pairs of weights, in three stages a step apart: none of a step's instructions waits for another of them
+      auto exponent = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) y[i][u] = fmaf(factor, x[i >> 3][2 * (i & 7) + u], -ref[i >> 3]);
+      };
+      auto power = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) w[i][u] = __builtin_amdgcn_exp2f(y[i][u]);
+      };
+      auto pack = [&](int i) __attribute__((always_inline)) {
+        const bf16x2_t p = {(__bf16)w[i][0], (__bf16)w[i][1]};
+        pk[CUR][i >> 3][i & 7] = __builtin_bit_cast(uint32_t, p);
+        any |= pk[CUR][i >> 3][i & 7];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) sum[i >> 3][u] += w[i][u];
+      };
+#pragma unroll
+      for (int t = T0; t < T1 && t < T0 + AHEAD; ++t) { if (CIN) frag[t] = carry[t - T0]; else fetch(t); }
+      auto product = [&](int t, int rb) __attribute__((always_inline)) {
+        if (t < T0 || t >= T1) return;
+        if (t < KS) s[NXT][rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[t], qfrag[rb][t < KS ? t : 0], t == 0 ? (f32x16_t){} : s[NXT][rb], 0, 0, 0);
+        else oacc[rb][(t - KS) % NBO] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[t], weights_of(rb, (t - KS) / NBO), oacc[rb][(t - KS) % NBO], 0, 0, 0);
+      };
+      // A step: two products, a fragment read AHEAD steps before its use, a row load, pairs of weights
+#pragma unroll
+      for (int t = 0; t < NS; ++t) {
+        product(t, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        if (t >= T0 && t + AHEAD < T1) fetch(t + AHEAD);
+        if (CUR == 1 && SC && t + AHEAD >= NS)                     // of K tile it + 1, second half
+          carry[t + AHEAD - NS] = *(lds_bf16x8*)((ka0 + (uint32_t)(k_slot((it + 1) & 1) * TILE_B + 32 * RB)) ^ (uint32_t)((t + AHEAD - NS) * 32));
+#pragma unroll
+        for (int i = t * PPS; i < (t + 1) * PPS; ++i) { if (i >= 2 * PPS) pack(i - 2 * PPS); exponent(i); }
+        __builtin_amdgcn_sched_barrier(0);
+        product(t, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        if (LD && t < NLD) {                                       // rows of K tile it + 2 and V tile it + 1
+          load_row(a.k_pool, at_k[t < NLD ? t : 0], t, k_slot(it & 1));
+          load_row(a.v_pool, at_v[t < NLD ? t : 0], t, k_slot((it + 1) & 1) + 1);
+        }
+        if (LD && t == NLD) { rows_of(it + 3); fetch_look(it + 4); }
+#pragma unroll
+        for (int i = t * PPS; i < (t + 1) * PPS; ++i) if (i >= PPS) power(i - PPS);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int i = 16 - PPS; i < 16; ++i) power(i);
+#pragma unroll
+      for (int i = 16 - 2 * PPS; i < 16; ++i) pack(i);
+      if (__builtin_amdgcn_ballot_w64((any & kPtTwo) != 0u) != 0) {
+        // first visible key of a row, or a logit far above the reference.  Straight-line code: a branch per lane here
+        // makes the compiler copy the accumulators on the common path too.
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb) {
+          float m = ref[rb];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) m = fmaxf(m, factor * x[rb][e] + kPtHead);
+          m = fmaxf(m, __shfl_xor(m, 32));                         // both halves of a row raise its reference together
+          const float f = __builtin_amdgcn_exp2f(ref[rb] - m);     // 1 where nothing changes, 0 while the reference is unset
+          lsum[rb] *= f;
+#pragma unroll
+          for (int nb = 0; nb < NBO; ++nb)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) oacc[rb][nb][e] *= f;
+          ref[rb] = m;
+        }
+        const bool big = (fabsf(ref[0]) > kPtBig && ref[0] != kPtUnset) || (fabsf(ref[1]) > kPtBig && ref[1] != kPtUnset);
+        if (__builtin_expect(f1 != INT_MIN && __builtin_amdgcn_ballot_w64(big) != 0, 0)) {
+          // An fma's exact product is off by up to 2^-24 of the logit from the rounded one that the reference came from, and with logits of 2^31 that
+          // alone would over- or underflow the exponential: from here on the logits are rounded first.
+          factor = 1.f; f1 = INT_MIN;
+          round_logits(x);
+          // the code without masks takes one more block as it is, whose scores are there already; a masked block rounds its own
+          if (CUR == 1 && SC && !MASKED) round_logits(s[NXT]);
+        }
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb) sum[rb][0] = sum[rb][1] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) { exponent(i); power(i); pack(i); }
+      }
+      lsum[0] += sum[0][0] + sum[0][1];
+      lsum[1] += sum[1][0] + sum[1][1];
+    };
+    // Buffers: the barrier between the blocks of tile `it` says that K tile it + 1 and V tile `it` have arrived and that K tile
+    // `it` and V tile it - 1 have been read, whose places K tile it + 2 and V tile it + 1 then take.
+    auto tile_barrier = [&]() __attribute__((always_inline)) {
+      __builtin_amdgcn_sched_barrier(0);
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    using B0 = std::integral_constant<int, 0>;
+    using B1 = std::integral_constant<int, 1>;
+    using Yes = std::true_type;
+    using No = std::false_type;
+    __syncthreads();                                               // the tiles of the tile before have been read
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    fetch_look(0); fetch_look(1); fetch_look(2); fetch_look(3);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    rows_of(0);
+#pragma unroll
+    for (int i = 0; i < NLD; ++i) load_row(a.k_pool, at_k[i], i, k_slot(0));
+    rows_of(1);
+#pragma unroll
+    for (int i = 0; i < NLD; ++i) { load_row(a.k_pool, at_k[i], i, k_slot(1)); load_row(a.v_pool, at_v[i], i, k_slot(0) + 1); }
+    rows_of(2);
+    tile_barrier();
+    if (idle) {
+      for (int it = 0; it + 1 < nt; ++it) {
+        tile_barrier();
+#pragma unroll
+        for (int i = 0; i < NLD; ++i) { load_row(a.k_pool, at_k[i], i, k_slot(it & 1)); load_row(a.v_pool, at_v[i], i, k_slot((it + 1) & 1) + 1); }
+        rows_of(it + 3); fetch_look(it + 4);
+      }
+      tile_barrier();
+      return;
+    }
+    // the scores of the first block
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[0][rb][e] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const bf16x8_t av = *(lds_bf16x8*)((ka0 + (uint32_t)(k_slot(0) * TILE_B)) ^ (uint32_t)(ks * 32));
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb) s[0][rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, qfrag[rb][ks], s[0][rb], 0, 0, 0);
+    }
+    body(B0{}, 0, Yes{}, No{}, No{}, Yes{});
+    // tiles in turn: second half of tile `it`, first half of tile it + 1.  (Three loops and not one: with both copies of the code in one loop
+    // the compiler spills registers.)
+    int it = 0;
+    for (; it + 1 < nt && it < f0; ++it) {
+      tile_barrier();
+      body(B1{}, it, Yes{}, Yes{}, Yes{}, Yes{});
+      body(B0{}, it + 1, Yes{}, Yes{}, No{}, Yes{});
+    }
+    for (; it + 1 < f1; ++it) {
+      tile_barrier();
+      body(B1{}, it, Yes{}, Yes{}, Yes{}, No{});
+      body(B0{}, it + 1, Yes{}, Yes{}, No{}, No{});
+    }
+    for (; it + 1 < nt; ++it) {
+      tile_barrier();
+      body(B1{}, it, Yes{}, Yes{}, Yes{}, Yes{});
+      body(B0{}, it + 1, Yes{}, Yes{}, No{}, Yes{});
+    }
+    tile_barrier();
+    body(B1{}, nt - 1, No{}, Yes{}, No{}, Yes{});
+    // the output of the last block
+    const uint32_t vt = va0 + (uint32_t)((k_slot((nt - 1) & 1) + 1) * TILE_B + 32 * RB);
+#pragma unroll
+    for (int k2 = 0; k2 < 2; ++k2)
+#pragma unroll
+      for (int nb = 0; nb < NBO; ++nb) {
+        s16x4_t v[2];
+#pragma unroll
+        for (int h8 = 0; h8 < 2; ++h8)
+          v[h8] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((vt ^ (uint32_t)(nb * 64 + h8 * VH)) + (uint32_t)((k2 * 16 + h8 * 8) * RB)));
+        const uint2 v0 = __builtin_bit_cast(uint2, v[0]), v1 = __builtin_bit_cast(uint2, v[1]);
+        const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, make_uint4(v0.x, v0.y, v1.x, v1.y));
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb) {
+          const uint32_t (&pw)[8] = pk[1][rb];
+          oacc[rb][nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8_t, make_uint4(pw[4 * k2], pw[4 * k2 + 1], pw[4 * k2 + 2], pw[4 * k2 + 3])),
+                                                                 oacc[rb][nb], 0, 0, 0);
+        }
+      }
+
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb) {
+      const int j = wave * 64 + rb * 32 + col;
+      const float l = lsum[rb] + __shfl_xor(lsum[rb], 32);
+      if (j >= nrows) continue;
+      const float m = ref[rb] * 0.69314718055994530942f;           // in units of the logits
+      if (whole) {
+        const size_t hb = out_row(j);
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        uint8_t* po = a.out + (hb * D + half * 4) * 2;
+#pragma unroll
+        for (int nb = 0; nb < NBO; ++nb)
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4) {
+            const float o0 = oacc[rb][nb][q4 * 4] * inv, o1 = oacc[rb][nb][q4 * 4 + 1] * inv, o2 = oacc[rb][nb][q4 * 4 + 2] * inv, o3 = oacc[rb][nb][q4 * 4 + 3] * inv;
+            *reinterpret_cast<uint2*>(po + (nb * 32 + q4 * 8) * 2) =
+                make_uint2(f32_to_bf16_bits(o0) | (f32_to_bf16_bits(o1) << 16), f32_to_bf16_bits(o2) | (f32_to_bf16_bits(o3) << 16));
+          }
+        if (half == 0 && a.lse != nullptr) a.lse[hb] = l > 0.f ? (ref[rb] + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : -INFINITY;
+      } else {
+        float* po = sh.part_o + (((size_t)wg * 2 + slot) * kPtRows + j) * D + half * 4;
+#pragma unroll
+        for (int nb = 0; nb < NBO; ++nb)
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4)
+            *reinterpret_cast<float4*>(po + nb * 32 + q4 * 8) = make_float4(oacc[rb][nb][q4 * 4], oacc[rb][nb][q4 * 4 + 1], oacc[rb][nb][q4 * 4 + 2], oacc[rb][nb][q4 * 4 + 3]);
+        if (half == 0) {
+          float* pm = sh.part_ml + (((size_t)wg * 2 + slot) * kPtRows + j) * 2;
+          pm[0] = l > 0.f ? m : -INFINITY; pm[1] = l;
+        }
+      }
+    }
+  });
+}
+
+template <int D>
+static hipError_t tall_one(const PagedAttnArgs& a, const ShareArgs& sh, hipStream_t s) {
+  constexpr int lds = 4 * kPtTile * D * 2 + 4 * kPtRing * 256 + 64;
+  if (lds > 65536) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_tall_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(paged_tall_kernel<D>, dim3(sh.wgs), dim3(256), lds, s, a, sh);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_tall(int D, const PagedAttnArgs& a, const ShareArgs& sh, hipStream_t s) {
+  return D == 64 ? tall_one<64>(a, sh, s) : tall_one<128>(a, sh, s);
+}
+
+}  // namespace ts

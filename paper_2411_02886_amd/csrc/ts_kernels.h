@@ -224,7 +224,8 @@ struct PagedAttnArgs {
   int B, C, T, H, H_kv, P, p_shift, max_seq_len, window;
   float sm_scale;
 };
-hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, hipStream_t s);
+size_t paged_attn_workspace(int dtype, int D, int G, int chunk);
+hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws, hipStream_t s);
 
 struct RopeAppendArgs {
   const uint8_t* q;            // null: append only
