@@ -69,7 +69,7 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
   const int st_row = lane / PPR, st_pos = lane % PPR;
   const float sm = a.sm_scale;
 
-  walk_share<KT>(a, sh, G, from, to, [&](int kvh, const SeqShape& sq, int r, const TileKeys& keys, int ua, int ub) {
+  walk_share<KT>(a, sh, G, from, to, [&](int kvh, const SeqShape& sq, int r, const TileKeys& keys, int ua, int ub, bool) -> bool {
     const int c0 = r * sh.tpt, ntok = min(sh.tpt, sq.n - c0), nrows = ntok * G;
     const int row0 = sq.row0 + c0, x0 = sq.N - sq.n + c0, x1 = x0 + ntok - 1;   // first row; places of the first and last token
     const bool whole = ua == 0 && ub == keys.units;
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
         if (ES == 2) reinterpret_cast<uint16_t*>(a.out)[o] = 0; else reinterpret_cast<float*>(a.out)[o] = 0.f;
         if (i % D == 0 && a.lse != nullptr) a.lse[o / D] = -INFINITY;
       }
-      return;
+      return false;
     }
     const int slot = ua > 0 ? 0 : 1;
     if (!whole && threadIdx.x == 0) {
@@ -354,6 +354,7 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
         }
       }
     }
+    return false;
   });
 }
 

@@ -1,15 +1,18 @@
 // Dense attention of new tokens, bf16, many rows per tile: chunks of prompts and whole ones, on the matrix cores.
 //
 // A tile is 256 rows (256 / G tokens times the G heads of a KV head).  Four waves, one per SIMD, own 64 rows each and walk the same
-// 64-key tiles, which arrive in LDS directly, two tiles ahead; every fragment read from LDS serves 64 rows.  In one piece of
+// 64-key tiles, which arrive in LDS directly, requested two tiles ahead; every fragment read from LDS serves 64 rows.  In one piece of
 // straight-line code a wave forms the weights of one block of 32 keys on the vector ALU while the matrix cores form the
 // scores of the next and add the output of the last one:
 //   * A wave issues in order, so the vector instructions are shared out behind every single product (two of those in a row make
 //     what follows wait until the first has left the matrix cores).  Four of them fit a product: fma, exp, the weight's sum
 //     and half a conversion.
-//   * The softmax's reference is not a running maximum: it is raised, with what has been added up so far, when a packed weight has
-//     a bit that only numbers of 2 and more have, which the first visible key of a row does.
-//   * Tiles that every row sees in full take a copy of the code without masks.
+//   * The softmax's reference is not a running maximum.  In tiles with masks, the first one among them, it is raised, with what has
+//     been added up so far, when a packed weight has a bit that only numbers of 2 and more have, which the first visible key of
+//     a row does.  Tiles that every row sees in full take a copy of the code without masks and without that: weights may grow to 2^64
+//     there, which costs no precision.  Should they grow further (logits 44 above all of the first tile's), or the reference be
+//     so large that logits have to be rounded first, the workgroup does the piece again with the former code throughout.  (With the
+//     code for raising in the loop the compiler moves accumulators about: 1000 instructions a tile instead of 600.)
 // Weights are rounded to bf16 for the product with V (half a step, 2^-8); their sum is of the floats before that rounding, so that the log-sum-exp
 // keeps 24 bits.
 #include "paged_shares.h"
@@ -25,9 +28,11 @@ typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 
 constexpr int kPtTile = 64;                   // keys per tile
 constexpr int kPtRows = 256;                  // rows per tile of the share
+constexpr int kPtBuf = 3;                     // tiles of K, and of V, in LDS
 constexpr int kPtRing = 4;                    // tiles whose page ids are in LDS
 constexpr float kPtUnset = -3.40282347e38f;   // reference exponent of a row that has seen no key: no finite logit lies below it
 constexpr uint32_t kPtTwo = 0x40004000u;      // bits that only bf16 numbers of 2 and more have (and infinities and NaN)
+constexpr float kPtMost = 1.8446744e19f;      // 2^64: sums of a block's weights that leave room for all others
 constexpr float kPtHead = 8.f;                // a raised reference lies this far above the largest exponent so far
 constexpr float kPtBig = 1048576.f;           // references beyond this: the logits are rounded before it is taken off them
 
@@ -46,10 +51,11 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
   constexpr int NLD = WK / KPI;               // loads per wave, tile and pool
   constexpr int TILE_B = kPtTile * RB;
   constexpr int VH = D == 128 ? 32 : 16;      // what eight keys more flip of a piece's place
-  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];   // [buffer][K tile, V tile], page ids [wave][ring][64], the share's ends
+  extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];   // [buffer][K tile, V tile], page ids [wave][ring][64], the share's ends, a flag
   // (nothing else is in LDS: places of pieces are flipped in the address, so the tiles have to begin at a multiple of a row)
-  SharePlace* s_place = reinterpret_cast<SharePlace*>(smem + 4 * TILE_B + 4 * kPtRing * 256);
+  SharePlace* s_place = reinterpret_cast<SharePlace*>(smem + 2 * kPtBuf * TILE_B + 4 * kPtRing * 256);
   long* s_scan = reinterpret_cast<long*>(s_place + 2);
+  int* s_bad = reinterpret_cast<int*>(s_scan + 4);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5, col = lane & 31;
@@ -76,10 +82,10 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
   // staging: this wave's 16 keys of a tile, load i covering keys 16 * wave + i * KPI + lane / PPR
   const int st_key = lane / PPR, st_pos = lane % PPR;
   const uint32_t lds_st = __builtin_amdgcn_readfirstlane(lds_base + (uint32_t)(wave * WK * RB));
-  const uint32_t look = __builtin_amdgcn_readfirstlane(lds_base + (uint32_t)(4 * TILE_B + wave * kPtRing * 256));
+  const uint32_t look = __builtin_amdgcn_readfirstlane(lds_base + (uint32_t)(2 * kPtBuf * TILE_B + wave * kPtRing * 256));
   const int row_shift = 31 - __builtin_clz((uint32_t)(a.H_kv * RB));   // H_kv is a power of two
 
-  walk_share<kPtTile>(a, sh, G, from, to, [&](int kvh, const SeqShape& sq, int r, const TileKeys& keys, int ua, int ub) __attribute__((always_inline)) {
+  walk_share<kPtTile>(a, sh, G, from, to, [&](int kvh, const SeqShape& sq, int r, const TileKeys& keys, int ua, int ub, bool again) __attribute__((always_inline)) -> bool {
     const int c0 = r * sh.tpt, ntok = min(sh.tpt, sq.n - c0), nrows = ntok * G;
     const int row0 = sq.row0 + c0, x0 = sq.N - sq.n + c0, x1 = x0 + ntok - 1;   // first row; places of the first and last token
     const bool whole = ua == 0 && ub == keys.units;
@@ -91,7 +97,7 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
         reinterpret_cast<uint16_t*>(a.out)[o] = 0;
         if (i % D == 0 && a.lse != nullptr) a.lse[o / D] = -INFINITY;
       }
-      return;
+      return false;
     }
     const int slot = ua > 0 ? 0 : 1;
     if (!whole && threadIdx.x == 0) {
@@ -101,9 +107,9 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
     const int32_t* pages = a.page_indices + a.page_indptr[sq.b];
     const int key0 = (keys.u0 + ua) * kPtTile, nt = ub - ua;       // first key and number of tiles
     // tiles [f0, f1) are seen in full by every row
-    const int f0 = a.window > 0 ? max((x1 - a.window + 1 - key0 + kPtTile - 1) / kPtTile, 0) : 0;
-    int f1 = x0 >= key0 ? min((x0 + 1 - key0) / kPtTile, nt) : 0;       // (INT_MIN once the logits are rounded before the reference is taken off)
-    const bool idle = wave * 64 >= nrows;                          // no row of this wave's: it stages keys for the others
+    const int f0 = again ? nt : a.window > 0 ? max((x1 - a.window + 1 - key0 + kPtTile - 1) / kPtTile, 0) : 0;
+    int f1 = again ? 0 : x0 >= key0 ? min((x0 + 1 - key0) / kPtTile, nt) : 0;       // (INT_MIN once the logits are rounded before the reference is taken off)
+    bool bad = false;                                              // a weight beyond what the code without raising can take
 
     // ---- query fragments (B operand of K Q^T): of the wave's two blocks of 32 rows, lane holds row = col, k = 16 * ks + 8 * half .. + 8
     int vis[2], low[2];                                            // last and first key that the row sees
@@ -133,8 +139,8 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
         for (int e = 0; e < 16; ++e) oacc[rb][nb][e] = 0.f;
 
     // ---- Memory to LDS, 16 bytes per lane: the wave's 64 lanes fill 1 KiB from the (uniform) LDS address.  Written in assembly because the
-    // compiler, which cannot tell the buffers apart, makes every later LDS read wait for the builtin form; completion is
-    // awaited by the vmcnt(0) before a tile's barrier.  Page ids come the same way, one tile earlier.
+    // compiler, which cannot tell the buffers apart, makes every later LDS read wait for the builtin form; completion is awaited by the
+    // vmcnt before a tile's barrier.  Page ids come the same way, three tiles earlier.
     auto fetch_look = [&](int it) __attribute__((always_inline)) {
       const int t = min(key0 + it * kPtTile + wave * WK + (lane & (WK - 1)), tmax);
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(look + (it & (kPtRing - 1)) * 256), "v"(pages + (t >> a.p_shift)) : "memory", "m0");
@@ -149,11 +155,12 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
         at_k[i] = ((uint32_t)page << a.p_shift) + (uint32_t)(t & (a.P - 1));
       }
     };
-    auto load_row = [&](const uint8_t* pool, uint32_t at, int i, int tile_slot) __attribute__((always_inline)) {
+    auto load_row = [&](const uint8_t* pool, uint32_t at, int i, uint32_t place) __attribute__((always_inline)) {
       const uint64_t off = ((uint64_t)at << row_shift) + (uint32_t)(kvh * RB + ((st_pos ^ pt_swz<D>((wave * WK + i * KPI + st_key) & 15)) * 16));
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds_st + (uint32_t)(tile_slot * TILE_B + i * 1024)), "v"(pool + off) : "memory", "m0");
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds_st + place + (uint32_t)(i * 1024)), "v"(pool + off) : "memory", "m0");
     };
-    auto k_slot = [&](int buf) { return buf * 2; };                // tile slots of the LDS: [buffer][K, V]
+    // places of tiles it, it + 1 and it + 2 in LDS (of K; V lies TILE_B behind), handed on from tile to tile
+    uint32_t p0 = 0, p1 = 2 * TILE_B, p2 = 4 * TILE_B;
 
     // ---- blocks of 32 keys, two to a tile.  While the vector ALU forms the weights of block j, the matrix cores form the scores of
     // block j + 1 and add the output of block j - 1.
@@ -167,7 +174,7 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
     };
     constexpr int AHEAD = 3;
     bf16x8_t carry[AHEAD];
-    auto body = [&](auto half_c, int it, auto with_scores, auto with_output, auto with_loads, auto masked_c) __attribute__((always_inline)) {
+    auto body = [&](auto half_c, int it, uint32_t k_at, uint32_t v_at, auto with_scores, auto with_output, auto with_loads, auto masked_c) __attribute__((always_inline)) {
       constexpr int CUR = decltype(half_c)::value, NXT = 1 - CUR;  // this block is half CUR of tile `it`
       constexpr bool SC = decltype(with_scores)::value, OUT = decltype(with_output)::value, LD = decltype(with_loads)::value;
       constexpr bool MASKED = decltype(masked_c)::value;
@@ -183,8 +190,7 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
           }
         if (__builtin_expect(f1 == INT_MIN, 0)) round_logits(x);
       }
-      const uint32_t kt = ka0 + (uint32_t)(k_slot((it + CUR) & 1) * TILE_B + NXT * 32 * RB);
-      const uint32_t vt = va0 + (uint32_t)((k_slot((it + CUR + 1) & 1) + 1) * TILE_B + NXT * 32 * RB);
+      const uint32_t kt = ka0 + k_at + (uint32_t)(NXT * 32 * RB), vt = va0 + v_at + (uint32_t)(TILE_B + NXT * 32 * RB);
       constexpr int NS = KS + 2 * NBO, T0 = SC ? 0 : KS, T1 = OUT ? NS : KS; // steps: scores, then output; two products each
       constexpr int PPS = 16 / NS;                                 // pairs of weights per step
       constexpr bool CIN = CUR == 0 && OUT;                        // this block's first fragments were read at the end of the one before
@@ -217,7 +223,7 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
       auto pack = [&](int i) __attribute__((always_inline)) {
         const bf16x2_t p = {(__bf16)w[i][0], (__bf16)w[i][1]};
         pk[CUR][i >> 3][i & 7] = __builtin_bit_cast(uint32_t, p);
-        any |= pk[CUR][i >> 3][i & 7];
+        if (MASKED) any |= pk[CUR][i >> 3][i & 7];
 #pragma unroll
         for (int u = 0; u < 2; ++u) sum[i >> 3][u] += w[i][u];
       };
@@ -235,17 +241,17 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
         __builtin_amdgcn_sched_barrier(0);
         if (t >= T0 && t + AHEAD < T1) fetch(t + AHEAD);
         if (CUR == 1 && SC && t + AHEAD >= NS)                     // of K tile it + 1, second half
-          carry[t + AHEAD - NS] = *(lds_bf16x8*)((ka0 + (uint32_t)(k_slot((it + 1) & 1) * TILE_B + 32 * RB)) ^ (uint32_t)((t + AHEAD - NS) * 32));
+          carry[t + AHEAD - NS] = *(lds_bf16x8*)((ka0 + p1 + (uint32_t)(32 * RB)) ^ (uint32_t)((t + AHEAD - NS) * 32));
 #pragma unroll
         for (int i = t * PPS; i < (t + 1) * PPS; ++i) { if (i >= 2 * PPS) pack(i - 2 * PPS); exponent(i); }
         __builtin_amdgcn_sched_barrier(0);
         product(t, 1);
         __builtin_amdgcn_sched_barrier(0);
-        if (LD && t < NLD) {                                       // rows of K tile it + 2 and V tile it + 1
-          load_row(a.k_pool, at_k[t < NLD ? t : 0], t, k_slot(it & 1));
-          load_row(a.v_pool, at_v[t < NLD ? t : 0], t, k_slot((it + 1) & 1) + 1);
+        if (LD && t < NLD) {                                       // rows of K tile it + 3 and V tile it + 2
+          load_row(a.k_pool, at_k[t < NLD ? t : 0], t, p0);
+          load_row(a.v_pool, at_v[t < NLD ? t : 0], t, p2 + TILE_B);
         }
-        if (LD && t == NLD) { rows_of(it + 3); fetch_look(it + 4); }
+        if (LD && t == NLD) { rows_of(it + 4); fetch_look(it + 6); }
 #pragma unroll
         for (int i = t * PPS; i < (t + 1) * PPS; ++i) if (i >= PPS) power(i - PPS);
         __builtin_amdgcn_sched_barrier(0);
@@ -254,7 +260,8 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
       for (int i = 16 - PPS; i < 16; ++i) power(i);
 #pragma unroll
       for (int i = 16 - 2 * PPS; i < 16; ++i) pack(i);
-      if (__builtin_amdgcn_ballot_w64((any & kPtTwo) != 0u) != 0) {
+      if (!MASKED) bad = bad || !(fmaxf(sum[0][0] + sum[0][1], sum[1][0] + sum[1][1]) <= kPtMost);
+      if (MASKED && __builtin_amdgcn_ballot_w64((any & kPtTwo) != 0u) != 0) {
         // first visible key of a row, or a logit far above the reference.  Straight-line code: a branch per lane here
         // makes the compiler copy the accumulators on the common path too.
 #pragma unroll
@@ -276,9 +283,7 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
           // An fma's exact product is off by up to 2^-24 of the logit from the rounded one that the reference came from, and with logits of 2^31 that
           // alone would over- or underflow the exponential: from here on the logits are rounded first.
           factor = 1.f; f1 = INT_MIN;
-          round_logits(x);
-          // the code without masks takes one more block as it is, whose scores are there already; a masked block rounds its own
-          if (CUR == 1 && SC && !MASKED) round_logits(s[NXT]);
+          round_logits(x);                                         // (later blocks round their own)
         }
 #pragma unroll
         for (int rb = 0; rb < 2; ++rb) sum[rb][0] = sum[rb][1] = 0.f;
@@ -288,41 +293,40 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
       lsum[0] += sum[0][0] + sum[0][1];
       lsum[1] += sum[1][0] + sum[1][1];
     };
-    // Buffers: the barrier between the blocks of tile `it` says that K tile it + 1 and V tile `it` have arrived and that K tile
-    // `it` and V tile it - 1 have been read, whose places K tile it + 2 and V tile it + 1 then take.
-    auto tile_barrier = [&]() __attribute__((always_inline)) {
+    // Buffers: the barrier between the blocks of tile `it` says that K tile it + 1 and V tile `it` have arrived (and the page ids of tile
+    // it + 4) and that K tile `it` and V tile it - 1 have been read, whose places K tile it + 3 and V tile it + 2 then take.  What tile it - 1
+    // requested -- K tile it + 2, V tile it + 1, page ids -- stays in flight.
+    constexpr int BATCH = 2 * NLD + 1;
+    auto tile_barrier = [&](auto in_flight) __attribute__((always_inline)) {
       __builtin_amdgcn_sched_barrier(0);
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(decltype(in_flight)::value) : "memory");
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
       __builtin_amdgcn_sched_barrier(0);
     };
+    auto next_tile = [&]() __attribute__((always_inline)) { const uint32_t p = p0; p0 = p1; p1 = p2; p2 = p; };
+    using One = std::integral_constant<int, BATCH>;
     using B0 = std::integral_constant<int, 0>;
     using B1 = std::integral_constant<int, 1>;
     using Yes = std::true_type;
     using No = std::false_type;
-    __syncthreads();                                               // the tiles of the tile before have been read
+    __syncthreads();                                               // the tiles of the piece before have been read
+    if (threadIdx.x == 0) *s_bad = 0;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     fetch_look(0); fetch_look(1); fetch_look(2); fetch_look(3);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     rows_of(0);
 #pragma unroll
-    for (int i = 0; i < NLD; ++i) load_row(a.k_pool, at_k[i], i, k_slot(0));
-    rows_of(1);
+    for (int i = 0; i < NLD; ++i) load_row(a.k_pool, at_k[i], i, p0);
 #pragma unroll
-    for (int i = 0; i < NLD; ++i) { load_row(a.k_pool, at_k[i], i, k_slot(1)); load_row(a.v_pool, at_v[i], i, k_slot(0) + 1); }
-    rows_of(2);
-    tile_barrier();
-    if (idle) {
-      for (int it = 0; it + 1 < nt; ++it) {
-        tile_barrier();
+    for (int n = 1; n < 3; ++n) {                                  // K tile n, V tile n - 1
+      rows_of(n);
 #pragma unroll
-        for (int i = 0; i < NLD; ++i) { load_row(a.k_pool, at_k[i], i, k_slot(it & 1)); load_row(a.v_pool, at_v[i], i, k_slot((it + 1) & 1) + 1); }
-        rows_of(it + 3); fetch_look(it + 4);
-      }
-      tile_barrier();
-      return;
+      for (int i = 0; i < NLD; ++i) { load_row(a.k_pool, at_k[i], i, n == 1 ? p1 : p2); load_row(a.v_pool, at_v[i], i, (n == 1 ? p0 : p1) + TILE_B); }
+      fetch_look(n + 3);
     }
+    rows_of(3);
+    tile_barrier(std::integral_constant<int, 2 * BATCH>{});
     // the scores of the first block
 #pragma unroll
     for (int rb = 0; rb < 2; ++rb)
@@ -330,33 +334,36 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
       for (int e = 0; e < 16; ++e) s[0][rb][e] = 0.f;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      const bf16x8_t av = *(lds_bf16x8*)((ka0 + (uint32_t)(k_slot(0) * TILE_B)) ^ (uint32_t)(ks * 32));
+      const bf16x8_t av = *(lds_bf16x8*)((ka0 + p0) ^ (uint32_t)(ks * 32));
 #pragma unroll
       for (int rb = 0; rb < 2; ++rb) s[0][rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, qfrag[rb][ks], s[0][rb], 0, 0, 0);
     }
-    body(B0{}, 0, Yes{}, No{}, No{}, Yes{});
+    body(B0{}, 0, p0, p0, Yes{}, No{}, No{}, Yes{});
     // tiles in turn: second half of tile `it`, first half of tile it + 1.  (Three loops and not one: with both copies of the code in one loop
     // the compiler spills registers.)
     int it = 0;
     for (; it + 1 < nt && it < f0; ++it) {
-      tile_barrier();
-      body(B1{}, it, Yes{}, Yes{}, Yes{}, Yes{});
-      body(B0{}, it + 1, Yes{}, Yes{}, No{}, Yes{});
+      tile_barrier(One{});
+      body(B1{}, it, p1, p0, Yes{}, Yes{}, Yes{}, Yes{});
+      body(B0{}, it + 1, p1, p0, Yes{}, Yes{}, No{}, Yes{});
+      next_tile();
     }
     for (; it + 1 < f1; ++it) {
-      tile_barrier();
-      body(B1{}, it, Yes{}, Yes{}, Yes{}, No{});
-      body(B0{}, it + 1, Yes{}, Yes{}, No{}, No{});
+      tile_barrier(One{});
+      body(B1{}, it, p1, p0, Yes{}, Yes{}, Yes{}, No{});
+      body(B0{}, it + 1, p1, p0, Yes{}, Yes{}, No{}, No{});
+      next_tile();
     }
     for (; it + 1 < nt; ++it) {
-      tile_barrier();
-      body(B1{}, it, Yes{}, Yes{}, Yes{}, Yes{});
-      body(B0{}, it + 1, Yes{}, Yes{}, No{}, Yes{});
+      tile_barrier(One{});
+      body(B1{}, it, p1, p0, Yes{}, Yes{}, Yes{}, Yes{});
+      body(B0{}, it + 1, p1, p0, Yes{}, Yes{}, No{}, Yes{});
+      next_tile();
     }
-    tile_barrier();
-    body(B1{}, nt - 1, No{}, Yes{}, No{}, Yes{});
+    tile_barrier(One{});
+    body(B1{}, nt - 1, p1, p0, No{}, Yes{}, No{}, Yes{});
     // the output of the last block
-    const uint32_t vt = va0 + (uint32_t)((k_slot((nt - 1) & 1) + 1) * TILE_B + 32 * RB);
+    const uint32_t vt = va0 + p0 + (uint32_t)(TILE_B + 32 * RB);
 #pragma unroll
     for (int k2 = 0; k2 < 2; ++k2)
 #pragma unroll
@@ -374,6 +381,9 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
                                                                  oacc[rb][nb], 0, 0, 0);
         }
       }
+    if (__builtin_amdgcn_ballot_w64(bad) != 0) *s_bad = 1;
+    __syncthreads();
+    if (*s_bad != 0) return true;
 
 #pragma unroll
     for (int rb = 0; rb < 2; ++rb) {
@@ -407,12 +417,13 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
         }
       }
     }
+    return false;
   });
 }
 
 template <int D>
 static hipError_t tall_one(const PagedAttnArgs& a, const ShareArgs& sh, hipStream_t s) {
-  constexpr int lds = 4 * kPtTile * D * 2 + 4 * kPtRing * 256 + 64;
+  constexpr int lds = 2 * kPtBuf * kPtTile * D * 2 + 4 * kPtRing * 256 + 128;
   if (lds > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_tall_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;

@@ -129,17 +129,19 @@ __device__ __forceinline__ int next_sequence(const PagedAttnArgs& a, const Share
   return a.B;
 }
 
-// A workgroup's walk over its share: fn(kvh, shape, r, keys, ua, ub) for units [ua, ub) of every tile in it.
+// A workgroup's walk over its share: fn(kvh, shape, r, keys, ua, ub, again) for units [ua, ub) of every tile in it; where it returns true it is
+// called again, with `again` set.
 template <int KT, typename F>
 __device__ __forceinline__ void walk_share(const PagedAttnArgs& a, const ShareArgs& sh, int G, const SharePlace& from, const SharePlace& to, F&& fn) {
   int kvh = from.kvh, b = from.b, r = from.r, ua = from.u;
   if (kvh >= a.H_kv) return;
   SeqShape s = seq_shape(a, sh, G, b);
+  bool again = false;
   for (;;) {
     const bool last = kvh == to.kvh && b == to.b && r == to.r;
     const TileKeys k = tile_keys<KT>(a, sh, s, r);
     const int ub = last ? to.u : k.units;
-    if (ub > ua) fn(kvh, s, r, k, ua, ub);
+    if (ub > ua) { again = fn(kvh, s, r, k, ua, ub, again); if (again) continue; }
     if (last) return;
     ua = 0;
     if (++r < s.tiles) continue;
