@@ -47,7 +47,7 @@ int32_t ts_paged_attn(const ts_problem* p, const void* q, const int32_t* q_indpt
   a.page_indptr = p->page_indptr; a.page_indices = p->page_indices; a.seq_lens = p->seq_lens; a.q_indptr = q_indptr;
   a.out = (uint8_t*)out; a.lse = lse;
   a.B = p->batch; a.C = p->chunk; a.T = num_rows; a.H = p->num_q_heads; a.H_kv = p->num_kv_heads;
-  a.P = p->page_size; a.p_shift = ilog2(p->page_size); a.max_seq_len = p->max_seq_len; a.window = window;
+  a.P = p->page_size; a.p_shift = ilog2(p->page_size); a.max_seq_len = p->max_seq_len; a.window = window < p->max_seq_len ? window : 0;   // one that reaches every token is none
   a.sm_scale = sm_scale;
   return launch_paged_attn(p->dtype, p->head_dim, a, ws, (hipStream_t)stream) == hipSuccess ? TS_OK : TS_ERR_HIP;
 }

@@ -2,6 +2,7 @@
 // merge of the tiles that shares have cut.
 #include "paged_shares.h"
 #include <limits.h>
+#include <algorithm>
 
 namespace ts {
 
@@ -10,21 +11,19 @@ hipError_t launch_paged_tall(int D, const PagedAttnArgs& a, const ShareArgs& sh,
 
 constexpr int kStreamWgs = 512, kTallWgs = 256, kTallRows = 256;
 
-// Joins the pieces of the tiles that were cut: a workgroup column stands for the workgroup whose share began the tile, the
-// pieces that follow lie in the workgroups behind it, up to the one that ends the tile.  RPB rows per workgroup, D / 4 lanes per
-// row, PG groups of lanes that share the pieces.
-template <int ES, int D, int RPB, int PG>
-__global__ __launch_bounds__((D / 4) * RPB * PG) void paged_merge_kernel(PagedAttnArgs a, ShareArgs sh, int rows) {
-  constexpr int LPR = D / 4;
+// Joins the pieces of the tiles that were cut: blockIdx.y stands for the workgroup whose share began the tile, the
+// pieces that follow lie in the workgroups behind it, up to the one that ends the tile.  D / 4 lanes per row, RPT rows per lane, PG
+// groups of lanes that share the pieces, US of which a lane has in flight: many of which may belong to a tile.
+template <int ES, int D, int THREADS, int RPT, int PG, int US>
+__global__ __launch_bounds__(THREADS) void paged_merge_kernel(PagedAttnArgs a, ShareArgs sh, int rows) {
+  constexpr int LPR = D / 4, LR = THREADS / (LPR * PG), RPB = LR * RPT;   // rows side by side, rows per workgroup
   __shared__ float4 s_o[PG][RPB][LPR];
   __shared__ float s_ml[PG][RPB][2];
-  const int w = blockIdx.x, G = a.H / a.H_kv;
+  const int w = blockIdx.y, G = a.H / a.H_kv;     // (rows first: the tiles that were cut may all be every fourth workgroup's, and so on two XCDs)
   const int32_t* d1 = sh.desc + (size_t)w * 8 + 4;
   if (d1[3] == kPieceNone) return;
   const int row0 = d1[0], kvh = d1[1], nrows = d1[2] * G;
-  const int lane = threadIdx.x & 63, sub = threadIdx.x % LPR, rr = threadIdx.x / LPR % RPB, pg = threadIdx.x / (LPR * RPB);
-  const int j = blockIdx.y * RPB + rr;
-  if ((int)blockIdx.y * RPB >= nrows) return;
+  const int lane = threadIdx.x & 63, sub = threadIdx.x % LPR, rr = threadIdx.x / LPR % LR, pg = threadIdx.x / (LPR * LR);
   int pieces = 1;                                       // this workgroup's, and those of the workgroups w + 1 .. w + pieces - 1
   for (;; pieces += 64) {
     const int i = w + pieces + lane;
@@ -32,69 +31,161 @@ __global__ __launch_bounds__((D / 4) * RPB * PG) void paged_merge_kernel(PagedAt
     if (end != 0) { pieces += __builtin_ctzll(end) + 1; break; }
   }
   pieces = min(pieces, sh.wgs - w);
+  for (int j0 = blockIdx.x * RPB; j0 < nrows; j0 += gridDim.x * RPB) {
+    float M[RPT], L[RPT];
+    float4 o[RPT];
+#pragma unroll
+    for (int t = 0; t < RPT; ++t) { M[t] = -INFINITY; L[t] = 0.f; o[t] = make_float4(0.f, 0.f, 0.f, 0.f); }
+    for (int p0 = pg; p0 < pieces; p0 += PG * US) {
+      float2 v[RPT][US];
+      float4 x[RPT][US];
+#pragma unroll
+      for (int u = 0; u < US; ++u) {
+        const int p = p0 + u * PG;
+        const size_t slot = (size_t)(w + p) * 2 + (p == 0 ? 1 : 0);
+        const bool there = p < pieces && (p == 0 || sh.desc[slot * 4 + 3] != kPieceNone);   // a share may hold no unit
+#pragma unroll
+        for (int t = 0; t < RPT; ++t) {
+          const int j = j0 + t * LR + rr;
+          v[t][u] = make_float2(-INFINITY, 0.f);
+          x[t][u] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (!there || j >= nrows) continue;
+          v[t][u] = *reinterpret_cast<const float2*>(sh.part_ml + (slot * rows + j) * 2);
+          x[t][u] = *reinterpret_cast<const float4*>(sh.part_o + (slot * rows + j) * D + sub * 4);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < RPT; ++t) {
+        float m = M[t];
+#pragma unroll
+        for (int u = 0; u < US; ++u) m = fmaxf(m, v[t][u].x);
+        if (m == -INFINITY) continue;
+        const float f = expf(M[t] - m);
+        L[t] *= f; o[t].x *= f; o[t].y *= f; o[t].z *= f; o[t].w *= f;
+#pragma unroll
+        for (int u = 0; u < US; ++u) {
+          const float g = expf(v[t][u].x - m);
+          L[t] = fmaf(g, v[t][u].y, L[t]);
+          o[t].x = fmaf(g, x[t][u].x, o[t].x); o[t].y = fmaf(g, x[t][u].y, o[t].y);
+          o[t].z = fmaf(g, x[t][u].z, o[t].z); o[t].w = fmaf(g, x[t][u].w, o[t].w);
+        }
+        M[t] = m;
+      }
+    }
+    if constexpr (PG > 1) {
+#pragma unroll
+      for (int t = 0; t < RPT; ++t) {
+        s_o[pg][t * LR + rr][sub] = o[t];
+        if (sub == 0) { s_ml[pg][t * LR + rr][0] = M[t]; s_ml[pg][t * LR + rr][1] = L[t]; }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int t = 0; t < RPT; ++t) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int g = 0; g < PG; ++g) m = fmaxf(m, s_ml[g][t * LR + rr][0]);
+        L[t] = 0.f; o[t] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (m != -INFINITY)
+#pragma unroll
+          for (int g = 0; g < PG; ++g) {
+            const float f = expf(s_ml[g][t * LR + rr][0] - m);
+            const float4 x = s_o[g][t * LR + rr][sub];
+            L[t] = fmaf(f, s_ml[g][t * LR + rr][1], L[t]);
+            o[t].x = fmaf(f, x.x, o[t].x); o[t].y = fmaf(f, x.y, o[t].y); o[t].z = fmaf(f, x.z, o[t].z); o[t].w = fmaf(f, x.w, o[t].w);
+          }
+        M[t] = m;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < RPT; ++t) {
+      const int j = j0 + t * LR + rr;
+      if (j >= nrows || pg != 0) continue;
+      const size_t hb = (size_t)(row0 + j / G) * a.H + kvh * G + j % G;
+      const float4 y = L[t] > 0.f ? make_float4(o[t].x / L[t], o[t].y / L[t], o[t].z / L[t], o[t].w / L[t]) : make_float4(0.f, 0.f, 0.f, 0.f);
+      if (ES == 2)
+        *reinterpret_cast<uint2*>(a.out + (hb * D + sub * 4) * 2) = make_uint2(f32_to_bf16_bits(y.x) | (f32_to_bf16_bits(y.y) << 16), f32_to_bf16_bits(y.z) | (f32_to_bf16_bits(y.w) << 16));
+      else *reinterpret_cast<float4*>(a.out + (hb * D + sub * 4) * 4) = y;
+      if (sub == 0 && a.lse != nullptr) a.lse[hb] = L[t] > 0.f ? M[t] + logf(L[t]) : -INFINITY;
+    }
+    if (PG > 1) __syncthreads();                        // the next rows take the same place
+  }
+}
+
+// The same for the tall kernel, whose pieces lie as in its registers: of each block of 32 rows (blockIdx.x), 16 bytes of the output
+// [D / 8][64 lanes], the lane's row lane % 32, its elements 8 i + 4 (lane / 32) .. + 3.
+template <int D>
+__global__ __launch_bounds__(256) void paged_merge_tall_kernel(PagedAttnArgs a, ShareArgs sh) {
+  constexpr int NT = D / 32, US = 3;                    // 16-byte pieces per thread, partial results in flight
+  const int w = blockIdx.y, G = a.H / a.H_kv;
+  const int32_t* d1 = sh.desc + (size_t)w * 8 + 4;
+  if (d1[3] == kPieceNone) return;
+  const int row0 = d1[0], kvh = d1[1], nrows = d1[2] * G;
+  const int lane = threadIdx.x & 63, j = blockIdx.x * 32 + (lane & 31);
+  if ((int)blockIdx.x * 32 >= nrows) return;
+  int pieces = 1;
+  for (;; pieces += 64) {
+    const int i = w + pieces + lane;
+    const uint64_t end = __builtin_amdgcn_ballot_w64(i >= sh.wgs || sh.desc[(size_t)i * 8 + 3] == kPieceEnds);
+    if (end != 0) { pieces += __builtin_ctzll(end) + 1; break; }
+  }
+  pieces = min(pieces, sh.wgs - w);
   float M = -INFINITY, L = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  constexpr int US = 4;                                 // pieces in flight per lane
-  for (int p0 = pg; p0 < pieces; p0 += PG * US) {
+  float4 o[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) o[t] = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int p0 = 0; p0 < pieces; p0 += US) {
     float2 v[US];
-    float4 x[US];
+    float4 x[US][NT];
 #pragma unroll
     for (int u = 0; u < US; ++u) {
-      const int p = p0 + u * PG;
-      v[u] = make_float2(-INFINITY, 0.f);
-      x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (p >= pieces || j >= nrows) continue;
+      const int p = p0 + u;
       const size_t slot = (size_t)(w + p) * 2 + (p == 0 ? 1 : 0);
-      if (p > 0 && sh.desc[slot * 4 + 3] == kPieceNone) continue;      // a share without a unit
-      v[u] = *reinterpret_cast<const float2*>(sh.part_ml + (slot * rows + j) * 2);
-      x[u] = *reinterpret_cast<const float4*>(sh.part_o + (slot * rows + j) * D + sub * 4);
+      const bool there = p < pieces && (p == 0 || sh.desc[slot * 4 + 3] != kPieceNone);   // a share may hold no unit
+      v[u] = make_float2(-INFINITY, 0.f);
+      if (there) v[u] = *reinterpret_cast<const float2*>(sh.part_ml + (slot * kTallRows + j) * 2);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        x[u][t] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (there) x[u][t] = *(reinterpret_cast<const float4*>(sh.part_o + slot * kTallRows * D) + (size_t)blockIdx.x * (D / 8 * 64) + t * 256 + threadIdx.x);
+      }
     }
     float m = M;
 #pragma unroll
     for (int u = 0; u < US; ++u) m = fmaxf(m, v[u].x);
     if (m == -INFINITY) continue;
     const float f = expf(M - m);
-    L *= f; o.x *= f; o.y *= f; o.z *= f; o.w *= f;
+    L *= f;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) { o[t].x *= f; o[t].y *= f; o[t].z *= f; o[t].w *= f; }
 #pragma unroll
     for (int u = 0; u < US; ++u) {
       const float g = expf(v[u].x - m);
       L = fmaf(g, v[u].y, L);
-      o.x = fmaf(g, x[u].x, o.x); o.y = fmaf(g, x[u].y, o.y); o.z = fmaf(g, x[u].z, o.z); o.w = fmaf(g, x[u].w, o.w);
-    }
-    M = m;
-  }
-  if constexpr (PG > 1) {
-    s_o[pg][rr][sub] = o;
-    if (sub == 0) { s_ml[pg][rr][0] = M; s_ml[pg][rr][1] = L; }
-    __syncthreads();
-    if (pg != 0) return;
-    float m = -INFINITY;
 #pragma unroll
-    for (int g = 0; g < PG; ++g) m = fmaxf(m, s_ml[g][rr][0]);
-    L = 0.f; o = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (m != -INFINITY)
-#pragma unroll
-      for (int g = 0; g < PG; ++g) {
-        const float f = expf(s_ml[g][rr][0] - m);
-        const float4 x = s_o[g][rr][sub];
-        L = fmaf(f, s_ml[g][rr][1], L);
-        o.x = fmaf(f, x.x, o.x); o.y = fmaf(f, x.y, o.y); o.z = fmaf(f, x.z, o.z); o.w = fmaf(f, x.w, o.w);
+      for (int t = 0; t < NT; ++t) {
+        o[t].x = fmaf(g, x[u][t].x, o[t].x); o[t].y = fmaf(g, x[u][t].y, o[t].y);
+        o[t].z = fmaf(g, x[u][t].z, o[t].z); o[t].w = fmaf(g, x[u][t].w, o[t].w);
       }
+    }
     M = m;
   }
   if (j >= nrows) return;
   const size_t hb = (size_t)(row0 + j / G) * a.H + kvh * G + j % G;
-  o = L > 0.f ? make_float4(o.x / L, o.y / L, o.z / L, o.w / L) : make_float4(0.f, 0.f, 0.f, 0.f);
-  if (ES == 2)
-    *reinterpret_cast<uint2*>(a.out + (hb * D + sub * 4) * 2) = make_uint2(f32_to_bf16_bits(o.x) | (f32_to_bf16_bits(o.y) << 16), f32_to_bf16_bits(o.z) | (f32_to_bf16_bits(o.w) << 16));
-  else *reinterpret_cast<float4*>(a.out + (hb * D + sub * 4) * 4) = o;
-  if (sub == 0 && a.lse != nullptr) a.lse[hb] = L > 0.f ? M + logf(L) : -INFINITY;
+  const float inv = L > 0.f ? 1.f / L : 0.f;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int d = 8 * (t * 4 + (threadIdx.x >> 6)) + 4 * (lane >> 5);
+    *reinterpret_cast<uint2*>(a.out + (hb * D + d) * 2) = make_uint2(f32_to_bf16_bits(o[t].x * inv) | (f32_to_bf16_bits(o[t].y * inv) << 16),
+                                                                     f32_to_bf16_bits(o[t].z * inv) | (f32_to_bf16_bits(o[t].w * inv) << 16));
+  }
+  if (threadIdx.x < 32 && a.lse != nullptr) a.lse[hb] = L > 0.f ? M + logf(L) : -INFINITY;
 }
 
 template <int ES, int D>
 static hipError_t merge(const PagedAttnArgs& a, const ShareArgs& sh, int rows, hipStream_t s) {
-  if (rows <= 64) hipLaunchKernelGGL((paged_merge_kernel<ES, D, 4, 8>), dim3(sh.wgs, rows / 4), dim3(D * 8), 0, s, a, sh, rows);
-  else hipLaunchKernelGGL((paged_merge_kernel<ES, D, 8, 1>), dim3(sh.wgs, rows / 8), dim3(D * 2), 0, s, a, sh, rows);
+  // (a tile with more rows than the bound says takes turns; the tall kernel's tiles are short only where their sequence is)
+  if (rows != kTallRows) hipLaunchKernelGGL((paged_merge_kernel<ES, D, D * 8, 1, 8, 4>), dim3((std::min(sh.tpt, a.C) * (a.H / a.H_kv) + 3) / 4, sh.wgs), dim3(D * 8), 0, s, a, sh, rows);
+  else hipLaunchKernelGGL(paged_merge_tall_kernel<D>, dim3(kTallRows / 32, sh.wgs), dim3(256), 0, s, a, sh);
   return hipGetLastError();
 }
 
@@ -141,6 +232,7 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
     const bool tall = !few && dtype == TS_BF16;
     const int kt = tall ? 64 : dtype == TS_BF16 ? 128 : 64;
     sh.min_keys = 2 * kt;
+    sh.tile_cost = tall ? 256 : 64;
     sh.wgs = most_wgs;
     hipError_t e;
     if (tall) e = launch_paged_tall(D, a, sh, s);

@@ -9,7 +9,6 @@
 // bf16 weights keep their 24 bits: each is the sum of three bf16 numbers, and V is multiplied with each of them.  The
 // softmax's reference is raised only when a weight exceeds what it allows, so that no maximum is taken in the loop.
 #include "paged_shares.h"
-#include <limits.h>
 
 namespace ts {
 
@@ -49,8 +48,7 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
   constexpr int DB = D / 16;                  // 16-row blocks of the transposed output
   constexpr int NQ = D / (ES == 2 ? 32 : 16); // 16-byte pieces of a query row per lane
   extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-  __shared__ SharePlace s_place[2];
-  __shared__ long s_scan[4];
+  __shared__ ShareScratch s_share;
   __shared__ float s_ml[4][16][2];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -58,7 +56,7 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
   const int H = a.H, G = a.H / a.H_kv;
   const int wg = share_of(blockIdx.x, sh.wgs);
   SharePlace from, to;
-  find_share<KT, 256>(a, sh, G, wg, s_place, s_scan, &from, &to);
+  find_share<KT, 256>(a, sh, G, wg, &s_share, &from, &to);
   int32_t* desc = sh.desc + (size_t)wg * 8;
   if (!sh.whole && threadIdx.x == 0) { desc[3] = kPieceNone; desc[7] = kPieceNone; }
 
@@ -68,6 +66,7 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
   const volatile int32_t* look = reinterpret_cast<const volatile int32_t*>(vt + TILE_B);   // two places of 64 page ids
   const int st_row = lane / PPR, st_pos = lane % PPR;
   const float sm = a.sm_scale;
+  const uint32_t reach = a.window > 0 ? (uint32_t)a.window : 0x7fffffffu;
 
   walk_share<KT>(a, sh, G, from, to, [&](int kvh, const SeqShape& sq, int r, const TileKeys& keys, int ua, int ub, bool) -> bool {
     const int c0 = r * sh.tpt, ntok = min(sh.tpt, sq.n - c0), nrows = ntok * G;
@@ -90,14 +89,13 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
     }
     const int32_t* pages = a.page_indices + a.page_indptr[sq.b];
 
-    // query rows (zero past the last): 16-byte pieces 4 i + kgrp of row cb * 16 + col; the row's place and the first key it sees
+    // query rows (zero past the last): 16-byte pieces 4 i + kgrp of row cb * 16 + col
     uint4 qf[CB][NQ];
-    int x[CB], low[CB];
+    uint32_t low[CB];                                              // first of the `reach` keys that the row sees (modulo 2^32: it may lie before key 0)
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
       const int j = cb * 16 + col;
-      x[cb] = j < nrows ? x0 + j / G : x1;
-      low[cb] = a.window > 0 ? x[cb] - a.window + 1 : INT_MIN;
+      low[cb] = (uint32_t)(j < nrows ? x0 + j / G : x1) - (reach - 1u);
 #pragma unroll
       for (int i = 0; i < NQ; ++i) {
         qf[cb][i] = make_uint4(0u, 0u, 0u, 0u);
@@ -199,7 +197,7 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                     // the K tile has been read
       if (more) { rows_of(i + 1, (i + 1) & 1); fetch_look(i + 2, i & 1); load_rows(a.k_pool, lds_k); }
       // ---- weights against the reference: exp(logit - reference)
-      const bool masked = k0 + TK - 1 > x0 || (a.window > 0 && k0 < x1 - a.window + 1);   // some row does not see some key
+      const bool masked = k0 + TK - 1 > x0 || (a.window > 0 && k0 <= x1 - a.window);   // some row does not see some key
       float p[CB][NE];
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) {
@@ -209,8 +207,7 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
           if (masked || big) {
 #pragma unroll
             for (int e = 0; e < NE; ++e) {
-              const int key = k0 + 16 * (e >> 2) + 4 * kgrp + (e & 3);
-              const float y = key <= x[cb] && key >= low[cb] ? s[cb][e] * sm : -INFINITY;
+              const float y = (uint32_t)(k0 + 16 * (e >> 2) + 4 * kgrp + (e & 3)) - low[cb] < reach ? s[cb][e] * sm : -INFINITY;
               p[cb][e] = __builtin_amdgcn_exp2f((y - ref[cb]) * kPsLog2e);
               sum += p[cb][e];
             }
@@ -225,8 +222,7 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
           float m = ref[cb];                                                 // first keys, or a logit far above the reference
 #pragma unroll
           for (int e = 0; e < NE; ++e) {
-            const int key = k0 + 16 * (e >> 2) + 4 * kgrp + (e & 3);
-            m = fmaxf(m, key <= x[cb] && key >= low[cb] ? s[cb][e] * sm + kPsHead : -INFINITY);
+            m = fmaxf(m, (uint32_t)(k0 + 16 * (e >> 2) + 4 * kgrp + (e & 3)) - low[cb] < reach ? s[cb][e] * sm + kPsHead : -INFINITY);
           }
           m = fmaxf(m, __shfl_xor(m, 16));
           m = fmaxf(m, __shfl_xor(m, 32));

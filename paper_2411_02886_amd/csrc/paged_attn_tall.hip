@@ -53,19 +53,20 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
   constexpr int VH = D == 128 ? 32 : 16;      // what eight keys more flip of a piece's place
   extern __shared__ __attribute__((aligned(1024))) uint8_t smem[];   // [buffer][K tile, V tile], page ids [wave][ring][64], the share's ends, a flag
   // (nothing else is in LDS: places of pieces are flipped in the address, so the tiles have to begin at a multiple of a row)
-  SharePlace* s_place = reinterpret_cast<SharePlace*>(smem + 2 * kPtBuf * TILE_B + 4 * kPtRing * 256);
-  long* s_scan = reinterpret_cast<long*>(s_place + 2);
-  int* s_bad = reinterpret_cast<int*>(s_scan + 4);
+  ShareScratch* s_share = reinterpret_cast<ShareScratch*>(smem + 2 * kPtBuf * TILE_B + 4 * kPtRing * 256);
+  int* s_bad = reinterpret_cast<int*>(s_share + 1);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int half = lane >> 5, col = lane & 31;
   const int H = a.H, G = a.H / a.H_kv;
   const int wg = share_of(blockIdx.x, sh.wgs);
   SharePlace from, to;
-  find_share<kPtTile, 256>(a, sh, G, wg, s_place, s_scan, &from, &to);
+  find_share<kPtTile, 256>(a, sh, G, wg, s_share, &from, &to);
   int32_t* desc = sh.desc + (size_t)wg * 8;
   if (!sh.whole && threadIdx.x == 0) { desc[3] = kPieceNone; desc[7] = kPieceNone; }
 
+  const uint32_t g_inv = 65536u / (uint32_t)G + 1u;             // exact for rows below 256
+  const uint32_t reach = a.window > 0 ? (uint32_t)a.window : 0x7fffffffu;
   float c2 = a.sm_scale * 1.44269504088896340736f;
   if (c2 == 0.f) c2 = 1e-37f;                                   // the same weights (all 1), and a hidden key still gets 0
   const float hidden = c2 > 0.f ? -INFINITY : INFINITY;         // c2 * hidden = -inf
@@ -90,7 +91,8 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
     const int row0 = sq.row0 + c0, x0 = sq.N - sq.n + c0, x1 = x0 + ntok - 1;   // first row; places of the first and last token
     const bool whole = ua == 0 && ub == keys.units;
     const int tmax = keys.end - 1;
-    auto out_row = [&](int j) -> size_t { return (size_t)(row0 + j / G) * H + kvh * G + j % G; };
+    auto token_of = [&](int j) -> int { return (int)(((uint32_t)j * g_inv) >> 16); };   // j / G
+    auto out_row = [&](int j) -> size_t { const int c = token_of(j); return (size_t)(row0 + c) * H + kvh * G + (j - c * G); };
     if (keys.end <= keys.first) {                                  // no row sees a token (one unit: the tile is not cut)
       for (int i = threadIdx.x; i < nrows * D; i += 256) {
         const size_t o = out_row(i / D) * D + i % D;
@@ -107,36 +109,9 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
     const int32_t* pages = a.page_indices + a.page_indptr[sq.b];
     const int key0 = (keys.u0 + ua) * kPtTile, nt = ub - ua;       // first key and number of tiles
     // tiles [f0, f1) are seen in full by every row
-    const int f0 = again ? nt : a.window > 0 ? max((x1 - a.window + 1 - key0 + kPtTile - 1) / kPtTile, 0) : 0;
+    const int f0 = again ? nt : a.window > 0 ? max((x1 - key0 - a.window + kPtTile) / kPtTile, 0) : 0;
     int f1 = again ? 0 : x0 >= key0 ? min((x0 + 1 - key0) / kPtTile, nt) : 0;       // (INT_MIN once the logits are rounded before the reference is taken off)
     bool bad = false;                                              // a weight beyond what the code without raising can take
-
-    // ---- query fragments (B operand of K Q^T): of the wave's two blocks of 32 rows, lane holds row = col, k = 16 * ks + 8 * half .. + 8
-    int vis[2], low[2];                                            // last and first key that the row sees
-    bf16x8_t qfrag[2][KS];
-#pragma unroll
-    for (int rb = 0; rb < 2; ++rb) {
-      const int j = wave * 64 + rb * 32 + col;
-      vis[rb] = j < nrows ? x0 + j / G : x1;
-      low[rb] = a.window > 0 ? vis[rb] - a.window + 1 : INT_MIN;
-      const uint8_t* qp = a.q + (out_row(min(j, nrows - 1)) * D + 8 * half) * 2;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (j < nrows) v = *reinterpret_cast<const uint4*>(qp + ks * 32);
-        qfrag[rb][ks] = __builtin_bit_cast(bf16x8_t, v);
-      }
-    }
-    float ref[2] = {kPtUnset, kPtUnset};                           // the rows' reference exponents
-    float lsum[2] = {0.f, 0.f};                                    // this lane's keys' weights
-    float factor = c2;                                             // 1 once the logits are rounded first
-    f32x16_t oacc[2][NBO];                                         // O^T: d = 32 * nb + 8 * (e / 4) + 4 * half + e % 4
-#pragma unroll
-    for (int rb = 0; rb < 2; ++rb)
-#pragma unroll
-      for (int nb = 0; nb < NBO; ++nb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) oacc[rb][nb][e] = 0.f;
 
     // ---- Memory to LDS, 16 bytes per lane: the wave's 64 lanes fill 1 KiB from the (uniform) LDS address.  Written in assembly because the
     // compiler, which cannot tell the buffers apart, makes every later LDS read wait for the builtin form; completion is awaited by the
@@ -162,6 +137,35 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
     // places of tiles it, it + 1 and it + 2 in LDS (of K; V lies TILE_B behind), handed on from tile to tile
     uint32_t p0 = 0, p1 = 2 * TILE_B, p2 = 4 * TILE_B;
 
+    fetch_look(0); fetch_look(1); fetch_look(2); fetch_look(3);
+
+    // ---- query fragments (B operand of K Q^T): of the wave's two blocks of 32 rows, lane holds row = col, k = 16 * ks + 8 * half .. + 8
+    uint32_t low[2];                                               // first of the `reach` keys that the row sees (modulo 2^32: it may lie before key 0)
+    bf16x8_t qfrag[2][KS];
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb) {
+      const int j = wave * 64 + rb * 32 + col;
+      low[rb] = (uint32_t)(j < nrows ? x0 + token_of(j) : x1) - (reach - 1u);
+      const uint8_t* qp = a.q + (out_row(min(j, nrows - 1)) * D + 8 * half) * 2;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (j < nrows) v = *reinterpret_cast<const uint4*>(qp + ks * 32);
+        qfrag[rb][ks] = __builtin_bit_cast(bf16x8_t, v);
+      }
+    }
+    float ref[2] = {kPtUnset, kPtUnset};                           // the rows' reference exponents
+    float lsum[2] = {0.f, 0.f};                                    // this lane's keys' weights
+    float factor = c2;                                             // 1 once the logits are rounded first
+    f32x16_t oacc[2][NBO];                                         // O^T: d = 32 * nb + 8 * (e / 4) + 4 * half + e % 4
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+      for (int nb = 0; nb < NBO; ++nb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) oacc[rb][nb][e] = 0.f;
+
+
     // ---- blocks of 32 keys, two to a tile.  While the vector ALU forms the weights of block j, the matrix cores form the scores of
     // block j + 1 and add the output of block j - 1.
     f32x16_t s[2][2];                                              // [block parity][row block] S^T: key 8 * (e / 4) + 4 * half + e % 4
@@ -185,8 +189,8 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
         for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const int key = j0 + 8 * (e >> 2) + (e & 3);
-            x[rb][e] = key <= vis[rb] && key >= low[rb] ? x[rb][e] : hidden;
+            const uint32_t key = (uint32_t)(j0 + 8 * (e >> 2) + (e & 3)) - low[rb];   // counted from the first that the row sees
+            x[rb][e] = key < reach ? x[rb][e] : hidden;
           }
         if (__builtin_expect(f1 == INT_MIN, 0)) round_logits(x);
       }
@@ -312,9 +316,7 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
     using No = std::false_type;
     __syncthreads();                                               // the tiles of the piece before have been read
     if (threadIdx.x == 0) *s_bad = 0;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    fetch_look(0); fetch_look(1); fetch_look(2); fetch_look(3);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // page ids and queries
     rows_of(0);
 #pragma unroll
     for (int i = 0; i < NLD; ++i) load_row(a.k_pool, at_k[i], i, p0);
@@ -337,6 +339,15 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
       const bf16x8_t av = *(lds_bf16x8*)((ka0 + p0) ^ (uint32_t)(ks * 32));
 #pragma unroll
       for (int rb = 0; rb < 2; ++rb) s[0][rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, qfrag[rb][ks], s[0][rb], 0, 0, 0);
+    }
+    // the first reference: above the block's largest exponent (a row that sees none of its keys, or one with large logits, gets its own later)
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb) {
+      float m = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) m = fmaxf(m, (uint32_t)(key0 + 4 * half + 8 * (e >> 2) + (e & 3)) - low[rb] < reach ? c2 * s[0][rb][e] : -INFINITY);
+      m = fmaxf(m, __shfl_xor(m, 32)) + kPtHead;
+      ref[rb] = fabsf(m) <= kPtBig ? m : kPtUnset;
     }
     body(B0{}, 0, p0, p0, Yes{}, No{}, No{}, Yes{});
     // tiles in turn: second half of tile `it`, first half of tile it + 1.  (Three loops and not one: with both copies of the code in one loop
@@ -382,39 +393,47 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
         }
       }
     if (__builtin_amdgcn_ballot_w64(bad) != 0) *s_bad = 1;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // tiles past the end that were requested: their places are used below
     __syncthreads();
     if (*s_bad != 0) return true;
 
+    // ---- results: whole tiles by way of LDS, 16 bytes of a row per lane; pieces as they lie in the registers (the merge knows)
+    uint8_t* mine = smem + wave * 64 * RB;
 #pragma unroll
     for (int rb = 0; rb < 2; ++rb) {
-      const int j = wave * 64 + rb * 32 + col;
+      const int jw = rb * 32 + col, j = wave * 64 + jw;
       const float l = lsum[rb] + __shfl_xor(lsum[rb], 32);
-      if (j >= nrows) continue;
-      const float m = ref[rb] * 0.69314718055994530942f;           // in units of the logits
       if (whole) {
-        const size_t hb = out_row(j);
         const float inv = l > 0.f ? 1.f / l : 0.f;
-        uint8_t* po = a.out + (hb * D + half * 4) * 2;
 #pragma unroll
         for (int nb = 0; nb < NBO; ++nb)
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4) {
-            const float o0 = oacc[rb][nb][q4 * 4] * inv, o1 = oacc[rb][nb][q4 * 4 + 1] * inv, o2 = oacc[rb][nb][q4 * 4 + 2] * inv, o3 = oacc[rb][nb][q4 * 4 + 3] * inv;
-            *reinterpret_cast<uint2*>(po + (nb * 32 + q4 * 8) * 2) =
-                make_uint2(f32_to_bf16_bits(o0) | (f32_to_bf16_bits(o1) << 16), f32_to_bf16_bits(o2) | (f32_to_bf16_bits(o3) << 16));
+            const bf16x2_t y0 = {(__bf16)(oacc[rb][nb][q4 * 4] * inv), (__bf16)(oacc[rb][nb][q4 * 4 + 1] * inv)};
+            const bf16x2_t y1 = {(__bf16)(oacc[rb][nb][q4 * 4 + 2] * inv), (__bf16)(oacc[rb][nb][q4 * 4 + 3] * inv)};
+            *reinterpret_cast<uint2*>(mine + jw * RB + (((nb * 4 + q4) ^ (jw & (PPR - 1))) * 16) + half * 8) =
+                make_uint2(__builtin_bit_cast(uint32_t, y0), __builtin_bit_cast(uint32_t, y1));
           }
-        if (half == 0 && a.lse != nullptr) a.lse[hb] = l > 0.f ? (ref[rb] + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : -INFINITY;
+        if (half == 0 && j < nrows && a.lse != nullptr) a.lse[out_row(j)] = l > 0.f ? (ref[rb] + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : -INFINITY;
       } else {
-        float* po = sh.part_o + (((size_t)wg * 2 + slot) * kPtRows + j) * D + half * 4;
+        float4* po = reinterpret_cast<float4*>(sh.part_o + ((size_t)wg * 2 + slot) * kPtRows * D) + (wave * 2 + rb) * (NBO * 4 * 64) + lane;
 #pragma unroll
         for (int nb = 0; nb < NBO; ++nb)
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4)
-            *reinterpret_cast<float4*>(po + nb * 32 + q4 * 8) = make_float4(oacc[rb][nb][q4 * 4], oacc[rb][nb][q4 * 4 + 1], oacc[rb][nb][q4 * 4 + 2], oacc[rb][nb][q4 * 4 + 3]);
+            po[(nb * 4 + q4) * 64] = make_float4(oacc[rb][nb][q4 * 4], oacc[rb][nb][q4 * 4 + 1], oacc[rb][nb][q4 * 4 + 2], oacc[rb][nb][q4 * 4 + 3]);
         if (half == 0) {
           float* pm = sh.part_ml + (((size_t)wg * 2 + slot) * kPtRows + j) * 2;
-          pm[0] = l > 0.f ? m : -INFINITY; pm[1] = l;
+          pm[0] = l > 0.f ? ref[rb] * 0.69314718055994530942f : -INFINITY; pm[1] = l;      // in units of the logits
         }
+      }
+    }
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < 64 / KPI; ++i) {
+        const int jw = i * KPI + st_key, j = wave * 64 + jw;
+        const uint4 y = *reinterpret_cast<const uint4*>(mine + jw * RB + ((st_pos ^ (jw & (PPR - 1))) * 16));
+        if (j < nrows) *reinterpret_cast<uint4*>(a.out + out_row(j) * RB + st_pos * 16) = y;
       }
     }
     return false;
@@ -423,7 +442,7 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
 
 template <int D>
 static hipError_t tall_one(const PagedAttnArgs& a, const ShareArgs& sh, hipStream_t s) {
-  constexpr int lds = 2 * kPtBuf * kPtTile * D * 2 + 4 * kPtRing * 256 + 128;
+  constexpr int lds = 2 * kPtBuf * kPtTile * D * 2 + 4 * kPtRing * 256 + sizeof(ShareScratch) + 16;
   if (lds > 65536) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_tall_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
