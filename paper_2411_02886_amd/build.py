@@ -25,8 +25,9 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=o
 
 # Flags of single files.  sparse_attn_chunk_wide: its kernel runs one wave per SIMD and needs both halves of the register file; the
 # results of its matrix products are read by vector instructions, which see the first half only, and without this option the
-# compiler keeps all of them in the second half and moves every score over (2113 moves in the kernel, with it 182).  paged_attn_tall: built the same way.
-FILE_FLAGS = {"sparse_attn_chunk_wide.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "paged_attn_tall.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+# compiler keeps all of them in the second half and moves every score over (2113 moves in the kernel, with it 182).  paged_attn_*: built the same way, for the same reason.
+FILE_FLAGS = {"sparse_attn_chunk_wide.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "paged_attn_tall.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+              "paged_attn_stream.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _deps():

@@ -11,6 +11,30 @@ hipError_t launch_paged_tall(int D, const PagedAttnArgs& a, const ShareArgs& sh,
 
 constexpr int kStreamWgs = 512, kTallWgs = 256, kTallRows = 256;
 
+// Pieces of the tile that workgroup w's share began: its own and those of workgroups w + 1 .. w + count - 1, up to the one that ends the tile; a
+// share in between may hold no unit of it.  The states of the first 64 are loaded beside w's own.
+struct Pieces {
+  int count;
+  uint64_t some;                                // of workgroups w + 1 .. w + 64: those that left a piece
+  __device__ __forceinline__ bool there(const ShareArgs& sh, int w, int p) const {
+    if (p == 0) return true;
+    return p <= 64 ? ((some >> (p - 1)) & 1) != 0 : sh.desc[(size_t)(w + p) * 8 + 3] != kPieceNone;
+  }
+};
+__device__ __forceinline__ int next_piece(const ShareArgs& sh, int w, int lane) {
+  return w + 1 + lane < sh.wgs ? sh.desc[(size_t)(w + 1 + lane) * 8 + 3] : kPieceEnds;
+}
+__device__ __forceinline__ Pieces find_pieces(const ShareArgs& sh, int w, int lane, int state) {
+  Pieces p{1, __builtin_amdgcn_ballot_w64(state != kPieceNone)};
+  for (;; state = next_piece(sh, w + p.count - 1, lane)) {
+    const uint64_t end = __builtin_amdgcn_ballot_w64(state == kPieceEnds);
+    if (end != 0) { p.count += __builtin_ctzll(end) + 1; break; }
+    p.count += 64;
+  }
+  p.count = min(p.count, sh.wgs - w);
+  return p;
+}
+
 // Joins the pieces of the tiles that were cut: blockIdx.y stands for the workgroup whose share began the tile, the
 // pieces that follow lie in the workgroups behind it, up to the one that ends the tile.  D / 4 lanes per row, RPT rows per lane, PG
 // groups of lanes that share the pieces, US of which a lane has in flight: many of which may belong to a tile.
@@ -21,16 +45,12 @@ __global__ __launch_bounds__(THREADS) void paged_merge_kernel(PagedAttnArgs a, S
   __shared__ float s_ml[PG][RPB][2];
   const int w = blockIdx.y, G = a.H / a.H_kv;     // (rows first: the tiles that were cut may all be every fourth workgroup's, and so on two XCDs)
   const int32_t* d1 = sh.desc + (size_t)w * 8 + 4;
+  const int lane = threadIdx.x & 63, next = next_piece(sh, w, lane);
   if (d1[3] == kPieceNone) return;
   const int row0 = d1[0], kvh = d1[1], nrows = d1[2] * G;
-  const int lane = threadIdx.x & 63, sub = threadIdx.x % LPR, rr = threadIdx.x / LPR % LR, pg = threadIdx.x / (LPR * LR);
-  int pieces = 1;                                       // this workgroup's, and those of the workgroups w + 1 .. w + pieces - 1
-  for (;; pieces += 64) {
-    const int i = w + pieces + lane;
-    const uint64_t end = __builtin_amdgcn_ballot_w64(i >= sh.wgs || sh.desc[(size_t)i * 8 + 3] == kPieceEnds);
-    if (end != 0) { pieces += __builtin_ctzll(end) + 1; break; }
-  }
-  pieces = min(pieces, sh.wgs - w);
+  const int sub = threadIdx.x % LPR, rr = threadIdx.x / LPR % LR, pg = threadIdx.x / (LPR * LR);
+  const Pieces pc = find_pieces(sh, w, lane, next);
+  const int pieces = pc.count;
   for (int j0 = blockIdx.x * RPB; j0 < nrows; j0 += gridDim.x * RPB) {
     float M[RPT], L[RPT];
     float4 o[RPT];
@@ -43,7 +63,7 @@ __global__ __launch_bounds__(THREADS) void paged_merge_kernel(PagedAttnArgs a, S
       for (int u = 0; u < US; ++u) {
         const int p = p0 + u * PG;
         const size_t slot = (size_t)(w + p) * 2 + (p == 0 ? 1 : 0);
-        const bool there = p < pieces && (p == 0 || sh.desc[slot * 4 + 3] != kPieceNone);   // a share may hold no unit
+        const bool there = p < pieces && pc.there(sh, w, p);
 #pragma unroll
         for (int t = 0; t < RPT; ++t) {
           const int j = j0 + t * LR + rr;
@@ -111,81 +131,62 @@ __global__ __launch_bounds__(THREADS) void paged_merge_kernel(PagedAttnArgs a, S
   }
 }
 
-// The same for the tall kernel, whose pieces lie as in its registers: of each block of 32 rows (blockIdx.x), 16 bytes of the output
-// [D / 8][64 lanes], the lane's row lane % 32, its elements 8 i + 4 (lane / 32) .. + 3.
+// The same for the tall kernel, whose pieces lie as in its registers: of each block of 32 rows 16 bytes of the output [D / 8][64 lanes], the
+// lane's row lane % 32, its elements 8 i + 4 (lane / 32) .. + 3.  A wave of a workgroup (blockIdx.x: block of rows, then i / 4) has one i.
 template <int D>
 __global__ __launch_bounds__(256) void paged_merge_tall_kernel(PagedAttnArgs a, ShareArgs sh) {
-  constexpr int NT = D / 32, US = 3;                    // 16-byte pieces per thread, partial results in flight
+  constexpr int PB = D / 32, US = 6;                    // workgroups per block of rows; partial results in flight
   const int w = blockIdx.y, G = a.H / a.H_kv;
   const int32_t* d1 = sh.desc + (size_t)w * 8 + 4;
+  const int lane = threadIdx.x & 63, next = next_piece(sh, w, lane);
   if (d1[3] == kPieceNone) return;
   const int row0 = d1[0], kvh = d1[1], nrows = d1[2] * G;
-  const int lane = threadIdx.x & 63, j = blockIdx.x * 32 + (lane & 31);
-  if ((int)blockIdx.x * 32 >= nrows) return;
-  int pieces = 1;
-  for (;; pieces += 64) {
-    const int i = w + pieces + lane;
-    const uint64_t end = __builtin_amdgcn_ballot_w64(i >= sh.wgs || sh.desc[(size_t)i * 8 + 3] == kPieceEnds);
-    if (end != 0) { pieces += __builtin_ctzll(end) + 1; break; }
-  }
-  pieces = min(pieces, sh.wgs - w);
+  const int block = blockIdx.x / PB, i = blockIdx.x % PB * 4 + (threadIdx.x >> 6), j = block * 32 + (lane & 31);
+  if (block * 32 >= nrows) return;
+  const Pieces pc = find_pieces(sh, w, lane, next);
+  const int pieces = pc.count;
   float M = -INFINITY, L = 0.f;
-  float4 o[NT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) o[t] = make_float4(0.f, 0.f, 0.f, 0.f);
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int p0 = 0; p0 < pieces; p0 += US) {
     float2 v[US];
-    float4 x[US][NT];
+    float4 x[US];
 #pragma unroll
     for (int u = 0; u < US; ++u) {
       const int p = p0 + u;
       const size_t slot = (size_t)(w + p) * 2 + (p == 0 ? 1 : 0);
-      const bool there = p < pieces && (p == 0 || sh.desc[slot * 4 + 3] != kPieceNone);   // a share may hold no unit
       v[u] = make_float2(-INFINITY, 0.f);
-      if (there) v[u] = *reinterpret_cast<const float2*>(sh.part_ml + (slot * kTallRows + j) * 2);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        x[u][t] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (there) x[u][t] = *(reinterpret_cast<const float4*>(sh.part_o + slot * kTallRows * D) + (size_t)blockIdx.x * (D / 8 * 64) + t * 256 + threadIdx.x);
-      }
+      x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (p >= pieces || !pc.there(sh, w, p)) continue;
+      v[u] = *reinterpret_cast<const float2*>(sh.part_ml + (slot * kTallRows + j) * 2);
+      x[u] = reinterpret_cast<const float4*>(sh.part_o + slot * kTallRows * D)[(block * (D / 8) + i) * 64 + lane];
     }
     float m = M;
 #pragma unroll
     for (int u = 0; u < US; ++u) m = fmaxf(m, v[u].x);
     if (m == -INFINITY) continue;
     const float f = expf(M - m);
-    L *= f;
-#pragma unroll
-    for (int t = 0; t < NT; ++t) { o[t].x *= f; o[t].y *= f; o[t].z *= f; o[t].w *= f; }
+    L *= f; o.x *= f; o.y *= f; o.z *= f; o.w *= f;
 #pragma unroll
     for (int u = 0; u < US; ++u) {
       const float g = expf(v[u].x - m);
       L = fmaf(g, v[u].y, L);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        o[t].x = fmaf(g, x[u][t].x, o[t].x); o[t].y = fmaf(g, x[u][t].y, o[t].y);
-        o[t].z = fmaf(g, x[u][t].z, o[t].z); o[t].w = fmaf(g, x[u][t].w, o[t].w);
-      }
+      o.x = fmaf(g, x[u].x, o.x); o.y = fmaf(g, x[u].y, o.y); o.z = fmaf(g, x[u].z, o.z); o.w = fmaf(g, x[u].w, o.w);
     }
     M = m;
   }
   if (j >= nrows) return;
   const size_t hb = (size_t)(row0 + j / G) * a.H + kvh * G + j % G;
   const float inv = L > 0.f ? 1.f / L : 0.f;
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const int d = 8 * (t * 4 + (threadIdx.x >> 6)) + 4 * (lane >> 5);
-    *reinterpret_cast<uint2*>(a.out + (hb * D + d) * 2) = make_uint2(f32_to_bf16_bits(o[t].x * inv) | (f32_to_bf16_bits(o[t].y * inv) << 16),
-                                                                     f32_to_bf16_bits(o[t].z * inv) | (f32_to_bf16_bits(o[t].w * inv) << 16));
-  }
-  if (threadIdx.x < 32 && a.lse != nullptr) a.lse[hb] = L > 0.f ? M + logf(L) : -INFINITY;
+  *reinterpret_cast<uint2*>(a.out + (hb * D + 8 * i + 4 * (lane >> 5)) * 2) =
+      make_uint2(f32_to_bf16_bits(o.x * inv) | (f32_to_bf16_bits(o.y * inv) << 16), f32_to_bf16_bits(o.z * inv) | (f32_to_bf16_bits(o.w * inv) << 16));
+  if (i == 0 && lane < 32 && a.lse != nullptr) a.lse[hb] = L > 0.f ? M + logf(L) : -INFINITY;
 }
 
 template <int ES, int D>
 static hipError_t merge(const PagedAttnArgs& a, const ShareArgs& sh, int rows, hipStream_t s) {
   // (a tile with more rows than the bound says takes turns; the tall kernel's tiles are short only where their sequence is)
-  if (rows != kTallRows) hipLaunchKernelGGL((paged_merge_kernel<ES, D, D * 8, 1, 8, 4>), dim3((std::min(sh.tpt, a.C) * (a.H / a.H_kv) + 3) / 4, sh.wgs), dim3(D * 8), 0, s, a, sh, rows);
-  else hipLaunchKernelGGL(paged_merge_tall_kernel<D>, dim3(kTallRows / 32, sh.wgs), dim3(256), 0, s, a, sh);
+  if (rows != kTallRows) hipLaunchKernelGGL((paged_merge_kernel<ES, D, 256, 4, 1024 / D, 2>), dim3((std::min(sh.tpt, a.C) * (a.H / a.H_kv) + 3) / 4, sh.wgs), dim3(256), 0, s, a, sh, rows);
+  else hipLaunchKernelGGL(paged_merge_tall_kernel<D>, dim3(kTallRows / 32 * (D / 32), sh.wgs), dim3(256), 0, s, a, sh);
   return hipGetLastError();
 }
 
@@ -205,11 +206,10 @@ static PagedPlan paged_plan(int dtype, int G, int chunk) {
   return PagedPlan{dtype == TS_BF16 ? 2 : 1, 1};
 }
 static int many_rows(int dtype) { return dtype == TS_BF16 ? kTallRows : 64; }
-static int many_wgs(int dtype, int D) { return dtype == TS_BF16 || D == 128 ? kTallWgs : kStreamWgs; }
 
 size_t paged_attn_workspace(int dtype, int D, int G, int chunk) {
   const PagedPlan pl = paged_plan(dtype, G, chunk);
-  return align_up(piece_bytes(kStreamWgs, 16 * pl.few_blocks, D) + (pl.many ? piece_bytes(many_wgs(dtype, D), many_rows(dtype), D) : 0), 256);
+  return align_up(piece_bytes(kStreamWgs, 16 * pl.few_blocks, D) + (pl.many ? piece_bytes(kTallWgs, many_rows(dtype), D) : 0), 256);
 }
 
 hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws, hipStream_t s) {
@@ -218,7 +218,7 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
   uint8_t* at = (uint8_t*)ws;
   for (int kind = 0; kind < 2; ++kind) {                 // few rows, many rows
     const bool few = kind == 0;
-    const int rows = few ? 16 * pl.few_blocks : many_rows(dtype), most_wgs = few ? kStreamWgs : many_wgs(dtype, D);
+    const int rows = few ? 16 * pl.few_blocks : many_rows(dtype), most_wgs = few ? kStreamWgs : kTallWgs;
     if (!few && !pl.many) break;
     ShareArgs sh{};
     sh.tpt = rows / G;
@@ -231,9 +231,13 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
     if (few && pl.many && a.q_indptr == nullptr) continue;   // every sequence has as many
     const bool tall = !few && dtype == TS_BF16;
     const int kt = tall ? 64 : dtype == TS_BF16 ? 128 : 64;
-    sh.min_keys = 2 * kt;
+    sh.min_keys = tall ? 2 * kt : kt;
     sh.tile_cost = tall ? 256 : 64;
     sh.wgs = most_wgs;
+    // A workgroup per tile, and no merge, where tiles are short.
+    const long tiles = (a.q_indptr != nullptr ? a.T / sh.tpt + std::min(a.B, a.T) : (long)a.B * ((a.C + sh.tpt - 1) / sh.tpt)) * a.H_kv;
+    const long units = (std::min((long)a.max_seq_len, a.window > 0 ? (long)a.window + sh.tpt : LONG_MAX) + kt - 1) / kt;
+    if (few ? tiles < (1l << 30) && (units * kt <= 512 || (tiles >= most_wgs && units <= 16)) : tiles <= most_wgs && units <= 16) { sh.whole = 1; sh.wgs = (int)tiles; }
     hipError_t e;
     if (tall) e = launch_paged_tall(D, a, sh, s);
     else e = launch_paged_stream(dtype, D, rows / 16, a, sh, s);

@@ -15,6 +15,7 @@ namespace ts {
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 
 constexpr float kPsUnset = -3.40282347e38f;   // reference logit before the first key: no finite logit lies below it
 constexpr float kPsHead = 4.f;                // a raised reference lies this far above the largest logit so far ...
@@ -36,7 +37,7 @@ struct StreamShape {
   static constexpr int RB = D * ES, PPR = RB / 16, RPI = 64 / PPR, NLD = TK / RPI;
   static constexpr int TILE_B = TK * RB;
   static constexpr int LDS = 4 * (2 * TILE_B + 512);   // the waves' tiles and look-ups; the waves' results fit the same place
-  static constexpr int PER_CU = CB * D * ES >= 2048 ? 1 : 2;
+  static constexpr int PER_CU = CB == 4 ? 1 : 2;
   static_assert(4 * 16 * (D + 4) * 4 <= LDS, "the waves' results");
 };
 
@@ -56,7 +57,8 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
   const int H = a.H, G = a.H / a.H_kv;
   const int wg = share_of(blockIdx.x, sh.wgs);
   SharePlace from, to;
-  find_share<KT, 256>(a, sh, G, wg, &s_share, &from, &to);
+  SeqShape first;
+  find_share<KT>(a, sh, G, wg, &s_share, &from, &to, &first);
   int32_t* desc = sh.desc + (size_t)wg * 8;
   if (!sh.whole && threadIdx.x == 0) { desc[3] = kPieceNone; desc[7] = kPieceNone; }
 
@@ -65,10 +67,12 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
   const uint32_t lds_k = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)kt);
   const volatile int32_t* look = reinterpret_cast<const volatile int32_t*>(vt + TILE_B);   // two places of 64 page ids
   const int st_row = lane / PPR, st_pos = lane % PPR;
+  typedef const __attribute__((address_space(3))) u32x4_t lds_u32x4;
   const float sm = a.sm_scale;
+  const int row_shift = 31 - __builtin_clz((uint32_t)(a.H_kv * RB));   // H_kv is a power of two
   const uint32_t reach = a.window > 0 ? (uint32_t)a.window : 0x7fffffffu;
 
-  walk_share<KT>(a, sh, G, from, to, [&](int kvh, const SeqShape& sq, int r, const TileKeys& keys, int ua, int ub, bool) -> bool {
+  walk_share<KT>(a, sh, G, from, to, first, [&](int kvh, const SeqShape& sq, int r, const TileKeys& keys, int ua, int ub, bool) -> bool {
     const int c0 = r * sh.tpt, ntok = min(sh.tpt, sq.n - c0), nrows = ntok * G;
     const int row0 = sq.row0 + c0, x0 = sq.N - sq.n + c0, x1 = x0 + ntok - 1;   // first row; places of the first and last token
     const bool whole = ua == 0 && ub == keys.units;
@@ -87,7 +91,7 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
       int32_t* d = desc + slot * 4;
       d[0] = row0; d[1] = kvh; d[2] = ntok; d[3] = ub == keys.units ? kPieceEnds : kPieceGoesOn;
     }
-    const int32_t* pages = a.page_indices + a.page_indptr[sq.b];
+    const int32_t* pages = a.page_indices + sq.page0;
 
     // query rows (zero past the last): 16-byte pieces 4 i + kgrp of row cb * 16 + col
     uint4 qf[CB][NQ];
@@ -109,25 +113,30 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
     const int key0 = (keys.u0 + ua) * KT + wave * TK;
     int nt = ub - ua;
     if (key0 + (nt - 1) * KT > tmax) --nt;
-    uint64_t off[NLD];                                             // this lane's pieces of a tile's rows in the pools
+    uint32_t at[NLD];                                              // a tile's rows (this lane's of each load) in the pools
     auto fetch_look = [&](int i, int place) {
       const int t = min(key0 + i * KT + (lane & (TK - 1)), tmax);
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(lds_k + 2 * TILE_B + place * 256), "v"(pages + (t >> a.p_shift)) : "memory", "m0");
     };
+    // (fresh(): the compiler forms the address anew in each turn of the loop.  It would keep all of them, dozens of registers, and spill.)
+    auto fresh = [](uint32_t x) -> uint32_t { if (CB > 1) asm volatile("" : "+v"(x)); return x; };
     auto rows_of = [&](int i, int place) {
+      const int my_row = (int)fresh(st_row);
 #pragma unroll
       for (int l = 0; l < NLD; ++l) {
-        const int row = l * RPI + st_row, t = min(key0 + i * KT + row, tmax);      // past the end: the last key again
-        const uint32_t at = ((uint32_t)look[place * 64 + row] << a.p_shift) + (uint32_t)(t & (a.P - 1));
-        off[l] = ((uint64_t)at * (uint32_t)a.H_kv + (uint32_t)kvh) * RB + (uint32_t)((st_pos ^ ps_swz<ES, D>(row & 15)) * 16);
+        const int row = l * RPI + my_row, t = min(key0 + i * KT + row, tmax);      // past the end: the last key again
+        at[l] = ((uint32_t)look[place * 64 + row] << a.p_shift) + (uint32_t)(t & (a.P - 1));
       }
     };
     // 1 KiB per load: the wave's lanes fill LDS from `dst` on.  In assembly, so that the compiler does not make every LDS read wait for
     // it; the waits stand below.  Non-temporal: with few rows per tile nobody else reads them.
     auto load_rows = [&](const uint8_t* pool, uint32_t dst) {
+      const int my_row = (int)fresh(st_row);
 #pragma unroll
-      for (int l = 0; l < NLD; ++l)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" :: "s"(dst + l * 1024), "v"(pool + off[l]) : "memory", "m0");
+      for (int l = 0; l < NLD; ++l) {
+        const uint64_t off = ((uint64_t)at[l] << row_shift) + (uint32_t)(kvh * RB + ((st_pos ^ ps_swz<ES, D>((l * RPI + my_row) & 15)) * 16));
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" :: "s"(dst + l * 1024), "v"(pool + off) : "memory", "m0");
+      }
     };
     float ref[CB], lsum[CB];                  // of row cb * 16 + col: reference logit (the same in its four lanes), this lane's keys' sum
     bool big = false;                         // some row's reference is large (the same for the whole wave)
@@ -150,50 +159,45 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
       const bool more = i + 1 < nt;
       const int k0 = key0 + i * KT;
       asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NLD) : "memory");            // this tile's K rows and the next one's page ids (its V rows follow them)
-      // ---- scores, element e: key 16 * (e / 4) + 4 * kgrp + e % 4.  Products are added up in four chains, which loses less than one
+      // ---- scores, element e: key 16 * (e / 4) + 4 * kgrp + e % 4.  Products are added up in four chains, which loses less than one (two where the
+      // registers hold no more)
       float s[CB][NE];
-      if constexpr (ES == 2) {
-        f32x4_t part[CB][NQ][2];
+      constexpr int NB = TK / 16, NC = CB == 1 ? 4 : 2;              // blocks of 16 keys, chains
+      f32x4_t part[CB][NC][NB];
 #pragma unroll
-        for (int ks = 0; ks < NQ; ++ks)
+      for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-          for (int kb = 0; kb < 2; ++kb) {
-            const uint4 kf = *reinterpret_cast<const uint4*>(kt + (kb * 16 + col) * RB + (((ks * 4 + kgrp) ^ ps_swz<ES, D>(col)) * 16));
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
-            for (int cb = 0; cb < CB; ++cb)
-              part[cb][ks][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf), __builtin_bit_cast(bf16x8_t, qf[cb][ks]),
-                                                                         (f32x4_t){0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-          }
+          for (int kb = 0; kb < NB; ++kb) part[cb][c][kb] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
+      const uint32_t k_at = fresh(lds_k + (uint32_t)(col * RB)), k_piece = fresh((uint32_t)(kgrp ^ ps_swz<ES, D>(col)));
 #pragma unroll
-        for (int cb = 0; cb < CB; ++cb)
+      for (int ks = 0; ks < NQ; ++ks)
 #pragma unroll
-          for (int e = 0; e < NE; ++e) {
-            s[cb][e] = part[cb][0][e >> 2][e & 3] + part[cb][1][e >> 2][e & 3];
-            if constexpr (NQ == 4) s[cb][e] += part[cb][2][e >> 2][e & 3] + part[cb][3][e >> 2][e & 3];
-          }
-      } else {
-        f32x4_t part[CB][4];
-#pragma unroll
-        for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) part[cb][c] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int ks = 0; ks < NQ; ++ks) {
-          const uint4 kf = *reinterpret_cast<const uint4*>(kt + col * RB + (((ks * 4 + kgrp) ^ ps_swz<ES, D>(col)) * 16));
-          const uint32_t kw[4] = {kf.x, kf.y, kf.z, kf.w};
+        for (int kb = 0; kb < NB; ++kb) {
+          const uint4 kf = __builtin_bit_cast(uint4, *(lds_u32x4*)(k_at + (uint32_t)(kb * 16 * RB) + ((k_piece ^ (uint32_t)(ks * 4)) * 16)));
 #pragma unroll
           for (int cb = 0; cb < CB; ++cb) {
-            const uint32_t qw[4] = {qf[cb][ks].x, qf[cb][ks].y, qf[cb][ks].z, qf[cb][ks].w};
+            if constexpr (ES == 2) {
+              f32x4_t& acc = part[cb][ks % NC][kb];
+              acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf), __builtin_bit_cast(bf16x8_t, qf[cb][ks]), acc, 0, 0, 0);
+            } else {
+              const uint32_t kw[4] = {kf.x, kf.y, kf.z, kf.w}, qw[4] = {qf[cb][ks].x, qf[cb][ks].y, qf[cb][ks].z, qf[cb][ks].w};
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
-              part[cb][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kw[c]), __uint_as_float(qw[c]), part[cb][c], 0, 0, 0);
+              for (int c = 0; c < 4; ++c) {
+                f32x4_t& acc = part[cb][c % NC][kb];
+                acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kw[c]), __uint_as_float(qw[c]), acc, 0, 0, 0);
+              }
+            }
           }
         }
 #pragma unroll
-        for (int cb = 0; cb < CB; ++cb)
+      for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-          for (int e = 0; e < NE; ++e) s[cb][e] = (part[cb][0][e] + part[cb][1][e]) + (part[cb][2][e] + part[cb][3][e]);
-      }
+        for (int e = 0; e < NE; ++e) {
+          s[cb][e] = part[cb][0][e >> 2][e & 3] + part[cb][1][e >> 2][e & 3];
+          if constexpr (NC == 4) s[cb][e] += part[cb][2][e >> 2][e & 3] + part[cb][3][e >> 2][e & 3];
+        }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                     // the K tile has been read
       if (more) { rows_of(i + 1, (i + 1) & 1); fetch_look(i + 2, i & 1); load_rows(a.k_pool, lds_k); }
       // ---- weights against the reference: exp(logit - reference)
@@ -260,13 +264,15 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
           }
         if (more) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NLD + 1) : "memory");   // this tile's V rows (page ids and the next K rows follow them)
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        const int vt_key = 4 * kgrp + (col >> 2), vt_c = (col & 3) >> 1, vt_b = (col & 1) * 8;   // V^T read: key, piece of the pair, half
+        // V^T read: key, piece of the pair, half
+        const int vt_key = 4 * kgrp + (col >> 2);
+        const uint32_t v_at = fresh(lds_k + (uint32_t)(TILE_B + vt_key * RB + (col & 1) * 8)), v_piece = fresh((uint32_t)(((col & 3) >> 1) ^ ps_swz<ES, D>(vt_key)));
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
           uint2 v[2];
 #pragma unroll
           for (int kb = 0; kb < 2; ++kb) {
-            const uint8_t* vp = vt + (kb * 16 + vt_key) * RB + (((db * 2 + vt_c) ^ ps_swz<ES, D>(vt_key)) * 16) + vt_b;
+            const uint32_t vp = v_at + (uint32_t)(kb * 16 * RB) + ((v_piece ^ (uint32_t)(db * 2)) * 16);
             v[kb] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)vp));
           }
           const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, make_uint4(v[0].x, v[0].y, v[1].x, v[1].y));
@@ -280,14 +286,15 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
       } else {
         if (more) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NLD + 1) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        const uint32_t v_at = fresh(lds_k + (uint32_t)(TILE_B + 4 * kgrp * RB)), v_piece = fresh((uint32_t)(col ^ (4 * kgrp)));
         // product e takes keys 4 * kgrp + e; a read of 16 bytes serves four blocks of the output, row i of block 4 q + c is d = 64 q + 4 i + c
 #pragma unroll
         for (int e = 0; e < NE; ++e)
 #pragma unroll
           for (int q = 0; q < D / 64; ++q) {
-            const int key = 4 * kgrp + e;
-            const float4 vf = *reinterpret_cast<const float4*>(vt + key * RB + (((16 * q + col) ^ ps_swz<ES, D>(key)) * 16));
-            const float vw[4] = {vf.x, vf.y, vf.z, vf.w};
+            const uint32_t vp = v_at + (uint32_t)(e * RB) + (((uint32_t)(16 * q) + (v_piece ^ (uint32_t)e)) * 16);   // key 4 * kgrp + e: its piece is flipped by itself
+            const uint4 vf = __builtin_bit_cast(uint4, *(lds_u32x4*)vp);
+            const float vw[4] = {__uint_as_float(vf.x), __uint_as_float(vf.y), __uint_as_float(vf.z), __uint_as_float(vf.w)};
 #pragma unroll
             for (int c = 0; c < 4; ++c)
 #pragma unroll

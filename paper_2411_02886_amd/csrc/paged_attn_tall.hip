@@ -61,7 +61,8 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
   const int H = a.H, G = a.H / a.H_kv;
   const int wg = share_of(blockIdx.x, sh.wgs);
   SharePlace from, to;
-  find_share<kPtTile, 256>(a, sh, G, wg, s_share, &from, &to);
+  SeqShape first;
+  find_share<kPtTile>(a, sh, G, wg, s_share, &from, &to, &first);
   int32_t* desc = sh.desc + (size_t)wg * 8;
   if (!sh.whole && threadIdx.x == 0) { desc[3] = kPieceNone; desc[7] = kPieceNone; }
 
@@ -86,18 +87,20 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
   const uint32_t look = __builtin_amdgcn_readfirstlane(lds_base + (uint32_t)(2 * kPtBuf * TILE_B + wave * kPtRing * 256));
   const int row_shift = 31 - __builtin_clz((uint32_t)(a.H_kv * RB));   // H_kv is a power of two
 
-  walk_share<kPtTile>(a, sh, G, from, to, [&](int kvh, const SeqShape& sq, int r, const TileKeys& keys, int ua, int ub, bool again) __attribute__((always_inline)) -> bool {
+  walk_share<kPtTile>(a, sh, G, from, to, first, [&](int kvh, const SeqShape& sq, int r, const TileKeys& keys, int ua, int ub, bool again) __attribute__((always_inline)) -> bool {
     const int c0 = r * sh.tpt, ntok = min(sh.tpt, sq.n - c0), nrows = ntok * G;
     const int row0 = sq.row0 + c0, x0 = sq.N - sq.n + c0, x1 = x0 + ntok - 1;   // first row; places of the first and last token
     const bool whole = ua == 0 && ub == keys.units;
     const int tmax = keys.end - 1;
     auto token_of = [&](int j) -> int { return (int)(((uint32_t)j * g_inv) >> 16); };   // j / G
-    auto out_row = [&](int j) -> size_t { const int c = token_of(j); return (size_t)(row0 + c) * H + kvh * G + (j - c * G); };
+    // the tile's row j in q, out and lse: a uniform first row and 32 bits behind it (j / G tokens of H rows, then j % G)
+    const size_t tile_row = (size_t)row0 * H + kvh * G;
+    auto row_at = [&](int j) -> uint32_t { return (uint32_t)token_of(j) * (uint32_t)(H - G) + (uint32_t)j; };
     if (keys.end <= keys.first) {                                  // no row sees a token (one unit: the tile is not cut)
       for (int i = threadIdx.x; i < nrows * D; i += 256) {
-        const size_t o = out_row(i / D) * D + i % D;
-        reinterpret_cast<uint16_t*>(a.out)[o] = 0;
-        if (i % D == 0 && a.lse != nullptr) a.lse[o / D] = -INFINITY;
+        const size_t o = tile_row + row_at(i / D);
+        reinterpret_cast<uint16_t*>(a.out)[o * D + i % D] = 0;
+        if (i % D == 0 && a.lse != nullptr) a.lse[o] = -INFINITY;
       }
       return false;
     }
@@ -106,7 +109,7 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
       int32_t* d = desc + slot * 4;
       d[0] = row0; d[1] = kvh; d[2] = ntok; d[3] = ub == keys.units ? kPieceEnds : kPieceGoesOn;
     }
-    const int32_t* pages = a.page_indices + a.page_indptr[sq.b];
+    const int32_t* pages = a.page_indices + sq.page0;
     const int key0 = (keys.u0 + ua) * kPtTile, nt = ub - ua;       // first key and number of tiles
     // tiles [f0, f1) are seen in full by every row
     const int f0 = again ? nt : a.window > 0 ? max((x1 - key0 - a.window + kPtTile) / kPtTile, 0) : 0;
@@ -146,11 +149,11 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
     for (int rb = 0; rb < 2; ++rb) {
       const int j = wave * 64 + rb * 32 + col;
       low[rb] = (uint32_t)(j < nrows ? x0 + token_of(j) : x1) - (reach - 1u);
-      const uint8_t* qp = a.q + (out_row(min(j, nrows - 1)) * D + 8 * half) * 2;
+      const uint32_t at = row_at(min(j, nrows - 1)) * RB + 16 * half;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         uint4 v = make_uint4(0, 0, 0, 0);
-        if (j < nrows) v = *reinterpret_cast<const uint4*>(qp + ks * 32);
+        if (j < nrows) v = *reinterpret_cast<const uint4*>(a.q + tile_row * RB + (at + ks * 32));
         qfrag[rb][ks] = __builtin_bit_cast(bf16x8_t, v);
       }
     }
@@ -414,7 +417,7 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
             *reinterpret_cast<uint2*>(mine + jw * RB + (((nb * 4 + q4) ^ (jw & (PPR - 1))) * 16) + half * 8) =
                 make_uint2(__builtin_bit_cast(uint32_t, y0), __builtin_bit_cast(uint32_t, y1));
           }
-        if (half == 0 && j < nrows && a.lse != nullptr) a.lse[out_row(j)] = l > 0.f ? (ref[rb] + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : -INFINITY;
+        if (half == 0 && j < nrows && a.lse != nullptr) a.lse[tile_row + row_at(j)] = l > 0.f ? (ref[rb] + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : -INFINITY;
       } else {
         float4* po = reinterpret_cast<float4*>(sh.part_o + ((size_t)wg * 2 + slot) * kPtRows * D) + (wave * 2 + rb) * (NBO * 4 * 64) + lane;
 #pragma unroll
@@ -433,7 +436,7 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
       for (int i = 0; i < 64 / KPI; ++i) {
         const int jw = i * KPI + st_key, j = wave * 64 + jw;
         const uint4 y = *reinterpret_cast<const uint4*>(mine + jw * RB + ((st_pos ^ (jw & (PPR - 1))) * 16));
-        if (j < nrows) *reinterpret_cast<uint4*>(a.out + out_row(j) * RB + st_pos * 16) = y;
+        if (j < nrows) *reinterpret_cast<uint4*>(a.out + tile_row * RB + (row_at(j) * RB + st_pos * 16)) = y;
       }
     }
     return false;

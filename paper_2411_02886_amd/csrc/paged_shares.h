@@ -29,42 +29,44 @@ struct ShareArgs {
 
 #ifdef __HIPCC__
 
-// floor(a / b) for 0 <= a < 2^53, 0 < b: a division of doubles and its correction (of 64-bit integers the compiler makes 150 instructions)
-__device__ __forceinline__ long floor_div(long a, long b) {
-  long q = (long)((double)a / (double)b);
-  const long r = a - q * b;
-  return r < 0 ? q - 1 : r >= b ? q + 1 : q;
+// Rooms are whole numbers held in doubles: exact below 2^53 (lines of 10^15 keys), and the double unit has a product in one instruction where
+// 64-bit integers take six.
+__device__ __forceinline__ double floor_div(double a, double b) {
+  const double q = floor(a / b), r = fma(-q, b, a);
+  return r < 0. ? q - 1. : r >= b ? q + 1. : q;
 }
 
-struct SeqShape { int b, row0, n, N, tiles; };   // sequence, first row, new tokens, length, tiles (0: takes no part)
+struct SeqShape { int b, row0, n, N, tiles, page0; };   // sequence, first row, new tokens, length, tiles (0: takes no part), first page's place
 
 __device__ __forceinline__ SeqShape seq_shape(const PagedAttnArgs& a, const ShareArgs& sh, int G, int b) {
   SeqShape s;
   s.b = b;
   const int r0 = a.q_indptr != nullptr ? min(max(a.q_indptr[b], 0), a.T) : b * a.C;
   const int r1 = a.q_indptr != nullptr ? min(max(a.q_indptr[b + 1], 0), a.T) : r0 + a.C;
+  s.page0 = a.page_indptr[b];
   s.row0 = r0;
   s.n = max(r1 - r0, 0);
   s.N = min(max(a.seq_lens[b], 0), a.max_seq_len);
   const long rows = (long)s.n * G;
-  s.tiles = rows > sh.more_rows && rows <= sh.most_rows ? (s.n + sh.tpt - 1) / sh.tpt : 0;
+  s.tiles = rows > sh.more_rows && rows <= sh.most_rows ? (int)((uint32_t)(s.n + sh.tpt - 1) / (uint32_t)sh.tpt) : 0;
   return s;
 }
 
 // room of a sequence's first r tiles
-__device__ __forceinline__ long tiles_room(const PagedAttnArgs& a, const ShareArgs& sh, const SeqShape& s, long r) {
+__device__ __forceinline__ double tiles_room(const PagedAttnArgs& a, const ShareArgs& sh, const SeqShape& s, int tiles) {
+  const double r = tiles;
   if (sh.whole) return r;
-  const long first = max(s.N - s.n, 0) + sh.tile_cost, tpt = sh.tpt;
-  if (a.window == 0) return r * first + tpt * (r * (r + 1) / 2);
-  const long cap = min((long)a.window, (long)a.max_seq_len) + tpt + sh.tile_cost;   // where the window cuts a tile's keys
-  const long grow = cap > first ? min(r, floor_div(cap - first - 1, tpt)) : 0;           // tiles that it does not cut
-  return grow * first + tpt * (grow * (grow + 1) / 2) + (r - grow) * cap;
+  const double first = max(s.N - s.n, 0) + sh.tile_cost, tpt = sh.tpt;
+  if (a.window == 0) return fma(r, first, tpt * (r * (r + 1.) * 0.5));
+  const double cap = (double)a.window + tpt + sh.tile_cost;                     // where the window cuts a tile's keys
+  const double grow = cap > first ? fmin(r, floor_div(cap - first - 1., tpt)) : 0.;   // tiles that it does not cut
+  return fma(grow, first, tpt * (grow * (grow + 1.) * 0.5)) + (r - grow) * cap;
 }
 
 // The i-th tile of a sequence in the line, and the room of the first i.
 __device__ __forceinline__ int tile_at(const SeqShape& s, int i) { return (i & 1) != 0 ? s.tiles - 1 - (i >> 1) : i >> 1; }
-__device__ __forceinline__ long line_room(const PagedAttnArgs& a, const ShareArgs& sh, const SeqShape& s, int i) {
-  return tiles_room(a, sh, s, (i + 1) >> 1) + tiles_room(a, sh, s, s.tiles) - tiles_room(a, sh, s, s.tiles - (i >> 1));
+__device__ __forceinline__ double line_room(const PagedAttnArgs& a, const ShareArgs& sh, const SeqShape& s, int i) {
+  return tiles_room(a, sh, s, (i + 1) >> 1) + (tiles_room(a, sh, s, s.tiles) - tiles_room(a, sh, s, s.tiles - (i >> 1)));
 }
 
 // keys that a tile's rows see, in units of KT keys from u0 on; at least one unit, though it may hold no visible key
@@ -74,7 +76,7 @@ __device__ __forceinline__ TileKeys tile_keys(const PagedAttnArgs& a, const Shar
   TileKeys k;
   const int c0 = r * sh.tpt, c1 = min(c0 + sh.tpt, s.n) - 1;
   k.end = max(s.N - s.n + c1 + 1, 0);
-  k.first = a.window > 0 ? max(s.N - s.n + c0 - a.window + 1, 0) : 0;
+  k.first = a.window > 0 ? (int)max((long)s.N - s.n + c0 - a.window + 1, 0l) : 0;
   k.u0 = (int)((uint32_t)k.first / KT);
   k.units = max((int)(((uint32_t)k.end + KT - 1) / KT) - k.u0, 1);
   return k;
@@ -82,77 +84,84 @@ __device__ __forceinline__ TileKeys tile_keys(const PagedAttnArgs& a, const Shar
 
 struct SharePlace { int kvh, b, i, u; };       // i: the tile's turn in its sequence
 
-// All threads of the workgroup (NT of them): begin and end of this workgroup's share, in scalar registers.
-struct ShareScratch { long sums[4], y[2]; int kvh[2], b[2]; SharePlace place[2]; };
-template <int KT, int NT>
+// All threads of the workgroup (256): begin and end of this workgroup's share, in scalar registers, and the sequence that it begins in.
+struct ShareScratch { double sums[4], y[2]; int kvh[2]; SeqShape shape[2]; SharePlace place[2]; };
+template <int KT>
 __device__ __forceinline__ void find_share(const PagedAttnArgs& a, const ShareArgs& sh, int G, int wg, ShareScratch* lds, SharePlace* from,
-                                           SharePlace* to) {
-  static_assert(NT == 256, "four waves");
+                                           SharePlace* to, SeqShape* first) {
   // which sequences the two ends lie in: a thread has `per` neighbouring ones
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, per = (a.B + NT - 1) / NT;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, per = (a.B + 255) >> 8;
   const int b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
-  long mine = 0;
+  SeqShape s{0, 0, 0, 0, 0, 0};
+  double mine = 0.;
   for (int b = b0; b < b1; ++b) {
-    const SeqShape s = seq_shape(a, sh, G, b);
+    s = seq_shape(a, sh, G, b);
     mine += tiles_room(a, sh, s, s.tiles);
   }
-  long upto = mine;
+  double upto = mine;
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) { const long x = __shfl_up(upto, d); if (lane >= d) upto += x; }
-  if (lane == 63) lds->sums[wave] = upto;
+  for (int d = 1; d < 64; d <<= 1) {
+    if (d >= a.B) break;                       // the sequences are fewer: the lanes behind them have nothing
+    const double x = __shfl_up(upto, d);
+    if (lane >= d) upto += x;
+  }
+  // (where the loop ended early the last lane has only its neighbours' rooms: the sum is the last sequence's)
+  if (lane == min(63, a.B - 1)) lds->sums[wave] = a.B < 64 && wave > 0 ? 0. : upto;
   if (tid < 2) lds->kvh[tid] = a.H_kv;         // the end of the line; also where lengths that change under the call lead nowhere
   __syncthreads();
-  long before = upto - mine, line = 0;
+  double before = upto - mine, line = 0.;
 #pragma unroll
-  for (int w = 0; w < NT / 64; ++w) { if (w < wave) before += lds->sums[w]; line += lds->sums[w]; }
-  const long all = line * a.H_kv;
-  const long share = sh.whole ? 1 : max((long)sh.min_keys, floor_div(all + sh.wgs - 1, sh.wgs));
+  for (int w = 0; w < 4; ++w) { if (w < wave) before += lds->sums[w]; line += lds->sums[w]; }
+  const double all = line * a.H_kv;
+  const double share = sh.whole ? 1. : fmax((double)sh.min_keys, floor_div(all + (sh.wgs - 1), sh.wgs));
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
-    const long x = (long)(wg + e) * share;
-    if (x >= all) continue;
-    const int kvh = (int)floor_div(x, line);
-    long y = x - kvh * line - before;
-    if (y < 0 || y >= mine) continue;          // another thread's sequences
-    int b = b0;
-    for (; b + 1 < b1; ++b) {
-      const SeqShape s = seq_shape(a, sh, G, b);
-      const long room = tiles_room(a, sh, s, s.tiles);
+    const double x = (wg + e) * share;
+    if (!(x < all)) continue;
+    const double kvh = floor_div(x, line);
+    double y = fma(-kvh, line, x) - before;
+    if (!(y >= 0. && y < mine)) continue;      // another thread's sequences
+    for (int b = b0; b + 1 < b1; ++b) {
+      s = seq_shape(a, sh, G, b);
+      const double room = tiles_room(a, sh, s, s.tiles);
       if (y < room) break;
       y -= room;
+      s = seq_shape(a, sh, G, b + 1);
     }
-    lds->kvh[e] = kvh; lds->b[e] = b; lds->y[e] = y;
+    lds->kvh[e] = (int)kvh; lds->shape[e] = s; lds->y[e] = y;
   }
   __syncthreads();
+  auto scalar = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  auto shape_of = [&](int e) {
+    const SeqShape& x = lds->shape[e];
+    return SeqShape{scalar(x.b), scalar(x.row0), scalar(x.n), scalar(x.N), scalar(x.tiles), scalar(x.page0)};
+  };
   // where in the sequence: a wave per end, 64 tiles (or steps of tiles) at a time
   if (wave < 2) {
-    SharePlace at{lds->kvh[wave], 0, 0, 0};
+    SharePlace at{scalar(lds->kvh[wave]), 0, 0, 0};
     if (at.kvh < a.H_kv) {
-      at.b = __builtin_amdgcn_readfirstlane(lds->b[wave]);
-      const long y = lds->y[wave];
-      const SeqShape s = seq_shape(a, sh, G, at.b);
-      int lo = 0, n = s.tiles;                 // the last tile that begins at or before y is one of lo .. lo + n - 1
+      const SeqShape q = shape_of(wave);
+      const double y = lds->y[wave];
+      int lo = 0, n = q.tiles;                 // the last tile that begins at or before y is one of lo .. lo + n - 1
       while (n > 1) {
-        const int step = (n + 63) >> 6, i = lo + lane * step;
-        const uint64_t past = __builtin_amdgcn_ballot_w64(lane * step >= n || line_room(a, sh, s, i) > y);   // the first lane's tile begins before it
+        const int step = (n + 63) >> 6;
+        const uint64_t past = __builtin_amdgcn_ballot_w64(lane * step >= n || line_room(a, sh, q, min(lo + lane * step, q.tiles)) > y) & ~1ull;
         const int k = (past == 0 ? 64 : __builtin_ctzll(past)) - 1;
         n = min(step, n - k * step);
         lo += k * step;
       }
-      const long begin = line_room(a, sh, s, lo), room = line_room(a, sh, s, lo + 1) - begin;
-      const TileKeys k = tile_keys<KT>(a, sh, s, tile_at(s, lo));
-      const int u = (int)floor_div((y - begin) * k.units, room);
-      const int near = (int)min(share / (KT * 24), (long)k.units);    // a cut so near an end would cost more than it evens out
-      at.i = lo; at.u = u < near ? 0 : k.units - u < near ? k.units : u;
+      const double begin = line_room(a, sh, q, lo), room = line_room(a, sh, q, lo + 1) - begin;
+      const TileKeys k = tile_keys<KT>(a, sh, q, tile_at(q, lo));
+      const int u = max((int)fmin(floor_div((y - begin) * k.units, room), (double)k.units), 0);
+      const int near = (int)fmin(share * (1. / (KT * 24)), (double)k.units);   // a cut so near an end would cost more than it evens out
+      at.b = q.b; at.i = lo; at.u = u < near ? 0 : k.units - u < near ? k.units : u;
     }
     if (lane == 0) lds->place[wave] = at;
   }
   __syncthreads();
-  auto scalar = [](const SharePlace& p) {
-    return SharePlace{__builtin_amdgcn_readfirstlane(p.kvh), __builtin_amdgcn_readfirstlane(p.b), __builtin_amdgcn_readfirstlane(p.i),
-                      __builtin_amdgcn_readfirstlane(p.u)};
-  };
-  *from = scalar(lds->place[0]); *to = scalar(lds->place[1]);
+  auto place_of = [&](int e) { const SharePlace& p = lds->place[e]; return SharePlace{scalar(p.kvh), scalar(p.b), scalar(p.i), scalar(p.u)}; };
+  *from = place_of(0); *to = place_of(1);
+  *first = shape_of(0);
 }
 
 // next sequence from b on that takes part (a.B: none); every wave by itself, 64 sequences at a time
@@ -169,10 +178,9 @@ __device__ __forceinline__ int next_sequence(const PagedAttnArgs& a, const Share
 // A workgroup's walk over its share: fn(kvh, shape, r, keys, ua, ub, again) for units [ua, ub) of every tile in it; where it returns true it is
 // called again, with `again` set.
 template <int KT, typename F>
-__device__ __forceinline__ void walk_share(const PagedAttnArgs& a, const ShareArgs& sh, int G, const SharePlace& from, const SharePlace& to, F&& fn) {
+__device__ __forceinline__ void walk_share(const PagedAttnArgs& a, const ShareArgs& sh, int G, const SharePlace& from, const SharePlace& to, SeqShape s, F&& fn) {
   int kvh = from.kvh, b = from.b, i = from.i, ua = from.u;
   if (kvh >= a.H_kv) return;
-  SeqShape s = seq_shape(a, sh, G, b);
   bool again = false;
   for (;;) {
     const bool last = kvh == to.kvh && b == to.b && i == to.i;
