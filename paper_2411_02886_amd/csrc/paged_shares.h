@@ -84,14 +84,66 @@ __device__ __forceinline__ TileKeys tile_keys(const PagedAttnArgs& a, const Shar
 
 struct SharePlace { int kvh, b, i, u; };       // i: the tile's turn in its sequence
 
-// All threads of the workgroup (256): begin and end of this workgroup's share, in scalar registers, and the sequence that it begins in.
+// The tile of a sequence that place y of its part of the line lies in, and the unit: by 32 or 64 lanes that have the same q and y (`first`:
+// the lowest of them, `many` of them), a step of tiles per lane and turn.
+template <int KT>
+__device__ __forceinline__ void find_unit(const PagedAttnArgs& a, const ShareArgs& sh, const SeqShape& q, double y, double share, int first, int many,
+                                          int* tile, int* unit) {
+  const int lane = (threadIdx.x & 63) - first;
+  int lo = 0, n = q.tiles;                     // the last tile that begins at or before y is one of lo .. lo + n - 1
+  while (__builtin_amdgcn_ballot_w64(n > 1) != 0) {
+    const int step = (n + many - 1) / many;
+    uint64_t past = __builtin_amdgcn_ballot_w64(lane * step >= n || line_room(a, sh, q, min(lo + lane * step, q.tiles)) > y) >> first;
+    past = (many == 32 ? past & 0xffffffffull : past) & ~1ull;
+    const int k = (past == 0 ? many : __builtin_ctzll(past)) - 1;
+    n = min(step, n - k * step);
+    lo += k * step;
+  }
+  const double begin = line_room(a, sh, q, lo), room = line_room(a, sh, q, lo + 1) - begin;
+  const TileKeys k = tile_keys<KT>(a, sh, q, tile_at(q, lo));
+  const int u = max((int)fmin(floor_div((y - begin) * k.units, room), (double)k.units), 0);
+  const int near = (int)fmin(share * (1. / (KT * 24)), (double)k.units);   // a cut so near an end would cost more than it evens out
+  *tile = lo;
+  *unit = u < near ? 0 : k.units - u < near ? k.units : u;
+}
+
+// Begin and end of this workgroup's share, in scalar registers, and the sequence that it begins in.  Called by all threads of the workgroup (256).
 struct ShareScratch { double sums[4], y[2]; int kvh[2]; SeqShape shape[2]; SharePlace place[2]; };
 template <int KT>
 __device__ __forceinline__ void find_share(const PagedAttnArgs& a, const ShareArgs& sh, int G, int wg, ShareScratch* lds, SharePlace* from,
                                            SharePlace* to, SeqShape* first) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  auto share_of_line = [&](double all) { return sh.whole ? 1. : fmax((double)sh.min_keys, floor_div(all + (sh.wgs - 1), sh.wgs)); };
+  if (a.B <= 64) {
+    // a lane per sequence, every wave for itself, both ends at once in the halves of the wave: no barrier, and half the time
+    SeqShape s{0, 0, 0, 0, 0, 0};
+    if (lane < a.B) s = seq_shape(a, sh, G, lane);
+    const double mine = tiles_room(a, sh, s, s.tiles);
+    double upto = mine;
+    for (int d = 1; d < a.B; d <<= 1) {
+      const double x = __shfl_up(upto, d);
+      if (lane >= d) upto += x;
+    }
+    const double line = __shfl(upto, a.B - 1), all = line * a.H_kv, share = share_of_line(all);
+    const int e = lane >> 5;                   // the end that this lane works on
+    const double x = (wg + e) * share;
+    const bool there = x < all;
+    const double kvh = there ? floor_div(x, line) : a.H_kv, y = fma(-kvh, line, x);
+    // its sequence: the first whose part of the line ends behind y
+    const uint64_t behind[2] = {__builtin_amdgcn_ballot_w64(upto > __shfl(y, 0)), __builtin_amdgcn_ballot_w64(upto > __shfl(y, 32))};
+    const int own = min((e == 0 ? behind[0] : behind[1]) != 0 ? __builtin_ctzll(e == 0 ? behind[0] : behind[1]) : 0, a.B - 1);
+    const SeqShape q{own, __shfl(s.row0, own), __shfl(s.n, own), __shfl(s.N, own), there ? __shfl(s.tiles, own) : 0, __shfl(s.page0, own)};
+    int tile = 0, unit = 0;
+    find_unit<KT>(a, sh, q, y - __shfl(upto - mine, own), share, e * 32, 32, &tile, &unit);
+    auto at = [](int x, int l) { return __builtin_amdgcn_readlane(x, l); };
+    const int kv = (int)kvh;
+    *from = SharePlace{at(kv, 0), at(own, 0), at(tile, 0), at(unit, 0)};
+    *to = SharePlace{at(kv, 32), at(own, 32), at(tile, 32), at(unit, 32)};
+    *first = SeqShape{at(q.b, 0), at(q.row0, 0), at(q.n, 0), at(q.N, 0), at(q.tiles, 0), at(q.page0, 0)};
+    return;
+  }
   // which sequences the two ends lie in: a thread has `per` neighbouring ones
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, per = (a.B + 255) >> 8;
-  const int b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
+  const int per = (a.B + 255) >> 8, b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
   SeqShape s{0, 0, 0, 0, 0, 0};
   double mine = 0.;
   for (int b = b0; b < b1; ++b) {
@@ -100,20 +152,14 @@ __device__ __forceinline__ void find_share(const PagedAttnArgs& a, const ShareAr
   }
   double upto = mine;
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    if (d >= a.B) break;                       // the sequences are fewer: the lanes behind them have nothing
-    const double x = __shfl_up(upto, d);
-    if (lane >= d) upto += x;
-  }
-  // (where the loop ended early the last lane has only its neighbours' rooms: the sum is the last sequence's)
-  if (lane == min(63, a.B - 1)) lds->sums[wave] = a.B < 64 && wave > 0 ? 0. : upto;
+  for (int d = 1; d < 64; d <<= 1) { const double x = __shfl_up(upto, d); if (lane >= d) upto += x; }
+  if (lane == 63) lds->sums[wave] = upto;
   if (tid < 2) lds->kvh[tid] = a.H_kv;         // the end of the line; also where lengths that change under the call lead nowhere
   __syncthreads();
   double before = upto - mine, line = 0.;
 #pragma unroll
   for (int w = 0; w < 4; ++w) { if (w < wave) before += lds->sums[w]; line += lds->sums[w]; }
-  const double all = line * a.H_kv;
-  const double share = sh.whole ? 1. : fmax((double)sh.min_keys, floor_div(all + (sh.wgs - 1), sh.wgs));
+  const double all = line * a.H_kv, share = share_of_line(all);
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
     const double x = (wg + e) * share;
@@ -136,25 +182,12 @@ __device__ __forceinline__ void find_share(const PagedAttnArgs& a, const ShareAr
     const SeqShape& x = lds->shape[e];
     return SeqShape{scalar(x.b), scalar(x.row0), scalar(x.n), scalar(x.N), scalar(x.tiles), scalar(x.page0)};
   };
-  // where in the sequence: a wave per end, 64 tiles (or steps of tiles) at a time
-  if (wave < 2) {
+  if (wave < 2) {                              // a wave per end
     SharePlace at{scalar(lds->kvh[wave]), 0, 0, 0};
     if (at.kvh < a.H_kv) {
       const SeqShape q = shape_of(wave);
-      const double y = lds->y[wave];
-      int lo = 0, n = q.tiles;                 // the last tile that begins at or before y is one of lo .. lo + n - 1
-      while (n > 1) {
-        const int step = (n + 63) >> 6;
-        const uint64_t past = __builtin_amdgcn_ballot_w64(lane * step >= n || line_room(a, sh, q, min(lo + lane * step, q.tiles)) > y) & ~1ull;
-        const int k = (past == 0 ? 64 : __builtin_ctzll(past)) - 1;
-        n = min(step, n - k * step);
-        lo += k * step;
-      }
-      const double begin = line_room(a, sh, q, lo), room = line_room(a, sh, q, lo + 1) - begin;
-      const TileKeys k = tile_keys<KT>(a, sh, q, tile_at(q, lo));
-      const int u = max((int)fmin(floor_div((y - begin) * k.units, room), (double)k.units), 0);
-      const int near = (int)fmin(share * (1. / (KT * 24)), (double)k.units);   // a cut so near an end would cost more than it evens out
-      at.b = q.b; at.i = lo; at.u = u < near ? 0 : k.units - u < near ? k.units : u;
+      at.b = q.b;
+      find_unit<KT>(a, sh, q, lds->y[wave], share, 0, 64, &at.i, &at.u);
     }
     if (lane == 0) lds->place[wave] = at;
   }
