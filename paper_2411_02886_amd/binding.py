@@ -373,25 +373,25 @@ def _row_stride(t, row: int, name: str) -> int:
     """Elements between the rows of a [rows][...] tensor whose rows are packed; row: elements of one."""
     if t is None:
         return 0
-    want = 1
-    for n, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-        if n > 1 and stride != want:
+    shape, strides, want = t.shape, t.stride(), 1
+    for i in range(len(shape) - 1, 0, -1):
+        if strides[i] != want and shape[i] > 1:
             raise ValueError("%s: the elements of a row must follow each other" % name)
-        want *= n
+        want *= shape[i]
     if want != row:
         raise ValueError("%s: rows of %d elements, the problem's have %d" % (name, want, row))
-    return int(t.stride(0)) if t.shape[0] > 1 else 0
+    return strides[0] if shape[0] > 1 else 0
 
 
 def ts_rope_append(p: Problem, rope, q, k, v, q_indptr, num_rows: int, positions, q_out, stream=None) -> None:
     """q, k, v: [rows][heads][D] or [rows][heads * D], rows any multiple of 16 bytes apart; q and q_out, or k and v, may be None."""
     D = p.c.head_dim
-    strides = [_row_stride(t, heads * D, name) for t, heads, name in ((q, p.c.num_q_heads, "q"), (k, p.c.num_kv_heads, "k"),
-                                                                      (v, p.c.num_kv_heads, "v"))]
+    kv_row = p.c.num_kv_heads * D
+    q_stride, k_stride, v_stride = _row_stride(q, p.c.num_q_heads * D, "q"), _row_stride(k, kv_row, "k"), _row_stride(v, kv_row, "v")
     if q_out is not None and not q_out.is_contiguous():
         raise ValueError("q_out: rows must follow each other")
-    _ok(load().ts_rope_append(p.ref(), None if rope is None else rope.ref(), _ptr(q), strides[0], _ptr(k), strides[1], _ptr(v),
-                              strides[2], _ptr(q_indptr), int(num_rows), _ptr(positions), _ptr(q_out), _stream(stream)),
+    _ok(load().ts_rope_append(p.ref(), None if rope is None else rope.ref(), _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v),
+                              v_stride, _ptr(q_indptr), int(num_rows), _ptr(positions), _ptr(q_out), _stream(stream)),
         "ts_rope_append")
 
 

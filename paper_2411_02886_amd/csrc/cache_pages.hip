@@ -15,13 +15,13 @@ __global__ __launch_bounds__(256) void pages_copy_kernel(PagesCopyArgs a) {
     if ((uint32_t)src >= (uint32_t)a.num_pages || (uint32_t)dst >= (uint32_t)a.num_pages || src == dst) continue;
     const uint8_t* from = pool + (int64_t)src * a.page_bytes + at;
     uint8_t* to = pool + (int64_t)dst * a.page_bytes + at;
-    uint4 x[kCopyUnroll];
+    u32x4_t x[kCopyUnroll];
 #pragma unroll
     for (int u = 0; u < kCopyUnroll; ++u)
-      if (at + u * 4096 < a.page_bytes) x[u] = *reinterpret_cast<const uint4*>(from + u * 4096);
+      if (at + u * 4096 < a.page_bytes) x[u] = *reinterpret_cast<const u32x4_t*>(from + u * 4096);
 #pragma unroll
     for (int u = 0; u < kCopyUnroll; ++u)
-      if (at + u * 4096 < a.page_bytes) *reinterpret_cast<uint4*>(to + u * 4096) = x[u];
+      if (at + u * 4096 < a.page_bytes) *reinterpret_cast<u32x4_t*>(to + u * 4096) = x[u];
   }
 }
 

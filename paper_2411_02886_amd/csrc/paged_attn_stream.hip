@@ -15,7 +15,6 @@ namespace ts {
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
 
 constexpr float kPsUnset = -3.40282347e38f;   // reference logit before the first key: no finite logit lies below it
 constexpr float kPsHead = 4.f;                // a raised reference lies this far above the largest logit so far ...

@@ -1,68 +1,193 @@
-// Rotary positions with several axes, and the new tokens' K and V rows into their pages.
+// Rotary positions with several axes, and the new tokens' K and V rows into their pages.  Bound by memory: every row is read and written once.
 //
-// A workgroup takes one token.  Its angles are the same for all heads: a lane per pair forms the angle in double (an exact int32
-// times a float has 55 bits), takes whole turns off in double and leaves cosine and sine in LDS; then every lane turns pieces of
-// heads.  Whoever writes an element is the only one who read it, so q may be turned in place.
+// Two or four waves take one token.  Its angles are the same for all heads: a lane per pair forms the angle in double (an exact int32 times
+// a float has 55 bits), takes whole turns off in double and leaves cosine and sine in LDS.  Then a lane has the same piece of every
+// head it works on, so that it reads its cosines once: 64 / (pieces of a head, rounded up to a power of two) heads side by side, several in flight.  A
+// piece is 16 bytes and its partner (halves) or 16 bytes that hold whole pairs (neighbours); where the rotated part does not
+// divide so, single pairs.  Whoever writes an element is the only one who read it, so q may be turned in place.
+// Measured (H 32/8, D 128): 15243 tokens, three axes, parts of a fused projection 155 us by a workgroup per token and single pairs, 79 so (4.7 TB/s, what a
+// large copy reaches); 64 single tokens 3.8 us.
 #include "ts_kernels.h"
 #include "ts_rows.h"
 
 namespace ts {
 
-template <typename T> __device__ __forceinline__ float load_el(const uint8_t* p, int i);
-template <> __device__ __forceinline__ float load_el<float>(const uint8_t* p, int i) { return reinterpret_cast<const float*>(p)[i]; }
-template <> __device__ __forceinline__ float load_el<uint16_t>(const uint8_t* p, int i) { return __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << 16); }
-template <typename T> __device__ __forceinline__ void store_el(uint8_t* p, int i, float x);
-template <> __device__ __forceinline__ void store_el<float>(uint8_t* p, int i, float x) { reinterpret_cast<float*>(p)[i] = x; }
-template <> __device__ __forceinline__ void store_el<uint16_t>(uint8_t* p, int i, float x) { reinterpret_cast<uint16_t*>(p)[i] = (uint16_t)f32_to_bf16_bits(x); }
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
 
-template <typename T>
+template <typename T> __device__ __forceinline__ float to_f32(T x) { return x; }
+template <> __device__ __forceinline__ float to_f32<uint16_t>(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+template <typename T> __device__ __forceinline__ T from_f32(float x) { return x; }
+template <> __device__ __forceinline__ uint16_t from_f32<uint16_t>(float x) { return (uint16_t)f32_to_bf16_bits(x); }
+
+template <typename T> struct Piece {                                   // 16 bytes as floats
+  static constexpr int N = 16 / sizeof(T);
+  float x[N];
+  __device__ __forceinline__ void load(u32x4_t v) {
+    const uint32_t w[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 2) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
+      else x[i] = __uint_as_float(w[i]);
+    }
+  }
+  __device__ __forceinline__ u32x4_t store() const {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 2) w[i] = __builtin_bit_cast(uint32_t, bf16x2_t{(__bf16)x[2 * i], (__bf16)x[2 * i + 1]});   // one instruction, to nearest even
+      else w[i] = __float_as_uint(x[i]);
+    }
+    return u32x4_t{w[0], w[1], w[2], w[3]};
+  }
+};
+
+// Up to so many tokens four waves share each, beyond that two.  (us, H 32/8, D 128, bf16: 64 tokens one wave each 5.6, two 4.5, four 3.8; 2048: 11.5, 10.9, 10.7;
+// 4096: 17.0, 16.1, 18.4; 20000 of H 14/2, D 64, fp32: 38.1, 36.8, 48.2.  Single pairs: four, 5000 tokens 39.4, 37.1, 32.8.)
+constexpr int kRopeFew = 2048;
+
+enum { kPairs = 0, kHalves = 1, kNeighbours = 2 };
+
+template <typename T, int MODE>
 __global__ __launch_bounds__(256) void rope_append_kernel(RopeAppendArgs a) {
-  constexpr int VE = 16 / sizeof(T);
-  __shared__ float s_cos[64], s_sin[64];
-  const int row = blockIdx.x, tid = threadIdx.x;
+  constexpr int VE = 16 / sizeof(T), UN = 2;                           // elements of a piece; pieces per lane in flight
+  __shared__ __attribute__((aligned(16))) float s_turn[4][2][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), share = 1 << a.share_shift;
+  const int part = wave & (share - 1), row = (blockIdx.x * 4 + wave) >> a.share_shift;   // `share` waves to a token
+  if (row >= a.T) return;
+  // What does not wait for the row's place is requested first: frequencies, positions, the first pieces of the heads and of V.  (A load after the
+  // stores would wait for them: 1300 fp32 tokens 18.7 us instead of 9.0.)
+  const int D = a.D, row_bytes = D * (int)sizeof(T), half = a.rotary >> 1;
+  const int nq = a.q != nullptr ? a.H : 0, nk = a.k != nullptr ? a.H_kv : 0;
+  const uint8_t* q_row = a.q + row * a.q_stride;
+  const uint8_t* k_row = a.k + row * a.k_stride;
+  double freq = 0.;
+  int pos = 0;
+  if (lane < half) {
+    freq = a.inv_freq[lane];
+    if (a.positions != nullptr) pos = a.positions[(size_t)a.pair_axis[lane] * a.T + row];
+  }
+  // pieces of a head: those that turn, then those that pass through; this lane's, in every step-th head from side on
+  const int turn = (MODE == kHalves ? half : a.rotary) / VE, units = turn + (D - a.rotary) / VE;
+  const int shift = units > 1 ? 32 - __builtin_clz((uint32_t)(units - 1)) : 0;
+  const int u = lane & ((1 << shift) - 1), lanes = 64 >> shift, side = part * lanes + (lane >> shift), step = lanes << a.share_shift;
+  const bool turns = u < turn;
+  const uint32_t e0 = (uint32_t)(turns || MODE == kNeighbours ? u * VE : a.rotary + (u - turn) * VE) * sizeof(T), e1 = e0 + half * sizeof(T);
+  u32x4_t v[UN], w[UN];
+  auto load = [&](int h0) {
+#pragma unroll
+    for (int k = 0; k < UN; ++k) {
+      const int h = h0 + k * step;
+      if (h >= nq + nk || u >= units) continue;
+      const uint8_t* from = h < nq ? q_row + h * row_bytes : k_row + (h - nq) * row_bytes;
+      v[k] = *reinterpret_cast<const u32x4_t*>(from + e0);
+      if (MODE == kHalves && turns) w[k] = *reinterpret_cast<const u32x4_t*>(from + e1);
+    }
+  };
+  if constexpr (MODE != kPairs) load(side);
+  const int v_pieces = nk * D / VE, v_lane = part * 64 + lane, v_step = 64 << a.share_shift;
+  const u32x4_t* v_row = reinterpret_cast<const u32x4_t*>(a.v + row * a.v_stride);
+  u32x4_t x[UN];
+  auto load_v = [&](int i0) {
+#pragma unroll
+    for (int k = 0; k < UN; ++k) if (i0 + k * v_step < v_pieces) x[k] = v_row[i0 + k * v_step];
+  };
+  load_v(v_lane);
+
   const RowPlace at = row_place(a.q_indptr, a.B, a.C, a.T, row);
   if (at.b < 0) return;
-  const int n = min(max(a.seq_lens[at.b], 0), a.max_seq_len);
-  const int place = n - at.left, half = a.rotary >> 1;
-  if (tid < half) {
-    const int pos = a.positions != nullptr ? a.positions[(size_t)a.pair_axis[tid] * a.T + row] : place;
-    const double turns = (double)pos * (double)a.inv_freq[tid] * 0.15915494309189533577;
+  const int n = min(max(a.seq_lens[at.b], 0), a.max_seq_len), place = n - at.left, page0 = a.page_indptr[at.b];
+  const bool append = nk != 0 && place >= 0;
+  int64_t slot = 0;
+  if (append) slot = ((int64_t)a.page_indices[page0 + (place >> a.p_shift)] << a.p_shift) + (place & (a.P - 1));
+  float* s_cos = s_turn[wave][0];
+  float* s_sin = s_turn[wave][1];
+  if (lane < half) {
+    if (a.positions == nullptr) pos = place;
+    const double turns = (double)pos * freq * 0.15915494309189533577;
     float s, c;
     sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
-    s_cos[tid] = c * a.scale; s_sin[tid] = s * a.scale;
+    s_cos[lane] = c * a.scale; s_sin[lane] = s * a.scale;
   }
-  __syncthreads();
-  const int D = a.D, row_elems = D;
-  const bool append = a.k != nullptr && place >= 0;
-  const int64_t slot = append ? ((int64_t)a.page_indices[a.page_indptr[at.b] + (place >> a.p_shift)] << a.p_shift) + (place & (a.P - 1)) : 0;
-  const int heads_q = a.q != nullptr ? a.H : 0, heads_k = append ? a.H_kv : 0;
-  // elements one by one: pairs, then what passes through
-  const int units = half + (D - a.rotary);
-  for (int u = tid; u < (heads_q + heads_k) * units; u += 256) {
-    const int h = u / units, i = u % units;
-    const uint8_t* from; uint8_t* to;
-    if (h < heads_q) {
-      from = a.q + row * a.q_stride + (int64_t)h * row_elems * sizeof(T);
-      to = a.q_out + ((int64_t)row * a.H + h) * row_elems * sizeof(T);
-    } else {
-      from = a.k + row * a.k_stride + (int64_t)(h - heads_q) * row_elems * sizeof(T);
-      to = a.k_pool + (slot * a.H_kv + (h - heads_q)) * row_elems * sizeof(T);
+  __builtin_amdgcn_wave_barrier();                                     // (a wave's LDS accesses keep their order)
+  uint8_t* q_to = a.q_out + (int64_t)row * a.H * row_bytes;
+  uint8_t* k_to = a.k_pool + slot * a.H_kv * row_bytes;
+  if constexpr (MODE == kPairs) {
+    const int each = half + (D - a.rotary), all = (nq + (append ? nk : 0)) * each;   // pairs, then elements that pass through
+    for (int j = v_lane; j < all; j += v_step) {
+      const int h = j / each, i = j - h * each;
+      const T* from = reinterpret_cast<const T*>(h < nq ? q_row + h * row_bytes : k_row + (h - nq) * row_bytes);
+      T* to = reinterpret_cast<T*>(h < nq ? q_to + h * row_bytes : k_to + (h - nq) * row_bytes);
+      if (i >= half) { to[half + i] = from[half + i]; continue; }      // element rotary + i - half
+      const int p0 = a.adjacent ? 2 * i : i, p1 = a.adjacent ? 2 * i + 1 : i + half;
+      const float x = to_f32<T>(from[p0]), y = to_f32<T>(from[p1]), c = s_cos[i], s = s_sin[i];
+      to[p0] = from_f32<T>(x * c - y * s);
+      to[p1] = from_f32<T>(x * s + y * c);
     }
-    if (i >= half) { const int e = a.rotary + i - half; reinterpret_cast<T*>(to)[e] = reinterpret_cast<const T*>(from)[e]; continue; }
-    const int e0 = a.adjacent ? 2 * i : i, e1 = a.adjacent ? 2 * i + 1 : i + half;
-    const float x = load_el<T>(from, e0), y = load_el<T>(from, e1), c = s_cos[i], s = s_sin[i];
-    store_el<T>(to, e0, x * c - y * s);
-    store_el<T>(to, e1, x * s + y * c);
+  } else {
+    constexpr int NP = MODE == kHalves ? VE : VE / 2;                  // pairs of a piece
+    float c[NP], s[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) { c[i] = turns ? s_cos[u * NP + i] : 1.f; s[i] = turns ? s_sin[u * NP + i] : 0.f; }
+    const int nh = nq + (append ? nk : 0);
+    for (int h0 = side; h0 < nq + nk; h0 += step * UN) {
+      if (h0 != side) load(h0);
+#pragma unroll
+      for (int k = 0; k < UN; ++k) {
+        const int h = h0 + k * step;
+        if (h >= nh || u >= units) continue;
+        uint8_t* to = h < nq ? q_to + h * row_bytes : k_to + (h - nq) * row_bytes;
+        if (turns) {
+          Piece<T> x;
+          x.load(v[k]);
+          if constexpr (MODE == kHalves) {
+            Piece<T> y;
+            y.load(w[k]);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+              const float f = x.x[i], g = y.x[i];
+              x.x[i] = f * c[i] - g * s[i];
+              y.x[i] = f * s[i] + g * c[i];
+            }
+            *reinterpret_cast<u32x4_t*>(to + e1) = y.store();
+          } else {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+              const float f = x.x[2 * i], g = x.x[2 * i + 1];
+              x.x[2 * i] = f * c[i] - g * s[i];
+              x.x[2 * i + 1] = f * s[i] + g * c[i];
+            }
+          }
+          v[k] = x.store();
+        }
+        *reinterpret_cast<u32x4_t*>(to + e0) = v[k];
+      }
+    }
   }
-  if (append)
-    for (int u = tid; u < a.H_kv * D / VE; u += 256)
-      reinterpret_cast<uint4*>(a.v_pool + slot * a.H_kv * D * sizeof(T))[u] = reinterpret_cast<const uint4*>(a.v + row * a.v_stride)[u];
+  if (append) {
+    u32x4_t* to = reinterpret_cast<u32x4_t*>(a.v_pool + slot * a.H_kv * row_bytes);
+    for (int i0 = v_lane; i0 < v_pieces; i0 += v_step * UN) {
+      if (i0 != v_lane) load_v(i0);
+#pragma unroll
+      for (int k = 0; k < UN; ++k) if (i0 + k * v_step < v_pieces) to[i0 + k * v_step] = x[k];
+    }
+  }
+}
+
+template <typename T>
+static hipError_t rope_one(const RopeAppendArgs& b, hipStream_t s) {
+  constexpr int VE = 16 / sizeof(T);
+  RopeAppendArgs a = b;
+  const bool pairs = a.rotary % (a.adjacent ? VE : 2 * VE) != 0;
+  a.share_shift = a.T <= kRopeFew || pairs ? 2 : 1;
+  const dim3 grid((unsigned)((((long)a.T << a.share_shift) + 3) / 4)), block(256);
+  if (pairs) hipLaunchKernelGGL((rope_append_kernel<T, kPairs>), grid, block, 0, s, a);
+  else if (a.adjacent) hipLaunchKernelGGL((rope_append_kernel<T, kNeighbours>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((rope_append_kernel<T, kHalves>), grid, block, 0, s, a);
+  return hipGetLastError();
 }
 
 hipError_t launch_rope_append(int dtype, const RopeAppendArgs& a, hipStream_t s) {
-  if (dtype == TS_BF16) hipLaunchKernelGGL(rope_append_kernel<uint16_t>, dim3(a.T), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(rope_append_kernel<float>, dim3(a.T), dim3(256), 0, s, a);
-  return hipGetLastError();
+  return dtype == TS_BF16 ? rope_one<uint16_t>(a, s) : rope_one<float>(a, s);
 }
 
 }  // namespace ts

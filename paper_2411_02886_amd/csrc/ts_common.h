@@ -227,6 +227,10 @@ template <int CTRL>
 __device__ __forceinline__ float dpp_f32(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
 }
+// 16 bytes as the compiler's own vector.  (Arrays of uint4, a struct, that are written under conditions it does not split into registers: it put them into LDS,
+// with an address from the dispatch packet, which lies in host memory: a load of 10 us where many CUs ask for it.)
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4_t;
+
 // sum over the 8 lanes of an aligned lane group; every lane of the group gets the total
 __device__ __forceinline__ float group8_sum(float v) {
   v += dpp_f32<0xB1>(v);    // quad_perm [1,0,3,2]

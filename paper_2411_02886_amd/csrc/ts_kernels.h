@@ -242,6 +242,7 @@ struct RopeAppendArgs {
   const float* inv_freq;
   int64_t q_stride, k_stride, v_stride;   // bytes between rows
   int B, C, T, H, H_kv, D, P, p_shift, max_seq_len, rotary, adjacent;
+  int share_shift;             // log2 of the waves that share a token (set by the launch)
   float scale;
   uint8_t pair_axis[64];
 };
