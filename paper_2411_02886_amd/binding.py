@@ -161,6 +161,7 @@ class Problem:
         self.c = _CProblem(batch, chunk, num_q_heads, num_kv_heads, head_dim, page_size, max_seq_len, dtype,
                            _ptr(k_pool), _ptr(v_pool), _ptr(page_indptr), _ptr(page_indices), _ptr(seq_lens),
                            int(num_initial), int(num_local))
+        self.q_row, self.kv_row = num_q_heads * head_dim, num_kv_heads * head_dim      # elements of a token's q, and of its k or v
 
     def ref(self):
         return ctypes.byref(self.c)
@@ -179,9 +180,10 @@ class Rope:
             raise ValueError("inv_freq: a contiguous float32 tensor")
         self._keep = inv_freq
         self.c = _CRope(_ptr(inv_freq), 2 * n, int(num_axes), int(bool(adjacent)), float(scale), (ctypes.c_uint8 * 64)(*axes))
+        self._ref = ctypes.byref(self.c)
 
     def ref(self):
-        return ctypes.byref(self.c)
+        return self._ref
 
 
 def rope_axes(sections, dealt=False):
@@ -374,6 +376,8 @@ def _row_stride(t, row: int, name: str) -> int:
     if t is None:
         return 0
     shape, strides, want = t.shape, t.stride(), 1
+    if len(shape) == 2 and shape[1] == row and strides[1] == 1:
+        return strides[0] if shape[0] > 1 else 0
     for i in range(len(shape) - 1, 0, -1):
         if strides[i] != want and shape[i] > 1:
             raise ValueError("%s: the elements of a row must follow each other" % name)
@@ -385,9 +389,7 @@ def _row_stride(t, row: int, name: str) -> int:
 
 def ts_rope_append(p: Problem, rope, q, k, v, q_indptr, num_rows: int, positions, q_out, stream=None) -> None:
     """q, k, v: [rows][heads][D] or [rows][heads * D], rows any multiple of 16 bytes apart; q and q_out, or k and v, may be None."""
-    D = p.c.head_dim
-    kv_row = p.c.num_kv_heads * D
-    q_stride, k_stride, v_stride = _row_stride(q, p.c.num_q_heads * D, "q"), _row_stride(k, kv_row, "k"), _row_stride(v, kv_row, "v")
+    q_stride, k_stride, v_stride = _row_stride(q, p.q_row, "q"), _row_stride(k, p.kv_row, "k"), _row_stride(v, p.kv_row, "v")
     if q_out is not None and not q_out.is_contiguous():
         raise ValueError("q_out: rows must follow each other")
     _ok(load().ts_rope_append(p.ref(), None if rope is None else rope.ref(), _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v),

@@ -237,7 +237,7 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
     // A workgroup per tile, and no merge, where tiles are short.
     const long tiles = (a.q_indptr != nullptr ? a.T / sh.tpt + std::min(a.B, a.T) : (long)a.B * ((a.C + sh.tpt - 1) / sh.tpt)) * a.H_kv;
     const long units = (std::min((long)a.max_seq_len, a.window > 0 ? (long)a.window + sh.tpt : LONG_MAX) + kt - 1) / kt;
-    if (few ? tiles < (1l << 30) && (units * kt <= 512 || (tiles >= most_wgs && units <= 16)) : tiles <= most_wgs && units <= 16) { sh.whole = 1; sh.wgs = (int)tiles; }
+    if (few ? tiles < (1l << 23) && (units * kt <= 512 || (tiles >= most_wgs && units <= 16)) : tiles <= most_wgs && units <= 16) { sh.whole = 1; sh.wgs = (int)tiles; }
     hipError_t e;
     if (tall) e = launch_paged_tall(D, a, sh, s);
     else e = launch_paged_stream(dtype, D, rows / 16, a, sh, s);

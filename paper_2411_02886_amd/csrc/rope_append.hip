@@ -9,6 +9,7 @@
 // large copy reaches); 64 single tokens 3.8 us.
 #include "ts_kernels.h"
 #include "ts_rows.h"
+#include <algorithm>
 
 namespace ts {
 
@@ -52,7 +53,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeAppendArgs a) {
   constexpr int VE = 16 / sizeof(T), UN = 2;                           // elements of a piece; pieces per lane in flight
   __shared__ __attribute__((aligned(16))) float s_turn[4][2][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), share = 1 << a.share_shift;
-  const int part = wave & (share - 1), row = (blockIdx.x * 4 + wave) >> a.share_shift;   // `share` waves to a token
+  const int part = wave & (share - 1), row = (int)((((uint64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + wave) >> a.share_shift);   // `share` waves to a token
   if (row >= a.T) return;
   // What does not wait for the row's place is requested first: frequencies, positions, the first pieces of the heads and of V.  (A load after the
   // stores would wait for them: 1300 fp32 tokens 18.7 us instead of 9.0.)
@@ -179,7 +180,8 @@ static hipError_t rope_one(const RopeAppendArgs& b, hipStream_t s) {
   RopeAppendArgs a = b;
   const bool pairs = a.rotary % (a.adjacent ? VE : 2 * VE) != 0;
   a.share_shift = a.T <= kRopeFew || pairs ? 2 : 1;
-  const dim3 grid((unsigned)((((long)a.T << a.share_shift) + 3) / 4)), block(256);
+  const long wgs = (((long)a.T << a.share_shift) + 3) / 4, wide = 1 << 20;      // (a grid has less than 2^32 threads in a dimension)
+  const dim3 grid((unsigned)std::min(wgs, wide), (unsigned)((wgs + wide - 1) / wide)), block(256);
   if (pairs) hipLaunchKernelGGL((rope_append_kernel<T, kPairs>), grid, block, 0, s, a);
   else if (a.adjacent) hipLaunchKernelGGL((rope_append_kernel<T, kNeighbours>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((rope_append_kernel<T, kHalves>), grid, block, 0, s, a);
