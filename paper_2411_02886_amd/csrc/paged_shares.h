@@ -132,7 +132,8 @@ __device__ __forceinline__ void find_share(const PagedAttnArgs& a, const ShareAr
     // its sequence: the first whose part of the line ends behind y
     const uint64_t behind[2] = {__builtin_amdgcn_ballot_w64(upto > __shfl(y, 0)), __builtin_amdgcn_ballot_w64(upto > __shfl(y, 32))};
     const int own = min((e == 0 ? behind[0] : behind[1]) != 0 ? __builtin_ctzll(e == 0 ? behind[0] : behind[1]) : 0, a.B - 1);
-    const SeqShape q{own, __shfl(s.row0, own), __shfl(s.n, own), __shfl(s.N, own), there ? __shfl(s.tiles, own) : 0, __shfl(s.page0, own)};
+    const int own_tiles = __shfl(s.tiles, own);         // (by all lanes: one that takes no part gives nothing)
+    const SeqShape q{own, __shfl(s.row0, own), __shfl(s.n, own), __shfl(s.N, own), there ? own_tiles : 0, __shfl(s.page0, own)};
     int tile = 0, unit = 0;
     find_unit<KT>(a, sh, q, y - __shfl(upto - mine, own), share, e * 32, 32, &tile, &unit);
     auto at = [](int x, int l) { return __builtin_amdgcn_readlane(x, l); };

@@ -275,3 +275,108 @@ def test_a_pool_beyond_32_bits(gpu):
         torch.cuda.synchronize()
         ref = attention(small, q, [chunk], 0, float(np.float32(sm)), [chunk * 4 > 32])
         check_attention(W.as_f32(to_host(out, bits16=True), BF).astype(np.float64), to_host(lse).astype(np.float64), ref, chunk)
+
+
+LOOSE = 1 << 20      # a bound far above the lengths: tiles are cut into shares however short they are
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H,H_kv", HEADS + [(128, 16), (96, 32)])
+def test_shares_of_every_head_layout(gpu, dtype, D, H, H_kv):
+    new, old = [65, 1, 0, 70, 3], [700, 900, 5, 131, 0]
+    c = Cache(dtype, H_kv, D, 16, [a + b for a, b in zip(new, old)], seed=H * 19 + D)
+    o, l, ref = run(gpu, c, H, new, seed=H, max_seq_len=LOOSE)
+    check_attention(o, l, ref, "prompts")
+    o, l, ref = run(gpu, c, H, [1] * 5, packed=False, seed=H, max_seq_len=LOOSE)
+    check_attention(o, l, ref, "tokens")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("window", [1, 63, 100, 1000])
+@pytest.mark.parametrize("D", [64, 128])
+def test_windows_in_shares(gpu, dtype, window, D):
+    new = [1, 90, 0, 5, 600, 1]
+    c = Cache(dtype, 2, D, 8, [3000, 290, 17, 5, 1517, 2], seed=window)
+    o, l, ref = run(gpu, c, 6, new, window=window, seed=3, max_seq_len=LOOSE)
+    check_attention(o, l, ref, window)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("B", [1, 2, 33, 63, 64, 65, 256, 257, 600])
+@pytest.mark.parametrize("loose", [False, True], ids=["", "loose bound"])
+def test_batches(gpu, dtype, B, loose):
+    rng = np.random.Generator(np.random.PCG64(B))
+    lens = rng.integers(0, 300, size=B).tolist()
+    c = Cache(dtype, 2, 64, 16, lens, seed=B)
+    bound = LOOSE if loose else None
+    o, l, ref = run(gpu, c, 8, [1] * B, packed=False, seed=B, max_seq_len=bound)
+    check_attention(o, l, ref, "tokens")
+    new = [min(n, int(rng.integers(0, 3) ** 6)) for n in lens]                   # 0, 1 or up to 64
+    o, l, ref = run(gpu, c, 8, new, seed=B, max_seq_len=bound, chunk=64)
+    check_attention(o, l, ref, "mixed")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [1, 130])
+@pytest.mark.parametrize("rise", [400.0, -400.0, 60.0])
+def test_logits_that_rise_or_fall_along_the_sequence(gpu, dtype, D, n, rise):
+    """From 0 to `rise` over 3000 tokens: far beyond what the first tiles' largest logit says, or far below it."""
+    N = 3000
+    c = Cache(dtype, 2, D, 16, [N, N - 900], seed=n)
+    for b in range(2):
+        at = c.slots(b)
+        t = np.arange(len(at)) / N
+        k = 0.1 * c.k[at] + (rise * t * math.sqrt(D) / D)[:, None, None]        # queries are near 1 in every element
+        bits = W.store(k.astype(np.float32), dtype)
+        c.k_bits[at], c.k[at] = bits, W.as_f32(bits, dtype).astype(np.float64)
+    rng = np.random.Generator(np.random.PCG64(5))
+    q = W.store((1 + 0.1 * rng.standard_normal((2 * n, 8, D))).astype(np.float32), dtype)
+    from paper_2411_02886_amd.runtime import to_device, to_host
+    for bound in (None, LOOSE):
+        p, _, _ = c.problem(8, chunk=n, max_seq_len=bound)
+        out = torch.zeros((2 * n, 8, D), dtype=torch.int16 if dtype == BF else torch.float32, device="cuda:0")
+        lse = torch.zeros((2 * n, 8), device="cuda:0")
+        gpu.ts_paged_attn(p, to_device(q), None, 2 * n, 0, 1 / math.sqrt(D), out, lse, workspace(gpu, p, 2 * n))
+        torch.cuda.synchronize()
+        ref = attention(c, q, [n, n], 0, float(np.float32(1 / math.sqrt(D))), [dtype == BF and n * 4 > 32] * 2)
+        check_attention(W.as_f32(to_host(out, bits16=dtype == BF), dtype).astype(np.float64), to_host(lse).astype(np.float64), ref, bound)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("n", [1, 100])
+def test_a_broken_sequence_leaves_the_others_alone(gpu, dtype, bad, n):
+    """Its own rows are unspecified; the call ends, and the other sequences' bits do not change."""
+    from paper_2411_02886_amd.runtime import to_device
+    lens = [900, 700, 333]
+    c = Cache(dtype, 2, 64, 16, lens, seed=4)
+    rng = np.random.Generator(np.random.PCG64(5))
+    q = to_device(W.store(rng.standard_normal((3 * n, 8, 64), dtype=np.float32), dtype))
+    got = []
+    for broken in (False, True):
+        p, k, v = c.problem(8, chunk=n, max_seq_len=LOOSE)
+        if broken:
+            at = torch.tensor(c.slots(1)[::7], device="cuda:0")
+            val = torch.tensor([bad]).to(torch.bfloat16).view(torch.int16)[0] if dtype == BF else torch.tensor(bad)
+            for x in (k, v):
+                x.view(-1, 2, 64)[at] = val.to("cuda:0")
+        out, lse = torch.zeros_like(q), torch.zeros((3 * n, 8), device="cuda:0")
+        gpu.ts_paged_attn(p, q, None, 3 * n, 0, 0.125, out, lse, workspace(gpu, p, 3 * n))
+        torch.cuda.synchronize()
+        got.append((out, lse))
+    for rows in (slice(0, n), slice(2 * n, 3 * n)):
+        assert torch.equal(got[0][0][rows], got[1][0][rows]) and torch.equal(got[0][1][rows], got[1][1][rows])
+
+
+def test_more_new_tokens_than_the_bound_says_in_shares(gpu):
+    new = [40, 3, 90]
+    for dtype in (BF, F32):
+        for H in (8, 4):
+            c = Cache(dtype, 2, 128, 16, [400, 3, 291], seed=2)
+            o, l, _ = run(gpu, c, H, new, seed=2, chunk=1, max_seq_len=LOOSE)
+            rng = np.random.Generator(np.random.PCG64(1002))
+            q = W.store(rng.standard_normal((sum(new), H, 128), dtype=np.float32), dtype)
+            ref = attention(c, q, new, 0, float(np.float32(1 / math.sqrt(128))), [dtype == BF] * 3)
+            check_attention(o, l, ref, dtype)
