@@ -325,8 +325,10 @@ int32_t ts_chunk_mean_query(const ts_problem* p, const void* q, void* q_mean, vo
 /* Attention of the new tokens over their whole sequence (dense: no selection, no index list), both dtypes:
  *   out[r][h][:] = sum_t softmax_t( <q[r][h], K[slot(b, t)][h/G]> * sm_scale ) * V[slot(b, t)][h/G]
  * for new token c = r - q_indptr[b] at place x = N_b - n_b + c over t in [max(0, x - window + 1), x]; window 0 = from 0 on (every
- * cached token and the chunk's own up to x).  Float accumulation, out rounded to p->dtype; bf16: where a sequence's rows
+ * cached token and the chunk's own up to x).  Float accumulation, out rounded to p->dtype; bf16: where chunk * G and a sequence's
  * n_b * G are more than 32, the weights that multiply V are rounded to bf16 (matrix-core operand; their sum is not).
+ * Pages that no new token sees (wholly in front of the first one's window, behind N_b) are not read.  A token that some of a sequence's rows see
+ * and others do not takes part in the latter with weight 0: its K may be anything, its V has to be finite.
  * q, out [device] [num_rows][H][D], 16-byte aligned, not overlapping; lse [device] float [num_rows][H] or NULL.
  * A row that sees no token (N_b < n_b: its place is negative) gets out = 0, lse = -inf.  Rows outside q_indptr[0] ..
  * q_indptr[B] are left as they are.  num_initial / num_local do not matter: every token is attended.

@@ -113,8 +113,10 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
     int nt = ub - ua;
     if (key0 + (nt - 1) * KT > tmax) --nt;
     uint32_t at[NLD];                                              // a tile's rows (this lane's of each load) in the pools
+    // (keys past the end or in front of the tile's first window stand for the nearest that some row sees: no other place of the pools is read)
+    auto seen = [&](int t) -> int { return min(max(t, keys.first), tmax); };
     auto fetch_look = [&](int i, int place) {
-      const int t = min(key0 + i * KT + (lane & (TK - 1)), tmax);
+      const int t = seen(key0 + i * KT + (lane & (TK - 1)));
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(lds_k + 2 * TILE_B + place * 256), "v"(pages + (t >> a.p_shift)) : "memory", "m0");
     };
     // (fresh(): the compiler forms the address anew in each turn of the loop.  It would keep all of them, dozens of registers, and spill.)
@@ -123,7 +125,7 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
       const int my_row = (int)fresh(st_row);
 #pragma unroll
       for (int l = 0; l < NLD; ++l) {
-        const int row = l * RPI + my_row, t = min(key0 + i * KT + row, tmax);      // past the end: the last key again
+        const int row = l * RPI + my_row, t = seen(key0 + i * KT + row);
         at[l] = ((uint32_t)look[place * 64 + row] << a.p_shift) + (uint32_t)(t & (a.P - 1));
       }
     };

@@ -119,15 +119,17 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
     // ---- Memory to LDS, 16 bytes per lane: the wave's 64 lanes fill 1 KiB from the (uniform) LDS address.  Written in assembly because the
     // compiler, which cannot tell the buffers apart, makes every later LDS read wait for the builtin form; completion is awaited by the
     // vmcnt before a tile's barrier.  Page ids come the same way, three tiles earlier.
+    // Keys past the end or in front of the tile's first window stand for the nearest that some row sees: no other place of the pools is read.
+    auto seen = [&](int t) __attribute__((always_inline)) -> int { return min(max(t, keys.first), tmax); };
     auto fetch_look = [&](int it) __attribute__((always_inline)) {
-      const int t = min(key0 + it * kPtTile + wave * WK + (lane & (WK - 1)), tmax);
+      const int t = seen(key0 + it * kPtTile + wave * WK + (lane & (WK - 1)));
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(look + (it & (kPtRing - 1)) * 256), "v"(pages + (t >> a.p_shift)) : "memory", "m0");
     };
     uint32_t at_k[NLD], at_v[NLD];                                 // rows of the K tile and of the V tile that are requested next
-    auto rows_of = [&](int it) __attribute__((always_inline)) {    // past the end: the last key again
+    auto rows_of = [&](int it) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < NLD; ++i) {
-        const int key = i * KPI + st_key, t = min(key0 + it * kPtTile + wave * WK + key, tmax);
+        const int key = i * KPI + st_key, t = seen(key0 + it * kPtTile + wave * WK + key);
         const int page = *(const volatile __attribute__((address_space(3))) int*)(look + (uint32_t)((it & (kPtRing - 1)) * 256 + key * 4));
         at_v[i] = at_k[i];
         at_k[i] = ((uint32_t)page << a.p_shift) + (uint32_t)(t & (a.P - 1));

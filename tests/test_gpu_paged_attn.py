@@ -380,3 +380,20 @@ def test_more_new_tokens_than_the_bound_says_in_shares(gpu):
             q = W.store(rng.standard_normal((sum(new), H, 128), dtype=np.float32), dtype)
             ref = attention(c, q, new, 0, float(np.float32(1 / math.sqrt(128))), [dtype == BF] * 3)
             check_attention(o, l, ref, dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("H,D", [(8, 64), (4, 128)])
+@pytest.mark.parametrize("window", [1, 20, 100, 300])
+def test_tokens_in_front_of_every_window_are_not_read(gpu, dtype, H, D, window):
+    new, lens = [1, 4, 13, 150], [900, 333, 517, 800]
+    c = Cache(dtype, 2, D, 16, lens, seed=window)
+    nan = 0x7fc0 if dtype == BF else np.nan
+    for b, (n, N) in enumerate(zip(new, lens)):
+        first = max(0, N - n - window + 1)
+        at = c.slots(b)[:first]
+        c.k_bits[at], c.v_bits[at] = nan, nan
+        c.pages[c.indptr[b]:c.indptr[b] + first // 16] = c.spare[0]            # pages of full NaN stand for those that are gone
+    for bound in (None, LOOSE):
+        o, l, ref = run(gpu, c, H, new, window=window, seed=9, max_seq_len=bound)
+        check_attention(o, l, ref, (window, bound))
