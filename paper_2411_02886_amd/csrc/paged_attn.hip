@@ -36,98 +36,76 @@ __device__ __forceinline__ Pieces find_pieces(const ShareArgs& sh, int w, int la
 }
 
 // Joins the pieces of the tiles that were cut: blockIdx.y stands for the workgroup whose share began the tile, the
-// pieces that follow lie in the workgroups behind it, up to the one that ends the tile.  D / 4 lanes per row, RPT rows per lane, PG
-// groups of lanes that share the pieces, US of which a lane has in flight: many of which may belong to a tile.
-template <int ES, int D, int THREADS, int RPT, int PG, int US>
-__global__ __launch_bounds__(THREADS) void paged_merge_kernel(PagedAttnArgs a, ShareArgs sh, int rows) {
-  constexpr int LPR = D / 4, LR = THREADS / (LPR * PG), RPB = LR * RPT;   // rows side by side, rows per workgroup
-  __shared__ float4 s_o[PG][RPB][LPR];
-  __shared__ float s_ml[PG][RPB][2];
+// pieces that follow lie in the workgroups behind it, up to the one that ends the tile: many of which may belong to a tile.  A workgroup per row: D / 4
+// lanes hold it, PG groups of them take the pieces in turn, with US in flight each, and meet in LDS.  Latency is all it costs (one token over 4096
+// keys, fp32: 13 us with the attention; with four rows per workgroup and two pieces in flight per group it was 18).
+template <int ES, int D, int US>
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a, ShareArgs sh, int rows) {
+  constexpr int LPR = D / 4, PG = 256 / LPR;
+  __shared__ float4 s_o[PG][LPR];
+  __shared__ float s_ml[PG][2];
   const int w = blockIdx.y, G = a.H / a.H_kv;     // (rows first: the tiles that were cut may all be every fourth workgroup's, and so on two XCDs)
   const int32_t* d1 = sh.desc + (size_t)w * 8 + 4;
   const int lane = threadIdx.x & 63, next = next_piece(sh, w, lane);
   if (d1[3] == kPieceNone) return;
   const int row0 = d1[0], kvh = d1[1], nrows = d1[2] * G;
-  const int sub = threadIdx.x % LPR, rr = threadIdx.x / LPR % LR, pg = threadIdx.x / (LPR * LR);
+  const int sub = threadIdx.x % LPR, pg = threadIdx.x / LPR;
   const Pieces pc = find_pieces(sh, w, lane, next);
   const int pieces = pc.count;
-  for (int j0 = blockIdx.x * RPB; j0 < nrows; j0 += gridDim.x * RPB) {
-    float M[RPT], L[RPT];
-    float4 o[RPT];
-#pragma unroll
-    for (int t = 0; t < RPT; ++t) { M[t] = -INFINITY; L[t] = 0.f; o[t] = make_float4(0.f, 0.f, 0.f, 0.f); }
+  for (int j = blockIdx.x; j < nrows; j += gridDim.x) {
+    float M = -INFINITY, L = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int p0 = pg; p0 < pieces; p0 += PG * US) {
-      float2 v[RPT][US];
-      float4 x[RPT][US];
+      float2 v[US];
+      float4 x[US];
 #pragma unroll
       for (int u = 0; u < US; ++u) {
         const int p = p0 + u * PG;
         const size_t slot = (size_t)(w + p) * 2 + (p == 0 ? 1 : 0);
-        const bool there = p < pieces && pc.there(sh, w, p);
-#pragma unroll
-        for (int t = 0; t < RPT; ++t) {
-          const int j = j0 + t * LR + rr;
-          v[t][u] = make_float2(-INFINITY, 0.f);
-          x[t][u] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (!there || j >= nrows) continue;
-          v[t][u] = *reinterpret_cast<const float2*>(sh.part_ml + (slot * rows + j) * 2);
-          x[t][u] = *reinterpret_cast<const float4*>(sh.part_o + (slot * rows + j) * D + sub * 4);
-        }
+        v[u] = make_float2(-INFINITY, 0.f);
+        x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (p >= pieces || !pc.there(sh, w, p)) continue;
+        v[u] = *reinterpret_cast<const float2*>(sh.part_ml + (slot * rows + j) * 2);
+        x[u] = *reinterpret_cast<const float4*>(sh.part_o + (slot * rows + j) * D + sub * 4);
       }
+      float m = M;
 #pragma unroll
-      for (int t = 0; t < RPT; ++t) {
-        float m = M[t];
+      for (int u = 0; u < US; ++u) m = fmaxf(m, v[u].x);
+      if (m == -INFINITY) continue;
+      const float f = expf(M - m);
+      L *= f; o.x *= f; o.y *= f; o.z *= f; o.w *= f;
 #pragma unroll
-        for (int u = 0; u < US; ++u) m = fmaxf(m, v[t][u].x);
-        if (m == -INFINITY) continue;
-        const float f = expf(M[t] - m);
-        L[t] *= f; o[t].x *= f; o[t].y *= f; o[t].z *= f; o[t].w *= f;
-#pragma unroll
-        for (int u = 0; u < US; ++u) {
-          const float g = expf(v[t][u].x - m);
-          L[t] = fmaf(g, v[t][u].y, L[t]);
-          o[t].x = fmaf(g, x[t][u].x, o[t].x); o[t].y = fmaf(g, x[t][u].y, o[t].y);
-          o[t].z = fmaf(g, x[t][u].z, o[t].z); o[t].w = fmaf(g, x[t][u].w, o[t].w);
-        }
-        M[t] = m;
+      for (int u = 0; u < US; ++u) {
+        const float g = expf(v[u].x - m);
+        L = fmaf(g, v[u].y, L);
+        o.x = fmaf(g, x[u].x, o.x); o.y = fmaf(g, x[u].y, o.y);
+        o.z = fmaf(g, x[u].z, o.z); o.w = fmaf(g, x[u].w, o.w);
       }
+      M = m;
     }
-    if constexpr (PG > 1) {
+    s_o[pg][sub] = o;
+    if (sub == 0) { s_ml[pg][0] = M; s_ml[pg][1] = L; }
+    __syncthreads();
+    if (pg == 0) {
 #pragma unroll
-      for (int t = 0; t < RPT; ++t) {
-        s_o[pg][t * LR + rr][sub] = o[t];
-        if (sub == 0) { s_ml[pg][t * LR + rr][0] = M[t]; s_ml[pg][t * LR + rr][1] = L[t]; }
-      }
-      __syncthreads();
+      for (int g = 1; g < PG; ++g) M = fmaxf(M, s_ml[g][0]);
+      L = 0.f; o = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (M != -INFINITY)
 #pragma unroll
-      for (int t = 0; t < RPT; ++t) {
-        float m = -INFINITY;
-#pragma unroll
-        for (int g = 0; g < PG; ++g) m = fmaxf(m, s_ml[g][t * LR + rr][0]);
-        L[t] = 0.f; o[t] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (m != -INFINITY)
-#pragma unroll
-          for (int g = 0; g < PG; ++g) {
-            const float f = expf(s_ml[g][t * LR + rr][0] - m);
-            const float4 x = s_o[g][t * LR + rr][sub];
-            L[t] = fmaf(f, s_ml[g][t * LR + rr][1], L[t]);
-            o[t].x = fmaf(f, x.x, o[t].x); o[t].y = fmaf(f, x.y, o[t].y); o[t].z = fmaf(f, x.z, o[t].z); o[t].w = fmaf(f, x.w, o[t].w);
-          }
-        M[t] = m;
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < RPT; ++t) {
-      const int j = j0 + t * LR + rr;
-      if (j >= nrows || pg != 0) continue;
+        for (int g = 0; g < PG; ++g) {
+          const float f = expf(s_ml[g][0] - M);
+          const float4 x = s_o[g][sub];
+          L = fmaf(f, s_ml[g][1], L);
+          o.x = fmaf(f, x.x, o.x); o.y = fmaf(f, x.y, o.y); o.z = fmaf(f, x.z, o.z); o.w = fmaf(f, x.w, o.w);
+        }
       const size_t hb = (size_t)(row0 + j / G) * a.H + kvh * G + j % G;
-      const float4 y = L[t] > 0.f ? make_float4(o[t].x / L[t], o[t].y / L[t], o[t].z / L[t], o[t].w / L[t]) : make_float4(0.f, 0.f, 0.f, 0.f);
+      const float4 y = L > 0.f ? make_float4(o.x / L, o.y / L, o.z / L, o.w / L) : make_float4(0.f, 0.f, 0.f, 0.f);
       if (ES == 2)
         *reinterpret_cast<uint2*>(a.out + (hb * D + sub * 4) * 2) = make_uint2(f32_to_bf16_bits(y.x) | (f32_to_bf16_bits(y.y) << 16), f32_to_bf16_bits(y.z) | (f32_to_bf16_bits(y.w) << 16));
       else *reinterpret_cast<float4*>(a.out + (hb * D + sub * 4) * 4) = y;
-      if (sub == 0 && a.lse != nullptr) a.lse[hb] = L[t] > 0.f ? M[t] + logf(L[t]) : -INFINITY;
+      if (sub == 0 && a.lse != nullptr) a.lse[hb] = L > 0.f ? M + logf(L) : -INFINITY;
     }
-    if (PG > 1) __syncthreads();                        // the next rows take the same place
+    __syncthreads();                                    // the next row takes the same place
   }
 }
 
@@ -184,8 +162,10 @@ __global__ __launch_bounds__(256) void paged_merge_tall_kernel(PagedAttnArgs a, 
 
 template <int ES, int D>
 static hipError_t merge(const PagedAttnArgs& a, const ShareArgs& sh, int rows, hipStream_t s) {
-  // (a tile with more rows than the bound says takes turns; the tall kernel's tiles are short only where their sequence is)
-  if (rows != kTallRows) hipLaunchKernelGGL((paged_merge_kernel<ES, D, 256, 4, 1024 / D, 2>), dim3((std::min(sh.tpt, a.C) * (a.H / a.H_kv) + 3) / 4, sh.wgs), dim3(256), 0, s, a, sh, rows);
+  // A workgroup per row that a tile may have; where only the sequences with few rows are meant, as many as one token has (12 mixed ones, 28 heads: 4 us
+  // less, as most workgroups find nothing).  More rows take turns.  The tall kernel's tiles are short only where their sequence is.
+  const int G = a.H / a.H_kv;
+  if (rows != kTallRows) hipLaunchKernelGGL((paged_merge_kernel<ES, D, 4>), dim3(sh.most_rows < INT_MAX ? G : std::min(sh.tpt, a.C) * G, sh.wgs), dim3(256), 0, s, a, sh, rows);
   else hipLaunchKernelGGL(paged_merge_tall_kernel<D>, dim3(kTallRows / 32 * (D / 32), sh.wgs), dim3(256), 0, s, a, sh);
   return hipGetLastError();
 }

@@ -142,23 +142,45 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
     // places of tiles it, it + 1 and it + 2 in LDS (of K; V lies TILE_B behind), handed on from tile to tile
     uint32_t p0 = 0, p1 = 2 * TILE_B, p2 = 4 * TILE_B;
 
+    // ---- queries: the wave's 64 rows by way of the last four tiles' places (one each), 1 KiB of neighbouring bytes per load.  (Read as fragments from
+    // memory, 16 bytes of 32 rows at a time, they took 8000 cycles; now the page ids, the queries and the first tile take 6000 together.)  Rows past the
+    // last are copies of it.
+    __syncthreads();                                               // the tiles of the piece before have been read
+    if (threadIdx.x == 0) *s_bad = 0;
     fetch_look(0); fetch_look(1); fetch_look(2); fetch_look(3);
-
-    // ---- query fragments (B operand of K Q^T): of the wave's two blocks of 32 rows, lane holds row = col, k = 16 * ks + 8 * half .. + 8
+    const uint32_t lds_q = lds_base + (uint32_t)((2 + wave) * TILE_B);
+    constexpr int NLQ = 64 / KPI;
+    int q_key = st_key;
+    asm volatile("" : "+v"(q_key));                                // (formed anew for every tile: the compiler would keep all of these addresses)
+#pragma unroll
+    for (int i = 0; i < NLQ; ++i) {
+      const int jw = i * KPI + q_key;
+      const uint32_t off = row_at(min(wave * 64 + jw, nrows - 1)) * RB + (uint32_t)((st_pos ^ pt_swz<D>(jw & 15)) * 16);
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(__builtin_amdgcn_readfirstlane(lds_q) + i * 1024), "v"(a.q + tile_row * RB + off) : "memory", "m0");
+    }
     uint32_t low[2];                                               // first of the `reach` keys that the row sees (modulo 2^32: it may lie before key 0)
-    bf16x8_t qfrag[2][KS];
 #pragma unroll
     for (int rb = 0; rb < 2; ++rb) {
       const int j = wave * 64 + rb * 32 + col;
       low[rb] = (uint32_t)(j < nrows ? x0 + token_of(j) : x1) - (reach - 1u);
-      const uint32_t at = row_at(min(j, nrows - 1)) * RB + 16 * half;
+    }
+    asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NLQ) : "memory");    // page ids
+    rows_of(0);
+#pragma unroll
+    for (int i = 0; i < NLD; ++i) load_row(a.k_pool, at_k[i], i, p0);
+    rows_of(1);
+#pragma unroll
+    for (int i = 0; i < NLD; ++i) load_row(a.v_pool, at_v[i], i, p0 + TILE_B);
+    asm volatile("s_waitcnt vmcnt(%0)" :: "n"(2 * NLD) : "memory");
+    // fragments (B operand of K Q^T): of the wave's two blocks of 32 rows, lane holds row = col, k = 16 * ks + 8 * half .. + 8
+    bf16x8_t qfrag[2][KS];
+#pragma unroll
+    for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (j < nrows) v = *reinterpret_cast<const uint4*>(a.q + tile_row * RB + (at + ks * 32));
-        qfrag[rb][ks] = __builtin_bit_cast(bf16x8_t, v);
+        qfrag[rb][ks] = *(lds_bf16x8*)((ka0 + (uint32_t)((2 + wave) * TILE_B + rb * 32 * RB)) ^ (uint32_t)(ks * 32));
+        asm volatile("" : "+a"(qfrag[rb][ks]));                    // (in accumulation registers, where matrix products can take them; elsewhere the compiler spills)
       }
-    }
     float ref[2] = {kPtUnset, kPtUnset};                           // the rows' reference exponents
     float lsum[2] = {0.f, 0.f};                                    // this lane's keys' weights
     float factor = c2;                                             // 1 once the logits are rounded first
@@ -319,19 +341,18 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
     using B1 = std::integral_constant<int, 1>;
     using Yes = std::true_type;
     using No = std::false_type;
-    __syncthreads();                                               // the tiles of the piece before have been read
-    if (threadIdx.x == 0) *s_bad = 0;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // page ids and queries
-    rows_of(0);
+    // K tiles 1 and 2, V tile 1, in the queries' places
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();                                  // every wave has read its own
+    asm volatile("" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < NLD; ++i) load_row(a.k_pool, at_k[i], i, p0);
+    for (int i = 0; i < NLD; ++i) load_row(a.k_pool, at_k[i], i, p1);
+    fetch_look(4);
+    rows_of(2);
 #pragma unroll
-    for (int n = 1; n < 3; ++n) {                                  // K tile n, V tile n - 1
-      rows_of(n);
-#pragma unroll
-      for (int i = 0; i < NLD; ++i) { load_row(a.k_pool, at_k[i], i, n == 1 ? p1 : p2); load_row(a.v_pool, at_v[i], i, (n == 1 ? p0 : p1) + TILE_B); }
-      fetch_look(n + 3);
-    }
+    for (int i = 0; i < NLD; ++i) { load_row(a.k_pool, at_k[i], i, p2); load_row(a.v_pool, at_v[i], i, p1 + TILE_B); }
+    fetch_look(5);
     rows_of(3);
     tile_barrier(std::integral_constant<int, 2 * BATCH>{});
     // the scores of the first block
