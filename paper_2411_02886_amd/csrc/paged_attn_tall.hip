@@ -92,10 +92,10 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
     const int row0 = sq.row0 + c0, x0 = sq.N - sq.n + c0, x1 = x0 + ntok - 1;   // first row; places of the first and last token
     const bool whole = ua == 0 && ub == keys.units;
     const int tmax = keys.end - 1;
-    auto token_of = [&](int j) -> int { return (int)(((uint32_t)j * g_inv) >> 16); };   // j / G
+    auto token_of = [&](uint32_t j) -> uint32_t { return __umul24(j, g_inv) >> 16; };   // j / G
     // the tile's row j in q, out and lse: a uniform first row and 32 bits behind it (j / G tokens of H rows, then j % G)
     const size_t tile_row = (size_t)row0 * H + kvh * G;
-    auto row_at = [&](int j) -> uint32_t { return (uint32_t)token_of(j) * (uint32_t)(H - G) + (uint32_t)j; };
+    auto row_at = [&](uint32_t j) -> uint32_t { return __umul24(token_of(j), (uint32_t)(H - G)) + j; };
     if (keys.end <= keys.first) {                                  // no row sees a token (one unit: the tile is not cut)
       for (int i = threadIdx.x; i < nrows * D; i += 256) {
         const size_t o = tile_row + row_at(i / D);
@@ -148,15 +148,16 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
     __syncthreads();                                               // the tiles of the piece before have been read
     if (threadIdx.x == 0) *s_bad = 0;
     fetch_look(0); fetch_look(1); fetch_look(2); fetch_look(3);
-    const uint32_t lds_q = lds_base + (uint32_t)((2 + wave) * TILE_B);
+    const uint32_t lds_q = __builtin_amdgcn_readfirstlane(lds_base + (uint32_t)((2 + wave) * TILE_B));
     constexpr int NLQ = 64 / KPI;
+    const uint8_t* q_base = a.q + tile_row * RB;
     int q_key = st_key;
     asm volatile("" : "+v"(q_key));                                // (formed anew for every tile: the compiler would keep all of these addresses)
+    const int q_pos = st_pos ^ pt_swz<D>(q_key);                   // (the load's own part of the row's number flips other bits)
 #pragma unroll
     for (int i = 0; i < NLQ; ++i) {
-      const int jw = i * KPI + q_key;
-      const uint32_t off = row_at(min(wave * 64 + jw, nrows - 1)) * RB + (uint32_t)((st_pos ^ pt_swz<D>(jw & 15)) * 16);
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(__builtin_amdgcn_readfirstlane(lds_q) + i * 1024), "v"(a.q + tile_row * RB + off) : "memory", "m0");
+      const uint32_t off = row_at((uint32_t)min(wave * 64 + i * KPI + q_key, nrows - 1)) * RB + (uint32_t)((q_pos ^ pt_swz<D>(i * KPI & 15)) * 16);
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds_q + i * 1024), "v"(off), "s"(q_base) : "memory", "m0");
     }
     uint32_t low[2];                                               // first of the `reach` keys that the row sees (modulo 2^32: it may lie before key 0)
 #pragma unroll
@@ -455,11 +456,14 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
       }
     }
     if (whole) {
+      uint8_t* o_base = a.out + tile_row * RB;
+      int o_key = st_key;
+      asm volatile("" : "+v"(o_key));
 #pragma unroll
       for (int i = 0; i < 64 / KPI; ++i) {
-        const int jw = i * KPI + st_key, j = wave * 64 + jw;
+        const int jw = i * KPI + o_key, j = wave * 64 + jw;
         const uint4 y = *reinterpret_cast<const uint4*>(mine + jw * RB + ((st_pos ^ (jw & (PPR - 1))) * 16));
-        if (j < nrows) *reinterpret_cast<uint4*>(a.out + tile_row * RB + (row_at(j) * RB + st_pos * 16)) = y;
+        if (j < nrows) *reinterpret_cast<uint4*>(o_base + (row_at((uint32_t)j) * RB + (uint32_t)(st_pos * 16))) = y;
       }
     }
     return false;
