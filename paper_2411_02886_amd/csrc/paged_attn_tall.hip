@@ -125,19 +125,20 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
       const int t = seen(key0 + it * kPtTile + wave * WK + (lane & (WK - 1)));
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" :: "s"(look + (it & (kPtRing - 1)) * 256), "v"(pages + (t >> a.p_shift)) : "memory", "m0");
     };
-    uint32_t at_k[NLD], at_v[NLD];                                 // rows of the K tile and of the V tile that are requested next
+    uint64_t at_k[NLD], at_v[NLD];                                 // places in a pool (this lane's) of the K tile's and the V tile's rows that are requested next
+    const uint8_t* const k_head = a.k_pool + kvh * RB;
+    const uint8_t* const v_head = a.v_pool + kvh * RB;
     auto rows_of = [&](int it) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < NLD; ++i) {
         const int key = i * KPI + st_key, t = seen(key0 + it * kPtTile + wave * WK + key);
         const int page = *(const volatile __attribute__((address_space(3))) int*)(look + (uint32_t)((it & (kPtRing - 1)) * 256 + key * 4));
         at_v[i] = at_k[i];
-        at_k[i] = ((uint32_t)page << a.p_shift) + (uint32_t)(t & (a.P - 1));
+        at_k[i] = ((uint64_t)(((uint32_t)page << a.p_shift) + (uint32_t)(t & (a.P - 1))) << row_shift) | (uint32_t)((st_pos ^ pt_swz<D>((wave * WK + key) & 15)) * 16);
       }
     };
-    auto load_row = [&](const uint8_t* pool, uint32_t at, int i, uint32_t place) __attribute__((always_inline)) {
-      const uint64_t off = ((uint64_t)at << row_shift) + (uint32_t)(kvh * RB + ((st_pos ^ pt_swz<D>((wave * WK + i * KPI + st_key) & 15)) * 16));
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds_st + place + (uint32_t)(i * 1024)), "v"(pool + off) : "memory", "m0");
+    auto load_row = [&](const uint8_t* pool, uint64_t at, int i, uint32_t place) __attribute__((always_inline)) {
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds_st + place + (uint32_t)(i * 1024)), "v"(pool + at) : "memory", "m0");
     };
     // places of tiles it, it + 1 and it + 2 in LDS (of K; V lies TILE_B behind), handed on from tile to tile
     uint32_t p0 = 0, p1 = 2 * TILE_B, p2 = 4 * TILE_B;
@@ -168,10 +169,10 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
     asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NLQ) : "memory");    // page ids
     rows_of(0);
 #pragma unroll
-    for (int i = 0; i < NLD; ++i) load_row(a.k_pool, at_k[i], i, p0);
+    for (int i = 0; i < NLD; ++i) load_row(k_head, at_k[i], i, p0);
     rows_of(1);
 #pragma unroll
-    for (int i = 0; i < NLD; ++i) load_row(a.v_pool, at_v[i], i, p0 + TILE_B);
+    for (int i = 0; i < NLD; ++i) load_row(v_head, at_v[i], i, p0 + TILE_B);
     asm volatile("s_waitcnt vmcnt(%0)" :: "n"(2 * NLD) : "memory");
     // fragments (B operand of K Q^T): of the wave's two blocks of 32 rows, lane holds row = col, k = 16 * ks + 8 * half .. + 8
     bf16x8_t qfrag[2][KS];
@@ -280,8 +281,8 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
         product(t, 1);
         __builtin_amdgcn_sched_barrier(0);
         if (LD && t < NLD) {                                       // rows of K tile it + 3 and V tile it + 2
-          load_row(a.k_pool, at_k[t < NLD ? t : 0], t, p0);
-          load_row(a.v_pool, at_v[t < NLD ? t : 0], t, p2 + TILE_B);
+          load_row(k_head, at_k[t < NLD ? t : 0], t, p0);
+          load_row(v_head, at_v[t < NLD ? t : 0], t, p2 + TILE_B);
         }
         if (LD && t == NLD) { rows_of(it + 4); fetch_look(it + 6); }
 #pragma unroll
@@ -348,11 +349,11 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
     __builtin_amdgcn_s_barrier();                                  // every wave has read its own
     asm volatile("" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < NLD; ++i) load_row(a.k_pool, at_k[i], i, p1);
+    for (int i = 0; i < NLD; ++i) load_row(k_head, at_k[i], i, p1);
     fetch_look(4);
     rows_of(2);
 #pragma unroll
-    for (int i = 0; i < NLD; ++i) { load_row(a.k_pool, at_k[i], i, p2); load_row(a.v_pool, at_v[i], i, p1 + TILE_B); }
+    for (int i = 0; i < NLD; ++i) { load_row(k_head, at_k[i], i, p2); load_row(v_head, at_v[i], i, p1 + TILE_B); }
     fetch_look(5);
     rows_of(3);
     tile_barrier(std::integral_constant<int, 2 * BATCH>{});
