@@ -343,11 +343,15 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
     using B1 = std::integral_constant<int, 1>;
     using Yes = std::true_type;
     using No = std::false_type;
-    // K tiles 1 and 2, V tile 1, in the queries' places
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();                                  // every wave has read its own
-    asm volatile("" ::: "memory");
+    tile_barrier(std::integral_constant<int, NLD>{});              // K tile 0 has arrived, and every wave has read its queries
+    // the scores of the first block; K tiles 1 and 2 and V tile 1 are requested meanwhile, in the queries' places
+    bf16x8_t k_first[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) k_first[ks] = *(lds_bf16x8*)((ka0 + p0) ^ (uint32_t)(ks * 32));
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb) s[0][rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_first[ks], qfrag[rb][ks], ks == 0 ? (f32x16_t){} : s[0][rb], 0, 0, 0);
 #pragma unroll
     for (int i = 0; i < NLD; ++i) load_row(k_head, at_k[i], i, p1);
     fetch_look(4);
@@ -356,18 +360,6 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
     for (int i = 0; i < NLD; ++i) { load_row(k_head, at_k[i], i, p2); load_row(v_head, at_v[i], i, p1 + TILE_B); }
     fetch_look(5);
     rows_of(3);
-    tile_barrier(std::integral_constant<int, 2 * BATCH>{});
-    // the scores of the first block
-#pragma unroll
-    for (int rb = 0; rb < 2; ++rb)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[0][rb][e] = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const bf16x8_t av = *(lds_bf16x8*)((ka0 + p0) ^ (uint32_t)(ks * 32));
-#pragma unroll
-      for (int rb = 0; rb < 2; ++rb) s[0][rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av, qfrag[rb][ks], s[0][rb], 0, 0, 0);
-    }
     // the first reference: above the block's largest exponent (a row that sees none of its keys, or one with large logits, gets its own later)
 #pragma unroll
     for (int rb = 0; rb < 2; ++rb) {
@@ -460,11 +452,16 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
       uint8_t* o_base = a.out + tile_row * RB;
       int o_key = st_key;
       asm volatile("" : "+v"(o_key));
+      u32x4_t y[64 / KPI];                                         // (all of them are read first: with a read and a store in turn, each would wait for the other)
 #pragma unroll
       for (int i = 0; i < 64 / KPI; ++i) {
-        const int jw = i * KPI + o_key, j = wave * 64 + jw;
-        const uint4 y = *reinterpret_cast<const uint4*>(mine + jw * RB + ((st_pos ^ (jw & (PPR - 1))) * 16));
-        if (j < nrows) *reinterpret_cast<uint4*>(o_base + (row_at((uint32_t)j) * RB + (uint32_t)(st_pos * 16))) = y;
+        const int jw = i * KPI + o_key;
+        y[i] = *reinterpret_cast<const u32x4_t*>(mine + jw * RB + ((st_pos ^ (jw & (PPR - 1))) * 16));
+      }
+#pragma unroll
+      for (int i = 0; i < 64 / KPI; ++i) {
+        const int j = wave * 64 + i * KPI + o_key;
+        if (j < nrows) *reinterpret_cast<u32x4_t*>(o_base + (row_at((uint32_t)j) * RB + (uint32_t)(st_pos * 16))) = y[i];
       }
     }
     return false;
