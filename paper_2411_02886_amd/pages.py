@@ -21,7 +21,7 @@ class PagePool:
         self.num_pages, self.page_size = int(num_pages), int(page_size)
         self.refs = np.zeros(self.num_pages, dtype=np.int32)      # sequences that hold the page
         self._free = list(range(self.num_pages))                  # a heap
-        self._pages, self._lens = {}, {}
+        self._pages, self._lens, self._spare = {}, {}, set()
 
     def __contains__(self, seq):
         return seq in self._pages
@@ -99,10 +99,20 @@ class PagePool:
         need = -(-int(tokens) // self.page_size)
         if need > len(self._free):
             raise MemoryError("%d pages wanted, %d free" % (need, len(self._free)))
-        return self._take(need)
+        pages = self._take(need)
+        self._spare.update(pages)
+        return pages
+
+    def _of_spare(self, pages):
+        pages = [int(page) for page in pages]
+        if len(set(pages)) != len(pages) or not self._spare.issuperset(pages):
+            raise ValueError("pages that are not spare, or one of them twice")
+        return pages
 
     def give_back(self, pages) -> None:
         """Returns spare pages that were not used."""
+        pages = self._of_spare(pages)
+        self._spare.difference_update(pages)
         self._release(pages)
 
     def replace(self, seq, pages, tokens: int) -> None:
@@ -111,24 +121,22 @@ class PagePool:
         need = -(-int(tokens) // self.page_size)
         if tokens < 0 or need > len(pages):
             raise ValueError("%d tokens do not fit %d pages" % (tokens, len(pages)))
-        old = self._pages[seq]
+        old, pages = self._pages[seq], self._of_spare(pages)
+        self._spare.difference_update(pages)
         self._pages[seq], self._lens[seq] = list(pages[:need]), int(tokens)
         self._release(old)
         self._release(pages[need:])
 
     def gather(self):
-        """Moves the pages in use to the low end of the pool.  Returns the page copies, [(src, dst)], to be made before the next
-        page is written; no page is in both columns."""
-        used = np.flatnonzero(self.refs)
-        high = used[used >= used.size]
-        low = np.flatnonzero(self.refs[:used.size] == 0)
-        to = np.arange(self.num_pages)
-        to[high] = low
-        moved = [(int(a), int(b)) for a, b in zip(high, low)]
+        """Moves the sequences' pages to the low end of the pool, the highest to the lowest free place; spare pages, which the caller
+        goes by, stay.  Returns the page copies, [(src, dst)], to be made before the next page is written; no page is in both columns."""
+        high = [int(page) for page in np.flatnonzero(self.refs)[::-1] if int(page) not in self._spare]
+        moved = [(a, b) for a, b in zip(high, sorted(self._free)) if a > b]
+        to = dict(moved)
         for pages in self._pages.values():
-            pages[:] = [int(to[page]) for page in pages]
-        self.refs[low] = self.refs[high]
-        self.refs[high] = 0
+            pages[:] = [to.get(page, page) for page in pages]
+        for a, b in moved:
+            self.refs[b], self.refs[a] = self.refs[a], 0
         self._free = [int(page) for page in np.flatnonzero(self.refs == 0)]     # ascending: a heap
         return moved
 

@@ -36,8 +36,9 @@ class _NewTokens:
     number per sequence with it."""
 
     def append(self, k, v, q=None, q_out=None, rope=None, positions=None, q_indptr=None):
-        """Writes the new tokens' K and V rows into their pages, keys turned by `rope`, and the turned queries into q_out."""
-        ts.ts_rope_append(self.problem, rope, q, k, v, q_indptr, k.shape[0], positions, q_out)
+        """Writes the new tokens' K and V rows into their pages, keys turned by `rope`, and the turned queries into q_out (either
+        alone: k and v, or q and q_out, None)."""
+        ts.ts_rope_append(self.problem, rope, q, k, v, q_indptr, (q if k is None else k).shape[0], positions, q_out)
 
     def attend_all(self, q, sm_scale=None, window=0, q_indptr=None, out=None, lse=None):
         """Attention of the new tokens over their whole sequence: no selection.  Without q_indptr q is the step's or chunk's

@@ -212,3 +212,26 @@ def test_page_pool_table_and_refusals():
         with pytest.raises(error):
             call()
     check(pool, ["a", "b"])
+
+
+def test_spare_pages_stay_where_the_caller_knows_them():
+    pool = PagePool(16, 4)
+    pool.add("a", 12)                               # 0, 1, 2
+    pool.add("b", 8)                                # 3, 4
+    spare = pool.spare(7)                           # 5, 6
+    pool.add("c", 12)                               # 7, 8, 9
+    pool.free("a")
+    moved = pool.gather()
+    assert moved == [(9, 0), (8, 1), (7, 2)] and pool.pages("c") == [2, 1, 0] and pool.pages("b") == [3, 4]
+    assert all(pool.refs[page] == 1 for page in spare)
+    for wrong in ([0], [spare[0], spare[0]], [15]):
+        with pytest.raises(ValueError):
+            pool.give_back(wrong)
+        with pytest.raises(ValueError):
+            pool.replace("b", wrong, 1)
+    assert pool.free_pages == 9 and pool.pages("b") == [3, 4]
+    pool.replace("b", spare, 3)                     # 3, 4 and the second spare page come back
+    assert pool.pages("b") == [spare[0]] and pool.free_pages == 12
+    with pytest.raises(ValueError):
+        pool.give_back(spare)                       # no longer spare
+    assert pool.gather() == [(5, 3)] and pool.pages("b") == [3] and pool.pages("c") == [2, 1, 0]
