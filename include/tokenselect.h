@@ -326,7 +326,7 @@ int32_t ts_chunk_mean_query(const ts_problem* p, const void* q, void* q_mean, vo
  *   out[r][h][:] = sum_t softmax_t( <q[r][h], K[slot(b, t)][h/G]> * sm_scale ) * V[slot(b, t)][h/G]
  * for new token c = r - q_indptr[b] at place x = N_b - n_b + c over t in [max(0, x - window + 1), x]; window 0 = from 0 on (every
  * cached token and the chunk's own up to x).  Float accumulation, out rounded to p->dtype; bf16: where chunk * G and a sequence's
- * n_b * G are more than 32, the weights that multiply V are rounded to bf16 (matrix-core operand; their sum is not).
+ * n_b * G are more than 32, the weights that multiply V may be rounded to bf16 (matrix-core operand; their sum is not).
  * Pages that no new token sees (wholly in front of the first one's window, behind N_b) are not read.  A token that some of a sequence's rows see
  * and others do not takes part in the latter with weight 0: its K may be anything, its V has to be finite.
  * q, out [device] [num_rows][H][D], 16-byte aligned, not overlapping; lse [device] float [num_rows][H] or NULL.

@@ -9,7 +9,10 @@ namespace ts {
 hipError_t launch_paged_stream(int dtype, int D, int blocks, const PagedAttnArgs& a, const ShareArgs& sh, hipStream_t s);
 hipError_t launch_paged_tall(int D, const PagedAttnArgs& a, const ShareArgs& sh, hipStream_t s);
 
-constexpr int kStreamWgs = 512, kTallWgs = 256, kTallRows = 256;
+constexpr int kTallRows = 256;
+// Workgroups that cut the line into shares: one per CU (128 / 192 / 256 / 512 of the stream kernel: a bf16 token over 131072 keys 129, 98, 91, 95 us, over
+// 1000 keys 10.9, 11.0, 11.1, 13.5, 16 drafts of 8 over 3000 keys 66, 51, 46, 49: fewer start, and fewer pieces are joined).
+constexpr int kShareWgs = 256;
 
 // Pieces of the tile that workgroup w's share began: its own and those of workgroups w + 1 .. w + count - 1, up to the one that ends the tile; a
 // share in between may hold no unit of it.  The states of the first 64 are loaded beside w's own.
@@ -170,64 +173,76 @@ static hipError_t merge(const PagedAttnArgs& a, const ShareArgs& sh, int rows, h
   return hipGetLastError();
 }
 
-// bytes that a kernel of `wgs` workgroups and tiles of `rows` rows leaves pieces in
-static size_t piece_bytes(int wgs, int rows, int D) {
-  return align_up((size_t)wgs * 32, 256) + align_up((size_t)wgs * 2 * rows * 2 * 4, 256) + (size_t)wgs * 2 * rows * D * 4;
+// bytes that tiles of `rows` rows leave pieces in
+static size_t piece_bytes(int rows, int D) {
+  return align_up((size_t)kShareWgs * 32, 256) + align_up((size_t)kShareWgs * 2 * rows * 2 * 4, 256) + (size_t)kShareWgs * 2 * rows * D * 4;
 }
 
-// The rows of a sequence and KV head, n * G, decide: up to 16 (one block of columns) or 32 by the stream kernel, which is bound by the memory; more by
-// the tall one (bf16), or by the stream kernel with 64 rows a tile (fp32, whose matrix products it is then bound by).  A packed batch may hold both kinds:
+// The rows of a sequence and KV head, n * G, decide: up to 16 (one block of columns) or 32 by the stream kernel, which is bound by the memory (8 tokens times
+// 4 heads over 3000 keys, one sequence 17 us, 16 of them 46; by the tall kernel 27 and 58); more by the tall one (bf16), or by the stream kernel with 64 rows a
+// tile (fp32, whose matrix products it is then bound by: 512 tokens over 4000 keys 362 us, with 32 rows 412).  A packed batch may hold both kinds:
 // two launches, each takes the sequences that are its.
-struct PagedPlan { int few_blocks, many; };   // blocks of 16 rows of the stream kernel for few rows; whether a sequence may have more
+struct PagedPlan { int few_rows, many_rows; };   // rows of the tiles of sequences with few rows, and of those with more (0: there are none)
 static PagedPlan paged_plan(int dtype, int G, int chunk) {
   const long rows = (long)chunk * G;
-  if (rows <= 16) return PagedPlan{1, 0};
-  if (rows <= 32) return PagedPlan{2, 0};
-  return PagedPlan{dtype == TS_BF16 ? 2 : 1, 1};
+  if (rows <= 16) return PagedPlan{16, 0};
+  if (rows <= 32) return PagedPlan{32, 0};
+  return dtype == TS_BF16 ? PagedPlan{32, kTallRows} : PagedPlan{16, 64};
 }
-static int many_rows(int dtype) { return dtype == TS_BF16 ? kTallRows : 64; }
 
 size_t paged_attn_workspace(int dtype, int D, int G, int chunk) {
   const PagedPlan pl = paged_plan(dtype, G, chunk);
-  return align_up(piece_bytes(kStreamWgs, 16 * pl.few_blocks, D) + (pl.many ? piece_bytes(kTallWgs, many_rows(dtype), D) : 0), 256);
+  return align_up(piece_bytes(pl.few_rows, D) + (pl.many_rows ? piece_bytes(pl.many_rows, D) : 0), 256);
 }
 
 hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws, hipStream_t s) {
   const int G = a.H / a.H_kv;
   const PagedPlan pl = paged_plan(dtype, G, a.C);
   uint8_t* at = (uint8_t*)ws;
-  for (int kind = 0; kind < 2; ++kind) {                 // few rows, many rows
-    const bool few = kind == 0;
-    const int rows = few ? 16 * pl.few_blocks : many_rows(dtype), most_wgs = few ? kStreamWgs : kTallWgs;
-    if (!few && !pl.many) break;
+  // bounds on the tiles and on the keys of one
+  auto tiles_of = [&](int tpt) -> long {
+    return (a.q_indptr != nullptr ? a.T / tpt + std::min(a.B, a.T) : (long)a.B * ((a.C + tpt - 1) / tpt)) * a.H_kv;
+  };
+  auto keys_of = [&](int tpt) -> long { return std::min((long)a.max_seq_len, a.window > 0 ? (long)a.window + tpt : LONG_MAX); };
+  auto run = [&](int rows, int more_rows, int most_rows, bool whole) -> hipError_t {
+    const bool tall = rows == kTallRows;
+    const int kt = tall || dtype == TS_F32 ? 64 : 128;
     ShareArgs sh{};
     sh.tpt = rows / G;
-    sh.more_rows = few || a.q_indptr == nullptr ? 0 : 16 * pl.few_blocks;
-    sh.most_rows = few && pl.many ? 16 * pl.few_blocks : INT_MAX;
-    sh.desc = (int32_t*)at;
-    sh.part_ml = (float*)(at + align_up((size_t)most_wgs * 32, 256));
-    sh.part_o = (float*)((uint8_t*)sh.part_ml + align_up((size_t)most_wgs * 2 * rows * 2 * 4, 256));
-    at += piece_bytes(most_wgs, rows, D);
-    if (few && pl.many && a.q_indptr == nullptr) continue;   // every sequence has as many
-    const bool tall = !few && dtype == TS_BF16;
-    const int kt = tall ? 64 : dtype == TS_BF16 ? 128 : 64;
+    sh.more_rows = more_rows;
+    sh.most_rows = most_rows;
+    sh.whole = whole ? 1 : 0;
+    // The smallest share (twice as much: a token over 1000 keys 1.4 us more, 64 tokens over 4000 keys 4 us), and what a tile's start and end cost (a quarter
+    // of it: 12 mixed chunks 192 us instead of 160; twice: prompts between 1 us less and 1 us more).
     sh.min_keys = tall ? 2 * kt : kt;
     sh.tile_cost = tall ? 256 : 64;
-    sh.wgs = most_wgs;
-    // A workgroup per tile, and no merge, where tiles are short.
-    const long tiles = (a.q_indptr != nullptr ? a.T / sh.tpt + std::min(a.B, a.T) : (long)a.B * ((a.C + sh.tpt - 1) / sh.tpt)) * a.H_kv;
-    const long units = (std::min((long)a.max_seq_len, a.window > 0 ? (long)a.window + sh.tpt : LONG_MAX) + kt - 1) / kt;
-    if (few ? tiles < (1l << 23) && (units * kt <= 512 || (tiles >= most_wgs && units <= 16)) : tiles <= most_wgs && units <= 16) { sh.whole = 1; sh.wgs = (int)tiles; }
-    hipError_t e;
-    if (tall) e = launch_paged_tall(D, a, sh, s);
-    else e = launch_paged_stream(dtype, D, rows / 16, a, sh, s);
-    if (e != hipSuccess) return e;
-    if (sh.whole) continue;
-    if (dtype == TS_BF16) e = D == 64 ? merge<2, 64>(a, sh, rows, s) : merge<2, 128>(a, sh, rows, s);
-    else e = D == 64 ? merge<4, 64>(a, sh, rows, s) : merge<4, 128>(a, sh, rows, s);
+    sh.wgs = whole ? (int)tiles_of(sh.tpt) : kShareWgs;
+    sh.desc = (int32_t*)at;
+    sh.part_ml = (float*)(at + align_up((size_t)kShareWgs * 32, 256));
+    sh.part_o = (float*)((uint8_t*)sh.part_ml + align_up((size_t)kShareWgs * 2 * rows * 2 * 4, 256));
+    at += piece_bytes(rows, D);
+    const hipError_t e = tall ? launch_paged_tall(D, a, sh, s) : launch_paged_stream(dtype, D, rows / 16, a, sh, s);
+    if (e != hipSuccess || whole) return e;
+    if (dtype == TS_BF16) return D == 64 ? merge<2, 64>(a, sh, rows, s) : merge<2, 128>(a, sh, rows, s);
+    return D == 64 ? merge<4, 64>(a, sh, rows, s) : merge<4, 128>(a, sh, rows, s);
+  };
+  // A workgroup per tile, and no merge, where tiles are short, or where there are enough of them that are not long.  (200 keys: 8.2 us, in shares 10.3; 64
+  // sequences of 250 to 500 keys, 512 tiles: 22.8 and 29; but 16 keys' units at most: 16 fp32 sequences of 1000 to 2000 keys 42 us instead of 17.)
+  auto few_whole = [&](int rows) -> bool {
+    const long tiles = tiles_of(rows / G), keys = keys_of(rows / G);
+    return tiles < (1l << 23) && (keys <= 512 || (tiles >= kShareWgs && keys <= 16 * (dtype == TS_F32 ? 64 : 128)));
+  };
+  if (!pl.many_rows) return run(pl.few_rows, 0, INT_MAX, few_whole(pl.few_rows));
+  // Short prompts have too few tiles for the chip: there 32 rows a tile for all sequences, at most two workgroups per CU.  (256 tokens 12.3 us, by 256 rows a
+  // tile 15.2, 512 tokens 19.3 and 20.8; 768, more tiles than that, 37 and 27.  fp32: 256 tokens 20.5, by 64 rows a tile 33, 400 39 and 48.)
+  if (tiles_of(32 / G) <= 2 * kShareWgs && keys_of(32 / G) <= 1024) return run(32, 0, INT_MAX, true);
+  if (a.q_indptr != nullptr) {                             // (without, every sequence has as many)
+    const hipError_t e = run(pl.few_rows, 0, pl.few_rows, few_whole(pl.few_rows));
     if (e != hipSuccess) return e;
   }
-  return hipSuccess;
+  // (256 tokens in shares: 21 us instead of 15.5, 1024 35.7 and 33.4; with a workgroup per tile for all: 2048 tokens 59 instead of 54)
+  const long tiles = tiles_of(pl.many_rows / G);
+  return run(pl.many_rows, a.q_indptr != nullptr ? pl.few_rows : 0, INT_MAX, tiles <= kShareWgs && keys_of(pl.many_rows / G) <= 1024);
 }
 
 }  // namespace ts

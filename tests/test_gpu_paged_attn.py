@@ -397,3 +397,23 @@ def test_tokens_in_front_of_every_window_are_not_read(gpu, dtype, H, D, window):
     for bound in (None, LOOSE):
         o, l, ref = run(gpu, c, H, new, window=window, seed=9, max_seq_len=bound)
         check_attention(o, l, ref, (window, bound))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("H,H_kv,D", [(32, 8, 128), (32, 8, 64), (28, 4, 128), (16, 16, 64), (24, 8, 128)])
+@pytest.mark.parametrize("window", [0, 77])
+def test_prompts_of_many_whole_tiles(gpu, dtype, H, H_kv, D, window):
+    """More than 512 tiles of 32 rows and no more than 256 large ones, up to 1024 keys: a workgroup per large tile."""
+    new, old = [421, 5, 300, 1, 64, 500], [200, 900, 0, 17, 0, 1]
+    c = Cache(dtype, H_kv, D, 16, [a + b for a, b in zip(new, old)], seed=H + D)
+    o, l, ref = run(gpu, c, H, new, window=window, seed=21, behind=2)
+    check_attention(o, l, ref, window)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("sm", [0.0, -0.3, 40.0])
+def test_scales_in_whole_large_tiles(gpu, dtype, sm):
+    new = [640, 260]
+    c = Cache(dtype, 8, 64, 16, [700, 270], seed=8)
+    o, l, ref = run(gpu, c, 32, new, sm=sm, seed=8)
+    check_attention(o, l, ref, sm)
