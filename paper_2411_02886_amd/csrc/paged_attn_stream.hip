@@ -69,6 +69,7 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
   typedef const __attribute__((address_space(3))) u32x4_t lds_u32x4;
   const float sm = a.sm_scale;
   const int row_shift = 31 - __builtin_clz((uint32_t)(a.H_kv * RB));   // H_kv is a power of two
+  const uint32_t g_inv = 65536u / (uint32_t)G + 1u;             // exact for rows below 256
   const uint32_t reach = a.window > 0 ? (uint32_t)a.window : 0x7fffffffu;
 
   walk_share<KT>(a, sh, G, from, to, first, [&](int kvh, const SeqShape& sq, int r, const TileKeys& keys, int ua, int ub, bool) -> bool {
@@ -76,12 +77,15 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
     const int row0 = sq.row0 + c0, x0 = sq.N - sq.n + c0, x1 = x0 + ntok - 1;   // first row; places of the first and last token
     const bool whole = ua == 0 && ub == keys.units;
     const int tmax = keys.end - 1;
-    auto out_row = [&](int j) -> size_t { return (size_t)(row0 + j / G) * H + kvh * G + j % G; };
+    auto token_of = [&](uint32_t j) -> uint32_t { return __umul24(j, g_inv) >> 16; };   // j / G
+    // the tile's row j in q, out and lse: a uniform first row and 32 bits behind it (j / G tokens of H rows, then j % G)
+    const size_t tile_row = (size_t)row0 * H + kvh * G;
+    auto row_at = [&](uint32_t j) -> uint32_t { return __umul24(token_of(j), (uint32_t)(H - G)) + j; };
     if (keys.end <= keys.first) {                                  // no row sees a token (one unit: the tile is not cut)
       for (int i = threadIdx.x; i < nrows * D; i += 256) {
-        const size_t o = out_row(i / D) * D + i % D;
-        if (ES == 2) reinterpret_cast<uint16_t*>(a.out)[o] = 0; else reinterpret_cast<float*>(a.out)[o] = 0.f;
-        if (i % D == 0 && a.lse != nullptr) a.lse[o / D] = -INFINITY;
+        const size_t o = tile_row + row_at((uint32_t)(i / D));
+        if (ES == 2) reinterpret_cast<uint16_t*>(a.out)[o * D + i % D] = 0; else reinterpret_cast<float*>(a.out)[o * D + i % D] = 0.f;
+        if (i % D == 0 && a.lse != nullptr) a.lse[o] = -INFINITY;
       }
       return false;
     }
@@ -91,22 +95,6 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
       d[0] = row0; d[1] = kvh; d[2] = ntok; d[3] = ub == keys.units ? kPieceEnds : kPieceGoesOn;
     }
     const int32_t* pages = a.page_indices + sq.page0;
-
-    // query rows (zero past the last): 16-byte pieces 4 i + kgrp of row cb * 16 + col
-    uint4 qf[CB][NQ];
-    uint32_t low[CB];                                              // first of the `reach` keys that the row sees (modulo 2^32: it may lie before key 0)
-#pragma unroll
-    for (int cb = 0; cb < CB; ++cb) {
-      const int j = cb * 16 + col;
-      low[cb] = (uint32_t)(j < nrows ? x0 + j / G : x1) - (reach - 1u);
-#pragma unroll
-      for (int i = 0; i < NQ; ++i) {
-        qf[cb][i] = make_uint4(0u, 0u, 0u, 0u);
-        if (j < nrows) qf[cb][i] = *reinterpret_cast<const uint4*>(a.q + out_row(j) * RB + (4 * i + kgrp) * 16);
-      }
-    }
-    __syncthreads();                                               // the tiles' place is free
-    __builtin_amdgcn_s_waitcnt(0x0f70);                            // vmcnt(0): from here on only the row and page loads are outstanding
 
     // the wave's tiles: tile i holds keys key0 + i * KT .. + TK; a last one without a key is left out
     const int key0 = (keys.u0 + ua) * KT + wave * TK;
@@ -121,6 +109,22 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
     };
     // (fresh(): the compiler forms the address anew in each turn of the loop.  It would keep all of them, dozens of registers, and spill.)
     auto fresh = [](uint32_t x) -> uint32_t { if (CB > 1) asm volatile("" : "+v"(x)); return x; };
+    __syncthreads();                                               // the tiles' place is free
+    if (nt > 0) fetch_look(0, 0);
+    // query rows (zero past the last): 16-byte pieces 4 i + kgrp of row cb * 16 + col
+    const uint8_t* q_base = a.q + tile_row * RB;
+    uint4 qf[CB][NQ];
+    uint32_t low[CB];                                              // first of the `reach` keys that the row sees (modulo 2^32: it may lie before key 0)
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      const int j = cb * 16 + col;
+      low[cb] = (uint32_t)(j < nrows ? x0 + token_of((uint32_t)j) : x1) - (reach - 1u);
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+        qf[cb][i] = make_uint4(0u, 0u, 0u, 0u);
+        if (j < nrows) qf[cb][i] = *reinterpret_cast<const uint4*>(q_base + (row_at((uint32_t)j) * RB + (uint32_t)((4 * i + kgrp) * 16)));
+      }
+    }
     auto rows_of = [&](int i, int place) {
       const int my_row = (int)fresh(st_row);
 #pragma unroll
@@ -148,9 +152,9 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[cb][db] = (f32x4_t){0.f, 0.f, 0.f, 0.f};
     }
+    __builtin_amdgcn_s_waitcnt(0x0f70);                            // vmcnt(0): from here on only the row and page loads are outstanding
+    asm volatile("" ::: "memory");
     if (nt > 0) {
-      fetch_look(0, 0);
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       rows_of(0, 0);
       fetch_look(1, 1);
       load_rows(a.k_pool, lds_k);
@@ -346,8 +350,9 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
           L = fmaf(f, s_ml[w4][jj][1], L);
         }
         if (whole) {
-          const size_t hb = out_row(j);
-          y = L > 0.f ? make_float4(y.x / L, y.y / L, y.z / L, y.w / L) : make_float4(0.f, 0.f, 0.f, 0.f);
+          const size_t hb = tile_row + row_at((uint32_t)j);
+          const float inv = L > 0.f ? 1.f / L : 0.f;
+          y = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
           if (ES == 2)
             *reinterpret_cast<uint2*>(a.out + (hb * D + d) * 2) = make_uint2(f32_to_bf16_bits(y.x) | (f32_to_bf16_bits(y.y) << 16), f32_to_bf16_bits(y.z) | (f32_to_bf16_bits(y.w) << 16));
           else *reinterpret_cast<float4*>(a.out + (hb * D + d) * 4) = y;

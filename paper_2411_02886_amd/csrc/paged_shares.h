@@ -9,6 +9,7 @@
 // neighbouring pieces, so that its L2 fetches the keys of a KV head once.
 #pragma once
 #include "ts_kernels.h"
+#include <limits.h>
 
 namespace ts {
 
@@ -113,6 +114,14 @@ template <int KT>
 __device__ __forceinline__ void find_share(const PagedAttnArgs& a, const ShareArgs& sh, int G, int wg, ShareScratch* lds, SharePlace* from,
                                            SharePlace* to, SeqShape* first) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (sh.whole && a.q_indptr == nullptr) {                 // as many tiles of every sequence: no search
+    const uint32_t each = (uint32_t)(a.C + sh.tpt - 1) / (uint32_t)sh.tpt, at = (uint32_t)wg / each;
+    const int b = (int)(at % (uint32_t)a.B), i = (int)((uint32_t)wg - at * each);
+    *from = SharePlace{(int)(at / (uint32_t)a.B), b, i, 0};
+    *to = SharePlace{from->kvh, b, i, INT_MAX};
+    *first = seq_shape(a, sh, G, b);
+    return;
+  }
   auto share_of_line = [&](double all) { return sh.whole ? 1. : fmax((double)sh.min_keys, floor_div(all + (sh.wgs - 1), sh.wgs)); };
   if (a.B <= 64) {
     // a lane per sequence, every wave for itself, both ends at once in the halves of the wave: no barrier, and half the time
@@ -220,7 +229,7 @@ __device__ __forceinline__ void walk_share(const PagedAttnArgs& a, const ShareAr
     const bool last = kvh == to.kvh && b == to.b && i == to.i;
     const int r = tile_at(s, i);
     const TileKeys k = tile_keys<KT>(a, sh, s, r);
-    const int ub = last ? to.u : k.units;
+    const int ub = last ? min(to.u, k.units) : k.units;
     if (ub > ua) { again = fn(kvh, s, r, k, ua, ub, again); if (again) continue; }
     if (last) return;
     ua = 0;
