@@ -375,7 +375,10 @@ def _row_stride(t, row: int, name: str) -> int:
     """Elements between the rows of a [rows][...] tensor whose rows are packed; row: elements of one."""
     if t is None:
         return 0
-    shape, strides, want = t.shape, t.stride(), 1
+    shape = t.shape
+    if len(shape) > 1 and t.is_contiguous() and t.numel() == shape[0] * row:      # the usual case, and the quickest answer
+        return 0
+    strides, want = t.stride(), 1
     if len(shape) == 2 and shape[1] == row and strides[1] == 1:
         return strides[0] if shape[0] > 1 else 0
     for i in range(len(shape) - 1, 0, -1):
