@@ -227,7 +227,7 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
     return D == 64 ? merge<4, 64>(a, sh, rows, s) : merge<4, 128>(a, sh, rows, s);
   };
   // A workgroup per tile, and no merge, where tiles are short, or where there are enough of them that are not long.  (200 keys: 8.2 us, in shares 10.3; 64
-  // sequences of 250 to 500 keys, 512 tiles: 22.8 and 29; but 16 keys' units at most: 16 fp32 sequences of 1000 to 2000 keys 42 us instead of 17.)
+  // sequences of 250 to 500 keys, 512 tiles: 22.8 and 29; but 16 fp32 sequences of 1000 to 2000 keys, 32 tiles, 42 us instead of 17.)
   auto few_whole = [&](int rows) -> bool {
     const long tiles = tiles_of(rows / G), keys = keys_of(rows / G);
     return tiles < (1l << 23) && (keys <= 512 || (tiles >= kShareWgs && keys <= 16 * (dtype == TS_F32 ? 64 : 128)));
@@ -240,7 +240,7 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
     const hipError_t e = run(pl.few_rows, 0, pl.few_rows, few_whole(pl.few_rows));
     if (e != hipSuccess) return e;
   }
-  // (256 tokens in shares: 21 us instead of 15.5, 1024 35.7 and 33.4; with a workgroup per tile for all: 2048 tokens 59 instead of 54)
+  // (1024 tokens 33.4 us, in shares 35.7; but 2048 with a workgroup per tile 59 instead of 54)
   const long tiles = tiles_of(pl.many_rows / G);
   return run(pl.many_rows, a.q_indptr != nullptr ? pl.few_rows : 0, INT_MAX, tiles <= kShareWgs && keys_of(pl.many_rows / G) <= 1024);
 }
