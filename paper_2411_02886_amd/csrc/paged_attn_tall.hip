@@ -134,15 +134,21 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
     uint64_t at_k[NLD], at_v[NLD];                                 // places in a pool (this lane's) of the K tile's and the V tile's rows that are requested next
     const uint8_t* const k_head = a.k_pool + kvh * RB;
     const uint8_t* const v_head = a.v_pool + kvh * RB;
-    auto rows_of = [&](int it) __attribute__((always_inline)) {
+    int page[NLD];
+    auto pages_of = [&](int it) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < NLD; ++i)
+        page[i] = *(const volatile __attribute__((address_space(3))) int*)(look + (uint32_t)((it & (kPtRing - 1)) * 256 + (i * KPI + st_key) * 4));
+    };
+    auto rows_at = [&](int it) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < NLD; ++i) {
         const int key = i * KPI + st_key, t = seen(key0 + it * kPtTile + wave * WK + key);
-        const int page = *(const volatile __attribute__((address_space(3))) int*)(look + (uint32_t)((it & (kPtRing - 1)) * 256 + key * 4));
         at_v[i] = at_k[i];
-        at_k[i] = ((uint64_t)(((uint32_t)page << a.p_shift) + (uint32_t)(t & (a.P - 1))) << row_shift) | (uint32_t)((st_pos ^ pt_swz<D>((wave * WK + key) & 15)) * 16);
+        at_k[i] = ((uint64_t)(((uint32_t)page[i] << a.p_shift) + (uint32_t)(t & (a.P - 1))) << row_shift) | (uint32_t)((st_pos ^ pt_swz<D>((wave * WK + key) & 15)) * 16);
       }
     };
+    auto rows_of = [&](int it) __attribute__((always_inline)) { pages_of(it); rows_at(it); };
     auto load_row = [&](const uint8_t* pool, uint64_t at, int i, uint32_t place) __attribute__((always_inline)) {
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(lds_st + place + (uint32_t)(i * 1024)), "v"(pool + at) : "memory", "m0");
     };
@@ -290,7 +296,8 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
           load_row(k_head, at_k[t < NLD ? t : 0], t, p0);
           load_row(v_head, at_v[t < NLD ? t : 0], t, p2 + TILE_B);
         }
-        if (LD && t == NLD) { rows_of(it + 4); fetch_look(it + 6); }
+        if (LD && t == NLD) { pages_of(it + 4); fetch_look(it + 6); }
+        if (CUR == 0 && OUT && t == 2) rows_at(it + 3);            // (of the ids that the block before has read: no wait stands between)
 #pragma unroll
         for (int i = t * PPS; i < (t + 1) * PPS; ++i) if (i >= PPS) power(i - PPS);
         __builtin_amdgcn_sched_barrier(0);
