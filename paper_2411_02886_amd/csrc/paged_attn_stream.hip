@@ -10,7 +10,7 @@
 // softmax's reference is raised only when a weight exceeds what it allows, so that no maximum is taken in the loop.
 // Measured: 8 bf16 tokens (H 32/8, D 128) over 16384 to 65536 keys 241 us, 6.4 TB/s; one over 1000 keys 11.0 us, over 131072 90 (5.9 TB/s); one fp32 token (8/2, 64) over
 // 4096 keys 11.7.  The fixed part of a call is about 10 us: two launches, the search for the share 1.5 us, page ids and queries 1.2, the first rows
-// 1, the waves' meeting 1.5.  fp32 with 64 rows a tile: 512 tokens (32/8, 128) over 4000 keys 362 us, 63 % of what a product by the library
+// 1, the waves' meeting 1.5.  fp32 with 64 rows a tile: 512 tokens (32/8, 128) over 4000 keys 351 us, 66 % of what a product by the library
 // reaches (154 TFLOP/s); a weight's exponential and its neighbours stand between the products of 16 x 16 x 4.
 #include "paged_shares.h"
 
@@ -68,7 +68,8 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
   uint8_t* kt = smem + wave * (2 * TILE_B + 512);
   uint8_t* vt = kt + TILE_B;
   const uint32_t lds_k = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)kt);
-  const volatile int32_t* look = reinterpret_cast<const volatile int32_t*>(vt + TILE_B);   // two places of 64 page ids
+  // two places of 64 page ids (as an LDS pointer: a flat load would wait for every row in flight)
+  const volatile __attribute__((address_space(3))) int32_t* look = (const volatile __attribute__((address_space(3))) int32_t*)(vt + TILE_B);
   const int st_row = lane / PPR, st_pos = lane % PPR;
   typedef const __attribute__((address_space(3))) u32x4_t lds_u32x4;
   const float sm = a.sm_scale;
