@@ -201,7 +201,7 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
   uint8_t* at = (uint8_t*)ws;
   // bounds on the tiles and on the keys of one
   auto tiles_of = [&](int tpt) -> long {
-    return (a.q_indptr != nullptr ? a.T / tpt + std::min(a.B, a.T) : (long)a.B * ((a.C + tpt - 1) / tpt)) * a.H_kv;
+    return (a.q_indptr != nullptr ? (long)a.T / tpt + a.B : (long)a.B * ((a.C + tpt - 1) / tpt)) * a.H_kv;
   };
   auto keys_of = [&](int tpt) -> long { return std::min((long)a.max_seq_len, a.window > 0 ? (long)a.window + tpt : LONG_MAX); };
   auto run = [&](int rows, int more_rows, int most_rows, bool whole) -> hipError_t {

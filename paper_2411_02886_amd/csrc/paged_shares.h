@@ -58,7 +58,6 @@ __device__ __forceinline__ SeqShape seq_shape(const PagedAttnArgs& a, const Shar
 // room of a sequence's first r tiles
 __device__ __forceinline__ double tiles_room(const PagedAttnArgs& a, const ShareArgs& sh, const SeqShape& s, int tiles) {
   const double r = tiles;
-  if (sh.whole) return r;
   const double first = max(s.N - s.n, 0) + sh.tile_cost, tpt = sh.tpt;
   if (a.window == 0) return fma(r, first, tpt * (r * (r + 1.) * 0.5));
   const double cap = (double)a.window + tpt + sh.tile_cost;                     // where the window cuts a tile's keys
@@ -124,7 +123,27 @@ __device__ __forceinline__ void find_share(const PagedAttnArgs& a, const ShareAr
     *first = seq_shape(a, sh, G, b);
     return;
   }
-  auto share_of_line = [&](double all) { return sh.whole ? 1. : fmax((double)sh.min_keys, floor_div(all + (sh.wgs - 1), sh.wgs)); };
+  if (sh.whole) {
+    // Sequence b has the tiles from (its first row) / tpt + b on: more places than tiles, but one that is found in a search by every wave for itself, 64
+    // sequences at a time.  (In the line below each of the workgroups would add up all sequences: 4096 of 100 keys 2159 us.)
+    const int each = sh.wgs / a.H_kv, kvh = wg / each, at = wg - kvh * each;
+    auto begin_of = [&](int b) -> int { return (int)((uint32_t)min(max(a.q_indptr[b], 0), a.T) / (uint32_t)sh.tpt) + b; };
+    *from = *to = SharePlace{a.H_kv, 0, 0, 0};             // nothing, unless a sequence is found
+    for (int lo = 0, n = a.B;;) {                          // of the places lo .. lo + n - 1 those that begin at or before `at` come first
+      const int step = (n + 63) >> 6, i = lane * step, begin = i < n ? begin_of(lo + i) : INT_MAX;
+      const int k = __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < n && begin <= at));
+      if (k == 0) return;
+      if (step == 1) {
+        const int b = lo + k - 1, turn = at - __builtin_amdgcn_readlane(begin, k - 1);
+        *first = seq_shape(a, sh, G, b);
+        if (turn < first->tiles) { *from = SharePlace{kvh, b, turn, 0}; *to = SharePlace{kvh, b, turn, INT_MAX}; }
+        return;
+      }
+      lo += (k - 1) * step;
+      n = min(step, n - (k - 1) * step);
+    }
+  }
+  auto share_of_line = [&](double all) { return fmax((double)sh.min_keys, floor_div(all + (sh.wgs - 1), sh.wgs)); };
   if (a.B <= 64) {
     // a lane per sequence, every wave for itself, both ends at once in the halves of the wave: no barrier, and half the time
     SeqShape s{0, 0, 0, 0, 0, 0};

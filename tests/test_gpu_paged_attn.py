@@ -417,3 +417,14 @@ def test_scales_in_whole_large_tiles(gpu, dtype, sm):
     c = Cache(dtype, 8, 64, 16, [700, 270], seed=8)
     o, l, ref = run(gpu, c, 32, new, sm=sm, seed=8)
     check_attention(o, l, ref, sm)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("B", [1, 63, 64, 65, 4096, 4097])
+def test_packed_batches_of_short_sequences(gpu, dtype, B):
+    """A search among 64 places at a time: one, two and three steps; sequences without new tokens between the others."""
+    new = [(0, 1, 3, 1, 17)[b % 5] if b % 64 < 60 else 0 for b in range(B)]
+    lens = [(n + b % 7) % 30 for b, n in enumerate(new)]
+    c = Cache(dtype, 2, 64, 4, lens, seed=B)
+    o, l, ref = run(gpu, c, 4, new, seed=B, behind=3)
+    check_attention(o, l, ref, B)
