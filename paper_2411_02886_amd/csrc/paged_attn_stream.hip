@@ -8,8 +8,8 @@
 // count that knows nothing of the rows in flight.
 // bf16 weights keep their 24 bits: each is the sum of three bf16 numbers, and V is multiplied with each of them.  The
 // softmax's reference is raised only when a weight exceeds what it allows, so that no maximum is taken in the loop.
-// Measured: 8 bf16 tokens (H 32/8, D 128) over 16384 to 65536 keys 241 us, 6.4 TB/s; one over 1000 keys 11.0 us, over 131072 90 (5.9 TB/s); one fp32 token (8/2, 64) over
-// 4096 keys 11.7.  The fixed part of a call is about 10 us: two launches, the search for the share 1.5 us, page ids and queries 1.2, the first rows
+// Measured: 8 bf16 tokens (H 32/8, D 128) over 16384 to 65536 keys 241 us, 6.4 TB/s; one over 1000 keys 10.8 us, over 131072 90 (5.9 TB/s); 64 packed sequences
+// of 300 keys 15; one fp32 token (8/2, 64) over 4096 keys 11.4.  The fixed part of a call is about 10 us: two launches, the search for the share 1.5 us, page ids and queries 1.2, the first rows
 // 1, the waves' meeting 1.5.  fp32 with 64 rows a tile: 512 tokens (32/8, 128) over 4000 keys 351 us, 66 % of what a product by the library
 // reaches (154 TFLOP/s); a weight's exponential and its neighbours stand between the products of 16 x 16 x 4.
 #include "paged_shares.h"
@@ -139,7 +139,8 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
       }
     };
     // 1 KiB per load: the wave's lanes fill LDS from `dst` on.  In assembly, so that the compiler does not make every LDS read wait for
-    // it; the waits stand below.  Non-temporal: with few rows per tile nobody else reads them.
+    // it; the waits stand below.  Non-temporal: with few rows per tile nobody else reads them (a batch of 64 over 6000 keys 257 us, else
+    // 286; where tiles share rows it makes no difference).
     auto load_rows = [&](const uint8_t* pool, uint32_t dst) {
       const int my_row = (int)fresh(st_row);
 #pragma unroll

@@ -8,7 +8,7 @@
 // there); the tile's pieces leave partial results, which a merge launch joins.  Workgroups of one XCD get
 // neighbouring pieces, so that its L2 fetches the keys of a KV head once.
 // The search costs 3700 cycles (1.5 us), half of it the latency of the lengths; nothing where every tile is a workgroup's and all sequences have as many (64 new
-// tokens 10.2 -> 8.5 us).  Measured: 8192 tokens of one sequence, four tiles a workgroup, 476 us; with the tiles in their natural order, nearly all of them cut, 660.
+// tokens 10.2 -> 8.5 us), little where it is a workgroup's in a packed batch.  Measured: 8192 tokens of one sequence, four tiles a workgroup, 490 us at the time; with the tiles in their natural order, nearly all of them cut, 660.
 #pragma once
 #include "ts_kernels.h"
 #include <limits.h>
