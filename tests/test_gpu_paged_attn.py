@@ -428,3 +428,20 @@ def test_packed_batches_of_short_sequences(gpu, dtype, B):
     c = Cache(dtype, 2, 64, 4, lens, seed=B)
     o, l, ref = run(gpu, c, 4, new, seed=B, behind=3)
     check_attention(o, l, ref, B)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("H,D", [(8, 64), (4, 128)])
+def test_keys_that_a_row_does_not_see_may_be_anything(gpu, dtype, bad, H, D):
+    """The last new token of each sequence has a broken key: the rows before it do not see it (its own are unspecified)."""
+    new, lens = [2, 9, 130, 40], [700, 9, 333, 1000]
+    c = Cache(dtype, 2, D, 16, lens, seed=6)
+    bits = {np.nan: 0x7fc0, np.inf: 0x7f80, -np.inf: 0xff80}[bad] if dtype == BF else bad
+    at = [int(c.slots(b)[-1]) for b in range(4)]
+    c.k_bits[at] = bits
+    last = np.cumsum(new) - 1
+    rows = np.setdiff1d(np.arange(sum(new)), last)
+    for bound in (None, LOOSE):
+        o, l, ref = run(gpu, c, H, new, seed=10, max_seq_len=bound)           # (c.k, which the reference reads, is whole)
+        check_attention(o[rows], l[rows], tuple(x[rows] for x in ref), (bad, bound))
