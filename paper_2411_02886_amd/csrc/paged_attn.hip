@@ -42,9 +42,9 @@ __device__ __forceinline__ Pieces find_pieces(const ShareArgs& sh, int w, int la
 // pieces that follow lie in the workgroups behind it, up to the one that ends the tile: many of which may belong to a tile.  A workgroup per row: D / 4
 // lanes hold it, PG groups of them take the pieces in turn, with US in flight each, and meet in LDS.  Latency is all it costs (one token over 4096
 // keys, fp32: 13 us with the attention; with four rows per workgroup and two pieces in flight per group it was 18).
-template <int ES, int D, int US>
-__global__ __launch_bounds__(256) void paged_merge_kernel(PagedAttnArgs a, ShareArgs sh, int rows) {
-  constexpr int LPR = D / 4, PG = 256 / LPR;
+template <int ES, int D, int THREADS, int US>
+__global__ __launch_bounds__(THREADS) void paged_merge_kernel(PagedAttnArgs a, ShareArgs sh, int rows) {
+  constexpr int LPR = D / 4, PG = THREADS / LPR;
   __shared__ float4 s_o[PG][LPR];
   __shared__ float s_ml[PG][2];
   const int w = blockIdx.y, G = a.H / a.H_kv;     // (rows first: the tiles that were cut may all be every fourth workgroup's, and so on two XCDs)
@@ -164,12 +164,18 @@ __global__ __launch_bounds__(256) void paged_merge_tall_kernel(PagedAttnArgs a, 
 }
 
 template <int ES, int D>
-static hipError_t merge(const PagedAttnArgs& a, const ShareArgs& sh, int rows, hipStream_t s) {
+static hipError_t merge(const PagedAttnArgs& a, const ShareArgs& sh, int rows, long tiles, hipStream_t s) {
+  if (rows == kTallRows) {                       // (tiles are short only where their sequence is)
+    hipLaunchKernelGGL(paged_merge_tall_kernel<D>, dim3(kTallRows / 32 * (D / 32), sh.wgs), dim3(256), 0, s, a, sh);
+    return hipGetLastError();
+  }
   // A workgroup per row that a tile may have; where only the sequences with few rows are meant, as many as one token has (12 mixed ones, 28 heads: 4 us
-  // less, as most workgroups find nothing).  More rows take turns.  The tall kernel's tiles are short only where their sequence is.
+  // less, as most workgroups find nothing).  More rows take turns.  Where there are many tiles, of few pieces then, a wave per row (16 drafts of 8 tokens
+  // over 3000 keys 38.9 us, by 256 threads 42.3; one token over 4000, 32 pieces a tile, 14.5 and 12.2).
   const int G = a.H / a.H_kv;
-  if (rows != kTallRows) hipLaunchKernelGGL((paged_merge_kernel<ES, D, 4>), dim3(sh.most_rows < INT_MAX ? G : std::min(sh.tpt, a.C) * G, sh.wgs), dim3(256), 0, s, a, sh, rows);
-  else hipLaunchKernelGGL(paged_merge_tall_kernel<D>, dim3(kTallRows / 32 * (D / 32), sh.wgs), dim3(256), 0, s, a, sh);
+  const dim3 grid(sh.most_rows < INT_MAX ? G : std::min(sh.tpt, a.C) * G, sh.wgs);
+  if (tiles * 4 >= sh.wgs) hipLaunchKernelGGL((paged_merge_kernel<ES, D, 64, 4>), grid, dim3(64), 0, s, a, sh, rows);
+  else hipLaunchKernelGGL((paged_merge_kernel<ES, D, 256, 4>), grid, dim3(256), 0, s, a, sh, rows);
   return hipGetLastError();
 }
 
@@ -223,8 +229,8 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
     at += piece_bytes(rows, D);
     const hipError_t e = tall ? launch_paged_tall(D, a, sh, s) : launch_paged_stream(dtype, D, rows / 16, a, sh, s);
     if (e != hipSuccess || whole) return e;
-    if (dtype == TS_BF16) return D == 64 ? merge<2, 64>(a, sh, rows, s) : merge<2, 128>(a, sh, rows, s);
-    return D == 64 ? merge<4, 64>(a, sh, rows, s) : merge<4, 128>(a, sh, rows, s);
+    if (dtype == TS_BF16) return D == 64 ? merge<2, 64>(a, sh, rows, tiles_of(sh.tpt), s) : merge<2, 128>(a, sh, rows, tiles_of(sh.tpt), s);
+    return D == 64 ? merge<4, 64>(a, sh, rows, tiles_of(sh.tpt), s) : merge<4, 128>(a, sh, rows, tiles_of(sh.tpt), s);
   };
   // A workgroup per tile, and no merge, where tiles are short, or where there are enough of them that are not long.  (200 keys: 8.2 us, in shares 10.3; 64
   // sequences of 250 to 500 keys, 512 tiles: 22.8 and 29; but 16 fp32 sequences of 1000 to 2000 keys, 32 tiles, 42 us instead of 17.)
