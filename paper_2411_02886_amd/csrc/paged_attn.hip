@@ -185,25 +185,31 @@ static size_t piece_bytes(int rows, int D) {
 }
 
 // The rows of a sequence and KV head, n * G, decide: up to 16 (one block of columns) or 32 by the stream kernel, which is bound by the memory (8 tokens times
-// 4 heads over 3000 keys, one sequence 17 us, 16 of them 46; by the tall kernel 27 and 58); more by the tall one (bf16), or by the stream kernel with 64 rows a
+// 4 heads over 3000 keys, one sequence 17 us, 16 of them 46; by the tall kernel 27 and 58), bf16 up to 64 by two of its tiles (16 tokens over 2000 keys 18.6 us,
+// by the tall kernel 27.7, 8 times 4000 47 and 53; with 96 rows it would be 75 and 52); more by the tall one (bf16), or by the stream kernel with 64 rows a
 // tile (fp32, whose matrix products it is then bound by: 512 tokens over 4000 keys 362 us, with 32 rows 412).  A packed batch may hold both kinds:
-// two launches, each takes the sequences that are its.
+// two launches, each takes the sequences that are its.  As its bound says little about most of its sequences, twice as many rows go without the second (8 of
+// 1 to 30 tokens over up to 4000 keys 42 us, else 76).
 struct PagedPlan { int few_rows, many_rows; };   // rows of the tiles of sequences with few rows, and of those with more (0: there are none)
-static PagedPlan paged_plan(int dtype, int G, int chunk) {
+static PagedPlan paged_plan(int dtype, int G, int chunk, bool packed) {
   const long rows = (long)chunk * G;
   if (rows <= 16) return PagedPlan{16, 0};
-  if (rows <= 32) return PagedPlan{32, 0};
+  if (rows <= (dtype == TS_BF16 ? 64 : 32) * (packed ? 2 : 1)) return PagedPlan{32, 0};
   return dtype == TS_BF16 ? PagedPlan{32, kTallRows} : PagedPlan{16, 64};
 }
 
 size_t paged_attn_workspace(int dtype, int D, int G, int chunk) {
-  const PagedPlan pl = paged_plan(dtype, G, chunk);
-  return align_up(piece_bytes(pl.few_rows, D) + (pl.many_rows ? piece_bytes(pl.many_rows, D) : 0), 256);
+  size_t most = 0;
+  for (const bool packed : {false, true}) {
+    const PagedPlan pl = paged_plan(dtype, G, chunk, packed);
+    most = std::max(most, align_up(piece_bytes(pl.few_rows, D) + (pl.many_rows ? piece_bytes(pl.many_rows, D) : 0), 256));
+  }
+  return most;
 }
 
 hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws, hipStream_t s) {
   const int G = a.H / a.H_kv;
-  const PagedPlan pl = paged_plan(dtype, G, a.C);
+  const PagedPlan pl = paged_plan(dtype, G, a.C, a.q_indptr != nullptr);
   uint8_t* at = (uint8_t*)ws;
   // bounds on the tiles and on the keys of one
   auto tiles_of = [&](int tpt) -> long {
@@ -241,7 +247,9 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
   if (!pl.many_rows) return run(pl.few_rows, 0, INT_MAX, few_whole(pl.few_rows));
   // Short prompts have too few tiles for the chip: there 32 rows a tile for all sequences, at most two workgroups per CU.  (256 tokens 12.3 us, by 256 rows a
   // tile 15.2, 512 tokens 19.3 and 20.8; 768, more tiles than that, 37 and 27.  fp32: 256 tokens 20.5, by 64 rows a tile 33, 400 39 and 48.)
-  if (tiles_of(32 / G) <= 2 * kShareWgs && keys_of(32 / G) <= 1024) return run(32, 0, INT_MAX, true);
+  // (fp32, whose larger tiles save less, also with more tiles of few keys: 16 sequences of 64 tokens 33 and 45, 4 of 256 60 and 60.)
+  const long small = tiles_of(32 / G), small_keys = keys_of(32 / G);
+  if (small_keys <= 1024 && (small <= 2 * kShareWgs || (dtype == TS_F32 && small * small_keys <= 1l << 18))) return run(32, 0, INT_MAX, true);
   if (a.q_indptr != nullptr) {                             // (without, every sequence has as many)
     const hipError_t e = run(pl.few_rows, 0, pl.few_rows, few_whole(pl.few_rows));
     if (e != hipSuccess) return e;
