@@ -3,8 +3,8 @@
 // Two or four waves take one token.  Its angles are the same for all heads: a lane per pair forms the angle in double (an exact int32 times
 // a float has 55 bits), takes whole turns off in double and leaves cosine and sine in LDS.  Then a lane has the same piece of every
 // head it works on, so that it reads its cosines once: 64 / (pieces of a head, rounded up to a power of two) heads side by side, several in flight.  A
-// piece is 16 bytes and its partner (halves) or 16 bytes that hold whole pairs (neighbours); where the rotated part does not
-// divide so, single pairs.  Whoever writes an element is the only one who read it, so q may be turned in place.
+// piece is 16 bytes and its partner (halves) or 16 bytes that hold whole pairs (neighbours); where the rotated part does not divide so, 8 bytes (3000 tokens of
+// H 40/8, 24 of 128 elements turned, 20 us), and where it does not divide at all, single pairs (42).  Whoever writes an element is the only one who read it, so q may be turned in place.
 // Measured (H 32/8, D 128): 15243 tokens, three axes, parts of a fused projection 155 us by a workgroup per token and single pairs, 79 so (4.7 TB/s, what a
 // large copy reaches); 64 single tokens 3.8 us.
 #include "ts_kernels.h"
@@ -20,25 +20,29 @@ template <> __device__ __forceinline__ float to_f32<uint16_t>(uint16_t x) { retu
 template <typename T> __device__ __forceinline__ T from_f32(float x) { return x; }
 template <> __device__ __forceinline__ uint16_t from_f32<uint16_t>(float x) { return (uint16_t)f32_to_bf16_bits(x); }
 
-template <typename T> struct Piece {                                   // 16 bytes as floats
-  static constexpr int N = 16 / sizeof(T);
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
+template <int BYTES> struct PieceWords { typedef u32x4_t type; };
+template <> struct PieceWords<8> { typedef u32x2_t type; };
+
+template <typename T, int BYTES> struct Piece {                        // 16 or 8 bytes as floats
+  static constexpr int N = BYTES / sizeof(T);
+  typedef typename PieceWords<BYTES>::type words_t;
   float x[N];
-  __device__ __forceinline__ void load(u32x4_t v) {
-    const uint32_t w[4] = {v[0], v[1], v[2], v[3]};
+  __device__ __forceinline__ void load(words_t v) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (sizeof(T) == 2) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
-      else x[i] = __uint_as_float(w[i]);
+    for (int i = 0; i < BYTES / 4; ++i) {
+      if constexpr (sizeof(T) == 2) { x[2 * i] = bf16_lo(v[i]); x[2 * i + 1] = bf16_hi(v[i]); }
+      else x[i] = __uint_as_float(v[i]);
     }
   }
-  __device__ __forceinline__ u32x4_t store() const {
-    uint32_t w[4];
+  __device__ __forceinline__ words_t store() const {
+    words_t w;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < BYTES / 4; ++i) {
       if constexpr (sizeof(T) == 2) w[i] = __builtin_bit_cast(uint32_t, bf16x2_t{(__bf16)x[2 * i], (__bf16)x[2 * i + 1]});   // one instruction, to nearest even
       else w[i] = __float_as_uint(x[i]);
     }
-    return u32x4_t{w[0], w[1], w[2], w[3]};
+    return w;
   }
 };
 
@@ -48,9 +52,11 @@ constexpr int kRopeFew = 2048;
 
 enum { kPairs = 0, kHalves = 1, kNeighbours = 2 };
 
-template <typename T, int MODE>
+template <typename T, int MODE, int BYTES>
 __global__ __launch_bounds__(256) void rope_append_kernel(RopeAppendArgs a) {
-  constexpr int VE = 16 / sizeof(T), UN = 2;                           // elements of a piece; pieces per lane in flight
+  constexpr int VE = BYTES / sizeof(T), UN = 2;                        // elements of a piece; pieces per lane in flight
+  typedef Piece<T, BYTES> piece_t;
+  typedef typename piece_t::words_t words_t;
   __shared__ __attribute__((aligned(16))) float s_turn[4][2][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), share = 1 << a.share_shift;
   const int part = wave & (share - 1), row = (int)((((uint64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + wave) >> a.share_shift);   // `share` waves to a token
@@ -73,19 +79,19 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeAppendArgs a) {
   const int u = lane & ((1 << shift) - 1), lanes = 64 >> shift, side = part * lanes + (lane >> shift), step = lanes << a.share_shift;
   const bool turns = u < turn;
   const uint32_t e0 = (uint32_t)(turns || MODE == kNeighbours ? u * VE : a.rotary + (u - turn) * VE) * sizeof(T), e1 = e0 + half * sizeof(T);
-  u32x4_t v[UN], w[UN];
+  words_t v[UN], w[UN];
   auto load = [&](int h0) {
 #pragma unroll
     for (int k = 0; k < UN; ++k) {
       const int h = h0 + k * step;
       if (h >= nq + nk || u >= units) continue;
       const uint8_t* from = h < nq ? q_row + h * row_bytes : k_row + (h - nq) * row_bytes;
-      v[k] = *reinterpret_cast<const u32x4_t*>(from + e0);
-      if (MODE == kHalves && turns) w[k] = *reinterpret_cast<const u32x4_t*>(from + e1);
+      v[k] = *reinterpret_cast<const words_t*>(from + e0);
+      if (MODE == kHalves && turns) w[k] = *reinterpret_cast<const words_t*>(from + e1);
     }
   };
   if constexpr (MODE != kPairs) load(side);
-  const int v_pieces = nk * D / VE, v_lane = part * 64 + lane, v_step = 64 << a.share_shift;
+  const int v_pieces = nk * D * (int)sizeof(T) / 16, v_lane = part * 64 + lane, v_step = 64 << a.share_shift;
   const u32x4_t* v_row = reinterpret_cast<const u32x4_t*>(a.v + row * a.v_stride);
   u32x4_t x[UN];
   auto load_v = [&](int i0) {
@@ -138,10 +144,10 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeAppendArgs a) {
         if (h >= nh || u >= units) continue;
         uint8_t* to = h < nq ? q_to + h * row_bytes : k_to + (h - nq) * row_bytes;
         if (turns) {
-          Piece<T> x;
+          piece_t x;
           x.load(v[k]);
           if constexpr (MODE == kHalves) {
-            Piece<T> y;
+            piece_t y;
             y.load(w[k]);
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
@@ -149,7 +155,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeAppendArgs a) {
               x.x[i] = f * c[i] - g * s[i];
               y.x[i] = f * s[i] + g * c[i];
             }
-            *reinterpret_cast<u32x4_t*>(to + e1) = y.store();
+            *reinterpret_cast<words_t*>(to + e1) = y.store();
           } else {
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
@@ -160,7 +166,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeAppendArgs a) {
           }
           v[k] = x.store();
         }
-        *reinterpret_cast<u32x4_t*>(to + e0) = v[k];
+        *reinterpret_cast<words_t*>(to + e0) = v[k];
       }
     }
   }
@@ -174,17 +180,24 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeAppendArgs a) {
   }
 }
 
+template <typename T, int BYTES>
+static void rope_launch(bool pairs, const RopeAppendArgs& a, dim3 grid, hipStream_t s) {
+  if (pairs) hipLaunchKernelGGL((rope_append_kernel<T, kPairs, 16>), grid, dim3(256), 0, s, a);
+  else if (a.adjacent) hipLaunchKernelGGL((rope_append_kernel<T, kNeighbours, BYTES>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((rope_append_kernel<T, kHalves, BYTES>), grid, dim3(256), 0, s, a);
+}
+
 template <typename T>
 static hipError_t rope_one(const RopeAppendArgs& b, hipStream_t s) {
-  constexpr int VE = 16 / sizeof(T);
   RopeAppendArgs a = b;
-  const bool pairs = a.rotary % (a.adjacent ? VE : 2 * VE) != 0;
+  // pieces of 16 bytes, or of 8, whichever divide the rotated part (its halves), or single pairs
+  auto divides = [&](int bytes) -> bool { return a.rotary % ((a.adjacent ? 1 : 2) * bytes / (int)sizeof(T)) == 0; };
+  const bool pairs = !divides(8);
   a.share_shift = a.T <= kRopeFew || pairs ? 2 : 1;
   const long wgs = (((long)a.T << a.share_shift) + 3) / 4, wide = 1 << 20;      // (a grid has less than 2^32 threads in a dimension)
-  const dim3 grid((unsigned)std::min(wgs, wide), (unsigned)((wgs + wide - 1) / wide)), block(256);
-  if (pairs) hipLaunchKernelGGL((rope_append_kernel<T, kPairs>), grid, block, 0, s, a);
-  else if (a.adjacent) hipLaunchKernelGGL((rope_append_kernel<T, kNeighbours>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((rope_append_kernel<T, kHalves>), grid, block, 0, s, a);
+  const dim3 grid((unsigned)std::min(wgs, wide), (unsigned)((wgs + wide - 1) / wide));
+  if (divides(16)) rope_launch<T, 16>(false, a, grid, s);
+  else rope_launch<T, 8>(pairs, a, grid, s);
   return hipGetLastError();
 }
 

@@ -194,3 +194,10 @@ def test_a_captured_call_reads_lengths_and_positions_when_it_runs(gpu):
             assert torch.equal(a, b), rep
         pos += 3
         lens -= 1
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("adjacent", [False, True], ids=["halves", "neighbours"])
+@pytest.mark.parametrize("rotary", [4, 8, 12, 20, 28, 36, 40, 56, 72, 100, 120, 124])
+def test_parts_that_divide_into_smaller_pieces_or_none(gpu, dtype, adjacent, rotary):
+    case(gpu, dtype, 6, 2, 128, 8, [5, 1, 20], [9, 1, 40], rotary, 2, seed=rotary, adjacent=adjacent)
