@@ -46,9 +46,10 @@ template <typename T, int BYTES> struct Piece {                        // 16 or 
   }
 };
 
-// Up to so many tokens four waves share each, beyond that two.  (us, H 32/8, D 128, bf16: 64 tokens one wave each 5.6, two 4.5, four 3.8; 2048: 11.5, 10.9, 10.7;
-// 4096: 17.0, 16.1, 18.4; 20000 of H 14/2, D 64, fp32: 38.1, 36.8, 48.2.  Single pairs: four, 5000 tokens 39.4, 37.1, 32.8.)
-constexpr int kRopeFew = 2048;
+// Up to so many tokens four waves share each; beyond that two, and one where a wave has the heads in two steps.  (us by one, two, four waves, bf16: 64 tokens of
+// H 32/8, D 128 5.6, 4.5, 3.8; 2048 11.5, 10.9, 10.7; 4096 17.0, 16.1, 18.4; 2000 of H 6/2, D 64 3.6, 4.1, 5.5, 30000 18.7, 28.3, 48.5; of H 16/4, D 128, three steps,
+// 7.4, 7.0, 8.0 and 72.5, 68.1, 81.1.  Single pairs: always four, 5000 tokens 39.4, 37.1, 32.8.)
+constexpr int kRopeFew = 1024;
 
 enum { kPairs = 0, kHalves = 1, kNeighbours = 2 };
 
@@ -193,7 +194,11 @@ static hipError_t rope_one(const RopeAppendArgs& b, hipStream_t s) {
   // pieces of 16 bytes, or of 8, whichever divide the rotated part (its halves), or single pairs
   auto divides = [&](int bytes) -> bool { return a.rotary % ((a.adjacent ? 1 : 2) * bytes / (int)sizeof(T)) == 0; };
   const bool pairs = !divides(8);
-  a.share_shift = a.T <= kRopeFew || pairs ? 2 : 1;
+  const int ve = (divides(16) ? 16 : 8) / (int)sizeof(T), units = (a.adjacent ? a.rotary : a.rotary / 2) / ve + (a.D - a.rotary) / ve;
+  int lanes = 64;                                // heads side by side
+  while (lanes * units > 64) lanes >>= 1;
+  const int heads = (a.q != nullptr ? a.H : 0) + (a.k != nullptr ? a.H_kv : 0);
+  a.share_shift = a.T <= kRopeFew || pairs ? 2 : heads <= 2 * lanes ? 0 : 1;
   const long wgs = (((long)a.T << a.share_shift) + 3) / 4, wide = 1 << 20;      // (a grid has less than 2^32 threads in a dimension)
   const dim3 grid((unsigned)std::min(wgs, wide), (unsigned)((wgs + wide - 1) / wide));
   if (divides(16)) rope_launch<T, 16>(false, a, grid, s);
