@@ -16,7 +16,7 @@
 // Weights are rounded to bf16 for the product with V (half a step, 2^-8); their sum is of the floats before that rounding, so that the log-sum-exp
 // keeps 24 bits.
 //
-// Measured (H 32/8, D 128): a prompt of 8192 tokens 470 to 482 us from card to card, 512 tokens over 131072 keys 904 to 946, 1.15 and 1.19 PFLOP/s; a bf16 product of 8192^3 by the library
+// Measured (H 32/8, D 128): a prompt of 8192 tokens 470 to 505 us from card to card, 512 tokens over 131072 keys 904 to 966, up to 1.17 and 1.22 PFLOP/s; a bf16 product of 8192^3 by the library
 // reaches 1.22 on the same card.  64 keys take 3350 cycles, of which the matrix cores work 2048 and 2500 go to issuing, and the clock falls to 1.8 to 2.0 GHz meanwhile (2.4 with
 // little work): power is the bound.  A tile's start and end cost 13000 cycles (page ids and queries 2100, the first tile and its scores 3700, the first block's weights
 // 2200, results 4400): what short prompts are bound by.  D 64: 2150 cycles where the matrix cores work 1024; exponentials, sums and
