@@ -146,7 +146,7 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
 #pragma unroll
       for (int l = 0; l < NLD; ++l) {
         const uint64_t off = ((uint64_t)at[l] << row_shift) + (uint32_t)(kvh * RB + ((st_pos ^ ps_swz<ES, D>((l * RPI + my_row) & 15)) * 16));
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" :: "s"(dst + l * 1024), "v"(pool + off) : "memory", "m0");
+        asm volatile("s_add_u32 m0, %0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" :: "s"(dst), "v"(pool + off), "i"(l * 1024) : "memory", "m0", "scc");
       }
     };
     float ref[CB], lsum[CB];                  // of row cb * 16 + col: reference logit (the same in its four lanes), this lane's keys' sum
