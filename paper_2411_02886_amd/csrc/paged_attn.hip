@@ -254,9 +254,10 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
     const hipError_t e = run(pl.few_rows, 0, pl.few_rows, few_whole(pl.few_rows));
     if (e != hipSuccess) return e;
   }
-  // (1024 tokens 33.4 us, in shares 35.7; but 2048 with a workgroup per tile 59 instead of 54)
+  // (1024 tokens 33.4 us, in shares 35.7; but 2048 with a workgroup per tile 59 instead of 54.  A packed batch's bound counts
+  // up to a tile per sequence too many: there twice the tiles, 24 of 1 to 100 tokens 46 us, in shares 51; four times would cost 64 of 64 tokens over 900 119 instead of 98.)
   const long tiles = tiles_of(pl.many_rows / G);
-  return run(pl.many_rows, a.q_indptr != nullptr ? pl.few_rows : 0, INT_MAX, tiles <= kShareWgs && keys_of(pl.many_rows / G) <= 1024);
+  return run(pl.many_rows, a.q_indptr != nullptr ? pl.few_rows : 0, INT_MAX, tiles <= kShareWgs * (a.q_indptr != nullptr ? 2 : 1) && keys_of(pl.many_rows / G) <= 1024);
 }
 
 }  // namespace ts
