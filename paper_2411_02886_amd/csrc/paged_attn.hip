@@ -211,9 +211,11 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
   const int G = a.H / a.H_kv;
   const PagedPlan pl = paged_plan(dtype, G, a.C, a.q_indptr != nullptr);
   uint8_t* at = (uint8_t*)ws;
-  // bounds on the tiles and on the keys of one
-  auto tiles_of = [&](int tpt) -> long {
-    return (a.q_indptr != nullptr ? (long)a.T / tpt + a.B : (long)a.B * ((a.C + tpt - 1) / tpt)) * a.H_kv;
+  // tiles of every sequence (0: not as many), and bounds on all tiles and on the keys of one.  A tile of few rows beside large ones is its whole sequence.
+  auto each_of = [&](int tpt, bool beside) -> int { return beside ? 1 : a.q_indptr != nullptr ? 0 : (a.C + tpt - 1) / tpt; };
+  auto tiles_of = [&](int tpt, bool beside) -> long {
+    const int each = each_of(tpt, beside);
+    return (each > 0 ? (long)a.B * each : (long)a.T / tpt + a.B) * a.H_kv;
   };
   auto keys_of = [&](int tpt) -> long { return std::min((long)a.max_seq_len, a.window > 0 ? (long)a.window + tpt : LONG_MAX); };
   auto run = [&](int rows, int more_rows, int most_rows, bool whole) -> hipError_t {
@@ -224,39 +226,42 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
     sh.more_rows = more_rows;
     sh.most_rows = most_rows;
     sh.whole = whole ? 1 : 0;
+    const bool beside = most_rows < INT_MAX;
+    sh.each = each_of(sh.tpt, beside);
     // The smallest share (twice as much: a token over 1000 keys 1.4 us more, 64 tokens over 4000 keys 4 us), and what a tile's start and end cost (a quarter
     // of it: 12 mixed chunks 192 us instead of 160; twice: prompts between 1 us less and 1 us more).
     sh.min_keys = tall ? 2 * kt : kt;
     sh.tile_cost = tall ? 256 : 64;
-    sh.wgs = whole ? (int)tiles_of(sh.tpt) : kShareWgs;
+    sh.wgs = whole ? (int)tiles_of(sh.tpt, beside) : kShareWgs;
     sh.desc = (int32_t*)at;
     sh.part_ml = (float*)(at + align_up((size_t)kShareWgs * 32, 256));
     sh.part_o = (float*)((uint8_t*)sh.part_ml + align_up((size_t)kShareWgs * 2 * rows * 2 * 4, 256));
     at += piece_bytes(rows, D);
     const hipError_t e = tall ? launch_paged_tall(D, a, sh, s) : launch_paged_stream(dtype, D, rows / 16, a, sh, s);
     if (e != hipSuccess || whole) return e;
-    if (dtype == TS_BF16) return D == 64 ? merge<2, 64>(a, sh, rows, tiles_of(sh.tpt), s) : merge<2, 128>(a, sh, rows, tiles_of(sh.tpt), s);
-    return D == 64 ? merge<4, 64>(a, sh, rows, tiles_of(sh.tpt), s) : merge<4, 128>(a, sh, rows, tiles_of(sh.tpt), s);
+    if (dtype == TS_BF16) return D == 64 ? merge<2, 64>(a, sh, rows, tiles_of(sh.tpt, beside), s) : merge<2, 128>(a, sh, rows, tiles_of(sh.tpt, beside), s);
+    return D == 64 ? merge<4, 64>(a, sh, rows, tiles_of(sh.tpt, beside), s) : merge<4, 128>(a, sh, rows, tiles_of(sh.tpt, beside), s);
   };
   // A workgroup per tile, and no merge, where tiles are short, or where there are enough of them that are not long.  (200 keys: 8.2 us, in shares 10.3; 64
-  // sequences of 250 to 500 keys, 512 tiles: 22.8 and 29; but 16 fp32 sequences of 1000 to 2000 keys, 32 tiles, 42 us instead of 17.)
-  auto few_whole = [&](int rows) -> bool {
-    const long tiles = tiles_of(rows / G), keys = keys_of(rows / G);
-    return tiles < (1l << 23) && (keys <= 512 || (tiles >= kShareWgs && keys <= 16 * (dtype == TS_F32 ? 64 : 128)));
+  // sequences of 250 to 500 keys, 512 tiles: 22.8 and 29; but 16 fp32 sequences of 1000 to 2000 keys, 32 tiles, 42 us instead of 17.)  Beside large
+  // tiles a second merge would cost more (14 chunks of 1 to 197 tokens over up to 770 keys 52 us, in shares 64).
+  auto few_whole = [&](int rows, bool beside) -> bool {
+    const long tiles = tiles_of(rows / G, beside), keys = keys_of(rows / G);
+    return tiles < (1l << 23) && (keys <= 512 || ((tiles >= kShareWgs || beside) && keys <= 16 * (dtype == TS_F32 ? 64 : 128)));
   };
-  if (!pl.many_rows) return run(pl.few_rows, 0, INT_MAX, few_whole(pl.few_rows));
+  if (!pl.many_rows) return run(pl.few_rows, 0, INT_MAX, few_whole(pl.few_rows, false));
   // Short prompts have too few tiles for the chip: there 32 rows a tile for all sequences, at most two workgroups per CU.  (256 tokens 12.3 us, by 256 rows a
   // tile 15.2, 512 tokens 19.3 and 20.8; 768, more tiles than that, 37 and 27.  fp32: 256 tokens 20.5, by 64 rows a tile 33, 400 39 and 48.)
   // (fp32, whose larger tiles save less, also with more tiles of few keys: 16 sequences of 64 tokens 33 and 45, 4 of 256 60 and 60.)
-  const long small = tiles_of(32 / G), small_keys = keys_of(32 / G);
+  const long small = tiles_of(32 / G, false), small_keys = keys_of(32 / G);
   if (small_keys <= 1024 && (small <= 2 * kShareWgs || (dtype == TS_F32 && small * small_keys <= 1l << 18))) return run(32, 0, INT_MAX, true);
   if (a.q_indptr != nullptr) {                             // (without, every sequence has as many)
-    const hipError_t e = run(pl.few_rows, 0, pl.few_rows, few_whole(pl.few_rows));
+    const hipError_t e = run(pl.few_rows, 0, pl.few_rows, few_whole(pl.few_rows, true));
     if (e != hipSuccess) return e;
   }
   // (1024 tokens 33.4 us, in shares 35.7; but 2048 with a workgroup per tile 59 instead of 54.  A packed batch's bound counts
   // up to a tile per sequence too many: there twice the tiles, 24 of 1 to 100 tokens 46 us, in shares 51; four times would cost 64 of 64 tokens over 900 119 instead of 98.)
-  const long tiles = tiles_of(pl.many_rows / G);
+  const long tiles = tiles_of(pl.many_rows / G, false);
   return run(pl.many_rows, a.q_indptr != nullptr ? pl.few_rows : 0, INT_MAX, tiles <= kShareWgs * (a.q_indptr != nullptr ? 2 : 1) && keys_of(pl.many_rows / G) <= 1024);
 }
 

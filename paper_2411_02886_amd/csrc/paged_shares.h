@@ -22,6 +22,7 @@ struct ShareArgs {
   int tpt;          // tokens per tile
   int more_rows, most_rows;   // sequences with more_rows < n * G <= most_rows take part
   int whole;        // a workgroup per tile, nothing is cut
+  int each;         // whole: tiles of every sequence that takes part, where they have as many; or 0
   int min_keys;     // smallest share
   int tile_cost;    // keys that a tile's start and end cost
   int wgs;          // workgroups of the launch
@@ -115,12 +116,12 @@ template <int KT>
 __device__ __forceinline__ void find_share(const PagedAttnArgs& a, const ShareArgs& sh, int G, int wg, ShareScratch* lds, SharePlace* from,
                                            SharePlace* to, SeqShape* first) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  if (sh.whole && a.q_indptr == nullptr) {                 // as many tiles of every sequence: no search
-    const uint32_t each = (uint32_t)(a.C + sh.tpt - 1) / (uint32_t)sh.tpt, at = (uint32_t)wg / each;
-    const int b = (int)(at % (uint32_t)a.B), i = (int)((uint32_t)wg - at * each);
-    *from = SharePlace{(int)(at / (uint32_t)a.B), b, i, 0};
-    *to = SharePlace{from->kvh, b, i, INT_MAX};
+  if (sh.whole && sh.each > 0) {                           // no search
+    const uint32_t at = (uint32_t)wg / (uint32_t)sh.each;
+    const int b = (int)(at % (uint32_t)a.B), i = (int)((uint32_t)wg - at * (uint32_t)sh.each);
     *first = seq_shape(a, sh, G, b);
+    *from = SharePlace{i < first->tiles ? (int)(at / (uint32_t)a.B) : a.H_kv, b, i, 0};
+    *to = SharePlace{from->kvh, b, i, INT_MAX};
     return;
   }
   if (sh.whole) {
