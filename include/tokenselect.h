@@ -325,8 +325,7 @@ int32_t ts_chunk_mean_query(const ts_problem* p, const void* q, void* q_mean, vo
 /* Attention of the new tokens over their whole sequence (dense: no selection, no index list), both dtypes:
  *   out[r][h][:] = sum_t softmax_t( <q[r][h], K[slot(b, t)][h/G]> * sm_scale ) * V[slot(b, t)][h/G]
  * for new token c = r - q_indptr[b] at place x = N_b - n_b + c over t in [max(0, x - window + 1), x]; window 0 = from 0 on (every
- * cached token and the chunk's own up to x).  Float accumulation, out rounded to p->dtype; bf16: where chunk * G and a sequence's
- * n_b * G are more than 32, the weights that multiply V may be rounded to bf16 (matrix-core operand; their sum is not).
+ * cached token and the chunk's own up to x).  Weights and sums in float, out rounded to p->dtype.
  * Pages that no new token sees (wholly in front of the first one's window, behind N_b) are not read.  A token that some of a sequence's rows see
  * and others do not takes part in the latter with weight 0: its K may be anything, its V has to be finite.
  * q, out [device] [num_rows][H][D], 16-byte aligned, not overlapping; lse [device] float [num_rows][H] or NULL.
@@ -339,6 +338,10 @@ int32_t ts_chunk_mean_query(const ts_problem* p, const void* q, void* q_mean, vo
 int32_t ts_paged_attn_workspace_bytes(const ts_problem* p, int32_t num_rows, size_t* bytes);
 int32_t ts_paged_attn(const ts_problem* p, const void* q, const int32_t* q_indptr, int32_t num_rows, int32_t window,
                       float sm_scale, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+/* The same, and the same workspace, where bf16 weights that multiply V may be rounded to bf16 (half a step, 2^-8 of each; their sum is of the floats
+ * before): prompts of thousands of tokens in half the time.  Sequences with up to 32 rows (n_b * G) and fp32 are computed as ts_paged_attn does. */
+int32_t ts_paged_attn_rounded(const ts_problem* p, const void* q, const int32_t* q_indptr, int32_t num_rows, int32_t window,
+                              float sm_scale, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
 
 /* Rotary positions with one to four axes (a text's place; time, height and width of a video's patches), and the new
  * tokens' K and V rows written into the pages: one launch.

@@ -10,5 +10,5 @@ from .binding import (  # noqa: F401
     ts_debug_set_topk_path, ts_debug_event_create, ts_debug_event_destroy, ts_debug_event_elapsed_ms,
     ts_debug_set_score_timing_events, ts_paged_qk_codes, ts_soft_vote_bounds, ts_topk_exact, ts_debug_set_codes_path, ts_topk_noalloc,
     ts_paged_qk_scores_checked, ts_paged_qk_codes_checked, ts_soft_vote_ranked, TS_TOPK_VOTE_HIST,
-    Rope, rope_axes, ts_paged_attn, ts_paged_attn_workspace_bytes, ts_rope_append, ts_pages_copy, ts_cache_compact,
+    Rope, rope_axes, ts_paged_attn, ts_paged_attn_rounded, ts_paged_attn_workspace_bytes, ts_rope_append, ts_pages_copy, ts_cache_compact,
 )

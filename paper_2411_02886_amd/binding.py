@@ -96,6 +96,7 @@ def load():
         L.ts_head_vote.argtypes = [pp, vp, i32, vp, vp, vp, sz, vp]
         L.ts_paged_attn_workspace_bytes.argtypes = [pp, i32, ctypes.POINTER(sz)]
         L.ts_paged_attn.argtypes = [pp, vp, vp, i32, i32, f32, vp, vp, vp, sz, vp]
+        L.ts_paged_attn_rounded.argtypes = L.ts_paged_attn.argtypes
         L.ts_rope_append.argtypes = [pp, ctypes.POINTER(_CRope), vp, i64, vp, i64, vp, i64, vp, i32, vp, vp, vp]
         L.ts_pages_copy.argtypes = [pp, vp, vp, i32, i32, vp]
         L.ts_cache_compact.argtypes = [pp, vp, i32, vp, vp, vp, vp, vp, vp]
@@ -113,7 +114,7 @@ def load():
                      "ts_debug_event_elapsed_ms", "ts_debug_set_score_timing_events", "ts_paged_qk_codes",
                      "ts_soft_vote_bounds", "ts_topk_exact", "ts_debug_set_codes_path", "ts_topk_noalloc",
                      "ts_paged_qk_scores_checked", "ts_paged_qk_codes_checked", "ts_soft_vote_ranked",
-                     "ts_paged_attn_workspace_bytes", "ts_paged_attn", "ts_rope_append", "ts_pages_copy", "ts_cache_compact"):
+                     "ts_paged_attn_workspace_bytes", "ts_paged_attn", "ts_paged_attn_rounded", "ts_rope_append", "ts_pages_copy", "ts_cache_compact"):
             getattr(L, name).restype = i32
         _lib = L
     return _lib
@@ -369,6 +370,11 @@ def ts_paged_attn_workspace_bytes(p: Problem, num_rows: int) -> int:
 def ts_paged_attn(p: Problem, q, q_indptr, num_rows: int, window: int, sm_scale: float, out, lse, ws, stream=None) -> None:
     _ok(load().ts_paged_attn(p.ref(), _ptr(q), _ptr(q_indptr), int(num_rows), int(window), float(sm_scale), _ptr(out), _ptr(lse),
                              _ptr(ws), _nbytes(ws), _stream(stream)), "ts_paged_attn")
+
+
+def ts_paged_attn_rounded(p: Problem, q, q_indptr, num_rows: int, window: int, sm_scale: float, out, lse, ws, stream=None) -> None:
+    _ok(load().ts_paged_attn_rounded(p.ref(), _ptr(q), _ptr(q_indptr), int(num_rows), int(window), float(sm_scale), _ptr(out), _ptr(lse),
+                                     _ptr(ws), _nbytes(ws), _stream(stream)), "ts_paged_attn_rounded")
 
 
 def _row_stride(t, row: int, name: str) -> int:

@@ -111,7 +111,7 @@ using namespace ts;
 
 extern "C" {
 
-int32_t ts_version(void) { return 400; }   // 0.4.0: dense attention, rotation + append, page copies and compaction joined (0.3.0: the checked score calls and the ranked vote)
+int32_t ts_version(void) { return 500; }   // 0.5.0: ts_paged_attn_rounded, ts_paged_attn keeps its weights in float (0.4.0: dense attention, rotation + append, page copies and compaction; 0.3.0: the checked score calls and the ranked vote)
 
 const char* ts_strerror(int32_t status) {
   switch (status) {

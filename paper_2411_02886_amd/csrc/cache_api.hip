@@ -17,6 +17,30 @@ static int32_t check_rows(const ts_problem* p, const int32_t* q_indptr, int32_t 
   return TS_OK;
 }
 
+static int32_t attend(const ts_problem* p, const void* q, const int32_t* q_indptr, int32_t num_rows, int32_t window, float sm_scale, void* out, float* lse,
+                      void* ws, size_t ws_bytes, bool round_weights, void* stream) {
+  int32_t st = check_problem(p);
+  if (st != TS_OK) return st;
+  if ((st = check_rows(p, q_indptr, num_rows)) != TS_OK) return st;
+  if (window < 0 || !(fabsf(sm_scale) < INFINITY)) return TS_ERR_INVALID_ARG;
+  if (p->k_pool == nullptr || p->v_pool == nullptr) return TS_ERR_INVALID_ARG;
+  if (num_rows == 0) return TS_OK;
+  if (q == nullptr || out == nullptr) return TS_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(p->k_pool) || !aligned16(p->v_pool)) return TS_ERR_INVALID_ARG;
+  const size_t es = p->dtype == TS_BF16 ? 2 : 4, bytes = (size_t)num_rows * p->num_q_heads * p->head_dim * es;
+  if (overlap(q, bytes, out, bytes)) return TS_ERR_INVALID_ARG;
+  const size_t need = paged_attn_workspace(p->dtype, p->head_dim, p->num_q_heads / p->num_kv_heads, p->chunk);
+  if (ws == nullptr || ((uintptr_t)ws & 255) != 0 || ws_bytes < need) return TS_ERR_WORKSPACE;
+  PagedAttnArgs a{};
+  a.q = (const uint8_t*)q; a.k_pool = (const uint8_t*)p->k_pool; a.v_pool = (const uint8_t*)p->v_pool;
+  a.page_indptr = p->page_indptr; a.page_indices = p->page_indices; a.seq_lens = p->seq_lens; a.q_indptr = q_indptr;
+  a.out = (uint8_t*)out; a.lse = lse;
+  a.B = p->batch; a.C = p->chunk; a.T = num_rows; a.H = p->num_q_heads; a.H_kv = p->num_kv_heads;
+  a.P = p->page_size; a.p_shift = ilog2(p->page_size); a.max_seq_len = p->max_seq_len; a.window = window < p->max_seq_len ? window : 0;   // one that reaches every token is none
+  a.sm_scale = sm_scale; a.round_weights = round_weights ? 1 : 0;
+  return launch_paged_attn(p->dtype, p->head_dim, a, ws, (hipStream_t)stream) == hipSuccess ? TS_OK : TS_ERR_HIP;
+}
+
 extern "C" {
 
 int32_t ts_paged_attn_workspace_bytes(const ts_problem* p, int32_t num_rows, size_t* bytes) {
@@ -29,27 +53,12 @@ int32_t ts_paged_attn_workspace_bytes(const ts_problem* p, int32_t num_rows, siz
 
 int32_t ts_paged_attn(const ts_problem* p, const void* q, const int32_t* q_indptr, int32_t num_rows, int32_t window,
                       float sm_scale, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
-  int32_t st = check_problem(p);
-  if (st != TS_OK) return st;
-  if ((st = check_rows(p, q_indptr, num_rows)) != TS_OK) return st;
-  if (window < 0 || !(fabsf(sm_scale) < INFINITY)) return TS_ERR_INVALID_ARG;
-  if (p->k_pool == nullptr || p->v_pool == nullptr) return TS_ERR_INVALID_ARG;
-  if (num_rows == 0) return TS_OK;
-  if (q == nullptr || out == nullptr) return TS_ERR_INVALID_ARG;
-  if (!aligned16(q) || !aligned16(out) || !aligned16(p->k_pool) || !aligned16(p->v_pool)) return TS_ERR_INVALID_ARG;
-  const size_t es = p->dtype == TS_BF16 ? 2 : 4, bytes = (size_t)num_rows * p->num_q_heads * p->head_dim * es;
-  if (overlap(q, bytes, out, bytes)) return TS_ERR_INVALID_ARG;
-  size_t need = 0;
-  if ((st = ts_paged_attn_workspace_bytes(p, num_rows, &need)) != TS_OK) return st;
-  if (ws == nullptr || ((uintptr_t)ws & 255) != 0 || ws_bytes < need) return TS_ERR_WORKSPACE;
-  PagedAttnArgs a{};
-  a.q = (const uint8_t*)q; a.k_pool = (const uint8_t*)p->k_pool; a.v_pool = (const uint8_t*)p->v_pool;
-  a.page_indptr = p->page_indptr; a.page_indices = p->page_indices; a.seq_lens = p->seq_lens; a.q_indptr = q_indptr;
-  a.out = (uint8_t*)out; a.lse = lse;
-  a.B = p->batch; a.C = p->chunk; a.T = num_rows; a.H = p->num_q_heads; a.H_kv = p->num_kv_heads;
-  a.P = p->page_size; a.p_shift = ilog2(p->page_size); a.max_seq_len = p->max_seq_len; a.window = window < p->max_seq_len ? window : 0;   // one that reaches every token is none
-  a.sm_scale = sm_scale;
-  return launch_paged_attn(p->dtype, p->head_dim, a, ws, (hipStream_t)stream) == hipSuccess ? TS_OK : TS_ERR_HIP;
+  return attend(p, q, q_indptr, num_rows, window, sm_scale, out, lse, ws, ws_bytes, false, stream);
+}
+
+int32_t ts_paged_attn_rounded(const ts_problem* p, const void* q, const int32_t* q_indptr, int32_t num_rows, int32_t window,
+                              float sm_scale, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  return attend(p, q, q_indptr, num_rows, window, sm_scale, out, lse, ws, ws_bytes, true, stream);
 }
 
 int32_t ts_rope_append(const ts_problem* p, const ts_rope* r, const void* q, int64_t q_stride, const void* k, int64_t k_stride,

@@ -185,23 +185,24 @@ static size_t piece_bytes(int rows, int D) {
 }
 
 // The rows of a sequence and KV head, n * G, decide: up to 16 (one block of columns) or 32 by the stream kernel, which is bound by the memory (8 tokens times
-// 4 heads over 3000 keys, one sequence 17 us, 16 of them 46; by the tall kernel 27 and 58), bf16 up to 64 by two of its tiles (16 tokens over 2000 keys 18.6 us,
-// by the tall kernel 27.7, 8 times 4000 47 and 53; with 96 rows it would be 75 and 52); more by the tall one (bf16), or by the stream kernel with 64 rows a
-// tile (fp32, whose matrix products it is then bound by: 512 tokens over 4000 keys 362 us, with 32 rows 412).  A packed batch may hold both kinds:
-// two launches, each takes the sequences that are its.  As its bound says little about most of its sequences, twice as many rows go without the second (8 of
-// 1 to 30 tokens over up to 4000 keys 42 us, else 76).
+// 4 heads over 2000 keys, one sequence 17 us, eight of them 25; by the tall kernel 32 and 47), bf16 up to 128 by four of its tiles (32 tokens over 2000 keys 21 us,
+// by the tall kernel 33, 8 times 2000 keys 38 and 48, 8 times 8000 145 and 128; with 192 rows these are 28 and 34, 51 and 48, 224 and 135); more by the tall one (bf16), or by
+// the stream kernel with 64 rows a tile (fp32, whose matrix products it is then bound by: 512 tokens over 4000 keys 362 us, with 32 rows 412).  A packed batch may hold both kinds:
+// two launches, each takes the sequences that are its.  fp32: as a packed batch's bound says little about most of its sequences, twice as many rows go without the second.
+// Rounded weights, for which the tall kernel needs half the time: up to 64 rows by the stream kernel (16 tokens over 2000 keys 18.6 us, by the tall kernel 27.7, 8
+// times 4000 47 and 53; with 96 rows it would be 75 and 52), twice that in packed batches (8 of 1 to 30 tokens over up to 4000 keys 42 us, else 76).
 struct PagedPlan { int few_rows, many_rows; };   // rows of the tiles of sequences with few rows, and of those with more (0: there are none)
-static PagedPlan paged_plan(int dtype, int G, int chunk, bool packed) {
+static PagedPlan paged_plan(int dtype, int G, int chunk, bool packed, bool rounded) {
   const long rows = (long)chunk * G;
   if (rows <= 16) return PagedPlan{16, 0};
-  if (rows <= (dtype == TS_BF16 ? 64 : 32) * (packed ? 2 : 1)) return PagedPlan{32, 0};
+  if (rows <= (dtype == TS_F32 ? (packed ? 64 : 32) : rounded && !packed ? 64 : 128)) return PagedPlan{32, 0};
   return dtype == TS_BF16 ? PagedPlan{32, kTallRows} : PagedPlan{16, 64};
 }
 
 size_t paged_attn_workspace(int dtype, int D, int G, int chunk) {
   size_t most = 0;
-  for (const bool packed : {false, true}) {
-    const PagedPlan pl = paged_plan(dtype, G, chunk, packed);
+  for (int form = 0; form < 4; ++form) {
+    const PagedPlan pl = paged_plan(dtype, G, chunk, (form & 1) != 0, (form & 2) != 0);
     most = std::max(most, align_up(piece_bytes(pl.few_rows, D) + (pl.many_rows ? piece_bytes(pl.many_rows, D) : 0), 256));
   }
   return most;
@@ -209,7 +210,7 @@ size_t paged_attn_workspace(int dtype, int D, int G, int chunk) {
 
 hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws, hipStream_t s) {
   const int G = a.H / a.H_kv;
-  const PagedPlan pl = paged_plan(dtype, G, a.C, a.q_indptr != nullptr);
+  const PagedPlan pl = paged_plan(dtype, G, a.C, a.q_indptr != nullptr, a.round_weights != 0);
   uint8_t* at = (uint8_t*)ws;
   // tiles of every sequence (0: not as many), and bounds on all tiles and on the keys of one.  A tile of few rows beside large ones is its whole sequence.
   auto each_of = [&](int tpt, bool beside) -> int { return beside ? 1 : a.q_indptr != nullptr ? 0 : (a.C + tpt - 1) / tpt; };
@@ -250,8 +251,8 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
     return tiles < (1l << 23) && (keys <= 512 || ((tiles >= kShareWgs || beside) && keys <= 16 * (dtype == TS_F32 ? 64 : 128)));
   };
   if (!pl.many_rows) return run(pl.few_rows, 0, INT_MAX, few_whole(pl.few_rows, false));
-  // Short prompts have too few tiles for the chip: there 32 rows a tile for all sequences, at most two workgroups per CU.  (256 tokens 12.3 us, by 256 rows a
-  // tile 15.2, 512 tokens 19.3 and 20.8; 768, more tiles than that, 37 and 27.  fp32: 256 tokens 20.5, by 64 rows a tile 33, 400 39 and 48.)
+  // Short prompts have too few tiles for the chip: there 32 rows a tile for all sequences, at most two workgroups per CU.  (256 tokens 10.6 us, by 256 rows a
+  // tile 20.7, 512 tokens 17 and 29, with rounded weights 20.8; 768, more tiles than that, 33 and 38, rounded 27, and 4 of 256 25 and 22.  fp32: 256 tokens 20.5, by 64 rows a tile 33, 400 39 and 48.)
   // (fp32, whose larger tiles save less, also with more tiles of few keys: 16 sequences of 64 tokens 33 and 45, 4 of 256 60 and 60.)
   const long small = tiles_of(32 / G, false), small_keys = keys_of(32 / G);
   if (small_keys <= 1024 && (small <= 2 * kShareWgs || (dtype == TS_F32 && small * small_keys <= 1l << 18))) return run(32, 0, INT_MAX, true);
@@ -259,10 +260,12 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
     const hipError_t e = run(pl.few_rows, 0, pl.few_rows, few_whole(pl.few_rows, true));
     if (e != hipSuccess) return e;
   }
-  // (1024 tokens 33.4 us, in shares 35.7; but 2048 with a workgroup per tile 59 instead of 54.  A packed batch's bound counts
-  // up to a tile per sequence too many: there twice the tiles, 24 of 1 to 100 tokens 46 us, in shares 51; four times would cost 64 of 64 tokens over 900 119 instead of 98.)
+  // (4 prompts of 512 tokens 35 us, in shares 40, 8 of 256 24.6 and 30.4; but one of 1024 52 and 44, 2 of 512 over 500 keys more 54 and 49.  With rounded weights
+  // 1024 tokens take 33.4 us, in shares 35.7, 2048 59 and 54.  A packed batch's bound counts up to a tile per sequence too many: there twice the tiles, 24 of 1
+  // to 100 tokens 36 us, in shares 41, 8 of 1 to 600 68 and 75; four times would cost 64 of 64 tokens over 900 119 instead of 98 (rounded).)
   const long tiles = tiles_of(pl.many_rows / G, false);
-  return run(pl.many_rows, a.q_indptr != nullptr ? pl.few_rows : 0, INT_MAX, tiles <= kShareWgs * (a.q_indptr != nullptr ? 2 : 1) && keys_of(pl.many_rows / G) <= 1024);
+  return run(pl.many_rows, a.q_indptr != nullptr ? pl.few_rows : 0, INT_MAX,
+             tiles <= kShareWgs * (a.q_indptr != nullptr ? 2 : 1) && keys_of(pl.many_rows / G) <= (a.round_weights ? 1024 : 768));
 }
 
 }  // namespace ts

@@ -5,20 +5,23 @@
 // straight-line code a wave forms the weights of one block of 32 keys on the vector ALU while the matrix cores form the
 // scores of the next and add the output of the last one:
 //   * A wave issues in order, so the vector instructions are shared out behind every single product (two of those in a row make
-//     what follows wait until the first has left the matrix cores).  Four of them fit a product: fma, exp, the weight's sum
+//     what follows wait until the first has left the matrix cores).  Four of them fit a product of 32 cycles with room: fma, exp, the weight's sum
 //     and half a conversion.
 //   * The softmax's reference is not a running maximum.  In tiles with masks, the first one among them, it is raised, with what has
-//     been added up so far, when a packed weight has a bit that only numbers of 2 and more have, which the first visible key of
+//     been added up so far, when a weight of 2 or more shows up, which the first visible key of
 //     a row does.  Tiles that every row sees in full take a copy of the code without masks and without that: weights may grow to 2^64
 //     there, which costs no precision.  Should they grow further (logits 44 above all of the first tile's), or the reference be
 //     so large that logits have to be rounded first, the workgroup does the piece again with the former code throughout.  (With the
 //     code for raising in the loop the compiler moves accumulators about: 1000 instructions a tile instead of 560.)
-// Weights are rounded to bf16 for the product with V (half a step, 2^-8); their sum is of the floats before that rounding, so that the log-sum-exp
-// keeps 24 bits.
+// Weights keep their 24 bits: V is multiplied with each of the three bf16 numbers that a weight is the sum of, and nothing is rounded before the result is; four
+// units of matrix work instead of two.  The caller may choose weights rounded to bf16 (half a step, 2^-8 of each; the relative error of results against 64 bits
+// is then 1.8e-3 instead of 1.7e-3, which is the results' own rounding); their sum is of the floats before that rounding, so that the log-sum-exp keeps 24 bits.
 //
-// Measured (H 32/8, D 128): a prompt of 8192 tokens 470 to 505 us from card to card, 512 tokens over 131072 keys 904 to 966, up to 1.17 and 1.22 PFLOP/s; a bf16 product of 8192^3 by the library
-// reaches 1.22 on the same card.  64 keys take 3350 cycles, of which the matrix cores work 2048 and 2500 go to issuing, and the clock falls to 1.8 to 2.0 GHz meanwhile (2.4 with
-// little work): power is the bound.  A tile's start and end cost 13000 cycles (page ids and queries 2100, the first tile and its scores 3700, the first block's weights
+// Measured (H 32/8, D 128): a prompt of 8192 tokens 861 us, 512 tokens over 131072 keys 1705, 1.28 and 1.29 PFLOP/s of products with the three parts counted; a bf16
+// product of 8192^3 by the library reaches 1.22 on the same card.  D 64, 8192 tokens: 523.  Power is the bound.
+// Rounded weights: 470 to 505 us from card to card, 904 to 966, up to 1.17 and 1.22 PFLOP/s; D 64 298.
+// 64 keys take 3350 cycles, of which the matrix cores work 2048 and 2500 go to issuing, and the clock falls to 1.8 to 2.0 GHz meanwhile (2.4 with
+// little work).  A tile's start and end cost 13000 cycles (page ids and queries 2100, the first tile and its scores 3700, the first block's weights
 // 2200, results 4400): what short prompts are bound by.  D 64: 2150 cycles where the matrix cores work 1024; exponentials, sums and
 // conversions are as many as for D 128, so the vector ALU is the bound.
 #include "paged_shares.h"
@@ -47,7 +50,7 @@ template <int D> __device__ __forceinline__ int pt_swz(int key) {
   return D == 128 ? (((key & 3) << 2) | ((key >> 2) & 3)) : ((((key >> 1) & 1) << 2) | (((key >> 2) & 1) << 1) | ((key >> 3) & 1));
 }
 
-template <int D>
+template <int D, bool FULL>                   // FULL: weights of 24 bits, else rounded to bf16
 __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, ShareArgs sh) {
   constexpr int KS = D / 16;                  // k-steps of Q K^T
   constexpr int NBO = D / 32;                 // 32-row blocks of the transposed output
@@ -210,16 +213,40 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
     // ---- blocks of 32 keys, two to a tile.  While the vector ALU forms the weights of block j, the matrix cores form the scores of
     // block j + 1 and add the output of block j - 1.
     f32x16_t s[2][2];                                              // [block parity][row block] S^T: key 8 * (e / 4) + 4 * half + e % 4
-    uint32_t pk[2][2][8];                                          // the weights, rounded to bf16
+    uint32_t pk[FULL ? 3 : 2][2][8];                               // [part][row block] the last block's weights; rounded ones [block parity][row block]
     auto round_logits = [&](f32x16_t (&x)[2]) __attribute__((always_inline)) {
 #pragma unroll
       for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
         for (int e = 0; e < 16; ++e) x[rb][e] *= c2;
     };
+    // Raises the rows' references above the logits x of a block, with what has been added up so far
+    auto raise = [&](f32x16_t (&x)[2]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb) {
+        float m = ref[rb];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) m = fmaxf(m, factor * x[rb][e] + kPtHead);
+        m = fmaxf(m, __shfl_xor(m, 32));                         // both halves of a row raise its reference together
+        const float f = __builtin_amdgcn_exp2f(ref[rb] - m);     // 1 where nothing changes, 0 while the reference is unset
+        lsum[rb] *= f;
+#pragma unroll
+        for (int nb = 0; nb < NBO; ++nb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) oacc[rb][nb][e] *= f;
+        ref[rb] = m;
+      }
+      const bool big = (fabsf(ref[0]) > kPtBig && ref[0] != kPtUnset) || (fabsf(ref[1]) > kPtBig && ref[1] != kPtUnset);
+      if (__builtin_expect(f1 != INT_MIN && __builtin_amdgcn_ballot_w64(big) != 0, 0)) {
+        // An fma's exact product is off by up to 2^-24 of the logit from the rounded one that the reference came from, and with logits of 2^31 that
+        // alone would over- or underflow the exponential: from here on the logits are rounded first.
+        factor = 1.f; f1 = INT_MIN;
+        round_logits(x);                                         // (later blocks round their own)
+      }
+    };
     constexpr int AHEAD = 3;
     bf16x8_t carry[AHEAD];
-    auto body = [&](auto half_c, int it, uint32_t k_at, uint32_t v_at, auto with_scores, auto with_output, auto with_loads, auto masked_c) __attribute__((always_inline)) {
+    auto body_rounded = [&](auto half_c, int it, uint32_t k_at, uint32_t v_at, auto with_scores, auto with_output, auto with_loads, auto masked_c) __attribute__((always_inline)) {
       constexpr int CUR = decltype(half_c)::value, NXT = 1 - CUR;  // this block is half CUR of tile `it`
       constexpr bool SC = decltype(with_scores)::value, OUT = decltype(with_output)::value, LD = decltype(with_loads)::value;
       constexpr bool MASKED = decltype(masked_c)::value;
@@ -310,27 +337,7 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
       if (MASKED && __builtin_amdgcn_ballot_w64((any & kPtTwo) != 0u) != 0) {
         // first visible key of a row, or a logit far above the reference.  Straight-line code: a branch per lane here
         // makes the compiler copy the accumulators on the common path too.
-#pragma unroll
-        for (int rb = 0; rb < 2; ++rb) {
-          float m = ref[rb];
-#pragma unroll
-          for (int e = 0; e < 16; ++e) m = fmaxf(m, factor * x[rb][e] + kPtHead);
-          m = fmaxf(m, __shfl_xor(m, 32));                         // both halves of a row raise its reference together
-          const float f = __builtin_amdgcn_exp2f(ref[rb] - m);     // 1 where nothing changes, 0 while the reference is unset
-          lsum[rb] *= f;
-#pragma unroll
-          for (int nb = 0; nb < NBO; ++nb)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) oacc[rb][nb][e] *= f;
-          ref[rb] = m;
-        }
-        const bool big = (fabsf(ref[0]) > kPtBig && ref[0] != kPtUnset) || (fabsf(ref[1]) > kPtBig && ref[1] != kPtUnset);
-        if (__builtin_expect(f1 != INT_MIN && __builtin_amdgcn_ballot_w64(big) != 0, 0)) {
-          // An fma's exact product is off by up to 2^-24 of the logit from the rounded one that the reference came from, and with logits of 2^31 that
-          // alone would over- or underflow the exponential: from here on the logits are rounded first.
-          factor = 1.f; f1 = INT_MIN;
-          round_logits(x);                                         // (later blocks round their own)
-        }
+        raise(x);
 #pragma unroll
         for (int rb = 0; rb < 2; ++rb) sum[rb][0] = sum[rb][1] = 0.f;
 #pragma unroll
@@ -339,6 +346,162 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
       lsum[0] += sum[0][0] + sum[0][1];
       lsum[1] += sum[1][0] + sum[1][1];
     };
+    // The same with weights of 24 bits, each the sum of three bf16 numbers that V is multiplied with.  The output takes three of four products then, and the order
+    // changes: first the output of block j - 1 while the weights of block j are formed in the place of its scores, then the scores of block
+    // j + 1; the weights of a k-step are split once the former block's weights of that k-step have been multiplied.  With masks the reference is raised
+    // before the weights are formed, when both the output of block j - 1 and the block's largest logit are there.
+    auto body_full = [&](auto half_c, int it, uint32_t k_at, uint32_t v_at, auto with_scores, auto with_output, auto with_loads, auto masked_c) __attribute__((always_inline)) {
+      constexpr int CUR = decltype(half_c)::value, NXT = 1 - CUR;
+      constexpr bool SC = decltype(with_scores)::value, OUT = decltype(with_output)::value, LD = decltype(with_loads)::value;
+      constexpr bool MASKED = decltype(masked_c)::value;
+      f32x16_t (&x)[2] = s[CUR];
+      const int j0 = key0 + it * kPtTile + CUR * 32 + 4 * half;
+      const uint32_t kt = ka0 + k_at + (uint32_t)(NXT * 32 * RB), vt = va0 + v_at + (uint32_t)(TILE_B + NXT * 32 * RB);
+      constexpr int VS = 2 * NBO, NS = VS + KS, G0 = OUT ? 0 : VS, G1 = SC ? NS : VS;   // steps: output (six products each), then scores (two)
+      constexpr bool CIN = CUR == 0 && OUT;
+      bf16x8_t frag[NS];
+      auto read_v = [&](uint32_t at, int g) __attribute__((always_inline)) -> bf16x8_t {
+        const int k2 = g / NBO, nb = g % NBO;
+        s16x4_t v[2];
+#pragma unroll
+        for (int h8 = 0; h8 < 2; ++h8)
+          v[h8] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((at ^ (uint32_t)(nb * 64 + h8 * VH)) + (uint32_t)((k2 * 16 + h8 * 8) * RB)));
+        const uint2 v0 = __builtin_bit_cast(uint2, v[0]), v1 = __builtin_bit_cast(uint2, v[1]);
+        return __builtin_bit_cast(bf16x8_t, make_uint4(v0.x, v0.y, v1.x, v1.y));
+      };
+      auto fetch = [&](int g) __attribute__((always_inline)) {
+        if (g < VS) frag[g] = read_v(vt, g);
+        else frag[g] = *(lds_bf16x8*)(kt ^ (uint32_t)((g - VS) * 32));
+      };
+      auto ahead = [&](int g) __attribute__((always_inline)) {
+        if (g >= G0 && g + AHEAD < G1) fetch(g + AHEAD);
+        if (CUR == 1 && SC && g + AHEAD >= NS) carry[g + AHEAD - NS] = read_v(va0 + p0 + (uint32_t)(TILE_B + 32 * RB), g + AHEAD - NS);   // of V tile it, second half
+      };
+      auto loads = [&](int g) __attribute__((always_inline)) {
+        if (LD && g < NLD) {                                       // rows of K tile it + 3 and V tile it + 2
+          load_row(k_head, at_k[g < NLD ? g : 0], g, p0);
+          load_row(v_head, at_v[g < NLD ? g : 0], g, p2 + TILE_B);
+        }
+        if (LD && g == NLD) { pages_of(it + 4); fetch_look(it + 6); }
+        if (CUR == 0 && OUT && g == 2) rows_at(it + 3);
+      };
+      // pair q of the 16 pairs of weights, those of k-step 0 first: elements 2 i and 2 i + 1 of row block rb
+      float sum[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
+      auto rb_of = [](int q) { return (q >> 2) & 1; };
+      auto i_of = [](int q) { return (q & 3) + 4 * (q >> 3); };
+      auto exponent = [&](int q) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) { float e = x[rb_of(q)][2 * i_of(q) + u]; x[rb_of(q)][2 * i_of(q) + u] = fmaf(factor, e, -ref[rb_of(q)]); }
+      };
+      auto power = [&](int q) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) x[rb_of(q)][2 * i_of(q) + u] = __builtin_amdgcn_exp2f(x[rb_of(q)][2 * i_of(q) + u]);
+      };
+      auto add = [&](int q) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) sum[rb_of(q)][u] += x[rb_of(q)][2 * i_of(q) + u];
+      };
+      // Parts are cut off, not rounded; the third holds the last 8 bits.  With masks the lower two are kept above 2^-30 of the weight, so that an infinite V row
+      // comes out infinite (0 * inf would be NaN); without, a result that is not finite has the piece done again.
+      auto split = [&](int q) __attribute__((always_inline)) {
+        float y0 = x[rb_of(q)][2 * i_of(q)], y1 = x[rb_of(q)][2 * i_of(q) + 1];
+        const float l0 = y0 * 9.3132257e-10f, l1 = y1 * 9.3132257e-10f;
+#pragma unroll
+        for (int c = 0; c < 3; ++c) {
+          pk[c][rb_of(q)][i_of(q)] = __builtin_amdgcn_perm(__float_as_uint(y1), __float_as_uint(y0), 0x07060302u);   // the high halves
+          if (c < 2) {
+            y0 -= __uint_as_float(__float_as_uint(y0) & 0xffff0000u);                    // (exact)
+            y1 -= __uint_as_float(__float_as_uint(y1) & 0xffff0000u);
+            if (MASKED) { y0 = fmaxf(y0, l0); y1 = fmaxf(y1, l1); }
+          }
+        }
+      };
+      auto output = [&](int g, int c, int rb) __attribute__((always_inline)) {
+        if (!OUT) return;
+        const int k2 = g / NBO, nb = g % NBO;
+        const uint32_t (&pw)[8] = pk[c][rb];
+        oacc[rb][nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[g], __builtin_bit_cast(bf16x8_t, make_uint4(pw[4 * k2], pw[4 * k2 + 1], pw[4 * k2 + 2], pw[4 * k2 + 3])),
+                                                               oacc[rb][nb], 0, 0, 0);
+      };
+      auto score = [&](int t, int rb) __attribute__((always_inline)) {
+        if (SC) s[NXT][rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[VS + t], qfrag[rb][t], t == 0 ? (f32x16_t){} : s[NXT][rb], 0, 0, 0);
+      };
+#pragma unroll
+      for (int g = G0; g < G1 && g < G0 + AHEAD; ++g) { if (CIN) frag[g] = carry[g - G0]; else fetch(g); }
+      constexpr int FORM = 16 / VS, SPLIT = 8 / NBO, LATE = 8 / KS;   // pairs formed per output step, split per output step of k-step 1, split per score step
+      if constexpr (MASKED) {
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const uint32_t key = (uint32_t)(j0 + 8 * (e >> 2) + (e & 3)) - low[rb];
+            x[rb][e] = key < reach ? x[rb][e] : hidden;
+          }
+        if (__builtin_expect(f1 == INT_MIN, 0)) round_logits(x);
+#pragma unroll
+        for (int g = 0; g < VS; ++g) {
+          ahead(g);
+          loads(g);
+#pragma unroll
+          for (int c = 0; c < 3; ++c) { output(g, c, 0); output(g, c, 1); }
+        }
+        float most[2] = {-INFINITY, -INFINITY};                    // exponents
+#pragma unroll
+        for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) most[rb] = fmaxf(most[rb], fmaf(factor, x[rb][e], -ref[rb]));
+        if (__builtin_amdgcn_ballot_w64(fmaxf(most[0], most[1]) >= 1.f) != 0) raise(x);
+#pragma unroll
+        for (int q = 0; q < 16; ++q) { exponent(q); power(q); add(q); }
+#pragma unroll
+        for (int t = 0; t < KS; ++t) { ahead(VS + t); score(t, 0); score(t, 1); }
+#pragma unroll
+        for (int q = 0; q < 16; ++q) split(q);
+      } else {
+#pragma unroll
+        for (int g = 0; g < VS; ++g) {
+#pragma unroll
+          for (int p = 0; p < 6; ++p) {
+            output(g, p >> 1, p & 1);
+            __builtin_amdgcn_sched_barrier(0);
+            if (p == 0) {
+              ahead(g);
+#pragma unroll
+              for (int q = g * FORM; q < (g + 1) * FORM; ++q) exponent(q);
+            }
+            if (p == 3) loads(g);
+            if (p >= 1 && p <= 4) {
+#pragma unroll
+              for (int k = (p - 1) * FORM / 4; k < p * FORM / 4; ++k) power(g * FORM + k);
+              if (g >= NBO) {
+#pragma unroll
+                for (int k = (p - 1) * SPLIT / 4; k < p * SPLIT / 4; ++k) split((g - NBO) * SPLIT + k);
+              }
+            }
+            if (p == 5) {
+#pragma unroll
+              for (int q = g * FORM; q < (g + 1) * FORM; ++q) add(q);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < KS; ++t) {
+          score(t, 0);
+          __builtin_amdgcn_sched_barrier(0);
+          ahead(VS + t);
+#pragma unroll
+          for (int q = 8 + t * LATE; q < 8 + (t + 1) * LATE; ++q) split(q);
+          __builtin_amdgcn_sched_barrier(0);
+          score(t, 1);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        bad = bad || !(fmaxf(sum[0][0] + sum[0][1], sum[1][0] + sum[1][1]) <= kPtMost);
+      }
+      lsum[0] += sum[0][0] + sum[0][1];
+      lsum[1] += sum[1][0] + sum[1][1];
+    };
+    auto body = [&](auto... args) __attribute__((always_inline)) { if constexpr (FULL) body_full(args...); else body_rounded(args...); };
     // Buffers: the barrier between the blocks of tile `it` says that K tile it + 1 and V tile `it` have arrived (and the page ids of tile
     // it + 4) and that K tile `it` and V tile it - 1 have been read, whose places K tile it + 3 and V tile it + 2 then take.  What tile it - 1
     // requested -- K tile it + 2, V tile it + 1, page ids -- stays in flight.
@@ -419,12 +582,24 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
         const uint2 v0 = __builtin_bit_cast(uint2, v[0]), v1 = __builtin_bit_cast(uint2, v[1]);
         const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, make_uint4(v0.x, v0.y, v1.x, v1.y));
 #pragma unroll
-        for (int rb = 0; rb < 2; ++rb) {
-          const uint32_t (&pw)[8] = pk[1][rb];
-          oacc[rb][nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8_t, make_uint4(pw[4 * k2], pw[4 * k2 + 1], pw[4 * k2 + 2], pw[4 * k2 + 3])),
-                                                                 oacc[rb][nb], 0, 0, 0);
-        }
+        for (int c = FULL ? 0 : 1; c < (FULL ? 3 : 2); ++c)
+#pragma unroll
+          for (int rb = 0; rb < 2; ++rb) {
+            const uint32_t (&pw)[8] = pk[c][rb];
+            oacc[rb][nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8_t, make_uint4(pw[4 * k2], pw[4 * k2 + 1], pw[4 * k2 + 2], pw[4 * k2 + 3])),
+                                                                   oacc[rb][nb], 0, 0, 0);
+          }
       }
+    if (FULL && !again) {                                          // an infinite V row times a part that is 0
+      float x = 0.f;
+#pragma unroll
+      for (int rb = 0; rb < 2; ++rb)
+#pragma unroll
+        for (int nb = 0; nb < NBO; ++nb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x = fmaf(oacc[rb][nb][e], 0.f, x);
+      bad = bad || !(x == 0.f);
+    }
     if (__builtin_amdgcn_ballot_w64(bad) != 0) *s_bad = 1;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // tiles past the end that were requested: their places are used below
     __syncthreads();
@@ -481,19 +656,20 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
   });
 }
 
-template <int D>
+template <int D, bool FULL>
 static hipError_t tall_one(const PagedAttnArgs& a, const ShareArgs& sh, hipStream_t s) {
   constexpr int lds = 2 * kPtBuf * kPtTile * D * 2 + 4 * kPtRing * 256 + sizeof(ShareScratch) + 16;
   if (lds > 65536) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_tall_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_tall_kernel<D, FULL>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(paged_tall_kernel<D>, dim3(sh.wgs), dim3(256), lds, s, a, sh);
+  hipLaunchKernelGGL((paged_tall_kernel<D, FULL>), dim3(sh.wgs), dim3(256), lds, s, a, sh);
   return hipGetLastError();
 }
 
 hipError_t launch_paged_tall(int D, const PagedAttnArgs& a, const ShareArgs& sh, hipStream_t s) {
-  return D == 64 ? tall_one<64>(a, sh, s) : tall_one<128>(a, sh, s);
+  if (a.round_weights) return D == 64 ? tall_one<64, false>(a, sh, s) : tall_one<128, false>(a, sh, s);
+  return D == 64 ? tall_one<64, true>(a, sh, s) : tall_one<128, true>(a, sh, s);
 }
 
 }  // namespace ts

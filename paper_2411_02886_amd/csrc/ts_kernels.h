@@ -222,6 +222,7 @@ struct PagedAttnArgs {
   uint8_t* out;                // [T][H][D]
   float* lse;                  // [T][H] or null
   int B, C, T, H, H_kv, P, p_shift, max_seq_len, window;
+  int round_weights;           // bf16, many rows: the weights that multiply V may be rounded to bf16
   float sm_scale;
 };
 size_t paged_attn_workspace(int dtype, int D, int G, int chunk);

@@ -40,9 +40,10 @@ class _NewTokens:
         alone: k and v, or q and q_out, None)."""
         ts.ts_rope_append(self.problem, rope, q, k, v, q_indptr, (q if k is None else k).shape[0], positions, q_out)
 
-    def attend_all(self, q, sm_scale=None, window=0, q_indptr=None, out=None, lse=None):
+    def attend_all(self, q, sm_scale=None, window=0, q_indptr=None, out=None, lse=None, round_weights=False):
         """Attention of the new tokens over their whole sequence: no selection.  Without q_indptr q is the step's or chunk's
-        query and the result is in self.out / self.lse; packed rows bring their own `out` (and `lse`)."""
+        query and the result is in self.out / self.lse; packed rows bring their own `out` (and `lse`).
+        round_weights: bf16 prompts in half the time, their weights rounded to bf16 (ts_paged_attn_rounded)."""
         sm = sm_scale if sm_scale is not None else 1.0 / float(np.sqrt(self.D))
         rows = self.B * self.problem.c.chunk if q_indptr is None else q.shape[0]
         if q_indptr is None:
@@ -50,7 +51,8 @@ class _NewTokens:
         nbytes = ts.ts_paged_attn_workspace_bytes(self.problem, rows)
         if getattr(self, "_all_ws", None) is None or self._all_ws.numel() * 4 < nbytes:
             self._all_ws = torch.empty((nbytes + 255) // 256 * 64, dtype=torch.int32, device=self.k_pool.device)
-        ts.ts_paged_attn(self.problem, q, q_indptr, rows, window, sm, out, lse, self._all_ws)
+        attend = ts.ts_paged_attn_rounded if round_weights else ts.ts_paged_attn
+        attend(self.problem, q, q_indptr, rows, window, sm, out, lse, self._all_ws)
 
 
 class DecodeLayer(_NewTokens):
