@@ -10,8 +10,8 @@
 //   * The softmax's reference is not a running maximum.  In tiles with masks, the first one among them, it is raised, with what has
 //     been added up so far, when a weight of 2 or more shows up, which the first visible key of
 //     a row does.  Tiles that every row sees in full take a copy of the code without masks and without that: weights may grow to 2^64
-//     there, which costs no precision.  Should they grow further (logits 44 above all of the first tile's), or the reference be
-//     so large that logits have to be rounded first, the workgroup does the piece again with the former code throughout.  (With the
+//     there, which costs no precision.  Should they grow further (logits 44 above all of the first tile's), the output not be finite (values of V beyond 2^64 may
+//     overflow with such weights), or the reference be so large that logits have to be rounded first, the workgroup does the piece again with the former code throughout.  (With the
 //     code for raising in the loop the compiler moves accumulators about: 1000 instructions a tile instead of 560.)
 // Weights keep their 24 bits: V is multiplied with each of the three bf16 numbers that a weight is the sum of, and nothing is rounded before the result is; four
 // units of matrix work instead of two.  The caller may choose weights rounded to bf16 (half a step, 2^-8 of each; the relative error of results against 64 bits
@@ -590,7 +590,7 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
                                                                    oacc[rb][nb], 0, 0, 0);
           }
       }
-    if (FULL && !again) {                                          // an infinite V row times a part that is 0
+    if (!again) {                                                  // large values of V times large weights, or an infinite one times a part that is 0
       float x = 0.f;
 #pragma unroll
       for (int rb = 0; rb < 2; ++rb)

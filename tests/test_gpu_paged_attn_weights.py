@@ -156,3 +156,25 @@ def test_attend_all_takes_the_choice(gpu, rounded):
     torch.cuda.synchronize()
     out, lse = W.as_f32(to_host(sel.out, bits16=True), BF).astype(np.float64).reshape(C, 8, 64), to_host(sel.lse).astype(np.float64).reshape(C, 8)
     check_attention(out, lse, attention(c, q, [C], 0, 0.125, [rounded]), rounded)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 300])
+@pytest.mark.parametrize("D", [64, 128])
+def test_large_values_beside_rising_logits_stay_finite(gpu, dtype, n, D):
+    """Logits rise by 40 along the sequence, values are around 2^100: a weight of 2^50 times one of them is no float, the result is.  (300 tokens
+    times 32 heads: large tiles, a workgroup's each.)"""
+    N, H, H_kv = 700, 32, 8
+    c = Cache(dtype, H_kv, D, 16, [N, N - 50], seed=1)
+    for b in range(2):
+        at = c.slots(b)
+        k = 0.1 * c.k[at] + (40.0 * np.arange(len(at)) / N * math.sqrt(D) / D)[:, None, None]
+        c.k_bits[at] = W.store(k.astype(np.float32), dtype)
+        c.v_bits[at] = W.store((2.0 ** 100 * c.v[at]).astype(np.float32), dtype)
+        c.k[at], c.v[at] = W.as_f32(c.k_bits[at], dtype), W.as_f32(c.v_bits[at], dtype)
+    q = W.store((1 + 0.1 * np.random.default_rng(5).standard_normal((2 * n, H, D))).astype(np.float32), dtype)
+    for rounded in (False, True):
+        for bound in (None, LOOSE):
+            out, lse, _, scale = call(gpu, c, H, [n, n], rounded=rounded, packed=False, bound=bound, q=q)
+            assert np.isfinite(out).all(), (rounded, bound)
+            check_attention(out, lse, attention(c, q, [n, n], 0, scale, [rounded and dtype == BF and n * 4 > 32] * 2), (rounded, bound))
