@@ -325,7 +325,7 @@ int32_t ts_chunk_mean_query(const ts_problem* p, const void* q, void* q_mean, vo
 /* Attention of the new tokens over their whole sequence (dense: no selection, no index list), both dtypes:
  *   out[r][h][:] = sum_t softmax_t( <q[r][h], K[slot(b, t)][h/G]> * sm_scale ) * V[slot(b, t)][h/G]
  * for new token c = r - q_indptr[b] at place x = N_b - n_b + c over t in [max(0, x - window + 1), x]; window 0 = from 0 on (every
- * cached token and the chunk's own up to x).  Weights and sums in float, out rounded to p->dtype.
+ * cached token and the chunk's own up to x).  A length beyond max_seq_len counts as max_seq_len here, N_b and x alike.  Weights and sums in float, out rounded to p->dtype.
  * Pages that no new token sees (wholly in front of the first one's window, behind N_b) are not read.  A token that some of a sequence's rows see
  * and others do not takes part in the latter with weight 0: its K may be anything, its V has to be finite.
  * q, out [device] [num_rows][H][D], 16-byte aligned, not overlapping; lse [device] float [num_rows][H] or NULL.
@@ -363,7 +363,7 @@ typedef struct ts_rope {
  * apart (0 = packed; a multiple of 16 bytes, at least a row: parts of a fused projection's output).  q and q_out
  * may be NULL together (append only), k and v too (turn only).  q_out may be q itself if q is packed; any other overlap is an error
  * where the library can see it.  r NULL: nothing is turned.  positions [device] int32 [num_axes][num_rows], or NULL: on every
- * axis a token's place N_b - n_b + c.  Rows that belong to no sequence, and rows whose place is negative or beyond max_seq_len, write nothing into the pages, and
+ * axis a token's place N_b - n_b + c (of the true N_b, beyond max_seq_len too).  Rows that belong to no sequence, and rows whose place is negative or beyond max_seq_len, write nothing into the pages, and
  * the former no q_out either.  Two sequences that share the page of a new token overwrite each other: give the second a page of its own first. */
 int32_t ts_rope_append(const ts_problem* p, const ts_rope* r, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
                        const void* v, int64_t v_stride, const int32_t* q_indptr, int32_t num_rows, const int32_t* positions,

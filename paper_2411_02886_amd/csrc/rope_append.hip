@@ -103,8 +103,8 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeAppendArgs a) {
 
   const RowPlace at = row_place(a.q_indptr, a.B, a.C, a.T, row);
   if (at.b < 0) return;
-  const int n = min(max(a.seq_lens[at.b], 0), a.max_seq_len), place = n - at.left, page0 = a.page_indptr[at.b];
-  const bool append = nk != 0 && place >= 0;
+  const int place = max(a.seq_lens[at.b], 0) - at.left, page0 = a.page_indptr[at.b];
+  const bool append = nk != 0 && place >= 0 && place < a.max_seq_len;  // (a step whose lengths have grown past the bound must not write over cached tokens)
   int64_t slot = 0;
   if (append) slot = ((int64_t)a.page_indices[page0 + (place >> a.p_shift)] << a.p_shift) + (place & (a.P - 1));
   float* s_cos = s_turn[wave][0];
