@@ -385,6 +385,8 @@ def _row_stride(t, row: int, name: str) -> int:
     if len(shape) > 1 and t.is_contiguous() and t.numel() == shape[0] * row:      # the usual case, and the quickest answer
         return 0
     strides, want = t.stride(), 1
+    if len(shape) > 1 and shape[0] > 1 and strides[0] < row:                      # (0 would mean packed)
+        raise ValueError("%s: rows that overlap, such as one that is expanded" % name)
     if len(shape) == 2 and shape[1] == row and strides[1] == 1:
         return strides[0] if shape[0] > 1 else 0
     for i in range(len(shape) - 1, 0, -1):
