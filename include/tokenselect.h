@@ -378,7 +378,8 @@ int32_t ts_pages_copy(const ts_problem* p, const int32_t* src, const int32_t* ds
  * [hi_b, N_b) (lo_b, hi_b of ts_problem) are copied in that order, one after the other, into the pages to_indices[to_indptr[b] ..
  * to_indptr[b+1] - 1]; to_lens[b] = their number, or what the pages hold if that is less (the rest is dropped).  The pages of a table row are not read
  * behind that number.  idx [device] int32 [B][idx_stride], count [device] int32 [B] as ts_topk leaves them (read as defensively as by
- * ts_sparse_paged_attn); to_* [device]; skip[b] != 0 leaves a sequence alone, to_lens[b] too.  The new pages must not
+ * ts_sparse_paged_attn); to_* [device]; to_lens may not be seq_lens nor overlap another array of the call (an error where the library sees its size: copy the
+ * new lengths over afterwards); skip[b] != 0 leaves a sequence alone, to_lens[b] too.  The new pages must not
  * be pages that the call reads (of any sequence), nor belong to two sequences.  Keys keep the positions that they were turned by.  chunk must be 1. */
 int32_t ts_cache_compact(const ts_problem* p, const int32_t* idx, int32_t idx_stride, const int32_t* count, const uint8_t* skip,
                          const int32_t* to_indptr, const int32_t* to_indices, int32_t* to_lens, void* stream);

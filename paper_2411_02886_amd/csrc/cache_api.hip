@@ -134,6 +134,11 @@ int32_t ts_cache_compact(const ts_problem* p, const int32_t* idx, int32_t idx_st
     return TS_ERR_INVALID_ARG;
   if (p->k_pool == nullptr || p->v_pool == nullptr || !aligned16(p->k_pool) || !aligned16(p->v_pool)) return TS_ERR_INVALID_ARG;
   if (p->chunk != 1) return TS_ERR_UNSUPPORTED;
+  // a sequence's first workgroup writes its new length while others still read the rest
+  const size_t B = (size_t)p->batch, lens = B * 4;
+  if (overlap(to_lens, lens, p->seq_lens, lens) || overlap(to_lens, lens, count, lens) || overlap(to_lens, lens, idx, B * (size_t)idx_stride * 4) ||
+      overlap(to_lens, lens, p->page_indptr, lens + 4) || overlap(to_lens, lens, to_indptr, lens + 4) || (skip != nullptr && overlap(to_lens, lens, skip, B)))
+    return TS_ERR_INVALID_ARG;
   CompactArgs a{};
   a.k_pool = (uint8_t*)const_cast<void*>(p->k_pool); a.v_pool = (uint8_t*)const_cast<void*>(p->v_pool);
   a.page_indptr = p->page_indptr; a.page_indices = p->page_indices; a.seq_lens = p->seq_lens;

@@ -174,7 +174,7 @@ class DecodeLayer(_NewTokens):
 
     def compact(self, to_indptr, to_indices, to_lens, skip=None):
         """Copies what attend() reads of every sequence (initial block, selection, recent block) densely into other pages;
-        to_lens gets the new lengths.  Attending all of the new pages then gives what attend() gives."""
+        to_lens gets the new lengths (not self.seq_lens: copy them there afterwards).  Attending all of the new pages then gives what attend() gives."""
         ts.ts_cache_compact(self.problem, self.idx, self.k, self.count, skip, to_indptr, to_indices, to_lens)
 
     def compact_form_pays(self) -> bool:

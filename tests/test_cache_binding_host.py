@@ -25,3 +25,16 @@ def test_rows_that_overlap_are_refused(what):
             a[what] = bad
             with pytest.raises(ValueError):
                 ts.ts_rope_append(problem(), None, a["q"], a["k"], a["v"], ind, 3, None, torch.zeros(3, 4, 64))
+
+
+def test_compact_refuses_new_lengths_in_the_place_of_what_it_reads():
+    """The old lengths are read by many workgroups while one writes the new ones."""
+    import ctypes
+
+    from paper_2411_02886_amd.binding import _CProblem
+    at = dict(k_pool=0x100000, v_pool=0x200000, page_indptr=0x300000, page_indices=0x400000, seq_lens=0x500000)
+    p = _CProblem(batch=6, chunk=1, num_q_heads=8, num_kv_heads=2, head_dim=64, page_size=16, max_seq_len=4096, dtype=ts.TS_BF16, num_initial=0,
+                  num_local=0, **at)
+    idx, count, skip, to_indptr, to = 0x600000, 0x700000, 0x800000, 0x900000, 0xa00000
+    for lens in (0x500000, 0x500000 + 20, 0x500000 - 20, count, count + 4, idx, idx + 6 * 4 * 4 - 4, 0x300000 + 24, to_indptr + 24, to_indptr - 4, skip + 4):
+        assert ts.load().ts_cache_compact(ctypes.byref(p), idx, 4, count, skip, to_indptr, to, lens, None) == -1, hex(lens)
