@@ -1,13 +1,30 @@
 """Which pages of a paged KV pool belong to which sequence: taking, sharing, copying on write, moving together and giving back.
 
 The table lives on the host, where a server decides what runs next; the pages' contents are moved by ts_pages_copy, once per
-layer, with the (source, destination) lists that the methods here return.  Nothing here touches a page.
+layer, with the (source, destination) lists that the methods here return, one after the other (copy_runs).  Nothing here touches a page.
 """
 from __future__ import annotations
 
 import heapq
 
 import numpy as np
+
+
+def copy_runs(copies):
+    """The list [(src, dst)] cut into runs [(begin, end)] whose copies need no order among them, as ts_pages_copy wants them: no page of a
+    run is written twice, or written by one pair and read by another."""
+    runs, begin, read, written = [], 0, set(), set()
+    for i, (a, b) in enumerate(copies):
+        if a == b:
+            continue
+        if a in written or b in written or b in read:
+            runs.append((begin, i))
+            begin, read, written = i, set(), set()
+        read.add(a)
+        written.add(b)
+    if len(copies) > begin:
+        runs.append((begin, len(copies)))
+    return runs
 
 
 class PagePool:

@@ -9,6 +9,7 @@ import numpy as np
 import torch
 
 from . import binding as ts
+from .pages import copy_runs
 
 
 def to_device(a: np.ndarray, device="cuda:0") -> torch.Tensor:
@@ -25,10 +26,12 @@ def to_host(t: torch.Tensor, bits16: bool = False) -> np.ndarray:
 
 
 def copy_pages(problem, copies, num_pages, device="cuda:0"):
-    """Makes the page copies [(src, dst)] that a PagePool asks for, in the pools of `problem` (one call per layer)."""
+    """Makes the page copies [(src, dst)] that a PagePool asks for, in the pools of `problem` (one call per layer).  The lists of several of its methods
+    may be joined: what an earlier pair concerns is copied before a later one reads or overwrites it."""
     if copies:
         pairs = torch.tensor(copies, dtype=torch.int32, device=device).t().contiguous()
-        ts.ts_pages_copy(problem, pairs[0], pairs[1], len(copies), num_pages)
+        for a, b in copy_runs(copies):
+            ts.ts_pages_copy(problem, pairs[0, a:b], pairs[1, a:b], b - a, num_pages)
 
 
 class _NewTokens:

@@ -38,3 +38,38 @@ def test_compact_refuses_new_lengths_in_the_place_of_what_it_reads():
     idx, count, skip, to_indptr, to = 0x600000, 0x700000, 0x800000, 0x900000, 0xa00000
     for lens in (0x500000, 0x500000 + 20, 0x500000 - 20, count, count + 4, idx, idx + 6 * 4 * 4 - 4, 0x300000 + 24, to_indptr + 24, to_indptr - 4, skip + 4):
         assert ts.load().ts_cache_compact(ctypes.byref(p), idx, 4, count, skip, to_indptr, to, lens, None) == -1, hex(lens)
+
+
+def test_copies_that_follow_each_other_are_cut_into_runs():
+    import numpy as np
+
+    from paper_2411_02886_amd.pages import PagePool, copy_runs
+    assert copy_runs([]) == [] and copy_runs([(1, 2), (1, 3), (4, 5)]) == [(0, 3)] and copy_runs([(7, 7)]) == [(0, 1)]
+    assert copy_runs([(5, 9), (9, 10)]) == [(0, 1), (1, 2)]                # reads what the first wrote
+    assert copy_runs([(5, 9), (3, 5)]) == [(0, 1), (1, 2)]                 # overwrites what the first reads
+    assert copy_runs([(5, 9), (9, 9), (4, 9)]) == [(0, 2), (2, 3)]         # writes the same page
+    rng = np.random.default_rng(0)
+    for _ in range(200):
+        copies = [tuple(int(x) for x in rng.integers(0, 9, 2)) for _ in range(int(rng.integers(0, 14)))]
+        want, got = np.arange(9), np.arange(9)
+        for a, b in copies:
+            want[b] = want[a]
+        at = 0
+        for begin, end in copy_runs(copies):
+            assert begin == at and end > begin
+            at = end
+            src, dst = [a for a, _ in copies[begin:end]], [b for _, b in copies[begin:end]]
+            pairs = {(a, b) for a, b in copies[begin:end] if a != b}
+            assert len({b for _, b in pairs}) == len([1 for a, b in copies[begin:end] if a != b]) and not {a for a, _ in pairs} & {b for _, b in pairs}
+            before = got.copy()
+            for a, b in zip(src, dst):
+                got[b] = before[a] if a != b else got[b]
+        assert at == len(copies) and np.array_equal(want, got)
+    # a fork grows, its own fork grows: the second copy reads what the first one wrote
+    pool = PagePool(8, 4)
+    pool.add("a", 2)
+    pool.fork("a", "b")
+    copies = pool.grow("b")
+    pool.fork("b", "c")
+    copies += pool.grow("c")
+    assert copies == [(0, 1), (1, 2)] and copy_runs(copies) == [(0, 1), (1, 2)]
