@@ -25,11 +25,11 @@ def to_host(t: torch.Tensor, bits16: bool = False) -> np.ndarray:
     return a.view(np.uint16) if bits16 else a
 
 
-def copy_pages(problem, copies, num_pages, device="cuda:0"):
+def copy_pages(problem, copies, num_pages, device=None):
     """Makes the page copies [(src, dst)] that a PagePool asks for, in the pools of `problem` (one call per layer).  The lists of several of its methods
-    may be joined: what an earlier pair concerns is copied before a later one reads or overwrites it."""
+    may be joined: what an earlier pair concerns is copied before a later one reads or overwrites it.  device: where the list goes; the pools' by default."""
     if copies:
-        pairs = torch.tensor(copies, dtype=torch.int32, device=device).t().contiguous()
+        pairs = torch.tensor(copies, dtype=torch.int32, device=problem._keep[0].device if device is None else device).t().contiguous()
         for a, b in copy_runs(copies):
             ts.ts_pages_copy(problem, pairs[0, a:b], pairs[1, a:b], b - a, num_pages)
 

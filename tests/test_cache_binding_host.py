@@ -73,3 +73,13 @@ def test_copies_that_follow_each_other_are_cut_into_runs():
     pool.fork("b", "c")
     copies += pool.grow("c")
     assert copies == [(0, 1), (1, 2)] and copy_runs(copies) == [(0, 1), (1, 2)]
+
+
+def test_a_list_of_copies_goes_where_the_pools_are(monkeypatch):
+    from paper_2411_02886_amd import runtime
+    calls = []
+    monkeypatch.setattr(runtime.ts, "ts_pages_copy", lambda p, src, dst, n, pages: calls.append((src, dst, n, pages)))
+    runtime.copy_pages(problem(), [(0, 1), (1, 2), (0, 3)], 9)
+    assert [(a.tolist(), b.tolist(), n, pages) for a, b, n, pages in calls] == [([0], [1], 1, 9), ([1, 0], [2, 3], 2, 9)]
+    assert all(t.device.type == "cpu" and t.is_contiguous() and t.dtype == torch.int32 for a, b, _, _ in calls for t in (a, b))
+    runtime.copy_pages(None, [], 9)
