@@ -124,22 +124,24 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-_raw_stream = None
+_raw_stream = _device = None
 
 
 def _current_stream() -> int:
     """Handle of the current stream of the current device.  Four of these are in every decode step, so the Stream object
     that torch.cuda.current_stream() builds (about 2 us) is left out."""
-    global _raw_stream
     if _raw_stream is None:
-        import torch
-        torch.cuda.init()
-        raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
-        if raw is not None and device is not None:
-            _raw_stream = lambda: raw(device())
-        else:
-            _raw_stream = lambda: torch.cuda.current_stream().cuda_stream
-    return _raw_stream()
+        _find_raw_stream()
+    return _raw_stream(_device())
+
+
+def _find_raw_stream() -> None:
+    global _raw_stream, _device
+    import torch
+    torch.cuda.init()
+    _raw_stream, _device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    if _raw_stream is None or _device is None:
+        _raw_stream, _device = (lambda i: torch.cuda.current_stream(i).cuda_stream), torch.cuda.current_device
 
 
 def _stream(stream) -> Optional[int]:
@@ -163,9 +165,12 @@ class Problem:
                            _ptr(k_pool), _ptr(v_pool), _ptr(page_indptr), _ptr(page_indices), _ptr(seq_lens),
                            int(num_initial), int(num_local))
         self.q_row, self.kv_row = num_q_heads * head_dim, num_kv_heads * head_dim      # elements of a token's q, and of its k or v
+        self._ref = ctypes.byref(self.c)
+        self.batch, self.heads, self.dtype = batch, num_q_heads, dtype
+        self.device = -1 if k_pool is None else k_pool.get_device()                    # -1: not on a GPU
 
     def ref(self):
-        return ctypes.byref(self.c)
+        return self._ref
 
 
 class Rope:
@@ -180,6 +185,7 @@ class Rope:
         if str(inv_freq.dtype) != "torch.float32" or not inv_freq.is_contiguous():
             raise ValueError("inv_freq: a contiguous float32 tensor")
         self._keep = inv_freq
+        self.num_axes, self.device = int(num_axes), inv_freq.get_device()
         self.c = _CRope(_ptr(inv_freq), 2 * n, int(num_axes), int(bool(adjacent)), float(scale), (ctypes.c_uint8 * 64)(*axes))
         self._ref = ctypes.byref(self.c)
 
@@ -361,20 +367,71 @@ def ts_sparse_paged_attn(p: Problem, q, idx, idx_stride: int, count, sm_scale: f
         "ts_sparse_paged_attn")
 
 
+_INT = _FLOAT = _MASK = _STORED = None      # element types: of index arrays, of lse, of skip masks, of q, k, v and results by the problem's
+
+
+def _load_types():
+    global _INT, _FLOAT, _MASK, _STORED
+    import torch
+    bits = [getattr(torch, name) for name in ("bfloat16", "int16", "uint16") if hasattr(torch, name)]      # bf16 may travel as raw bits
+    _FLOAT, _MASK, _INT = (torch.float32,), (torch.uint8, torch.bool), (torch.int32,)
+    _STORED = {TS_F32: _FLOAT, TS_BF16: tuple(bits)}
+
+
+def _refuse(p: Problem, t, name: str, types, need: str):
+    if t.dtype not in types:
+        raise ValueError("%s: a tensor of %s" % (name, " or ".join(str(x) for x in types)))
+    if t.get_device() != p.device:
+        raise ValueError("%s: on the device of the pools" % name)
+    raise ValueError("%s: %s" % (name, need))
+
+
+def _at(p: Problem, t, name: str, types, count: int):
+    """Address of a tensor that the library takes as an array of `count` elements, or an error where it would read something else."""
+    if t is None:
+        return None
+    if t.dtype in types and t.get_device() == p.device and t.numel() >= count and t.is_contiguous():
+        return t.data_ptr()
+    _refuse(p, t, name, types, "%d elements one after the other" % count)
+
+
+def _stream_of(p: Problem, stream):
+    """The stream that a call on the problem's pools goes to; without one the current device has to be theirs."""
+    if p.device < 0 and p.c.k_pool is not None:
+        raise ValueError("the pools are not on a GPU")
+    if stream is not None or p.device < 0:
+        return _stream(stream)
+    if _raw_stream is None:
+        _find_raw_stream()
+    device = _device()
+    if device != p.device:
+        raise ValueError("the pools are on device %d, the current one is %d" % (p.device, device))
+    return _raw_stream(device) or None
+
+
 def ts_paged_attn_workspace_bytes(p: Problem, num_rows: int) -> int:
     out = ctypes.c_size_t(0)
     _ok(load().ts_paged_attn_workspace_bytes(p.ref(), int(num_rows), ctypes.byref(out)), "ts_paged_attn_workspace_bytes")
     return int(out.value)
 
 
+def _attend(call, where, p: Problem, q, q_indptr, num_rows, window, sm_scale, out, lse, ws, stream):
+    n = int(num_rows)
+    if _STORED is None:
+        _load_types()
+    stored = _STORED.get(p.dtype, ())
+    if ws is not None and ws.get_device() != p.device:
+        raise ValueError("ws: on the device of the pools")
+    _ok(call(p.ref(), _at(p, q, "q", stored, n * p.q_row), _at(p, q_indptr, "q_indptr", _INT, p.batch + 1), n, int(window), float(sm_scale),
+             _at(p, out, "out", stored, n * p.q_row), _at(p, lse, "lse", _FLOAT, n * p.heads), _ptr(ws), _nbytes(ws), _stream_of(p, stream)), where)
+
+
 def ts_paged_attn(p: Problem, q, q_indptr, num_rows: int, window: int, sm_scale: float, out, lse, ws, stream=None) -> None:
-    _ok(load().ts_paged_attn(p.ref(), _ptr(q), _ptr(q_indptr), int(num_rows), int(window), float(sm_scale), _ptr(out), _ptr(lse),
-                             _ptr(ws), _nbytes(ws), _stream(stream)), "ts_paged_attn")
+    _attend(load().ts_paged_attn, "ts_paged_attn", p, q, q_indptr, num_rows, window, sm_scale, out, lse, ws, stream)
 
 
 def ts_paged_attn_rounded(p: Problem, q, q_indptr, num_rows: int, window: int, sm_scale: float, out, lse, ws, stream=None) -> None:
-    _ok(load().ts_paged_attn_rounded(p.ref(), _ptr(q), _ptr(q_indptr), int(num_rows), int(window), float(sm_scale), _ptr(out), _ptr(lse),
-                                     _ptr(ws), _nbytes(ws), _stream(stream)), "ts_paged_attn_rounded")
+    _attend(load().ts_paged_attn_rounded, "ts_paged_attn_rounded", p, q, q_indptr, num_rows, window, sm_scale, out, lse, ws, stream)
 
 
 def _row_stride(t, row: int, name: str) -> int:
@@ -398,20 +455,54 @@ def _row_stride(t, row: int, name: str) -> int:
     return strides[0] if shape[0] > 1 else 0
 
 
+def _rows_at(p: Problem, t, row: int, name: str, types, num_rows: int):
+    """(address, elements between the rows or 0 for packed) of a [rows][...] tensor; row: elements of one."""
+    if t is None:
+        return None, 0
+    shape = t.shape
+    if t.dtype in types and t.get_device() == p.device and shape[0] >= num_rows:
+        if len(shape) == 2 and shape[1] == row and shape[0] > 1:                  # parts of a projection, the quickest answer
+            strides = t.stride()
+            if strides[1] == 1 and strides[0] >= row:
+                return t.data_ptr(), strides[0]
+        return t.data_ptr(), _row_stride(t, row, name)
+    _refuse(p, t, name, types, "%d rows" % num_rows)
+
+
 def ts_rope_append(p: Problem, rope, q, k, v, q_indptr, num_rows: int, positions, q_out, stream=None) -> None:
     """q, k, v: [rows][heads][D] or [rows][heads * D], rows any multiple of 16 bytes apart; q and q_out, or k and v, may be None."""
-    q_stride, k_stride, v_stride = _row_stride(q, p.q_row, "q"), _row_stride(k, p.kv_row, "k"), _row_stride(v, p.kv_row, "v")
-    if q_out is not None and not q_out.is_contiguous():
-        raise ValueError("q_out: rows must follow each other")
-    _ok(load().ts_rope_append(p.ref(), None if rope is None else rope.ref(), _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v),
-                              v_stride, _ptr(q_indptr), int(num_rows), _ptr(positions), _ptr(q_out), _stream(stream)),
-        "ts_rope_append")
+    n = int(num_rows)
+    if _STORED is None:
+        _load_types()
+    stored, axes = _STORED.get(p.dtype, ()), 0
+    q_at, q_stride = _rows_at(p, q, p.q_row, "q", stored, n)
+    k_at, k_stride = _rows_at(p, k, p.kv_row, "k", stored, n)
+    v_at, v_stride = _rows_at(p, v, p.kv_row, "v", stored, n)
+    if rope is not None:
+        axes = rope.num_axes
+        if rope.device != p.device and rope.c.rotary_dim:
+            raise ValueError("inv_freq: on the device of the pools")
+    _ok(load().ts_rope_append(p.ref(), None if rope is None else rope.ref(), q_at, q_stride, k_at, k_stride, v_at, v_stride,
+                              _at(p, q_indptr, "q_indptr", _INT, p.batch + 1), n, _at(p, positions, "positions", _INT, axes * n),
+                              _at(p, q_out, "q_out", stored, n * p.q_row), _stream_of(p, stream)), "ts_rope_append")
 
 
 def ts_pages_copy(p: Problem, src, dst, n: int, num_pages: int, stream=None) -> None:
-    _ok(load().ts_pages_copy(p.ref(), _ptr(src), _ptr(dst), int(n), int(num_pages), _stream(stream)), "ts_pages_copy")
+    if _STORED is None:
+        _load_types()
+    n, elements = int(n), int(num_pages) * p.c.page_size * p.kv_row
+    for pool in p._keep[:2]:
+        if pool is not None and pool.numel() < elements:
+            raise ValueError("num_pages: %d, the pools hold fewer" % num_pages)
+    _ok(load().ts_pages_copy(p.ref(), _at(p, src, "src", _INT, n), _at(p, dst, "dst", _INT, n), n, int(num_pages), _stream_of(p, stream)),
+        "ts_pages_copy")
 
 
 def ts_cache_compact(p: Problem, idx, idx_stride: int, count, skip, to_indptr, to_indices, to_lens, stream=None) -> None:
-    _ok(load().ts_cache_compact(p.ref(), _ptr(idx), int(idx_stride), _ptr(count), _ptr(skip), _ptr(to_indptr), _ptr(to_indices),
-                                _ptr(to_lens), _stream(stream)), "ts_cache_compact")
+    if _STORED is None:
+        _load_types()
+    B = p.batch
+    _ok(load().ts_cache_compact(p.ref(), _at(p, idx, "idx", _INT, B * int(idx_stride)), int(idx_stride), _at(p, count, "count", _INT, B),
+                                _at(p, skip, "skip", _MASK, B), _at(p, to_indptr, "to_indptr", _INT, B + 1),
+                                _at(p, to_indices, "to_indices", _INT, 1), _at(p, to_lens, "to_lens", _INT, B), _stream_of(p, stream)),
+        "ts_cache_compact")

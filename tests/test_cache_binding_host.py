@@ -83,3 +83,81 @@ def test_a_list_of_copies_goes_where_the_pools_are(monkeypatch):
     assert [(a.tolist(), b.tolist(), n, pages) for a, b, n, pages in calls] == [([0], [1], 1, 9), ([1, 0], [2, 3], 2, 9)]
     assert all(t.device.type == "cpu" and t.is_contiguous() and t.dtype == torch.int32 for a, b, _, _ in calls for t in (a, b))
     runtime.copy_pages(None, [], 9)
+
+
+def ints(*shape):
+    return torch.zeros(*shape, dtype=torch.int32)
+
+
+def attend(p, **kw):
+    a = dict(q=torch.zeros(3, 4, 64), ind=ints(2), out=torch.zeros(3, 4, 64), lse=torch.zeros(3, 4), ws=torch.zeros(1 << 10))
+    a.update(kw)
+    for call in (ts.ts_paged_attn, ts.ts_paged_attn_rounded):
+        call(p, a["q"], a["ind"], 3, 0, 0.1, a["out"], a["lse"], a["ws"])
+
+
+def append(p, rope=None, **kw):
+    a = dict(q=torch.zeros(3, 4, 64), k=torch.zeros(3, 2, 64), v=torch.zeros(3, 128), ind=ints(2), pos=None, q_out=torch.zeros(3, 4, 64))
+    a.update(kw)
+    ts.ts_rope_append(p, rope, a["q"], a["k"], a["v"], a["ind"], 3, a["pos"], a["q_out"])
+
+
+def copy(p, n=2, pages=1, **kw):
+    a = dict(src=ints(2), dst=ints(2))
+    a.update(kw)
+    ts.ts_pages_copy(p, a["src"], a["dst"], n, pages)
+
+
+def compact(p, stride=4, **kw):
+    a = dict(idx=ints(1, 4), count=ints(1), skip=None, to_indptr=ints(2), to_indices=ints(3), to_lens=ints(1))
+    a.update(kw)
+    ts.ts_cache_compact(p, a["idx"], stride, a["count"], a["skip"], a["to_indptr"], a["to_indices"], a["to_lens"])
+
+
+WRONG_TYPES = [(attend, n) for n in ("q", "ind", "out", "lse")] + [(append, n) for n in ("q", "k", "v", "ind", "pos", "q_out")] + \
+    [(copy, n) for n in ("src", "dst")] + [(compact, n) for n in ("idx", "count", "skip", "to_indptr", "to_indices", "to_lens")]
+NAMES = dict(ind="q_indptr", pos="positions")
+
+
+@pytest.mark.parametrize("call,name", WRONG_TYPES, ids=lambda x: getattr(x, "__name__", x))
+def test_types_lengths_and_gaps_are_looked_at(call, name):
+    """A torch int64 tensor is what cumsum and arange give; it would be read as pairs of int32."""
+    z = torch.zeros(16 * 128)
+    p = problem(k_pool=z, v_pool=z)
+    rope = dict(rope=ts.Rope(inv_freq=torch.ones(32))) if call is append else {}
+    whole = dict(q=(3, 4, 64), out=(3, 4, 64), q_out=(3, 4, 64), k=(3, 2, 64), v=(3, 2, 64), lse=(3, 4), ind=(2,), pos=(1, 3), src=(2,), dst=(2,), idx=(1, 4),
+                 count=(1,), skip=(1,), to_indptr=(2,), to_indices=(1,), to_lens=(1,))[name]
+    right = torch.float32 if len(whole) == 3 or name == "lse" else torch.uint8 if name == "skip" else torch.int32
+    for wrong in {torch.int64, torch.float64, torch.float16, torch.bfloat16, torch.float32} - {right}:
+        with pytest.raises(ValueError, match=NAMES.get(name, name)):
+            call(p, **rope, **{name: torch.zeros(*whole, dtype=wrong)})
+    with pytest.raises(ValueError, match=NAMES.get(name, name)):           # too short
+        call(p, **rope, **{name: torch.zeros(*whole, dtype=right)[:-1] if whole != (1, 3) else torch.zeros(1, 2, dtype=right)})
+    if len(whole) != 3 or name in ("out", "q_out"):
+        if max(whole) > 1:
+            with pytest.raises(ValueError, match=NAMES.get(name, name)):   # with gaps
+                call(p, **rope, **{name: torch.zeros(*whole, 2, dtype=right)[..., 0]})
+    with pytest.raises(ValueError, match="not on a GPU"):                  # all as it should be: pools in host memory are refused
+        call(p, **rope)
+
+
+def test_bf16_travels_as_such_or_as_bits():
+    z = torch.zeros(16 * 128, dtype=torch.bfloat16)
+    p = problem(ts.TS_BF16, k_pool=z, v_pool=z)
+    for dtype in (torch.bfloat16, torch.int16):
+        x = torch.zeros(3, 4, 64, dtype=dtype)
+        with pytest.raises(ValueError, match="not on a GPU"):
+            attend(p, q=x, out=x.clone())
+    for dtype in (torch.float16, torch.float32):
+        with pytest.raises(ValueError, match="^q"):
+            attend(p, q=torch.zeros(3, 4, 64, dtype=dtype))
+
+
+def test_more_pages_than_the_pools_hold_are_refused():
+    z = torch.zeros(2, 16, 2, 64)
+    with pytest.raises(ValueError, match="num_pages"):
+        copy(problem(k_pool=z, v_pool=z), pages=3)
+    with pytest.raises(ValueError, match="num_pages"):
+        copy(problem(k_pool=z, v_pool=z[:1]), pages=2)
+    with pytest.raises(ValueError, match="not on a GPU"):
+        copy(problem(k_pool=z, v_pool=None), pages=2)
