@@ -102,11 +102,11 @@ __global__ __launch_bounds__(THREADS) void paged_merge_kernel(PagedAttnArgs a, S
           o.x = fmaf(f, x.x, o.x); o.y = fmaf(f, x.y, o.y); o.z = fmaf(f, x.z, o.z); o.w = fmaf(f, x.w, o.w);
         }
       const size_t hb = (size_t)(row0 + j / G) * a.H + kvh * G + j % G;
-      const float4 y = L > 0.f ? make_float4(o.x / L, o.y / L, o.z / L, o.w / L) : make_float4(0.f, 0.f, 0.f, 0.f);
+      const float4 y = L == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(o.x / L, o.y / L, o.z / L, o.w / L);   // (a sum that is no number stays one)
       if (ES == 2)
         *reinterpret_cast<uint2*>(a.out + (hb * D + sub * 4) * 2) = make_uint2(f32_to_bf16_bits(y.x) | (f32_to_bf16_bits(y.y) << 16), f32_to_bf16_bits(y.z) | (f32_to_bf16_bits(y.w) << 16));
       else *reinterpret_cast<float4*>(a.out + (hb * D + sub * 4) * 4) = y;
-      if (sub == 0 && a.lse != nullptr) a.lse[hb] = L > 0.f ? M + logf(L) : -INFINITY;
+      if (sub == 0 && a.lse != nullptr) a.lse[hb] = L == 0.f ? -INFINITY : M + logf(L);
     }
     __syncthreads();                                    // the next row takes the same place
   }
@@ -157,10 +157,10 @@ __global__ __launch_bounds__(256) void paged_merge_tall_kernel(PagedAttnArgs a, 
   }
   if (j >= nrows) return;
   const size_t hb = (size_t)(row0 + j / G) * a.H + kvh * G + j % G;
-  const float inv = L > 0.f ? 1.f / L : 0.f;
+  const float inv = L == 0.f ? 0.f : 1.f / L;
   *reinterpret_cast<uint2*>(a.out + (hb * D + 8 * i + 4 * (lane >> 5)) * 2) =
       make_uint2(f32_to_bf16_bits(o.x * inv) | (f32_to_bf16_bits(o.y * inv) << 16), f32_to_bf16_bits(o.z * inv) | (f32_to_bf16_bits(o.w * inv) << 16));
-  if (i == 0 && lane < 32 && a.lse != nullptr) a.lse[hb] = L > 0.f ? M + logf(L) : -INFINITY;
+  if (i == 0 && lane < 32 && a.lse != nullptr) a.lse[hb] = L == 0.f ? -INFINITY : M + logf(L);
 }
 
 template <int ES, int D>

@@ -357,15 +357,15 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
         }
         if (whole) {
           const size_t hb = tile_row + row_at((uint32_t)j);
-          const float inv = L > 0.f ? 1.f / L : 0.f;
+          const float inv = L == 0.f ? 0.f : 1.f / L;       // (a sum that is no number stays one)
           y = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
           if (ES == 2)
             *reinterpret_cast<uint2*>(a.out + (hb * D + d) * 2) = make_uint2(f32_to_bf16_bits(y.x) | (f32_to_bf16_bits(y.y) << 16), f32_to_bf16_bits(y.z) | (f32_to_bf16_bits(y.w) << 16));
           else *reinterpret_cast<float4*>(a.out + (hb * D + d) * 4) = y;
-          if (d == 0 && a.lse != nullptr) a.lse[hb] = L > 0.f ? m + logf(L) : -INFINITY;
+          if (d == 0 && a.lse != nullptr) a.lse[hb] = L == 0.f ? -INFINITY : m + logf(L);
         } else {
           *reinterpret_cast<float4*>(part_o + j * D + d) = y;
-          if (d == 0) { part_ml[2 * j] = L > 0.f ? m : -INFINITY; part_ml[2 * j + 1] = L; }
+          if (d == 0) { part_ml[2 * j] = L == 0.f ? -INFINITY : m; part_ml[2 * j + 1] = L; }
         }
       }
     }

@@ -612,7 +612,7 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
       const int jw = rb * 32 + col, j = wave * 64 + jw;
       const float l = lsum[rb] + __shfl_xor(lsum[rb], 32);
       if (whole) {
-        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const float inv = l == 0.f ? 0.f : 1.f / l;             // (a sum that is no number stays one)
 #pragma unroll
         for (int nb = 0; nb < NBO; ++nb)
 #pragma unroll
@@ -622,7 +622,7 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
             *reinterpret_cast<uint2*>(mine + jw * RB + (((nb * 4 + q4) ^ (jw & (PPR - 1))) * 16) + half * 8) =
                 make_uint2(__builtin_bit_cast(uint32_t, y0), __builtin_bit_cast(uint32_t, y1));
           }
-        if (half == 0 && j < nrows && a.lse != nullptr) a.lse[tile_row + row_at(j)] = l > 0.f ? (ref[rb] + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f : -INFINITY;
+        if (half == 0 && j < nrows && a.lse != nullptr) a.lse[tile_row + row_at(j)] = l == 0.f ? -INFINITY : (ref[rb] + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
       } else {
         float4* po = reinterpret_cast<float4*>(sh.part_o + ((size_t)wg * 2 + slot) * kPtRows * D) + (wave * 2 + rb) * (NBO * 4 * 64) + lane;
 #pragma unroll
@@ -632,7 +632,7 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
             po[(nb * 4 + q4) * 64] = make_float4(oacc[rb][nb][q4 * 4], oacc[rb][nb][q4 * 4 + 1], oacc[rb][nb][q4 * 4 + 2], oacc[rb][nb][q4 * 4 + 3]);
         if (half == 0) {
           float* pm = sh.part_ml + (((size_t)wg * 2 + slot) * kPtRows + j) * 2;
-          pm[0] = l > 0.f ? ref[rb] * 0.69314718055994530942f : -INFINITY; pm[1] = l;      // in units of the logits
+          pm[0] = l == 0.f ? -INFINITY : ref[rb] * 0.69314718055994530942f; pm[1] = l;      // in units of the logits
         }
       }
     }
