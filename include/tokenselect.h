@@ -347,7 +347,7 @@ int32_t ts_paged_attn_rounded(const ts_problem* p, const void* q, const int32_t*
  * tokens' K and V rows written into the pages: one launch.
  * Pair i of a head (i < rotary_dim / 2) is the elements (i, i + rotary_dim / 2), or (2 i, 2 i + 1) with `adjacent`, and turns by
  *   angle = positions[pair_axis[i]][r] * inv_freq[i]:   (x, y) -> scale * (x cos - y sin, x sin + y cos)
- * (the angle and its reduction in double: any int32 position; sine, cosine and the products in float, rounded once to p->dtype).
+ * (angle, reduction, sine and cosine in double: any int32 position; these rounded to float, the products in float, the result rounded once to p->dtype).
  * Elements from rotary_dim on pass through unchanged. */
 #define TS_ROPE_MAX_AXES 4
 typedef struct ts_rope {

@@ -1,7 +1,8 @@
 // Rotary positions with several axes, and the new tokens' K and V rows into their pages.  Bound by memory: every row is read and written once.
 //
-// Two or four waves take one token.  Its angles are the same for all heads: a lane per pair forms the angle in double (an exact int32 times
-// a float has 55 bits), takes whole turns off in double and leaves cosine and sine in LDS.  Then a lane has the same piece of every
+// One, two or four waves take one token.  Its angles are the same for all heads: a lane per pair forms the angle in double (an exact int32 times
+// a float has 55 bits), takes whole turns off, and leaves cosine and sine, formed in double and rounded once, in LDS (in float they cost 0.1 us less a call, and fp32
+// results were off by 4.1e-8 instead of 3.0e-8).  Then a lane has the same piece of every
 // head it works on, so that it reads its cosines once: 64 / (pieces of a head, rounded up to a power of two) heads side by side, several in flight.  A
 // piece is 16 bytes and its partner (halves) or 16 bytes that hold whole pairs (neighbours); where the rotated part does not divide so, 8 bytes (3000 tokens of
 // H 40/8, 24 of 128 elements turned, 20 us), and where it does not divide at all, single pairs (42).  Whoever writes an element is the only one who read it, so q may be turned in place.
@@ -112,9 +113,9 @@ __global__ __launch_bounds__(256) void rope_append_kernel(RopeAppendArgs a) {
   if (lane < half) {
     if (a.positions == nullptr) pos = place;
     const double turns = (double)pos * freq * 0.15915494309189533577;
-    float s, c;
-    sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
-    s_cos[lane] = c * a.scale; s_sin[lane] = s * a.scale;
+    double s, c;
+    sincospi(2.0 * (turns - rint(turns)), &s, &c);
+    s_cos[lane] = (float)(c * a.scale); s_sin[lane] = (float)(s * a.scale);
   }
   __builtin_amdgcn_wave_barrier();                                     // (a wave's LDS accesses keep their order)
   uint8_t* q_to = a.q_out + (int64_t)row * a.H * row_bytes;
