@@ -161,3 +161,45 @@ def test_more_pages_than_the_pools_hold_are_refused():
         copy(problem(k_pool=z, v_pool=z[:1]), pages=2)
     with pytest.raises(ValueError, match="not on a GPU"):
         copy(problem(k_pool=z, v_pool=None), pages=2)
+
+
+class FakeLayer:
+    """What attend_all and append need of a layer, with calls that are written down instead of launched."""
+
+    def __init__(self, monkeypatch, B=2, C=1):
+        from paper_2411_02886_amd import runtime
+        self.calls, self.stream, self.bytes = [], 7, 1 << 12
+        fake, ts0 = self, runtime.ts
+
+        class Layer(runtime._NewTokens):
+            def __init__(self):
+                z = ints(9)
+                self.k_pool, self.B, self.D = torch.zeros(4, 16, 2, 64), B, 64
+                self.problem = ts.Problem(batch=B, chunk=C, num_q_heads=4, num_kv_heads=2, head_dim=64, page_size=16, max_seq_len=64, dtype=ts.TS_F32,
+                                          k_pool=self.k_pool, v_pool=self.k_pool, page_indptr=z, page_indices=z, seq_lens=z)
+                self.out, self.lse = torch.zeros(B, C, 4, 64), torch.zeros(B, C, 4)
+
+        for name in ("ts_paged_attn", "ts_paged_attn_rounded", "ts_rope_append"):
+            monkeypatch.setattr(ts0, name, lambda *a, name=name: fake.calls.append((name,) + a))
+        monkeypatch.setattr(ts0, "ts_paged_attn_workspace_bytes", lambda p, rows: fake.bytes * p.c.chunk)
+        monkeypatch.setattr(ts0, "_current_stream", lambda: fake.stream)
+        self.layer = Layer()
+
+
+def test_each_stream_has_a_workspace_of_its_own_and_none_is_replaced(monkeypatch):
+    f = FakeLayer(monkeypatch)
+    q = torch.zeros(2, 1, 4, 64)
+    ws = []
+    for stream, size in ((7, 1 << 12), (8, 1 << 12), (7, 1 << 14), (7, 1 << 12), (8, 1 << 12)):
+        f.stream, f.bytes = stream, size
+        f.layer.attend_all(q)
+        ws.append(f.calls[-1][9])
+        assert ws[-1].numel() * 4 >= size
+    at = [w.data_ptr() for w in ws]
+    assert len({at[0], at[1], at[2]}) == 3 and at[3] == at[0] and at[4] == at[1]
+    own = torch.zeros(1 << 12)
+    f.layer.attend_all(q, ws=own)
+    assert f.calls[-1][9] is own
+    g = FakeLayer(monkeypatch)                      # another layer, another workspace
+    g.layer.attend_all(q)
+    assert g.calls[-1][9].data_ptr() not in at

@@ -38,3 +38,25 @@ def test_joined_lists_of_page_copies_are_made_in_their_order(gpu):
     copy_pages(p, copies, NP)
     torch.cuda.synchronize()
     assert not k.any() and not v.any()
+
+
+def test_two_streams_attend_on_one_layer(gpu):
+    from paper_2411_02886_amd.runtime import DecodeLayer, to_device, to_host
+    c = Cache(BF, 2, 64, 16, [9000, 4000, 2500], seed=8)
+    lay = DecodeLayer(dtype=BF, H=8, H_kv=2, D=64, P=16, k=16, k_pool=c.k_bits.reshape(-1, 16, 2, 64), v_pool=c.v_bits.reshape(-1, 16, 2, 64),
+                      page_indptr=c.indptr, page_indices=c.pages, seq_lens=c.lens)
+    rng = np.random.default_rng(1)
+    q = [W.store(rng.standard_normal((3, 8, 64), dtype=np.float32), BF) for _ in range(2)]
+    dev = [to_device(x) for x in q]
+    got = [(torch.zeros((3, 8, 64), dtype=torch.int16, device="cuda:0"), torch.zeros((3, 8), device="cuda:0")) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for rep in range(20):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                lay.attend_all(dev[i], out=got[i][0], lse=got[i][1])
+    torch.cuda.synchronize()
+    assert len({w.data_ptr() for w in lay._all_ws.values()}) == 2
+    for i in range(2):
+        check_attention(W.as_f32(to_host(got[i][0], bits16=True), BF).astype(np.float64), to_host(got[i][1]).astype(np.float64),
+                        attention(c, q[i], [1] * 3, 0, 0.125, [False] * 3), i)
