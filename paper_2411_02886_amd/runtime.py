@@ -40,7 +40,8 @@ class _NewTokens:
 
     def append(self, k, v, q=None, q_out=None, rope=None, positions=None, q_indptr=None):
         """Writes the new tokens' K and V rows into their pages, keys turned by `rope`, and the turned queries into q_out (either
-        alone: k and v, or q and q_out, None)."""
+        alone: k and v, or q and q_out, None).  Rows [rows][heads][D] or [rows][heads * D], or as a step or chunk has them, [B][C][heads][D]."""
+        q, k, v = (t.flatten(0, 1) if t is not None and t.dim() == 4 else t for t in (q, k, v))
         ts.ts_rope_append(self.problem, rope, q, k, v, q_indptr, (q if k is None else k).shape[0], positions, q_out)
 
     def attend_all(self, q, sm_scale=None, window=0, q_indptr=None, out=None, lse=None, round_weights=False, ws=None):

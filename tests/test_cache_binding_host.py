@@ -203,3 +203,18 @@ def test_each_stream_has_a_workspace_of_its_own_and_none_is_replaced(monkeypatch
     g = FakeLayer(monkeypatch)                      # another layer, another workspace
     g.layer.attend_all(q)
     assert g.calls[-1][9].data_ptr() not in at
+
+
+def test_append_takes_the_shapes_that_attend_all_takes(monkeypatch):
+    f = FakeLayer(monkeypatch, B=2, C=3)
+    q, k = torch.zeros(2, 3, 4, 64), torch.zeros(2, 3, 2, 64)
+    f.layer.append(k, k, q=q, q_out=torch.zeros_like(q))
+    _, _, _, q1, k1, v1, _, rows, _, _ = f.calls[-1]
+    assert rows == 6 and tuple(q1.shape) == (6, 4, 64) and tuple(k1.shape) == tuple(v1.shape) == (6, 2, 64) and q1.data_ptr() == q.data_ptr()
+    f.layer.append(None, None, q=q, q_out=q)
+    assert f.calls[-1][7] == 6
+    fused = torch.zeros(2, 3, 8, 64)                # parts of a projection stay views
+    f.layer.append(fused[:, :, 4:6], fused[:, :, 6:], q=fused[:, :, :4], q_out=q)
+    assert [t.data_ptr() - fused.data_ptr() for t in f.calls[-1][3:6]] == [0, 4 * 256, 6 * 256] and f.calls[-1][4].stride(0) == 512
+    f.layer.append(k.view(6, 128), k.view(6, 128))  # rows as before
+    assert f.calls[-1][7] == 6 and f.calls[-1][4].dim() == 2

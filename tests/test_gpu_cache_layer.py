@@ -60,3 +60,24 @@ def test_two_streams_attend_on_one_layer(gpu):
     for i in range(2):
         check_attention(W.as_f32(to_host(got[i][0], bits16=True), BF).astype(np.float64), to_host(got[i][1]).astype(np.float64),
                         attention(c, q[i], [1] * 3, 0, 0.125, [False] * 3), i)
+
+
+def test_a_chunk_is_appended_and_attended_in_one_shape(gpu):
+    """[B][C][heads][D] parts of a projection, for append and attend_all alike."""
+    from paper_2411_02886_amd.runtime import ChunkSelector, to_device, to_host
+    B, C, H, H_kv, D, P = 2, 20, 8, 2, 64, 16
+    c = Cache(BF, H_kv, D, P, [70, 33], seed=8)
+    x = W.store(np.random.default_rng(2).standard_normal((B, C, H + 2 * H_kv, D), dtype=np.float32), BF)
+    for b in range(B):
+        at = c.slots(b)[-C:]
+        for bits, now, part in ((c.k_bits, c.k, x[b, :, H:H + H_kv]), (c.v_bits, c.v, x[b, :, H + H_kv:])):
+            now[at] = W.as_f32(part, BF)
+    sel = ChunkSelector(C=C, H=H, H_kv=H_kv, D=D, P=P, k=8, k_pool=c.k_bits.reshape(-1, P, H_kv, D), v_pool=c.v_bits.reshape(-1, P, H_kv, D),
+                        page_indptr=c.indptr, page_indices=c.pages, seq_lens=c.lens)
+    dev = to_device(x)
+    q = torch.zeros((B, C, H, D), dtype=torch.int16, device="cuda:0")
+    sel.append(dev[:, :, H:H + H_kv], dev[:, :, H + H_kv:], q=dev[:, :, :H], q_out=q)
+    sel.attend_all(q)
+    torch.cuda.synchronize()
+    check_attention(W.as_f32(to_host(sel.out, bits16=True), BF).astype(np.float64).reshape(B * C, H, D), to_host(sel.lse).astype(np.float64).reshape(B * C, H),
+                    attention(c, x[:, :, :H].reshape(B * C, H, D), [C, C], 0, 0.125, [False] * 2), "chunk")
