@@ -172,6 +172,14 @@ class Problem:
     def ref(self):
         return self._ref
 
+    def with_chunk(self, chunk: int):
+        """The same problem with another number of new tokens per sequence."""
+        c = self.c
+        k_pool, v_pool, page_indptr, page_indices, seq_lens = self._keep
+        return Problem(batch=c.batch, chunk=chunk, num_q_heads=c.num_q_heads, num_kv_heads=c.num_kv_heads, head_dim=c.head_dim, page_size=c.page_size,
+                       max_seq_len=c.max_seq_len, dtype=c.dtype, k_pool=k_pool, v_pool=v_pool, page_indptr=page_indptr, page_indices=page_indices,
+                       seq_lens=seq_lens, num_initial=c.num_initial, num_local=c.num_local)
+
 
 class Rope:
     """ts_rope plus a reference that keeps the frequencies alive.  pair_axis: the position axis of each pair (rotary_dim / 2

@@ -44,24 +44,36 @@ class _NewTokens:
         q, k, v = (t.flatten(0, 1) if t is not None and t.dim() == 4 else t for t in (q, k, v))
         ts.ts_rope_append(self.problem, rope, q, k, v, q_indptr, (q if k is None else k).shape[0], positions, q_out)
 
-    def attend_all(self, q, sm_scale=None, window=0, q_indptr=None, out=None, lse=None, round_weights=False, ws=None):
+    def _with_chunk(self, chunk):
+        """The layer's problem with another number of new tokens per sequence."""
+        kept = self.__dict__.get("_chunks")
+        if kept is None or kept[0] is not self.problem:
+            kept = self._chunks = (self.problem, {})
+        if chunk not in kept[1]:
+            kept[1][chunk] = self.problem.with_chunk(chunk)
+        return kept[1][chunk]
+
+    def attend_all(self, q, sm_scale=None, window=0, q_indptr=None, out=None, lse=None, round_weights=False, ws=None, most_new=None):
         """Attention of the new tokens over their whole sequence: no selection.  Without q_indptr q is the step's or chunk's
         query and the result is in self.out / self.lse; packed rows bring their own `out` (and `lse`).
         round_weights: bf16 prompts in half the time, their weights rounded to bf16 (ts_paged_attn_rounded).
         ws: the workspace; by default one that the layer keeps for the current stream.  Calls that may run at once need one each: graphs that are
-        replayed on different streams and were captured on one bring their own."""
+        replayed on different streams and were captured on one bring their own.
+        most_new: packed rows: the most that a sequence has, which the choice of a kernel goes by (any number is computed).  The layer's chunk by
+        default, 1 in a DecodeLayer: prompts among the rows want it said."""
         sm = sm_scale if sm_scale is not None else 1.0 / float(np.sqrt(self.D))
         rows = self.B * self.problem.c.chunk if q_indptr is None else q.shape[0]
         if q_indptr is None:
             out, lse = self.out if out is None else out, self.lse if lse is None else lse
-        nbytes = ts.ts_paged_attn_workspace_bytes(self.problem, rows)
+        problem = self.problem if q_indptr is None or most_new is None else self._with_chunk(int(most_new))
+        nbytes = ts.ts_paged_attn_workspace_bytes(problem, rows)
         if ws is None:
             kept, key = self.__dict__.setdefault("_all_ws", {}), (ts._current_stream(), nbytes)
             if key not in kept:                   # (none is ever replaced: a graph may hold it)
                 kept[key] = torch.empty((nbytes + 255) // 256 * 64, dtype=torch.int32, device=self.k_pool.device)
             ws = kept[key]
         attend = ts.ts_paged_attn_rounded if round_weights else ts.ts_paged_attn
-        attend(self.problem, q, q_indptr, rows, window, sm, out, lse, ws)
+        attend(problem, q, q_indptr, rows, window, sm, out, lse, ws)
 
 
 class DecodeLayer(_NewTokens):

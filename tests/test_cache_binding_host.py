@@ -218,3 +218,21 @@ def test_append_takes_the_shapes_that_attend_all_takes(monkeypatch):
     assert [t.data_ptr() - fused.data_ptr() for t in f.calls[-1][3:6]] == [0, 4 * 256, 6 * 256] and f.calls[-1][4].stride(0) == 512
     f.layer.append(k.view(6, 128), k.view(6, 128))  # rows as before
     assert f.calls[-1][7] == 6 and f.calls[-1][4].dim() == 2
+
+
+def test_packed_rows_may_say_how_many_a_sequence_has(monkeypatch):
+    f = FakeLayer(monkeypatch)
+    lay, q, ind = f.layer, torch.zeros(40, 4, 64), ints(3)
+    for most in (40, 16, 40):
+        lay.attend_all(q, q_indptr=ind, out=q.clone(), most_new=most)
+        p, ws = f.calls[-1][1], f.calls[-1][9]
+        assert p.c.chunk == most and ws.numel() * 4 >= f.bytes * most and f.calls[-1][4] == 40
+        assert [getattr(p.c, n) for n, _ in p.c._fields_ if n != "chunk"] == [getattr(lay.problem.c, n) for n, _ in p.c._fields_ if n != "chunk"]
+    assert f.calls[0][1] is f.calls[2][1] and lay.problem.c.chunk == 1
+    lay.attend_all(q, q_indptr=ind, out=q.clone())
+    assert f.calls[-1][1] is lay.problem
+    lay.problem = lay.problem.with_chunk(1)         # another pool: the kept ones are dropped
+    lay.attend_all(q, q_indptr=ind, out=q.clone(), most_new=40)
+    assert f.calls[-1][1] is not f.calls[0][1]
+    lay.attend_all(torch.zeros(2, 1, 4, 64), most_new=40)       # a step's own rows: the layer's chunk
+    assert f.calls[-1][1] is lay.problem

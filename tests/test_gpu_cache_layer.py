@@ -81,3 +81,21 @@ def test_a_chunk_is_appended_and_attended_in_one_shape(gpu):
     torch.cuda.synchronize()
     check_attention(W.as_f32(to_host(sel.out, bits16=True), BF).astype(np.float64).reshape(B * C, H, D), to_host(sel.lse).astype(np.float64).reshape(B * C, H),
                     attention(c, x[:, :, :H].reshape(B * C, H, D), [C, C], 0, 0.125, [False] * 2), "chunk")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+def test_prompts_on_a_decode_layer(gpu, dtype):
+    """Packed prompts with and without a bound on their lengths."""
+    from paper_2411_02886_amd.runtime import DecodeLayer, to_device, to_host
+    c = Cache(dtype, 2, 64, 16, [900, 400, 250], seed=8)
+    lay = DecodeLayer(dtype=dtype, H=8, H_kv=2, D=64, P=16, k=16, k_pool=c.k_bits.reshape(-1, 16, 2, 64), v_pool=c.v_bits.reshape(-1, 16, 2, 64),
+                      page_indptr=c.indptr, page_indices=c.pages, seq_lens=c.lens)
+    new = [300, 1, 60]
+    q = W.store(np.random.default_rng(1).standard_normal((361, 8, 64), dtype=np.float32), dtype)
+    ref = attention(c, q, new, 0, 0.125, [False] * 3)
+    out, lse, ind = to_device(np.zeros_like(q)), torch.zeros((361, 8), device="cuda:0"), to_device(np.cumsum([0] + new).astype(np.int32))
+    for most in (None, 300, 1000, 2):
+        out.zero_(), lse.zero_()
+        lay.attend_all(to_device(q), q_indptr=ind, out=out, lse=lse, most_new=most)
+        torch.cuda.synchronize()
+        check_attention(W.as_f32(to_host(out, bits16=dtype == BF), dtype).astype(np.float64), to_host(lse).astype(np.float64), ref, most)
