@@ -188,21 +188,23 @@ static size_t piece_bytes(int rows, int D) {
 // 4 heads over 2000 keys, one sequence 17 us, eight of them 25; by the tall kernel 32 and 47), bf16 up to 128 by four of its tiles (32 tokens over 2000 keys 21 us,
 // by the tall kernel 33, 8 times 2000 keys 38 and 48, 8 times 8000 145 and 128; with 192 rows these are 28 and 34, 51 and 48, 224 and 135); more by the tall one (bf16), or by
 // the stream kernel with 64 rows a tile (fp32, whose matrix products it is then bound by: 512 tokens over 4000 keys 362 us, with 32 rows 412).  A packed batch may hold both kinds:
-// two launches, each takes the sequences that are its.  fp32: as a packed batch's bound says little about most of its sequences, twice as many rows go without the second.
+// two launches, each takes the sequences that are its.  fp32: as a packed batch's bound says little about most of its sequences, twice as many rows go without the second
+// (12 tokens over 3000 keys 28.7 us, else 42.8; 8 times 87 and 84).
 // Rounded weights, for which the tall kernel needs half the time: up to 64 rows by the stream kernel (16 tokens over 2000 keys 18.6 us, by the tall kernel 27.7, 8
-// times 4000 47 and 53; with 96 rows it would be 75 and 52), twice that in packed batches (8 of 1 to 30 tokens over up to 4000 keys 42 us, else 76).
+// times 4000 47 and 53; with 96 rows it would be 75 and 52), twice that where a packed batch's sequences are
+// shorter than the bound (loose: less than three quarters of it on average; 8 of 1 to 30 tokens over up to 4000 keys 42 us, else 76; but 8 of 24 each 73 and 57).
 struct PagedPlan { int few_rows, many_rows; };   // rows of the tiles of sequences with few rows, and of those with more (0: there are none)
-static PagedPlan paged_plan(int dtype, int G, int chunk, bool packed, bool rounded) {
+static PagedPlan paged_plan(int dtype, int G, int chunk, bool packed, bool loose, bool rounded) {
   const long rows = (long)chunk * G;
   if (rows <= 16) return PagedPlan{16, 0};
-  if (rows <= (dtype == TS_F32 ? (packed ? 64 : 32) : rounded && !packed ? 64 : 128)) return PagedPlan{32, 0};
+  if (rows <= (dtype == TS_F32 ? (packed ? 64 : 32) : rounded && !loose ? 64 : 128)) return PagedPlan{32, 0};
   return dtype == TS_BF16 ? PagedPlan{32, kTallRows} : PagedPlan{16, 64};
 }
 
 size_t paged_attn_workspace(int dtype, int D, int G, int chunk) {
   size_t most = 0;
   for (int form = 0; form < 4; ++form) {
-    const PagedPlan pl = paged_plan(dtype, G, chunk, (form & 1) != 0, (form & 2) != 0);
+    const PagedPlan pl = paged_plan(dtype, G, chunk, (form & 1) != 0, (form & 1) != 0, (form & 2) != 0);
     most = std::max(most, align_up(piece_bytes(pl.few_rows, D) + (pl.many_rows ? piece_bytes(pl.many_rows, D) : 0), 256));
   }
   return most;
@@ -210,7 +212,7 @@ size_t paged_attn_workspace(int dtype, int D, int G, int chunk) {
 
 hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws, hipStream_t s) {
   const int G = a.H / a.H_kv;
-  const PagedPlan pl = paged_plan(dtype, G, a.C, a.q_indptr != nullptr, a.round_weights != 0);
+  const PagedPlan pl = paged_plan(dtype, G, a.C, a.q_indptr != nullptr, (long)a.T * 4 <= (long)a.B * a.C * 3, a.round_weights != 0);
   uint8_t* at = (uint8_t*)ws;
   // tiles of every sequence (0: not as many), and bounds on all tiles and on the keys of one.  A tile of few rows beside large ones is its whole sequence.
   auto each_of = [&](int tpt, bool beside) -> int { return beside ? 1 : a.q_indptr != nullptr ? 0 : (a.C + tpt - 1) / tpt; };

@@ -178,3 +178,13 @@ def test_large_values_beside_rising_logits_stay_finite(gpu, dtype, n, D):
             out, lse, _, scale = call(gpu, c, H, [n, n], rounded=rounded, packed=False, bound=bound, q=q)
             assert np.isfinite(out).all(), (rounded, bound)
             check_attention(out, lse, attention(c, q, [n, n], 0, scale, [rounded and dtype == BF and n * 4 > 32] * 2), (rounded, bound))
+
+
+@pytest.mark.parametrize("rounded", [False, True], ids=["", "rounded"])
+@pytest.mark.parametrize("n", [3, 12, 24, 30, 50])
+@pytest.mark.parametrize("bound", [None, LOOSE], ids=["", "loose bound"])
+def test_full_packed_batches_are_computed_as_padded_ones(gpu, rounded, n, bound):
+    """The same rows, described by q_indptr or by the chunk: the same kernel, the same bits."""
+    c = Cache(BF, 2, 64, 16, [3000, 2000, 1500, 700], seed=n)
+    a, b = (call(gpu, c, 8, [n] * 4, rounded=rounded, packed=packed, bound=bound) for packed in (True, False))
+    assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
