@@ -247,10 +247,11 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
   };
   // A workgroup per tile, and no merge, where tiles are short, or where there are enough of them that are not long.  (200 keys: 8.2 us, in shares 10.3; 64
   // sequences of 250 to 500 keys, 512 tiles: 22.8 and 29; but 16 fp32 sequences of 1000 to 2000 keys, 32 tiles, 42 us instead of 17.)  Beside large
-  // tiles a second merge would cost more (14 chunks of 1 to 197 tokens over up to 770 keys 52 us, in shares 64).
+  // tiles a second merge costs more, up to 1024 keys (14 chunks of 1 to 197 tokens over up to 770 keys 52 us, in shares 64; one to four single tokens beside a prompt of
+  // 512: over 300 keys 42 and 44 to 48, over 600 45.5 and 44.5, over 1000 53 and 47, 16 of them over 1000 52 and 53; but one to four over 1500 keys 59 and 47, over 2000 66 and 48).
   auto few_whole = [&](int rows, bool beside) -> bool {
     const long tiles = tiles_of(rows / G, beside), keys = keys_of(rows / G);
-    return tiles < (1l << 23) && (keys <= 512 || ((tiles >= kShareWgs || beside) && keys <= 16 * (dtype == TS_F32 ? 64 : 128)));
+    return tiles < (1l << 23) && (keys <= (beside ? 1024 : 512) || (tiles >= kShareWgs && keys <= 16 * (dtype == TS_F32 ? 64 : 128)));
   };
   if (!pl.many_rows) return run(pl.few_rows, 0, INT_MAX, few_whole(pl.few_rows, false));
   // Short prompts have too few tiles for the chip: there 32 rows a tile for all sequences, at most two workgroups per CU.  (256 tokens 10.6 us, by 256 rows a

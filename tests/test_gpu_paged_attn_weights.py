@@ -188,3 +188,14 @@ def test_full_packed_batches_are_computed_as_padded_ones(gpu, rounded, n, bound)
     c = Cache(BF, 2, 64, 16, [3000, 2000, 1500, 700], seed=n)
     a, b = (call(gpu, c, 8, [n] * 4, rounded=rounded, packed=packed, bound=bound) for packed in (True, False))
     assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("longest", [900, 1024, 1025, 1500, 2100])
+@pytest.mark.parametrize("rounded", [False, True], ids=["", "rounded"])
+def test_single_tokens_beside_a_prompt(gpu, dtype, longest, rounded):
+    """Sequences with few rows by a workgroup each or in shares, beside large tiles."""
+    new, lens = [1, 200, 1, 2, 0, 1], [longest, 200, 3, longest - 7, 50, 1]
+    c = Cache(dtype, 2, 64, 16, lens, seed=longest)
+    out, lse, q, sm = call(gpu, c, 8, new, rounded=rounded)
+    check_attention(out, lse, attention(c, q, new, 0, sm, [rounded and dtype == BF and n * 4 > 32 for n in new]), longest)
