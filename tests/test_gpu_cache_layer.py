@@ -99,3 +99,39 @@ def test_prompts_on_a_decode_layer(gpu, dtype):
         lay.attend_all(to_device(q), q_indptr=ind, out=out, lse=lse, most_new=most)
         torch.cuda.synchronize()
         check_attention(W.as_f32(to_host(out, bits16=dtype == BF), dtype).astype(np.float64), to_host(lse).astype(np.float64), ref, most)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("new", [[1, 3, 0, 2], [40, 1, 0, 90], [300, 5, 200, 1]])
+@pytest.mark.parametrize("B", [4, 70])
+def test_rows_in_front_of_the_first_sequence_and_behind_the_last(gpu, dtype, new, B):
+    """q_indptr may begin above 0: those rows are nobody's, as are the ones behind its end."""
+    from paper_2411_02886_amd.runtime import to_device, to_host
+    H, H_kv, D, front, behind = 8, 2, 64, 7, 5
+    new = new + [1, 0] * ((B - 4) // 2)
+    lens = [n + 11 * (b % 5) for b, n in enumerate(new)]
+    c = Cache(dtype, H_kv, D, 16, lens, seed=B)
+    T = front + sum(new) + behind
+    x = W.store(np.random.default_rng(2).standard_normal((T, H + 2 * H_kv, D), dtype=np.float32), dtype)
+    mine = slice(front, T - behind)
+    ind = to_device((front + np.cumsum([0] + new)).astype(np.int32))
+    for b in range(B):
+        at, r = c.slots(b)[lens[b] - new[b]:], front + sum(new[:b])
+        for bits, now, part in ((c.k_bits, c.k, x[r:r + new[b], H:H + H_kv]), (c.v_bits, c.v, x[r:r + new[b], H + H_kv:])):
+            now[at] = W.as_f32(part, dtype)
+    for bound in (None, 1 << 20):
+        p, kp, vp = c.problem(H, chunk=max(new), max_seq_len=bound)
+        dev = to_device(x)
+        q_out, out = (torch.full((T, H, D), 7, dtype=dev.dtype, device="cuda:0") for _ in "ab")
+        lse = torch.full((T, H), 7.0, device="cuda:0")
+        gpu.ts_rope_append(p, None, dev[:, :H], dev[:, H:H + H_kv], dev[:, H + H_kv:], ind, T, None, q_out)
+        ws = torch.empty((gpu.ts_paged_attn_workspace_bytes(p, T) + 255) // 256 * 64, dtype=torch.int32, device="cuda:0")
+        gpu.ts_paged_attn(p, q_out, ind, T, 0, 0.125, out, lse, ws)
+        torch.cuda.synchronize()
+        nobody = np.r_[0:front, T - behind:T]
+        assert all(np.all(to_host(t)[nobody] == 7) for t in (q_out, out, lse))
+        ref = attention(c, x[mine, :H], new, 0, 0.125, [False] * B)
+        check_attention(W.as_f32(to_host(out, bits16=dtype == BF), dtype).astype(np.float64)[mine], to_host(lse).astype(np.float64)[mine], ref, bound)
+        for t, want in ((kp, c.k), (vp, c.v)):
+            got = W.as_f32(to_host(t, bits16=dtype == BF).reshape(want.shape), dtype)
+            assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(got[~np.isnan(got)], want[~np.isnan(want)].astype(np.float32))
