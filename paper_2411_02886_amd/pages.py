@@ -113,6 +113,8 @@ class PagePool:
 
     def spare(self, tokens: int):
         """Pages for `tokens` tokens that belong to no sequence yet: where a compaction writes (see replace, give_back)."""
+        if tokens < 0:
+            raise ValueError("tokens < 0")
         need = -(-int(tokens) // self.page_size)
         if need > len(self._free):
             raise MemoryError("%d pages wanted, %d free" % (need, len(self._free)))

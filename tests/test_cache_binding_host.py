@@ -236,3 +236,11 @@ def test_packed_rows_may_say_how_many_a_sequence_has(monkeypatch):
     assert f.calls[-1][1] is not f.calls[0][1]
     lay.attend_all(torch.zeros(2, 1, 4, 64), most_new=40)       # a step's own rows: the layer's chunk
     assert f.calls[-1][1] is lay.problem
+
+
+def test_a_negative_number_of_spare_tokens_is_refused():
+    from paper_2411_02886_amd.pages import PagePool
+    pool = PagePool(4, 4)
+    with pytest.raises(ValueError):
+        pool.spare(-5)
+    assert pool.spare(0) == [] and pool.free_pages == 4
