@@ -17,12 +17,12 @@
 // units of matrix work instead of two.  The caller may choose weights rounded to bf16 (half a step, 2^-8 of each; the relative error of results against 64 bits
 // is then 1.8e-3 instead of 1.7e-3, which is the results' own rounding); their sum is of the floats before that rounding, so that the log-sum-exp keeps 24 bits.
 //
-// Measured (H 32/8, D 128): a prompt of 8192 tokens 861 us, 512 tokens over 131072 keys 1705, 1.28 and 1.29 PFLOP/s of products with the three parts counted; a bf16
-// product of 8192^3 by the library reaches 1.22 on the same card.  D 64, 8192 tokens: 523.  Power is the bound.
-// Rounded weights: 470 to 505 us from card to card, 904 to 966, up to 1.17 and 1.22 PFLOP/s; D 64 298.
-// 64 keys take 3350 cycles, of which the matrix cores work 2048 and 2500 go to issuing, and the clock falls to 1.8 to 2.0 GHz meanwhile (2.4 with
-// little work).  A tile's start and end cost 13000 cycles (page ids and queries 2100, the first tile and its scores 3700, the first block's weights
-// 2200, results 4400): what short prompts are bound by.  D 64: 2150 cycles where the matrix cores work 1024; exponentials, sums and
+// Measured (H 32/8, D 128): a prompt of 8192 tokens 835 to 883 us from card to card, 512 tokens over 131072 keys 1650 to 1715, up to 1.32 and 1.33 PFLOP/s of
+// products with the three parts counted; a bf16 product of 8192^3 by the library reaches 1.22 on such a card.  64 keys take 6300 cycles, of which the matrix cores
+// work 4096, at a clock of 2.0 GHz (2.4 with little work).  D 64, 8192 tokens: 523 us, 4040 cycles where the matrix cores work 2048: the vector ALU is the bound.
+// Rounded weights: 470 to 505 us, 904 to 966, up to 1.17 and 1.22 PFLOP/s: 3350 cycles for 64 keys, of which the matrix cores work 2048 and 2500 go to issuing,
+// at 1.8 to 2.0 GHz.  A tile's start and end cost 13000 cycles (page ids and queries 2100, the first tile and its scores 3700, the first block's weights
+// 2200, results 4400): what short prompts are bound by.  D 64: 298 us, 2150 cycles where the matrix cores work 1024; exponentials, sums and
 // conversions are as many as for D 128, so the vector ALU is the bound.
 #include "paged_shares.h"
 #include <limits.h>

@@ -6,8 +6,8 @@
 // head it works on, so that it reads its cosines once: 64 / (pieces of a head, rounded up to a power of two) heads side by side, several in flight.  A
 // piece is 16 bytes and its partner (halves) or 16 bytes that hold whole pairs (neighbours); where the rotated part does not divide so, 8 bytes (3000 tokens of
 // H 40/8, 24 of 128 elements turned, 20 us), and where it does not divide at all, single pairs (42).  Whoever writes an element is the only one who read it, so q may be turned in place.
-// Measured (H 32/8, D 128): 15243 tokens, three axes, parts of a fused projection 155 us by a workgroup per token and single pairs, 79 so (4.7 TB/s, what a
-// large copy reaches); 64 single tokens 3.8 us.
+// Measured (H 32/8, D 128): 15243 tokens, three axes, parts of a fused projection 155 us by a workgroup per token and single pairs, 75 so (5.0 TB/s, what a
+// large copy reaches); 64 single tokens 4.5 us in a captured graph.
 #include "ts_kernels.h"
 #include "ts_rows.h"
 #include <algorithm>
@@ -48,8 +48,8 @@ template <typename T, int BYTES> struct Piece {                        // 16 or 
 };
 
 // Up to so many tokens four waves share each; beyond that two, and one where a wave has the heads in two steps.  (us by one, two, four waves, bf16: 64 tokens of
-// H 32/8, D 128 5.6, 4.5, 3.8; 2048 11.5, 10.9, 10.7; 4096 17.0, 16.1, 18.4; 2000 of H 6/2, D 64 3.6, 4.1, 5.5, 30000 18.7, 28.3, 48.5; of H 16/4, D 128, three steps,
-// 7.4, 7.0, 8.0 and 72.5, 68.1, 81.1.  Single pairs: always four, 5000 tokens 39.4, 37.1, 32.8.)
+// H 32/8, D 128 6.2, 5.1, 4.5; 2048 11.4, 11.1, 11.1; 4096 17.7, 16.8, 19.4; 2000 of H 6/2, D 64 4.5, 5.1, 6.6, 30000 21.6, 33.0, 55.8; of H 16/4, D 128, three steps,
+// 7.0, 6.9, 8.2 and 72.1, 70.4, 81.0.  Single pairs: always four, 5000 tokens of H 40/8 with 26 of 128 elements turned 79, 72, 62.)
 constexpr int kRopeFew = 1024;
 
 enum { kPairs = 0, kHalves = 1, kNeighbours = 2 };
