@@ -244,3 +244,15 @@ def test_a_negative_number_of_spare_tokens_is_refused():
     with pytest.raises(ValueError):
         pool.spare(-5)
     assert pool.spare(0) == [] and pool.free_pages == 4
+
+
+def test_the_rounded_form_refuses_what_the_other_does(monkeypatch):
+    import test_cache_host
+    lib = ts.load()
+
+    class Rounded:
+        ts_paged_attn = staticmethod(lib.ts_paged_attn_rounded)
+
+    with monkeypatch.context() as m:
+        m.setattr(test_cache_host.ts, "load", lambda: Rounded)
+        test_cache_host.test_paged_attn_refusals()
