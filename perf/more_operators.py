@@ -178,11 +178,11 @@ def _encode(rows, fmt):
 
 
 def _pool(c, slots, g, x, name):
-    """A pool of random rows, in pieces of 2^25 elements."""
-    shape, step = (slots, c["H_kv"], c["D"]), max(1, (1 << 25) // (c["H_kv"] * c["D"]))
+    """A pool of random rows [slots][heads][D], in pieces of 2^25 elements; scales [pages][heads][P]."""
+    P, shape, step = c["P"], (slots, c["H_kv"], c["D"]), max(1, (1 << 25) // (c["P"] * c["H_kv"] * c["D"])) * c["P"]
     tdt = _TORCH[c["dtype"]]
     pool = torch.empty(shape, dtype=tdt if not c["fmt"] else torch.int8 if c["fmt"] == "int8" else torch.float8_e4m3fn, device=_DEV)
-    scale = torch.empty(shape[:2], device=_DEV) if c["fmt"] else None
+    scale = torch.empty((slots // P, c["H_kv"], P), device=_DEV) if c["fmt"] else None
     lean = x.get("lean_at") if name == "k" else None
     for a in range(0, slots, step):
         rows = torch.randn((min(step, slots - a),) + shape[1:], generator=g, device=_DEV)
@@ -191,7 +191,8 @@ def _pool(c, slots, g, x, name):
             rows[mine] += x["lean"]
         rows = rows.to(tdt)
         if c["fmt"]:
-            pool[a:a + step], scale[a:a + step] = _encode(rows, c["fmt"])
+            pool[a:a + step], mine = _encode(rows, c["fmt"])
+            scale[a // P:(a + step) // P] = mine.view(-1, P, c["H_kv"]).transpose(1, 2)
         else:
             pool[a:a + step] = rows
     x[name + "_pool"], x[name + "_scale"] = pool, scale
@@ -265,8 +266,8 @@ def prepare(case, seed):
                                   k_pool=pools[0], v_pool=pools[1], page_indptr=x["indptr"], page_indices=x["pages"], seq_lens=x["lens"])
         s["quant"] = None
         if c["fmt"]:
-            s["quant"] = ts.QuantCache(k_codes=x["k_pool"].view(shape), v_codes=x["v_pool"].view(shape), k_scale=x["k_scale"].view(shape[:3]),
-                                       v_scale=x["v_scale"].view(shape[:3]), format=ts.TS_INT8 if c["fmt"] == "int8" else ts.TS_E4M3)
+            s["quant"] = ts.QuantCache(k_codes=x["k_pool"].view(shape), v_codes=x["v_pool"].view(shape), k_scale=x["k_scale"],
+                                       v_scale=x["v_scale"], format=ts.TS_INT8 if c["fmt"] == "int8" else ts.TS_E4M3)
         s["ind"] = x["q_indptr"] if c["packed"] else None
         if c["op"] in ("attn", "tree"):
             n = (ts.ts_quant_attn_workspace_bytes if c["fmt"] else ts.ts_paged_attn_workspace_bytes)(s["problem"], T)
@@ -322,7 +323,11 @@ def _row_places(x, P):
 def _values(c, x, name, at):
     """Rows `at` of a pool as the values that they stand for, in 32 bits."""
     rows = x[name + "_pool"][at].float()
-    return rows * x[name + "_scale"][at][..., None] if c["fmt"] else rows
+    return rows * x[name + "_scale"][at // c["P"], :, at % c["P"]][..., None] if c["fmt"] else rows
+
+
+def _encode_rows(c, x, name, slot, rows):
+    x[name + "_pool"][slot], x[name + "_scale"][slot // c["P"], :, slot % c["P"]] = _encode(rows, c["fmt"])
 
 
 def _turn(c, rows, cos, sin):
@@ -348,8 +353,8 @@ def _plain_store(s):
         cos, sin = angle.cos(), angle.sin()
         q = _turn(c, x["q"].view(T, c["H"], c["D"]).double(), cos, sin).to(tdt)
         k = _turn(c, x["k"].view(T, c["H_kv"], c["D"]).double(), cos, sin).to(tdt)
-        x["k_pool"][slot], x["k_scale"][slot] = _encode(k, c["fmt"])
-        x["v_pool"][slot], x["v_scale"][slot] = _encode(x["v"].view(T, c["H_kv"], c["D"]), c["fmt"])
+        _encode_rows(c, x, "k", slot, k)
+        _encode_rows(c, x, "v", slot, x["v"].view(T, c["H_kv"], c["D"]))
     got = dict(k=_values(c, x, "k", slot).to(tdt), v=_values(c, x, "v", slot).to(tdt))
     return dict(got, q=q, k_scale=x["k_scale"], v_scale=x["v_scale"]) if c["op"] == "store" else got
 
@@ -362,10 +367,12 @@ def _plain_keep(s):
     i = torch.arange(x["stride"], device=_DEV)[None, :].expand_as(path)
     at = lambda t: x["pages"][(x["indptr"][:-1, None].long() + t // c["P"])[i < count]].long() * c["P"] + (t % c["P"])[i < count]
     src, dst = at(base + path), at(base + i)
-    for name in ("k_pool", "v_pool", "k_scale", "v_scale"):
-        if x[name] is not None:
-            pool = x[name].view(torch.int8) if x[name].dim() == 3 and c["fmt"] else x[name]
-            pool[dst] = pool[src]
+    for name in "kv":
+        pool, scale = x[name + "_pool"], x[name + "_scale"]
+        if c["fmt"]:
+            pool = pool.view(torch.int8)
+            scale[dst // c["P"], :, dst % c["P"]] = scale[src // c["P"], :, src % c["P"]]
+        pool[dst] = pool[src]
     x["to_lens"].copy_((base + count)[:, 0])
     return _kept_pools(c, x)
 
@@ -468,7 +475,7 @@ def _exact_store(c, x):
                       for a, n, o in zip(x["indptr"].tolist(), new, old)])
     slot = page * P + place % P
     if c["op"] == "read":
-        return {n: x[n + "_pool"][slot].double() * x[n + "_scale"][slot].double()[..., None] for n in "kv"}
+        return {n: x[n + "_pool"][slot].double() * x[n + "_scale"].transpose(1, 2).reshape(-1, H_kv)[slot].double()[..., None] for n in "kv"}
     q, k, v = (x[n].double().view(-1, h, D).clone() for n, h in (("q", H), ("k", H_kv), ("v", H_kv)))
     for i in range(c["rotary"] // 2):
         z = torch.polar(torch.ones_like(place, dtype=torch.float64), place.double() * float(x["inv_freq"][i]))[:, None]
@@ -479,8 +486,9 @@ def _exact_store(c, x):
     got = dict(q=q)
     for n, rows in (("k", k.to(tdt)), ("v", v)):        # what a cache of the layer's type would hold is quantised
         got[n], scale = _exact_rows(c, rows)
-        got[n + "_scale"] = x[n + "_scale"].double()
-        got[n + "_scale"][slot] = scale
+        flat = x[n + "_scale"].double().transpose(1, 2).reshape(-1, H_kv)
+        flat[slot] = scale
+        got[n + "_scale"] = flat.view(-1, P, H_kv).transpose(1, 2)
     return got
 
 
@@ -491,7 +499,13 @@ def _exact_keep(c, x):
     for b, m in enumerate(_kept(c)):
         place = lambda t: x["pages"].long()[int(x["indptr"][b]) + t // P] * P + t % P
         of[place(old[b] + torch.arange(m, device=_DEV))] = place(old[b] + x["path"][b, :m].long())
-    got = {n: pools[n][of] if pools[n].dtype == torch.int8 else pools[n][of].double() for n in pools if n != "lens"}
+    got = {}
+    for n in pools:
+        if n.endswith("pool"):
+            got[n] = pools[n][of] if c["fmt"] else pools[n][of].double()
+        elif n.endswith("scale"):
+            flat = pools[n].transpose(1, 2).reshape(-1, c["H_kv"])[of]
+            got[n] = flat.view(-1, P, c["H_kv"]).transpose(1, 2).double()
     return dict(got, lens=_int32([o + m for o, m in zip(old, _kept(c))]))
 
 
@@ -529,7 +543,7 @@ def _exact_attn(c, x):
         for kv in range(H_kv):
             k, v = (x[p + "_pool"][slot, kv].double() for p in "kv")
             if c["fmt"]:
-                k, v = (r * x[p + "_scale"][slot, kv].double()[:, None] for p, r in (("k", k), ("v", v)))
+                k, v = (r * x[p + "_scale"][slot // P, kv, slot % P].double()[:, None] for p, r in (("k", k), ("v", v)))
             for a in range(0, n, step):
                 m = min(step, n - a)
                 qs = x["q"][row + a:row + a + m, kv * G:(kv + 1) * G].double().reshape(m * G, D)
