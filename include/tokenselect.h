@@ -384,6 +384,36 @@ int32_t ts_pages_copy(const ts_problem* p, const int32_t* src, const int32_t* ds
 int32_t ts_cache_compact(const ts_problem* p, const int32_t* idx, int32_t idx_stride, const int32_t* count, const uint8_t* skip,
                          const int32_t* to_indptr, const int32_t* to_indices, int32_t* to_lens, void* stream);
 
+/* ---- The cache in 8 bits.  A row (K or V of one token and KV head, D elements x as a cache of p->dtype would hold them) is kept as D codes of
+ * a byte and one float:
+ *   m = max |x_i|,  scale = m / Q,  code_i = x_i Q / m rounded to nearest, ties to even;  the row stands for code_i * scale
+ * with Q = 127 and whole numbers (TS_INT8), or Q = 448 and e4m3 numbers (TS_E4M3: sign, 4 bits of exponent, 3 of mantissa, no infinities).  The quotients
+ * and the scale are formed in double and rounded once.  m = 0: scale and codes 0.  A row that holds an infinity or a NaN: scale NaN, codes 0.
+ * Codes lie as a pool's rows do; scales by page, head and place in the page, so that the tokens of a page and head follow each other.
+ * The page table is the problem's; its k_pool and v_pool do not matter to the ts_quant_* calls and may be NULL. */
+typedef enum ts_code { TS_INT8 = 0, TS_E4M3 = 1 } ts_code;
+typedef struct ts_quant {
+  void* k_codes;   /* [device] [num_pages][P][H_kv][D] bytes, 16-byte aligned                          */
+  void* v_codes;   /* [device] the same                                                                */
+  float* k_scale;  /* [device] [num_pages][H_kv][P], 16-byte aligned                                   */
+  float* v_scale;  /* [device] the same                                                                */
+  int32_t code;    /* ts_code                                                                          */
+} ts_quant;
+
+/* ts_rope_append into an 8-bit cache: the queries turned into q_out, keys turned and written as codes with V, one launch.  The same arguments (q and
+ * q_out may be NULL together, k and v not) and the same rules for rows, places and overlaps.  Turned rows are formed in double, scale * (x cos - y sin) and
+ * so on, rounded to float and then to p->dtype; the codes are those of the key that p->dtype holds. */
+int32_t ts_quant_append(const ts_problem* p, const ts_quant* c, const ts_rope* r, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                        const void* v, int64_t v_stride, const int32_t* q_indptr, int32_t num_rows, const int32_t* positions, void* q_out, void* stream);
+
+/* Reads tokens back: the rows are the last n_b tokens of each sequence (all of them: n_b = N_b), as everywhere here, and k_out, v_out [device]
+ * [num_rows][H_kv][D] in p->dtype, 16-byte aligned, get code * scale (a float product, rounded once to p->dtype).  Rows that stand for no token of the cache (place negative or beyond
+ * max_seq_len) get 0; rows that belong to no sequence are left as they are.  Either of k_out and v_out may be NULL. */
+int32_t ts_quant_read(const ts_problem* p, const ts_quant* c, const int32_t* q_indptr, int32_t num_rows, void* k_out, void* v_out, void* stream);
+
+/* ts_pages_copy for an 8-bit cache: codes and scales of K and V.  The same rules. */
+int32_t ts_quant_pages_copy(const ts_problem* p, const ts_quant* c, const int32_t* src, const int32_t* dst, int32_t n, int32_t num_pages, void* stream);
+
 /* ======================================================================================================
  * Everything below is for benchmarks and tests, not for serving code: process-wide tuning knobs and timing
  * helpers.  They are not thread-safe and must not be changed while a call on another thread is between

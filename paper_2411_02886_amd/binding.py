@@ -16,6 +16,7 @@ _LIB_PATH = os.path.join(_HERE, "libtokenselect.so")
 _HEADER = os.path.join(os.path.dirname(_HERE), "include", "tokenselect.h")
 
 TS_F32, TS_BF16 = 0, 1
+TS_INT8, TS_E4M3 = 0, 1                # ts_code
 TS_TOPK_FLAT_VOTES = 1
 TS_TOPK_VOTE_HIST = 2
 
@@ -45,6 +46,11 @@ class _CSelcache(ctypes.Structure):
 class _CRope(ctypes.Structure):
     _fields_ = [("inv_freq", ctypes.c_void_p), ("rotary_dim", ctypes.c_int32), ("num_axes", ctypes.c_int32),
                 ("adjacent", ctypes.c_int32), ("scale", ctypes.c_float), ("pair_axis", ctypes.c_uint8 * 64)]
+
+
+class _CQuant(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("v_codes", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("code", ctypes.c_int32)]
 
 
 _lib = None
@@ -100,6 +106,10 @@ def load():
         L.ts_rope_append.argtypes = [pp, ctypes.POINTER(_CRope), vp, i64, vp, i64, vp, i64, vp, i32, vp, vp, vp]
         L.ts_pages_copy.argtypes = [pp, vp, vp, i32, i32, vp]
         L.ts_cache_compact.argtypes = [pp, vp, i32, vp, vp, vp, vp, vp, vp]
+        pc = ctypes.POINTER(_CQuant)
+        L.ts_quant_append.argtypes = [pp, pc, ctypes.POINTER(_CRope), vp, i64, vp, i64, vp, i64, vp, i32, vp, vp, vp]
+        L.ts_quant_read.argtypes = [pp, pc, vp, i32, vp, vp, vp]
+        L.ts_quant_pages_copy.argtypes = [pp, pc, vp, vp, i32, i32, vp]
         L.ts_debug_set_score_variant.argtypes = [i32, i32, i32]
         L.ts_debug_set_topk_path.argtypes = [i32]
         L.ts_debug_set_codes_path.argtypes = [i32, i32]
@@ -114,7 +124,8 @@ def load():
                      "ts_debug_event_elapsed_ms", "ts_debug_set_score_timing_events", "ts_paged_qk_codes",
                      "ts_soft_vote_bounds", "ts_topk_exact", "ts_debug_set_codes_path", "ts_topk_noalloc",
                      "ts_paged_qk_scores_checked", "ts_paged_qk_codes_checked", "ts_soft_vote_ranked",
-                     "ts_paged_attn_workspace_bytes", "ts_paged_attn", "ts_paged_attn_rounded", "ts_rope_append", "ts_pages_copy", "ts_cache_compact"):
+                     "ts_paged_attn_workspace_bytes", "ts_paged_attn", "ts_paged_attn_rounded", "ts_rope_append", "ts_pages_copy", "ts_cache_compact",
+                     "ts_quant_append", "ts_quant_read", "ts_quant_pages_copy"):
             getattr(L, name).restype = i32
         _lib = L
     return _lib
@@ -167,7 +178,7 @@ class Problem:
         self.q_row, self.kv_row = num_q_heads * head_dim, num_kv_heads * head_dim      # elements of a token's q, and of its k or v
         self._ref = ctypes.byref(self.c)
         self.batch, self.heads, self.dtype = batch, num_q_heads, dtype
-        self.device = -1 if k_pool is None else k_pool.get_device()                    # -1: not on a GPU
+        self.device = -1 if (k_pool is None and seq_lens is None) else (seq_lens if k_pool is None else k_pool).get_device()   # -1: not on a GPU
 
     def ref(self):
         return self._ref
@@ -196,6 +207,39 @@ class Rope:
         self.num_axes, self.device = int(num_axes), inv_freq.get_device()
         self.c = _CRope(_ptr(inv_freq), 2 * n, int(num_axes), int(bool(adjacent)), float(scale), (ctypes.c_uint8 * 64)(*axes))
         self._ref = ctypes.byref(self.c)
+
+    def ref(self):
+        return self._ref
+
+
+class QuantCache:
+    """ts_quant plus references that keep its tensors alive: the codes and scales of K and V.  k_codes, v_codes [pages][P][H_kv][D] of one byte
+    (int8 or uint8; float8_e4m3fn for TS_E4M3), k_scale, v_scale float32 [pages][H_kv][P]."""
+
+    def __init__(self, *, k_codes, v_codes, k_scale, v_scale, format):
+        if format not in (TS_INT8, TS_E4M3):
+            raise ValueError("format: TS_INT8 or TS_E4M3")
+        types = ("torch.uint8", "torch.int8" if format == TS_INT8 else "torch.float8_e4m3fn")
+        for name, t, dims in (("k_codes", k_codes, 4), ("v_codes", v_codes, 4), ("k_scale", k_scale, 3), ("v_scale", v_scale, 3)):
+            if str(t.dtype) not in (types if dims == 4 else ("torch.float32",)):
+                raise ValueError("%s: a tensor of %s" % (name, " or ".join(types) if dims == 4 else "float32"))
+            if t.dim() != dims or not t.is_contiguous() or t.get_device() != k_codes.get_device():
+                raise ValueError("%s: %d dimensions, contiguous, on the device of k_codes" % (name, dims))
+        pages, P, H_kv, D = k_codes.shape
+        if v_codes.shape != k_codes.shape or k_scale.shape != (pages, H_kv, P) or v_scale.shape != k_scale.shape:
+            raise ValueError("codes [pages][P][H_kv][D] and scales [pages][H_kv][P] of the same pages")
+        self._keep = (k_codes, v_codes, k_scale, v_scale)
+        self.shape, self.num_pages, self.format, self.device = (P, H_kv, D), pages, format, k_codes.get_device()
+        self.c = _CQuant(_ptr(k_codes), _ptr(v_codes), _ptr(k_scale), _ptr(v_scale), format)
+        self._ref = ctypes.byref(self.c)
+
+    @classmethod
+    def empty(cls, num_pages, page_size, num_kv_heads, head_dim, format, device="cuda:0"):
+        """A cache of zeroed pages."""
+        import torch
+        codes = [torch.zeros((num_pages, page_size, num_kv_heads, head_dim), dtype=torch.uint8, device=device) for _ in "kv"]
+        scale = [torch.zeros((num_pages, num_kv_heads, page_size), dtype=torch.float32, device=device) for _ in "kv"]
+        return cls(k_codes=codes[0], v_codes=codes[1], k_scale=scale[0], v_scale=scale[1], format=format)
 
     def ref(self):
         return self._ref
@@ -405,7 +449,7 @@ def _at(p: Problem, t, name: str, types, count: int):
 
 def _stream_of(p: Problem, stream):
     """The stream that a call on the problem's pools goes to; without one the current device has to be theirs."""
-    if p.device < 0 and p.c.k_pool is not None:
+    if p.device < 0 and (p.c.k_pool or p.c.seq_lens) is not None:
         raise ValueError("the pools are not on a GPU")
     if stream is not None or p.device < 0:
         return _stream(stream)
@@ -514,3 +558,50 @@ def ts_cache_compact(p: Problem, idx, idx_stride: int, count, skip, to_indptr, t
                                 _at(p, skip, "skip", _MASK, B), _at(p, to_indptr, "to_indptr", _INT, B + 1),
                                 _at(p, to_indices, "to_indices", _INT, 1), _at(p, to_lens, "to_lens", _INT, B), _stream_of(p, stream)),
         "ts_cache_compact")
+
+
+def _quant_of(p: Problem, c: QuantCache):
+    """The cache's struct, if it is one of the problem's shape on its device."""
+    if c.shape != (p.c.page_size, p.c.num_kv_heads, p.c.head_dim):
+        raise ValueError("the cache has pages of (tokens, KV heads, head size) %s, the problem %s"
+                         % (c.shape, (p.c.page_size, p.c.num_kv_heads, p.c.head_dim)))
+    if c.device != p.device:
+        raise ValueError("the cache: on the device of the problem")
+    return c.ref()
+
+
+def ts_quant_append(p: Problem, c: QuantCache, rope, q, k, v, q_indptr, num_rows: int, positions, q_out, stream=None) -> None:
+    """Rows as ts_rope_append takes them; q and q_out may be None."""
+    n = int(num_rows)
+    if _STORED is None:
+        _load_types()
+    stored, axes, quant = _STORED.get(p.dtype, ()), 0, _quant_of(p, c)
+    q_at, q_stride = _rows_at(p, q, p.q_row, "q", stored, n)
+    k_at, k_stride = _rows_at(p, k, p.kv_row, "k", stored, n)
+    v_at, v_stride = _rows_at(p, v, p.kv_row, "v", stored, n)
+    if rope is not None:
+        axes = rope.num_axes
+        if rope.device != p.device and rope.c.rotary_dim:
+            raise ValueError("inv_freq: on the device of the pools")
+    _ok(load().ts_quant_append(p.ref(), quant, None if rope is None else rope.ref(), q_at, q_stride, k_at, k_stride, v_at, v_stride,
+                               _at(p, q_indptr, "q_indptr", _INT, p.batch + 1), n, _at(p, positions, "positions", _INT, axes * n),
+                               _at(p, q_out, "q_out", stored, n * p.q_row), _stream_of(p, stream)), "ts_quant_append")
+
+
+def ts_quant_read(p: Problem, c: QuantCache, q_indptr, num_rows: int, k_out, v_out, stream=None) -> None:
+    n = int(num_rows)
+    if _STORED is None:
+        _load_types()
+    stored, quant = _STORED.get(p.dtype, ()), _quant_of(p, c)
+    _ok(load().ts_quant_read(p.ref(), quant, _at(p, q_indptr, "q_indptr", _INT, p.batch + 1), n, _at(p, k_out, "k_out", stored, n * p.kv_row),
+                             _at(p, v_out, "v_out", stored, n * p.kv_row), _stream_of(p, stream)), "ts_quant_read")
+
+
+def ts_quant_pages_copy(p: Problem, c: QuantCache, src, dst, n: int, num_pages: int, stream=None) -> None:
+    if _STORED is None:
+        _load_types()
+    n, quant = int(n), _quant_of(p, c)
+    if num_pages > c.num_pages:
+        raise ValueError("num_pages: %d, the cache holds %d" % (num_pages, c.num_pages))
+    _ok(load().ts_quant_pages_copy(p.ref(), quant, _at(p, src, "src", _INT, n), _at(p, dst, "dst", _INT, n), n, int(num_pages), _stream_of(p, stream)),
+        "ts_quant_pages_copy")

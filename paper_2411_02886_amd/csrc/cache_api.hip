@@ -1,21 +1,7 @@
 // C ABI of the cache's own calls: filling, attending and moving it.  Argument checks and launches.
-#include "ts_kernels.h"
-#include <math.h>
+#include "api_checks.h"
 
 using namespace ts;
-
-static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-static bool overlap(const void* a, size_t an, const void* b, size_t bn) {
-  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-  return x < y + bn && y < x + an;
-}
-
-// rows of new tokens: without q_indptr every sequence has `chunk` of them
-static int32_t check_rows(const ts_problem* p, const int32_t* q_indptr, int32_t num_rows) {
-  if (num_rows < 0) return TS_ERR_INVALID_ARG;
-  if (q_indptr == nullptr && (int64_t)num_rows != (int64_t)p->batch * p->chunk && num_rows != 0) return TS_ERR_INVALID_ARG;
-  return TS_OK;
-}
 
 static int32_t attend(const ts_problem* p, const void* q, const int32_t* q_indptr, int32_t num_rows, int32_t window, float sm_scale, void* out, float* lse,
                       void* ws, size_t ws_bytes, bool round_weights, void* stream) {
@@ -68,35 +54,12 @@ int32_t ts_rope_append(const ts_problem* p, const ts_rope* r, const void* q, int
   if (st != TS_OK) return st;
   if ((st = check_rows(p, q_indptr, num_rows)) != TS_OK) return st;
   const int D = p->head_dim;
-  if (r != nullptr) {
-    if (r->rotary_dim < 0 || r->rotary_dim > D || (r->rotary_dim & 1) != 0) return TS_ERR_INVALID_ARG;
-    if (r->num_axes < 1 || r->num_axes > TS_ROPE_MAX_AXES || (r->adjacent != 0 && r->adjacent != 1)) return TS_ERR_INVALID_ARG;
-    if (!(fabsf(r->scale) < INFINITY) || (r->rotary_dim > 0 && r->inv_freq == nullptr)) return TS_ERR_INVALID_ARG;
-    for (int i = 0; i < r->rotary_dim / 2; ++i)
-      if (r->pair_axis[i] >= r->num_axes) return TS_ERR_INVALID_ARG;
-  }
+  if ((st = check_rope(r, D)) != TS_OK) return st;
   if (num_rows == 0) return TS_OK;
   if ((q == nullptr) != (q_out == nullptr) || (k == nullptr) != (v == nullptr) || (q == nullptr && k == nullptr)) return TS_ERR_INVALID_ARG;
+  if (k != nullptr && (p->k_pool == nullptr || p->v_pool == nullptr || !aligned16(p->k_pool) || !aligned16(p->v_pool))) return TS_ERR_INVALID_ARG;
+  if ((st = check_append_rows(p, q, &q_stride, k, &k_stride, v, &v_stride, num_rows, q_out)) != TS_OK) return st;
   const int64_t es = p->dtype == TS_BF16 ? 2 : 4;
-  const int64_t qrow = (int64_t)p->num_q_heads * D, krow = (int64_t)p->num_kv_heads * D;
-  if (q_stride == 0) q_stride = qrow;
-  if (k_stride == 0) k_stride = krow;
-  if (v_stride == 0) v_stride = krow;
-  if (q != nullptr) {
-    if (!aligned16(q) || !aligned16(q_out) || q_stride < qrow || (q_stride * es) % 16 != 0) return TS_ERR_INVALID_ARG;
-    const size_t in = (size_t)((num_rows - 1) * q_stride + qrow) * es, out = (size_t)num_rows * qrow * es;
-    if (!(q == q_out && q_stride == qrow) && overlap(q, in, q_out, out)) return TS_ERR_INVALID_ARG;
-    if (k != nullptr) {
-      // k and v are read while q_out is written: parts of one projection next to q are refused with it, q_out = q needs them apart
-      if (overlap(k, (size_t)((num_rows - 1) * k_stride + krow) * es, q_out, out) ||
-          overlap(v, (size_t)((num_rows - 1) * v_stride + krow) * es, q_out, out)) return TS_ERR_INVALID_ARG;
-    }
-  }
-  if (k != nullptr) {
-    if (p->k_pool == nullptr || p->v_pool == nullptr) return TS_ERR_INVALID_ARG;
-    if (!aligned16(k) || !aligned16(v) || !aligned16(p->k_pool) || !aligned16(p->v_pool)) return TS_ERR_INVALID_ARG;
-    if (k_stride < krow || v_stride < krow || (k_stride * es) % 16 != 0 || (v_stride * es) % 16 != 0) return TS_ERR_INVALID_ARG;
-  }
   RopeAppendArgs a{};
   a.q = (const uint8_t*)q; a.k = (const uint8_t*)k; a.v = (const uint8_t*)v; a.q_out = (uint8_t*)q_out;
   a.k_pool = (uint8_t*)const_cast<void*>(p->k_pool); a.v_pool = (uint8_t*)const_cast<void*>(p->v_pool);

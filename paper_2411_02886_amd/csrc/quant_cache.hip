@@ -1,0 +1,256 @@
+// A cache in 8 bits: new tokens turned, quantised and written into their pages, tokens read back, pages copied.  Bound by memory: every
+// row is read and written once.
+//
+// Writing: one, two or four waves take a token, as in rotation and append of a plain cache.  D / 8 lanes hold a row of eight elements each, so that
+// a row's largest absolute value is three or four steps of the lanes' network away; a lane has the same elements of every row it
+// works on and keeps their cosines and sines.  All arithmetic is in double, which this machine does at the rate of float: a
+// turned key next to the middle of two stored values, or a quotient next to the middle of two codes, falls as the definition says.  A quotient x Q / m is
+// formed by the row's reciprocal and one correction with the exact remainder (Markstein's division): a quotient that is a double -- every tie
+// between two codes is -- comes out exactly.
+#include "ts_kernels.h"
+#include "ts_rows.h"
+#include "ts_codes.h"
+#include <algorithm>
+
+namespace ts {
+
+template <typename T> struct Eight;                                    // eight stored elements
+template <> struct Eight<uint16_t> {
+  u32x4_t w;
+  __device__ __forceinline__ void load(const uint8_t* at) { w = *reinterpret_cast<const u32x4_t*>(at); }
+  __device__ __forceinline__ float get(int i) const { return (i & 1) != 0 ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]); }
+};
+template <> struct Eight<float> {
+  u32x4_t w[2];
+  __device__ __forceinline__ void load(const uint8_t* at) { w[0] = reinterpret_cast<const u32x4_t*>(at)[0]; w[1] = reinterpret_cast<const u32x4_t*>(at)[1]; }
+  __device__ __forceinline__ float get(int i) const { return __uint_as_float(w[i >> 2][i & 3]); }
+};
+template <typename T> __device__ __forceinline__ float load_one(const uint8_t* at);
+template <> __device__ __forceinline__ float load_one<float>(const uint8_t* at) { return *reinterpret_cast<const float*>(at); }
+template <> __device__ __forceinline__ float load_one<uint16_t>(const uint8_t* at) { return __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(at) << 16); }
+
+__device__ __forceinline__ uint32_t round_bf16(float x) {              // bits; NaN stays NaN
+  return __builtin_bit_cast(uint16_t, (__bf16)x);
+}
+__device__ __forceinline__ void store_eight(uint16_t*, uint8_t* at, const float (&x)[8]) {
+  u32x4_t w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = round_bf16(x[2 * i]) | (round_bf16(x[2 * i + 1]) << 16);
+  *reinterpret_cast<u32x4_t*>(at) = w;
+}
+__device__ __forceinline__ void store_eight(float*, uint8_t* at, const float (&x)[8]) {
+  reinterpret_cast<u32x4_t*>(at)[0] = u32x4_t{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+  reinterpret_cast<u32x4_t*>(at)[1] = u32x4_t{__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7])};
+}
+
+template <int CTRL> __device__ __forceinline__ uint32_t dpp_max_u32(uint32_t v) {
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true));
+}
+
+// e4m3 of a double of at most 448, to nearest even: rounded to the code's step here (a float next to the middle of two codes would lose
+// on which side it lies), so that the conversion is exact; with the sign of x, which the quotient of a zero has lost
+__device__ __forceinline__ float e4m3_value(double z, float x) {
+  const int behind = 4 - max(__builtin_amdgcn_frexp_exp(z), -5);       // |z| < 2^exponent; three bits behind the leading one, 2^-9 the smallest
+  return __builtin_copysignf((float)__builtin_amdgcn_ldexp(rint(__builtin_amdgcn_ldexp(z, behind)), -behind), x);
+}
+
+template <typename T, int CODE, int D>
+__global__ __launch_bounds__(256) void quant_append_kernel(RopeAppendArgs a, QuantPools c) {
+  constexpr int LPR = D / 8, RPW = 64 / LPR, ES = sizeof(T), RB = D * ES;   // lanes of a row, rows side by side in a wave, bytes of a row
+  __shared__ __attribute__((aligned(16))) double s_turn[4][64][2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), share = 1 << a.share_shift;
+  const int part = wave & (share - 1), row = (int)((((uint64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + wave) >> a.share_shift);
+  if (row >= a.T) return;
+  const int half = a.rotary >> 1, nq = a.q != nullptr ? a.H : 0, nk = a.H_kv;
+  const uint8_t* q_row = a.q + row * a.q_stride;
+  const uint8_t* k_row = a.k + row * a.k_stride;
+  const uint8_t* v_row = a.v + row * a.v_stride;
+  double freq = 0.;
+  int pos = 0;
+  if (lane < half) {
+    freq = a.inv_freq[lane];
+    if (a.positions != nullptr) pos = a.positions[(size_t)a.pair_axis[lane] * a.T + row];
+  }
+  const RowPlace at = row_place(a.q_indptr, a.B, a.C, a.T, row);
+  if (at.b < 0) return;
+  const int place = max(a.seq_lens[at.b], 0) - at.left, page0 = a.page_indptr[at.b];
+  const bool append = place >= 0 && place < a.max_seq_len;             // (a step whose lengths have grown past the bound must not write over cached tokens)
+  int64_t page = 0;
+  if (append) page = a.page_indices[page0 + (place >> a.p_shift)];
+  if (lane < half) {
+    if (a.positions == nullptr) pos = place;
+    const double turns = (double)pos * freq * 0.15915494309189533577;
+    double s, co;
+    sincospi(2.0 * (turns - rint(turns)), &s, &co);
+    s_turn[wave][lane][0] = co * a.scale; s_turn[wave][lane][1] = s * a.scale;
+  }
+  __builtin_amdgcn_wave_barrier();                                     // (a wave's LDS accesses keep their order)
+
+  // this lane's elements e0 .. e0 + 7 of every row: x -> x * co + partner * si
+  const int u = lane % LPR, e0 = u * 8;
+  double co[8], si[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int e = e0 + i;
+    const bool turns = e < a.rotary, first = a.adjacent ? (e & 1) == 0 : e < half;
+    const int pair = a.adjacent ? e >> 1 : first ? e : e - half;
+    co[i] = turns ? s_turn[wave][turns ? pair : 0][0] : 1.;
+    si[i] = turns ? s_turn[wave][turns ? pair : 0][1] : 0.;
+    if (first) si[i] = -si[i];
+  }
+  const bool any = e0 < a.rotary, in_piece = a.adjacent != 0, whole = (half & 7) == 0;
+  const int64_t slot = (page << a.p_shift) + (place & (a.P - 1));
+  const int all = nq + 2 * nk;
+  for (int h = part * RPW + lane / LPR; h < all; h += RPW << a.share_shift) {
+    const bool is_q = h < nq, is_v = h >= nq + nk;
+    const int kv = is_v ? h - nq - nk : h - nq;                        // its KV head
+    const uint8_t* from = is_q ? q_row + (int64_t)h * RB : (is_v ? v_row : k_row) + (int64_t)kv * RB;
+    Eight<T> own, other;
+    own.load(from + e0 * ES);
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = own.get(i);
+    if (any && !is_v) {
+      float y[8];
+      if (in_piece) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = x[i ^ 1];
+      } else if (whole) {                                              // (then the turned part is whole pieces too)
+        other.load(from + (e0 < half ? e0 + half : e0 - half) * ES);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = other.get(i);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int e = e0 + i;
+          y[i] = e < a.rotary ? load_one<T>(from + (e < half ? e + half : e - half) * ES) : 0.f;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (e0 + i < a.rotary) x[i] = (float)fma((double)x[i], co[i], (double)y[i] * si[i]);
+    }
+    if (is_q) { store_eight((T*)nullptr, a.q_out + ((int64_t)row * a.H + h) * RB + e0 * ES, x); continue; }
+    if (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(round_bf16(x[i]) << 16);
+    }
+    uint32_t m = 0;                                                    // bits of the largest absolute value; those of infinities and NaN are larger still
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7fffffffu);
+    m = dpp_max_u32<0xB1>(m);     // quad_perm [1,0,3,2]
+    m = dpp_max_u32<0x4E>(m);     // quad_perm [2,3,0,1]
+    m = dpp_max_u32<0x141>(m);    // row_half_mirror
+    if (LPR == 16) m = dpp_max_u32<0x140>(m);                          // row_mirror
+    if (!append) continue;
+    const bool finite = m < 0x7f800000u;
+    const double most = __uint_as_float(m), inv = 1. / most;
+    uint32_t w[2] = {0u, 0u};
+    if (finite && m != 0u) {
+      double z[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const double n = (double)x[i] * kCodeTop<CODE>, q0 = n * inv;
+        z[i] = fma(fma(-q0, most, n), inv, q0);
+      }
+      if constexpr (CODE == TS_INT8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i >> 2] |= ((uint32_t)(int)rint(z[i]) & 0xffu) << (8 * (i & 3));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) {
+          int v = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_value(z[i], x[i]), e4m3_value(z[i + 1], x[i + 1]), 0, false);
+          w[i >> 2] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(e4m3_value(z[i + 2], x[i + 2]), e4m3_value(z[i + 3], x[i + 3]), v, true);
+        }
+      }
+    }
+    *reinterpret_cast<uint2*>((is_v ? c.v_codes : c.k_codes) + (slot * nk + kv) * D + e0) = make_uint2(w[0], w[1]);
+    if (u == 0)
+      (is_v ? c.v_scale : c.k_scale)[(page * nk + kv) * a.P + (place & (a.P - 1))] = finite ? (float)(most / kCodeTop<CODE>) : __uint_as_float(0x7fc00000u);
+  }
+}
+
+template <typename T, int CODE>
+static hipError_t append_one(const RopeAppendArgs& b, const QuantPools& c, hipStream_t s) {
+  RopeAppendArgs a = b;
+  a.share_shift = a.T <= 1024 ? 2 : 1;
+  const long wgs = (((long)a.T << a.share_shift) + 3) / 4, wide = 1 << 20;      // (a grid has less than 2^32 threads in a dimension)
+  const dim3 grid((unsigned)std::min(wgs, wide), (unsigned)((wgs + wide - 1) / wide));
+  if (a.D == 64) hipLaunchKernelGGL((quant_append_kernel<T, CODE, 64>), grid, dim3(256), 0, s, a, c);
+  else hipLaunchKernelGGL((quant_append_kernel<T, CODE, 128>), grid, dim3(256), 0, s, a, c);
+  return hipGetLastError();
+}
+
+hipError_t launch_quant_append(int dtype, const RopeAppendArgs& a, const QuantPools& c, hipStream_t s) {
+  if (dtype == TS_BF16) return c.code == TS_INT8 ? append_one<uint16_t, TS_INT8>(a, c, s) : append_one<uint16_t, TS_E4M3>(a, c, s);
+  return c.code == TS_INT8 ? append_one<float, TS_INT8>(a, c, s) : append_one<float, TS_E4M3>(a, c, s);
+}
+
+// A wave per row: pieces of eight codes, K's, then V's.
+template <typename T, int CODE>
+__global__ __launch_bounds__(256) void quant_read_kernel(QuantReadArgs a, QuantPools c) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = (int)(((uint64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + wave);
+  if (row >= a.T) return;
+  const RowPlace at = row_place(a.q_indptr, a.B, a.C, a.T, row);
+  if (at.b < 0) return;
+  const int place = max(a.seq_lens[at.b], 0) - at.left;
+  const bool there = place >= 0 && place < a.max_seq_len;
+  int64_t page = 0;
+  if (there) page = a.page_indices[a.page_indptr[at.b] + (place >> a.p_shift)];
+  const int in_page = place & (a.P - 1), d_shift = a.D == 64 ? 3 : 4, each = a.H_kv << d_shift;   // pieces of K, and of V
+  const int64_t slot = (page << a.p_shift) + in_page;
+  for (int i = lane; i < 2 * each; i += 64) {
+    const bool is_v = i >= each;
+    const int j = is_v ? i - each : i, kv = j >> d_shift;
+    uint8_t* out = is_v ? a.v_out : a.k_out;
+    if (out == nullptr) continue;
+    float x[8] = {};
+    if (there) {
+      const uint2 w = *reinterpret_cast<const uint2*>((is_v ? c.v_codes : c.k_codes) + slot * a.H_kv * a.D + j * 8);
+      const float scale = (is_v ? c.v_scale : c.k_scale)[(page * a.H_kv + kv) * a.P + in_page];
+      float y[2][4];
+      codes_to_f32<CODE>(w.x, y[0]);
+      codes_to_f32<CODE>(w.y, y[1]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = y[e >> 2][e & 3] * scale;
+    }
+    store_eight((T*)nullptr, out + ((int64_t)row * a.H_kv * a.D + j * 8) * sizeof(T), x);
+  }
+}
+
+hipError_t launch_quant_read(int dtype, const QuantReadArgs& a, const QuantPools& c, hipStream_t s) {
+  const long wgs = ((long)a.T + 3) / 4, wide = 1 << 20;
+  const dim3 grid((unsigned)std::min(wgs, wide), (unsigned)((wgs + wide - 1) / wide));
+  if (dtype == TS_BF16) {
+    if (c.code == TS_INT8) hipLaunchKernelGGL((quant_read_kernel<uint16_t, TS_INT8>), grid, dim3(256), 0, s, a, c);
+    else hipLaunchKernelGGL((quant_read_kernel<uint16_t, TS_E4M3>), grid, dim3(256), 0, s, a, c);
+  } else {
+    if (c.code == TS_INT8) hipLaunchKernelGGL((quant_read_kernel<float, TS_INT8>), grid, dim3(256), 0, s, a, c);
+    else hipLaunchKernelGGL((quant_read_kernel<float, TS_E4M3>), grid, dim3(256), 0, s, a, c);
+  }
+  return hipGetLastError();
+}
+
+// The scales of copied pages (P * H_kv floats, as few as one: no wider pieces).  blockIdx.y: K or V; pairs are dealt to gridDim.x.
+__global__ __launch_bounds__(256) void quant_scales_copy_kernel(QuantPools c, const int32_t* src, const int32_t* dst, int n, int num_pages, int each) {
+  float* pool = blockIdx.y == 0 ? c.k_scale : c.v_scale;
+  for (int i = blockIdx.x; i < n; i += gridDim.x) {
+    const int from = src[i], to = dst[i];
+    if ((uint32_t)from >= (uint32_t)num_pages || (uint32_t)to >= (uint32_t)num_pages || from == to) continue;
+    for (int e = threadIdx.x; e < each; e += 256) pool[(int64_t)to * each + e] = pool[(int64_t)from * each + e];
+  }
+}
+
+hipError_t launch_quant_pages_copy(const QuantPools& c, const int32_t* src, const int32_t* dst, int n, int num_pages, int P, int H_kv, int D, hipStream_t s) {
+  PagesCopyArgs a{};
+  a.src = src; a.dst = dst; a.n = n; a.num_pages = num_pages;
+  a.k_pool = c.k_codes; a.v_pool = c.v_codes;
+  a.page_bytes = (int64_t)P * H_kv * D;
+  const hipError_t e = launch_pages_copy(a, s);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(quant_scales_copy_kernel, dim3((unsigned)std::min(n, 16384), 2), dim3(256), 0, s, c, src, dst, n, num_pages, P * H_kv);
+  return hipGetLastError();
+}
+
+}  // namespace ts

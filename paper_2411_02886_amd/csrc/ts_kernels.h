@@ -275,6 +275,27 @@ struct CompactArgs {
 };
 hipError_t launch_cache_compact(const CompactArgs& a, int B, hipStream_t s);
 
+// the cache in 8 bits (quant_api.hip)
+struct QuantPools {
+  uint8_t* k_codes;
+  uint8_t* v_codes;
+  float* k_scale;
+  float* v_scale;
+  int code;                    // ts_code
+};
+hipError_t launch_quant_append(int dtype, const RopeAppendArgs& a, const QuantPools& c, hipStream_t s);   // (a's pools are not used)
+struct QuantReadArgs {
+  const int32_t* page_indptr;
+  const int32_t* page_indices;
+  const int32_t* seq_lens;
+  const int32_t* q_indptr;
+  uint8_t* k_out;              // null: not wanted
+  uint8_t* v_out;
+  int B, C, T, H_kv, D, P, p_shift, max_seq_len;
+};
+hipError_t launch_quant_read(int dtype, const QuantReadArgs& a, const QuantPools& c, hipStream_t s);
+hipError_t launch_quant_pages_copy(const QuantPools& c, const int32_t* src, const int32_t* dst, int n, int num_pages, int P, int H_kv, int D, hipStream_t s);
+
 int32_t check_problem(const ts_problem* p);   // the shape and pointer checks that every call begins with (api.hip)
 
 hipError_t launch_chunk_mean_query(const void* q, void* out, int B, int C, int n, hipStream_t s);
