@@ -414,6 +414,33 @@ int32_t ts_quant_read(const ts_problem* p, const ts_quant* c, const int32_t* q_i
 /* ts_pages_copy for an 8-bit cache: codes and scales of K and V.  The same rules. */
 int32_t ts_quant_pages_copy(const ts_problem* p, const ts_quant* c, const int32_t* src, const int32_t* dst, int32_t n, int32_t num_pages, void* stream);
 
+/* ---- Drafted trees: the new tokens of a sequence are nodes of a tree (several roots are fine), one draft path each from a root down, and are attended
+ * in one call.  mask [device] uint32 [num_rows][mask_words] says which new tokens of its sequence a row sees, itself among them: bit j % 32 of word j / 32 for new token j.
+ * The row of new token c, with base = N_b - n_b and seen = bits of its row, sees
+ *   the cached tokens t < base (window > 0: those with t >= base + seen - window, as if the new tokens it sees followed the cached ones),
+ *   and the new tokens j < n_b, at their places base + j, whose bit is set (whatever the window).
+ * Any bits will do (a caller's own: several drafts, pictures that see all of themselves); new tokens from 32 * mask_words on are seen by nobody. */
+
+/* The mask of trees.  parents [device] int32 [num_rows]: for new token c of a sequence the new token that it follows, in [0, c); anything else makes it a root.
+ *   mask[r] = the bits of c and of all that lead to it,  positions[r] = N_b - n_b + (their number) - 1
+ * positions [device] int32 [num_rows] (what ts_rope_append takes), or NULL.  mask_words >= 1; bits of new tokens beyond are dropped.  Rows that belong to no sequence are left as they
+ * are.  Uses batch, chunk and seq_lens of p; its pools may be NULL. */
+int32_t ts_tree_mask(const ts_problem* p, const int32_t* parents, const int32_t* q_indptr, int32_t num_rows, uint32_t* mask, int32_t mask_words,
+                     int32_t* positions, void* stream);
+
+/* ts_paged_attn with a mask among the new tokens: rows, results, rows that see nothing, sums, workspace (ts_paged_attn_workspace_bytes) as there.  A new
+ * token's V has to be finite, seen or not; its K may be anything where it is not seen. */
+int32_t ts_tree_attn(const ts_problem* p, const void* q, const int32_t* q_indptr, int32_t num_rows, int32_t window, const uint32_t* mask, int32_t mask_words,
+                     float sm_scale, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Keeps an accepted path: K and V of new token path[b][i] move to the place of new token i, i < count[b], so that the path follows the cached tokens, and
+ * to_lens[b] = N_b - n_b + count[b] (at least 0).  path [device] int32 [B][path_stride], ascending (a node comes after its parent, so path[b][i] >= i: a smaller entry counts as i, one
+ * beyond the last new token as that); count [device] int32 [B], clamped to [0, min(path_stride, n_b)]; to_lens [device] int32 [B], which may not
+ * overlap another array of the call (copy the new lengths over afterwards).  Places that are negative or beyond max_seq_len are not read or written.  The new tokens' pages may not
+ * belong to two sequences.  c NULL: the problem's pools; else the 8-bit cache, codes and scales. */
+int32_t ts_tree_keep(const ts_problem* p, const ts_quant* c, const int32_t* path, int32_t path_stride, const int32_t* count, const int32_t* q_indptr,
+                     int32_t* to_lens, void* stream);
+
 /* ======================================================================================================
  * Everything below is for benchmarks and tests, not for serving code: process-wide tuning knobs and timing
  * helpers.  They are not thread-safe and must not be changed while a call on another thread is between

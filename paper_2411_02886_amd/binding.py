@@ -110,6 +110,9 @@ def load():
         L.ts_quant_append.argtypes = [pp, pc, ctypes.POINTER(_CRope), vp, i64, vp, i64, vp, i64, vp, i32, vp, vp, vp]
         L.ts_quant_read.argtypes = [pp, pc, vp, i32, vp, vp, vp]
         L.ts_quant_pages_copy.argtypes = [pp, pc, vp, vp, i32, i32, vp]
+        L.ts_tree_mask.argtypes = [pp, vp, vp, i32, vp, i32, vp, vp]
+        L.ts_tree_attn.argtypes = [pp, vp, vp, i32, i32, vp, i32, f32, vp, vp, vp, sz, vp]
+        L.ts_tree_keep.argtypes = [pp, pc, vp, i32, vp, vp, vp, vp]
         L.ts_debug_set_score_variant.argtypes = [i32, i32, i32]
         L.ts_debug_set_topk_path.argtypes = [i32]
         L.ts_debug_set_codes_path.argtypes = [i32, i32]
@@ -125,7 +128,7 @@ def load():
                      "ts_soft_vote_bounds", "ts_topk_exact", "ts_debug_set_codes_path", "ts_topk_noalloc",
                      "ts_paged_qk_scores_checked", "ts_paged_qk_codes_checked", "ts_soft_vote_ranked",
                      "ts_paged_attn_workspace_bytes", "ts_paged_attn", "ts_paged_attn_rounded", "ts_rope_append", "ts_pages_copy", "ts_cache_compact",
-                     "ts_quant_append", "ts_quant_read", "ts_quant_pages_copy"):
+                     "ts_quant_append", "ts_quant_read", "ts_quant_pages_copy", "ts_tree_mask", "ts_tree_attn", "ts_tree_keep"):
             getattr(L, name).restype = i32
         _lib = L
     return _lib
@@ -419,14 +422,15 @@ def ts_sparse_paged_attn(p: Problem, q, idx, idx_stride: int, count, sm_scale: f
         "ts_sparse_paged_attn")
 
 
-_INT = _FLOAT = _MASK = _STORED = None      # element types: of index arrays, of lse, of skip masks, of q, k, v and results by the problem's
+_INT = _FLOAT = _MASK = _STORED = _WORDS = None      # element types: of index arrays, of lse, of skip masks, of q, k, v and results by the problem's
 
 
 def _load_types():
-    global _INT, _FLOAT, _MASK, _STORED
+    global _INT, _FLOAT, _MASK, _STORED, _WORDS
     import torch
     bits = [getattr(torch, name) for name in ("bfloat16", "int16", "uint16") if hasattr(torch, name)]      # bf16 may travel as raw bits
     _FLOAT, _MASK, _INT = (torch.float32,), (torch.uint8, torch.bool), (torch.int32,)
+    _WORDS = tuple(getattr(torch, name) for name in ("int32", "uint32") if hasattr(torch, name))
     _STORED = {TS_F32: _FLOAT, TS_BF16: tuple(bits)}
 
 
@@ -605,3 +609,46 @@ def ts_quant_pages_copy(p: Problem, c: QuantCache, src, dst, n: int, num_pages: 
         raise ValueError("num_pages: %d, the cache holds %d" % (num_pages, c.num_pages))
     _ok(load().ts_quant_pages_copy(p.ref(), quant, _at(p, src, "src", _INT, n), _at(p, dst, "dst", _INT, n), n, int(num_pages), _stream_of(p, stream)),
         "ts_quant_pages_copy")
+
+
+def _mask_of(p: Problem, mask, num_rows: int):
+    """(address, words) of a mask [rows][words]."""
+    if mask is None:
+        return None, 0
+    if mask.dim() != 2:
+        raise ValueError("mask: [rows][words]")
+    words = mask.shape[1]
+    return _at(p, mask, "mask", _WORDS, num_rows * words), words
+
+
+def ts_tree_mask(p: Problem, parents, q_indptr, num_rows: int, mask, positions, stream=None) -> None:
+    """mask: int32 (or uint32) [rows][words]; positions: int32 [rows] or [1][rows], or None."""
+    n = int(num_rows)
+    if _STORED is None:
+        _load_types()
+    mask_at, words = _mask_of(p, mask, n)
+    _ok(load().ts_tree_mask(p.ref(), _at(p, parents, "parents", _INT, n), _at(p, q_indptr, "q_indptr", _INT, p.batch + 1), n, mask_at, words,
+                            _at(p, positions, "positions", _INT, n), _stream_of(p, stream)), "ts_tree_mask")
+
+
+def ts_tree_attn(p: Problem, q, q_indptr, num_rows: int, window: int, mask, sm_scale: float, out, lse, ws, stream=None) -> None:
+    n = int(num_rows)
+    if _STORED is None:
+        _load_types()
+    stored = _STORED.get(p.dtype, ())
+    if ws is not None and ws.get_device() != p.device:
+        raise ValueError("ws: on the device of the pools")
+    mask_at, words = _mask_of(p, mask, n)
+    _ok(load().ts_tree_attn(p.ref(), _at(p, q, "q", stored, n * p.q_row), _at(p, q_indptr, "q_indptr", _INT, p.batch + 1), n, int(window), mask_at, words,
+                            float(sm_scale), _at(p, out, "out", stored, n * p.q_row), _at(p, lse, "lse", _FLOAT, n * p.heads), _ptr(ws), _nbytes(ws),
+                            _stream_of(p, stream)), "ts_tree_attn")
+
+
+def ts_tree_keep(p: Problem, c, path, path_stride: int, count, q_indptr, to_lens, stream=None) -> None:
+    """c: a QuantCache, or None for the problem's pools."""
+    if _STORED is None:
+        _load_types()
+    B = p.batch
+    _ok(load().ts_tree_keep(p.ref(), None if c is None else _quant_of(p, c), _at(p, path, "path", _INT, B * int(path_stride)), int(path_stride),
+                            _at(p, count, "count", _INT, B), _at(p, q_indptr, "q_indptr", _INT, B + 1), _at(p, to_lens, "to_lens", _INT, B),
+                            _stream_of(p, stream)), "ts_tree_keep")

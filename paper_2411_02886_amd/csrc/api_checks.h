@@ -11,6 +11,16 @@ inline bool overlap(const void* a, size_t an, const void* b, size_t bn) {
   return x < y + bn && y < x + an;
 }
 
+inline int32_t check_quant(const ts_problem* p, const ts_quant* c, QuantPools* pools) {
+  const int32_t st = check_problem(p);
+  if (st != TS_OK) return st;
+  if (c == nullptr || (c->code != TS_INT8 && c->code != TS_E4M3)) return TS_ERR_INVALID_ARG;
+  for (const void* x : {(const void*)c->k_codes, (const void*)c->v_codes, (const void*)c->k_scale, (const void*)c->v_scale})
+    if (x == nullptr || !aligned16(x)) return TS_ERR_INVALID_ARG;
+  *pools = QuantPools{(uint8_t*)c->k_codes, (uint8_t*)c->v_codes, c->k_scale, c->v_scale, c->code};
+  return TS_OK;
+}
+
 // rows of new tokens: without q_indptr every sequence has `chunk` of them
 inline int32_t check_rows(const ts_problem* p, const int32_t* q_indptr, int32_t num_rows) {
   if (num_rows < 0) return TS_ERR_INVALID_ARG;

@@ -4,7 +4,7 @@
 using namespace ts;
 
 static int32_t attend(const ts_problem* p, const void* q, const int32_t* q_indptr, int32_t num_rows, int32_t window, float sm_scale, void* out, float* lse,
-                      void* ws, size_t ws_bytes, bool round_weights, void* stream) {
+                      void* ws, size_t ws_bytes, bool round_weights, void* stream, const uint32_t* mask = nullptr, int32_t mask_words = 0) {
   int32_t st = check_problem(p);
   if (st != TS_OK) return st;
   if ((st = check_rows(p, q_indptr, num_rows)) != TS_OK) return st;
@@ -24,6 +24,7 @@ static int32_t attend(const ts_problem* p, const void* q, const int32_t* q_indpt
   a.B = p->batch; a.C = p->chunk; a.T = num_rows; a.H = p->num_q_heads; a.H_kv = p->num_kv_heads;
   a.P = p->page_size; a.p_shift = ilog2(p->page_size); a.max_seq_len = p->max_seq_len; a.window = window < p->max_seq_len ? window : 0;   // one that reaches every token is none
   a.sm_scale = sm_scale; a.round_weights = round_weights ? 1 : 0;
+  a.mask = mask; a.mask_words = mask_words;
   return launch_paged_attn(p->dtype, p->head_dim, a, ws, (hipStream_t)stream) == hipSuccess ? TS_OK : TS_ERR_HIP;
 }
 
@@ -45,6 +46,14 @@ int32_t ts_paged_attn(const ts_problem* p, const void* q, const int32_t* q_indpt
 int32_t ts_paged_attn_rounded(const ts_problem* p, const void* q, const int32_t* q_indptr, int32_t num_rows, int32_t window,
                               float sm_scale, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
   return attend(p, q, q_indptr, num_rows, window, sm_scale, out, lse, ws, ws_bytes, true, stream);
+}
+
+int32_t ts_tree_attn(const ts_problem* p, const void* q, const int32_t* q_indptr, int32_t num_rows, int32_t window, const uint32_t* mask, int32_t mask_words,
+                     float sm_scale, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  const int32_t st = check_problem(p);
+  if (st != TS_OK) return st;
+  if (mask_words < 1 || num_rows < 0 || (num_rows > 0 && (mask == nullptr || ((uintptr_t)mask & 3) != 0))) return TS_ERR_INVALID_ARG;
+  return attend(p, q, q_indptr, num_rows, window, sm_scale, out, lse, ws, ws_bytes, false, stream, mask, mask_words);
 }
 
 int32_t ts_rope_append(const ts_problem* p, const ts_rope* r, const void* q, int64_t q_stride, const void* k, int64_t k_stride,

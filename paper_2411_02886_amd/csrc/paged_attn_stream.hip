@@ -44,7 +44,7 @@ struct StreamShape {
   static_assert(4 * 16 * (D + 4) * 4 <= LDS, "the waves' results");
 };
 
-template <int ES, int D, int CB>
+template <int ES, int D, int CB, bool TREE>   // TREE: a mask among the new tokens
 __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_stream_kernel(PagedAttnArgs a, ShareArgs sh) {
   using S = StreamShape<ES, D, CB>;
   constexpr int TK = S::TK, KT = S::KT, RB = S::RB, PPR = S::PPR, RPI = S::RPI, NLD = S::NLD, TILE_B = S::TILE_B;
@@ -61,7 +61,7 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
   const int wg = share_of(blockIdx.x, sh.wgs);
   SharePlace from, to;
   SeqShape first;
-  find_share<KT>(a, sh, G, wg, &s_share, &from, &to, &first);
+  find_share<KT>(a, sh, G, wg, &s_share, &from, &to, &first, TREE);
   int32_t* desc = sh.desc + (size_t)wg * 8;
   if (!sh.whole && threadIdx.x == 0) { desc[3] = kPieceNone; desc[7] = kPieceNone; }
 
@@ -79,7 +79,8 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
 
   walk_share<KT>(a, sh, G, from, to, first, [&](int kvh, const SeqShape& sq, int r, const TileKeys& keys, int ua, int ub, bool) -> bool {
     const int c0 = r * sh.tpt, ntok = min(sh.tpt, sq.n - c0), nrows = ntok * G;
-    const int row0 = sq.row0 + c0, x0 = sq.N - sq.n + c0, x1 = x0 + ntok - 1;   // first row; places of the first and last token
+    const int row0 = sq.row0 + c0, base = sq.N - sq.n;
+    const int x0 = TREE ? base - 1 : base + c0, x1 = TREE ? base + sq.n - 1 : x0 + ntok - 1;   // places of the first and last token (TREE: that all rows see, that some row may)
     const bool whole = ua == 0 && ub == keys.units;
     const int tmax = keys.end - 1;
     auto token_of = [&](uint32_t j) -> uint32_t { return __umul24(j, g_inv) >> 16; };   // j / G
@@ -123,7 +124,8 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
       const int j = cb * 16 + col;
-      low[cb] = (uint32_t)(j < nrows ? x0 + token_of((uint32_t)j) : x1) - (reach - 1u);
+      if constexpr (TREE) low[cb] = (uint32_t)tree_low(a, row0 + min((int)token_of((uint32_t)j), ntok - 1), sq.n, base);
+      else low[cb] = (uint32_t)(j < nrows ? x0 + token_of((uint32_t)j) : x1) - (reach - 1u);
 #pragma unroll
       for (int i = 0; i < NQ; ++i) {
         qf[cb][i] = make_uint4(0u, 0u, 0u, 0u);
@@ -213,6 +215,16 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
       if (more) { rows_of(i + 1, (i + 1) & 1); fetch_look(i + 2, i & 1); load_rows(a.k_pool, lds_k); }
       // ---- weights against the reference: exp(logit - reference)
       const bool masked = k0 + TK - 1 > x0 || (a.window > 0 && k0 <= x1 - a.window);   // some row does not see some key
+      uint32_t bits[CB];                                                     // TREE: the keys that the row sees, from k0 on
+      if constexpr (TREE) {
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+          bits[cb] = masked ? tree_bits(a, row0 + min((int)token_of((uint32_t)(cb * 16 + col)), ntok - 1), sq.n, base, (int)low[cb], k0) : ~0u;
+      }
+      auto sees = [&](int cb, int e) -> bool {
+        const int i = 16 * (e >> 2) + 4 * kgrp + (e & 3);
+        return TREE ? (bits[cb] >> i & 1u) != 0u : (uint32_t)(k0 + i) - low[cb] < reach;
+      };
       float p[CB][NE];
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) {
@@ -222,7 +234,7 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
           if (masked || big) {
 #pragma unroll
             for (int e = 0; e < NE; ++e) {
-              const float y = (uint32_t)(k0 + 16 * (e >> 2) + 4 * kgrp + (e & 3)) - low[cb] < reach ? s[cb][e] * sm : -INFINITY;
+              const float y = sees(cb, e) ? s[cb][e] * sm : -INFINITY;
               p[cb][e] = __builtin_amdgcn_exp2f((y - ref[cb]) * kPsLog2e);
               sum += p[cb][e];
             }
@@ -237,7 +249,7 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
           float m = ref[cb];                                                 // first keys, or a logit far above the reference
 #pragma unroll
           for (int e = 0; e < NE; ++e) {
-            m = fmaxf(m, (uint32_t)(k0 + 16 * (e >> 2) + 4 * kgrp + (e & 3)) - low[cb] < reach ? s[cb][e] * sm + kPsHead : -INFINITY);
+            m = fmaxf(m, sees(cb, e) ? s[cb][e] * sm + kPsHead : -INFINITY);
           }
           m = fmaxf(m, __shfl_xor(m, 16));
           m = fmaxf(m, __shfl_xor(m, 32));
@@ -370,27 +382,32 @@ __global__ __launch_bounds__(256, (StreamShape<ES, D, CB>::PER_CU)) void paged_s
       }
     }
     return false;
-  });
+  }, TREE);
 }
 
-template <int ES, int D, int CB>
+template <int ES, int D, int CB, bool TREE>
 static hipError_t stream_one(const PagedAttnArgs& a, const ShareArgs& sh, hipStream_t s) {
   using S = StreamShape<ES, D, CB>;
   if (S::LDS > 65536) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_stream_kernel<ES, D, CB>), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_stream_kernel<ES, D, CB, TREE>), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((paged_stream_kernel<ES, D, CB>), dim3(sh.wgs), dim3(256), S::LDS, s, a, sh);
+  hipLaunchKernelGGL((paged_stream_kernel<ES, D, CB, TREE>), dim3(sh.wgs), dim3(256), S::LDS, s, a, sh);
   return hipGetLastError();
 }
 
-hipError_t launch_paged_stream(int dtype, int D, int blocks, const PagedAttnArgs& a, const ShareArgs& sh, hipStream_t s) {
+template <bool TREE>
+static hipError_t stream_some(int dtype, int D, int blocks, const PagedAttnArgs& a, const ShareArgs& sh, hipStream_t s) {
   if (dtype == TS_BF16) {
-    if (D == 64) return blocks == 1 ? stream_one<2, 64, 1>(a, sh, s) : stream_one<2, 64, 2>(a, sh, s);
-    return blocks == 1 ? stream_one<2, 128, 1>(a, sh, s) : stream_one<2, 128, 2>(a, sh, s);
+    if (D == 64) return blocks == 1 ? stream_one<2, 64, 1, TREE>(a, sh, s) : stream_one<2, 64, 2, TREE>(a, sh, s);
+    return blocks == 1 ? stream_one<2, 128, 1, TREE>(a, sh, s) : stream_one<2, 128, 2, TREE>(a, sh, s);
   }
-  if (D == 64) return blocks == 1 ? stream_one<4, 64, 1>(a, sh, s) : blocks == 2 ? stream_one<4, 64, 2>(a, sh, s) : stream_one<4, 64, 4>(a, sh, s);
-  return blocks == 1 ? stream_one<4, 128, 1>(a, sh, s) : blocks == 2 ? stream_one<4, 128, 2>(a, sh, s) : stream_one<4, 128, 4>(a, sh, s);
+  if (D == 64) return blocks == 1 ? stream_one<4, 64, 1, TREE>(a, sh, s) : blocks == 2 ? stream_one<4, 64, 2, TREE>(a, sh, s) : stream_one<4, 64, 4, TREE>(a, sh, s);
+  return blocks == 1 ? stream_one<4, 128, 1, TREE>(a, sh, s) : blocks == 2 ? stream_one<4, 128, 2, TREE>(a, sh, s) : stream_one<4, 128, 4, TREE>(a, sh, s);
+}
+
+hipError_t launch_paged_stream(int dtype, int D, int blocks, const PagedAttnArgs& a, const ShareArgs& sh, hipStream_t s) {
+  return a.mask != nullptr ? stream_some<true>(dtype, D, blocks, a, sh, s) : stream_some<false>(dtype, D, blocks, a, sh, s);
 }
 
 }  // namespace ts

@@ -56,9 +56,10 @@ __device__ __forceinline__ SeqShape seq_shape(const PagedAttnArgs& a, const Shar
   return s;
 }
 
-// room of a sequence's first r tiles
-__device__ __forceinline__ double tiles_room(const PagedAttnArgs& a, const ShareArgs& sh, const SeqShape& s, int tiles) {
+// room of a sequence's first r tiles (tree: the mask among the new tokens may let every row see all of them)
+__device__ __forceinline__ double tiles_room(const PagedAttnArgs& a, const ShareArgs& sh, const SeqShape& s, int tiles, bool tree) {
   const double r = tiles;
+  if (tree) return r * ((double)(a.window > 0 ? min(s.N, a.window + s.n) : s.N) + sh.tile_cost);
   const double first = max(s.N - s.n, 0) + sh.tile_cost, tpt = sh.tpt;
   if (a.window == 0) return fma(r, first, tpt * (r * (r + 1.) * 0.5));
   const double cap = (double)a.window + tpt + sh.tile_cost;                     // where the window cuts a tile's keys
@@ -68,18 +69,18 @@ __device__ __forceinline__ double tiles_room(const PagedAttnArgs& a, const Share
 
 // The i-th tile of a sequence in the line, and the room of the first i.
 __device__ __forceinline__ int tile_at(const SeqShape& s, int i) { return (i & 1) != 0 ? s.tiles - 1 - (i >> 1) : i >> 1; }
-__device__ __forceinline__ double line_room(const PagedAttnArgs& a, const ShareArgs& sh, const SeqShape& s, int i) {
-  return tiles_room(a, sh, s, (i + 1) >> 1) + (tiles_room(a, sh, s, s.tiles) - tiles_room(a, sh, s, s.tiles - (i >> 1)));
+__device__ __forceinline__ double line_room(const PagedAttnArgs& a, const ShareArgs& sh, const SeqShape& s, int i, bool tree) {
+  return tiles_room(a, sh, s, (i + 1) >> 1, tree) + (tiles_room(a, sh, s, s.tiles, tree) - tiles_room(a, sh, s, s.tiles - (i >> 1), tree));
 }
 
 // keys that a tile's rows see, in units of KT keys from u0 on; at least one unit, though it may hold no visible key
 struct TileKeys { int first, end, u0, units; };
 template <int KT>
-__device__ __forceinline__ TileKeys tile_keys(const PagedAttnArgs& a, const ShareArgs& sh, const SeqShape& s, int r) {
+__device__ __forceinline__ TileKeys tile_keys(const PagedAttnArgs& a, const ShareArgs& sh, const SeqShape& s, int r, bool tree) {
   TileKeys k;
   const int c0 = r * sh.tpt, c1 = min(c0 + sh.tpt, s.n) - 1;
-  k.end = max(s.N - s.n + c1 + 1, 0);
-  k.first = a.window > 0 ? (int)max((long)s.N - s.n + c0 - a.window + 1, 0l) : 0;
+  k.end = tree ? s.N : max(s.N - s.n + c1 + 1, 0);
+  k.first = a.window > 0 ? (int)max((long)s.N - s.n + (tree ? -1 : c0) - a.window + 1, 0l) : 0;   // (a row that sees no new token stands in front of them)
   k.u0 = (int)((uint32_t)k.first / KT);
   k.units = max((int)(((uint32_t)k.end + KT - 1) / KT) - k.u0, 1);
   return k;
@@ -91,19 +92,19 @@ struct SharePlace { int kvh, b, i, u; };       // i: the tile's turn in its sequ
 // the lowest of them, `many` of them), a step of tiles per lane and turn.
 template <int KT>
 __device__ __forceinline__ void find_unit(const PagedAttnArgs& a, const ShareArgs& sh, const SeqShape& q, double y, double share, int first, int many,
-                                          int* tile, int* unit) {
+                                          int* tile, int* unit, bool tree) {
   const int lane = (threadIdx.x & 63) - first;
   int lo = 0, n = q.tiles;                     // the last tile that begins at or before y is one of lo .. lo + n - 1
   while (__builtin_amdgcn_ballot_w64(n > 1) != 0) {
     const int step = (n + many - 1) / many;
-    uint64_t past = __builtin_amdgcn_ballot_w64(lane * step >= n || line_room(a, sh, q, min(lo + lane * step, q.tiles)) > y) >> first;
+    uint64_t past = __builtin_amdgcn_ballot_w64(lane * step >= n || line_room(a, sh, q, min(lo + lane * step, q.tiles), tree) > y) >> first;
     past = (many == 32 ? past & 0xffffffffull : past) & ~1ull;
     const int k = (past == 0 ? many : __builtin_ctzll(past)) - 1;
     n = min(step, n - k * step);
     lo += k * step;
   }
-  const double begin = line_room(a, sh, q, lo), room = line_room(a, sh, q, lo + 1) - begin;
-  const TileKeys k = tile_keys<KT>(a, sh, q, tile_at(q, lo));
+  const double begin = line_room(a, sh, q, lo, tree), room = line_room(a, sh, q, lo + 1, tree) - begin;
+  const TileKeys k = tile_keys<KT>(a, sh, q, tile_at(q, lo), tree);
   const int u = max((int)fmin(floor_div((y - begin) * k.units, room), (double)k.units), 0);
   const int near = (int)fmin(share * (1. / (KT * 24)), (double)k.units);   // a cut so near an end would cost more than it evens out
   *tile = lo;
@@ -114,7 +115,7 @@ __device__ __forceinline__ void find_unit(const PagedAttnArgs& a, const ShareArg
 struct ShareScratch { double sums[4], y[2]; int kvh[2]; SeqShape shape[2]; SharePlace place[2]; };
 template <int KT>
 __device__ __forceinline__ void find_share(const PagedAttnArgs& a, const ShareArgs& sh, int G, int wg, ShareScratch* lds, SharePlace* from,
-                                           SharePlace* to, SeqShape* first) {
+                                           SharePlace* to, SeqShape* first, bool tree = false) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (sh.whole && sh.each > 0) {                           // no search
     const uint32_t at = (uint32_t)wg / (uint32_t)sh.each;
@@ -149,7 +150,7 @@ __device__ __forceinline__ void find_share(const PagedAttnArgs& a, const ShareAr
     // a lane per sequence, every wave for itself, both ends at once in the halves of the wave: no barrier, and half the time
     SeqShape s{0, 0, 0, 0, 0, 0};
     if (lane < a.B) s = seq_shape(a, sh, G, lane);
-    const double mine = tiles_room(a, sh, s, s.tiles);
+    const double mine = tiles_room(a, sh, s, s.tiles, tree);
     double upto = mine;
     for (int d = 1; d < a.B; d <<= 1) {
       const double x = __shfl_up(upto, d);
@@ -166,7 +167,7 @@ __device__ __forceinline__ void find_share(const PagedAttnArgs& a, const ShareAr
     const int own_tiles = __shfl(s.tiles, own);         // (by all lanes: one that takes no part gives nothing)
     const SeqShape q{own, __shfl(s.row0, own), __shfl(s.n, own), __shfl(s.N, own), there ? own_tiles : 0, __shfl(s.page0, own)};
     int tile = 0, unit = 0;
-    find_unit<KT>(a, sh, q, y - __shfl(upto - mine, own), share, e * 32, 32, &tile, &unit);
+    find_unit<KT>(a, sh, q, y - __shfl(upto - mine, own), share, e * 32, 32, &tile, &unit, tree);
     auto at = [](int x, int l) { return __builtin_amdgcn_readlane(x, l); };
     const int kv = (int)kvh;
     *from = SharePlace{at(kv, 0), at(own, 0), at(tile, 0), at(unit, 0)};
@@ -180,7 +181,7 @@ __device__ __forceinline__ void find_share(const PagedAttnArgs& a, const ShareAr
   double mine = 0.;
   for (int b = b0; b < b1; ++b) {
     s = seq_shape(a, sh, G, b);
-    mine += tiles_room(a, sh, s, s.tiles);
+    mine += tiles_room(a, sh, s, s.tiles, tree);
   }
   double upto = mine;
 #pragma unroll
@@ -201,7 +202,7 @@ __device__ __forceinline__ void find_share(const PagedAttnArgs& a, const ShareAr
     if (!(y >= 0. && y < mine)) continue;      // another thread's sequences
     for (int b = b0; b + 1 < b1; ++b) {
       s = seq_shape(a, sh, G, b);
-      const double room = tiles_room(a, sh, s, s.tiles);
+      const double room = tiles_room(a, sh, s, s.tiles, tree);
       if (y < room) break;
       y -= room;
       s = seq_shape(a, sh, G, b + 1);
@@ -219,7 +220,7 @@ __device__ __forceinline__ void find_share(const PagedAttnArgs& a, const ShareAr
     if (at.kvh < a.H_kv) {
       const SeqShape q = shape_of(wave);
       at.b = q.b;
-      find_unit<KT>(a, sh, q, lds->y[wave], share, 0, 64, &at.i, &at.u);
+      find_unit<KT>(a, sh, q, lds->y[wave], share, 0, 64, &at.i, &at.u, tree);
     }
     if (lane == 0) lds->place[wave] = at;
   }
@@ -243,14 +244,15 @@ __device__ __forceinline__ int next_sequence(const PagedAttnArgs& a, const Share
 // A workgroup's walk over its share: fn(kvh, shape, r, keys, ua, ub, again) for units [ua, ub) of every tile in it; where it returns true it is
 // called again, with `again` set.
 template <int KT, typename F>
-__device__ __forceinline__ void walk_share(const PagedAttnArgs& a, const ShareArgs& sh, int G, const SharePlace& from, const SharePlace& to, SeqShape s, F&& fn) {
+__device__ __forceinline__ void walk_share(const PagedAttnArgs& a, const ShareArgs& sh, int G, const SharePlace& from, const SharePlace& to, SeqShape s, F&& fn,
+                                           bool tree = false) {
   int kvh = from.kvh, b = from.b, i = from.i, ua = from.u;
   if (kvh >= a.H_kv) return;
   bool again = false;
   for (;;) {
     const bool last = kvh == to.kvh && b == to.b && i == to.i;
     const int r = tile_at(s, i);
-    const TileKeys k = tile_keys<KT>(a, sh, s, r);
+    const TileKeys k = tile_keys<KT>(a, sh, s, r, tree);
     const int ub = last ? min(to.u, k.units) : k.units;
     if (ub > ua) { again = fn(kvh, s, r, k, ua, ub, again); if (again) continue; }
     if (last) return;
@@ -261,6 +263,32 @@ __device__ __forceinline__ void walk_share(const PagedAttnArgs& a, const ShareAr
     if (b >= a.B) { if (++kvh >= a.H_kv) return; b = next_sequence(a, sh, G, 0); }
     s = seq_shape(a, sh, G, b);
   }
+}
+
+// Masks among the new tokens.  What row `row` of a sequence sees, as bits of the 32 keys from k0 on: cached ones (places below `base`) from `low` on, and new ones
+// whose bit is set.  Nothing is read for keys that are all cached.
+__device__ __forceinline__ uint32_t tree_bits(const PagedAttnArgs& a, int row, int n, int base, int low, int k0) {
+  const int d = k0 - base;                     // the first key, counted among the new ones
+  uint32_t bits = 0u;
+  if (d < 0) {
+    const int many = min(-d, 32), cut = min(max(low - k0, 0), 32);
+    bits = (uint32_t)(((1ull << many) - 1ull) & ~((1ull << cut) - 1ull));
+  }
+  if (d <= -32 || d >= n) return bits;
+  const uint32_t* words = a.mask + (size_t)row * a.mask_words;
+  const int w = d >> 5, left = n - d;          // (w = -1: the first word's bits move up)
+  const uint64_t pair = (uint64_t)(w >= 0 && w < a.mask_words ? words[w] : 0u) | ((uint64_t)(w + 1 < a.mask_words ? words[w + 1] : 0u) << 32);
+  const uint32_t now = (uint32_t)(pair >> (d & 31));
+  return bits | (left < 32 ? now & ((1u << left) - 1u) : now);
+}
+
+// first cached token that the row's window reaches
+__device__ __forceinline__ int tree_low(const PagedAttnArgs& a, int row, int n, int base) {
+  if (a.window == 0) return 0;
+  const uint32_t* words = a.mask + (size_t)row * a.mask_words;
+  int seen = 0;
+  for (int w = 0; w < a.mask_words && w * 32 < n; ++w) seen += __builtin_popcount(n - w * 32 < 32 ? words[w] & ((1u << (n - w * 32)) - 1u) : words[w]);
+  return max(base + seen - a.window, 0);
 }
 
 // which piece a workgroup stands for: those of an XCD (workgroup L runs on XCD L % 8) follow each other

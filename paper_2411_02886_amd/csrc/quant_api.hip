@@ -3,16 +3,6 @@
 
 using namespace ts;
 
-static int32_t check_quant(const ts_problem* p, const ts_quant* c, QuantPools* pools) {
-  const int32_t st = check_problem(p);
-  if (st != TS_OK) return st;
-  if (c == nullptr || (c->code != TS_INT8 && c->code != TS_E4M3)) return TS_ERR_INVALID_ARG;
-  for (const void* x : {(const void*)c->k_codes, (const void*)c->v_codes, (const void*)c->k_scale, (const void*)c->v_scale})
-    if (x == nullptr || !aligned16(x)) return TS_ERR_INVALID_ARG;
-  *pools = QuantPools{(uint8_t*)c->k_codes, (uint8_t*)c->v_codes, c->k_scale, c->v_scale, c->code};
-  return TS_OK;
-}
-
 extern "C" {
 
 int32_t ts_quant_append(const ts_problem* p, const ts_quant* c, const ts_rope* r, const void* q, int64_t q_stride, const void* k, int64_t k_stride,

@@ -224,6 +224,8 @@ struct PagedAttnArgs {
   int B, C, T, H, H_kv, P, p_shift, max_seq_len, window;
   int round_weights;           // bf16, many rows: the weights that multiply V may be rounded to bf16
   float sm_scale;
+  const uint32_t* mask;        // [T][mask_words]: which new tokens a row sees; null: those up to itself
+  int mask_words;
 };
 size_t paged_attn_workspace(int dtype, int D, int G, int chunk);
 hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws, hipStream_t s);
@@ -295,6 +297,32 @@ struct QuantReadArgs {
 };
 hipError_t launch_quant_read(int dtype, const QuantReadArgs& a, const QuantPools& c, hipStream_t s);
 hipError_t launch_quant_pages_copy(const QuantPools& c, const int32_t* src, const int32_t* dst, int n, int num_pages, int P, int H_kv, int D, hipStream_t s);
+
+// drafted trees (draft_api.hip)
+struct TreeMaskArgs {
+  const int32_t* parents;
+  const int32_t* q_indptr;
+  const int32_t* seq_lens;
+  uint32_t* mask;
+  int32_t* positions;          // null: not wanted
+  int C, T, words;
+};
+hipError_t launch_tree_mask(const TreeMaskArgs& a, int B, hipStream_t s);
+struct TreeKeepArgs {
+  uint8_t* k;                  // rows, stored values or codes
+  uint8_t* v;
+  float* k_scale;              // null: a plain cache
+  float* v_scale;
+  const int32_t* page_indptr;
+  const int32_t* page_indices;
+  const int32_t* seq_lens;
+  const int32_t* q_indptr;
+  const int32_t* path;
+  const int32_t* count;
+  int32_t* to_lens;
+  int path_stride, C, H_kv, p_shift, max_seq_len, row_bytes;
+};
+hipError_t launch_tree_keep(const TreeKeepArgs& a, int B, hipStream_t s);
 
 int32_t check_problem(const ts_problem* p);   // the shape and pointer checks that every call begins with (api.hip)
 

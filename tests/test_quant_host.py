@@ -78,6 +78,48 @@ def test_pages_copy_refusals():
     assert call(n=0, src=None, dst=None) == OK
 
 
+def tree_mask(p=None, parents=A, ind=None, rows=2, mask=0x200000, words=3, pos=0x300000):
+    return ts.load().ts_tree_mask(p or cproblem(), parents, ind, rows, mask, words, pos, None)
+
+
+def test_tree_mask_refusals():
+    for kw in (dict(parents=None), dict(mask=None), dict(words=0), dict(words=-1), dict(rows=3), dict(rows=-1), dict(mask=A + 4), dict(pos=A), dict(pos=0x200000 + 20),
+               dict(mask=A - 8), dict(p=cproblem(seq_lens=None)), dict(p=cproblem(seq_lens=0x200004))):
+        assert tree_mask(**kw) == BAD, kw
+    assert tree_mask(p=cproblem(head_dim=80)) == UNSUP
+    assert tree_mask(rows=0, parents=None, mask=None, pos=None) == OK
+
+
+def tree_attn(p=None, q=A, ind=None, rows=2, window=0, mask=0x500000, words=1, sm=0.1, out=0x900000, lse=None, ws=0x2000000, ws_bytes=BIG):
+    return ts.load().ts_tree_attn(p or cproblem(k_pool=A, v_pool=A), q, ind, rows, window, mask, words, sm, out, lse, ws, ws_bytes, None)
+
+
+def test_tree_attn_refusals():
+    pools = dict(k_pool=A, v_pool=A)
+    for kw in (dict(q=None), dict(out=None), dict(rows=3), dict(rows=-1), dict(window=-1), dict(sm=float("nan")), dict(sm=float("inf")),
+               dict(mask=None), dict(mask=0x500002), dict(words=0), dict(words=-4),
+               dict(q=A + 8), dict(out=0x900004), dict(out=A), dict(p=cproblem()), dict(p=cproblem(**dict(pools, v_pool=None))),
+               dict(p=cproblem(**dict(pools, k_pool=A + 2))), dict(p=cproblem(**pools, seq_lens=None))):
+        assert tree_attn(**kw) == BAD, kw
+    assert tree_attn(p=cproblem(**pools, head_dim=96)) == UNSUP
+    for kw in (dict(ws=None), dict(ws=0x2000010), dict(ws_bytes=16)):
+        assert tree_attn(**kw) == WS, kw
+    assert tree_attn(rows=0, q=None, out=None, mask=None, ws=None, ws_bytes=0) == OK
+
+
+def keep(p=None, c=None, path=0x500000, stride=4, count=0x600000, ind=None, to=0x700000):
+    return ts.load().ts_tree_keep(p or cproblem(k_pool=0x100000, v_pool=0x200000), c, path, stride, count, ind, to, None)
+
+
+def test_tree_keep_refusals():
+    for kw in (dict(path=None), dict(count=None), dict(to=None), dict(stride=0), dict(p=cproblem()), dict(p=cproblem(k_pool=A)), dict(p=cproblem(k_pool=A + 4, v_pool=A)),
+               dict(to=A), dict(to=A + 4), dict(to=A - 4), dict(to=0x500000 + 2 * 4 * 4 - 4), dict(to=0x600004), dict(ind=0x700004), dict(ind=0x700000 - 8)):
+        assert keep(**kw) == BAD, kw
+    for c in BAD_QUANT[1:]:
+        assert keep(c=c) == BAD
+    assert keep(p=cproblem(k_pool=A, v_pool=A, page_size=12)) == UNSUP
+
+
 # ---- the binding
 
 def problem(**kw):
@@ -130,7 +172,27 @@ def b_copy(p, c, **kw):
     ts.ts_quant_pages_copy(p, c, a["src"], a["dst"], 2, 3)
 
 
-CALLS = [(b_append, n) for n in ("q", "k", "v", "ind", "pos", "q_out")] + [(b_read, n) for n in ("ind", "k_out", "v_out")] + [(b_copy, n) for n in ("src", "dst")]
+def b_mask(p, c, **kw):
+    a = dict(parents=ints(3), ind=ints(2), mask=ints(3, 1), positions=ints(3))
+    a.update(kw)
+    ts.ts_tree_mask(p, a["parents"], a["ind"], 3, a["mask"], a["positions"])
+
+
+def b_tree(p, c, **kw):
+    a = dict(q=torch.zeros(3, 4, 64), ind=ints(2), mask=ints(3, 1), out=torch.zeros(3, 4, 64), lse=torch.zeros(3, 4))
+    a.update(kw)
+    ts.ts_tree_attn(p, a["q"], a["ind"], 3, 0, a["mask"], 0.1, a["out"], a["lse"], torch.zeros(64))
+
+
+def b_keep(p, c, **kw):
+    a = dict(path=ints(1, 4), count=ints(1), ind=ints(2), to_lens=ints(1))
+    a.update(kw)
+    ts.ts_tree_keep(p, c, a["path"], 4, a["count"], a["ind"], a["to_lens"])
+
+
+SHAPED = ("b_append", "b_read", "b_copy", "b_keep")          # calls that compare the cache with the problem
+CALLS = [(b_mask, n) for n in ("parents", "ind", "mask", "positions")] + [(b_tree, n) for n in ("q", "ind", "mask", "out", "lse")] + \
+    [(b_keep, n) for n in ("path", "count", "ind", "to_lens")] + [(b_append, n) for n in ("q", "k", "v", "ind", "pos", "q_out")] + [(b_read, n) for n in ("ind", "k_out", "v_out")] + [(b_copy, n) for n in ("src", "dst")]
 
 
 @pytest.mark.parametrize("call,name", CALLS, ids=lambda x: getattr(x, "__name__", x))
@@ -140,11 +202,12 @@ def test_wrong_types_lengths_and_devices_are_refused(call, name):
     with pytest.raises(ValueError):
         call(problem(), c, **{name: bad})
     if name not in ("pos",):
+        short = ints(1)[:0] if name in ("ind", "src", "dst", "parents", "positions", "path", "count", "to_lens") else ints(1, 1) if name == "mask" else torch.zeros(1, 2, 64)
         with pytest.raises(ValueError):
-            call(problem(), c, **{name: ints(1)[:0] if name in ("ind", "src", "dst") else torch.zeros(1, 2, 64)})
+            call(problem(), c, **{name: short[:, :1, :1] if name == "lse" else short})
     with pytest.raises(ValueError, match="not on a GPU"):
         call(problem(), c)
-    for p in (problem(page_size=8), problem(head_dim=128), problem(num_kv_heads=4)):
+    for p in () if call.__name__ not in SHAPED else (problem(page_size=8), problem(head_dim=128), problem(num_kv_heads=4)):
         with pytest.raises(ValueError, match="the cache has pages"):
             call(p, c)
 
