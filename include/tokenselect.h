@@ -411,6 +411,16 @@ int32_t ts_quant_append(const ts_problem* p, const ts_quant* c, const ts_rope* r
  * max_seq_len) get 0; rows that belong to no sequence are left as they are.  Either of k_out and v_out may be NULL. */
 int32_t ts_quant_read(const ts_problem* p, const ts_quant* c, const int32_t* q_indptr, int32_t num_rows, void* k_out, void* v_out, void* stream);
 
+/* ts_paged_attn over an 8-bit cache: K and V are what the codes and scales stand for.  The same rows, window, results, rows that see nothing; weights and sums in
+ * float (the products of q and codes are summed before the scale is applied).  mask NULL: causal, as there; else a mask among the new tokens [num_rows][mask_words], see ts_tree_mask.
+ * Codes are finite numbers, so that no key or value that a row does not see can disturb it (e4m3: the two codes of NaN, 127 and 255, do not come from ts_quant_append; where they
+ * stand in a cache, rows that share a tile with one that sees them may be NaN too).
+ * ws: ts_quant_attn_workspace_bytes() bytes, 256-byte aligned, contents irrelevant on entry and exit; one for num_rows, chunk, batch and max_seq_len
+ * serves every call with fewer or smaller ones and the same heads and dtype.  sm_scale finite, window >= 0. */
+int32_t ts_quant_attn_workspace_bytes(const ts_problem* p, int32_t num_rows, size_t* bytes);
+int32_t ts_quant_attn(const ts_problem* p, const ts_quant* c, const void* q, const int32_t* q_indptr, int32_t num_rows, int32_t window, const uint32_t* mask,
+                      int32_t mask_words, float sm_scale, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
 /* ts_pages_copy for an 8-bit cache: codes and scales of K and V.  The same rules. */
 int32_t ts_quant_pages_copy(const ts_problem* p, const ts_quant* c, const int32_t* src, const int32_t* dst, int32_t n, int32_t num_pages, void* stream);
 

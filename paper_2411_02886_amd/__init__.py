@@ -12,5 +12,5 @@ from .binding import (  # noqa: F401
     ts_paged_qk_scores_checked, ts_paged_qk_codes_checked, ts_soft_vote_ranked, TS_TOPK_VOTE_HIST,
     Rope, rope_axes, ts_paged_attn, ts_paged_attn_rounded, ts_paged_attn_workspace_bytes, ts_rope_append, ts_pages_copy, ts_cache_compact,
     TS_INT8, TS_E4M3, QuantCache, ts_quant_append, ts_quant_read, ts_quant_pages_copy,
-    ts_tree_mask, ts_tree_attn, ts_tree_keep,
+    ts_tree_mask, ts_tree_attn, ts_tree_keep, ts_quant_attn, ts_quant_attn_workspace_bytes,
 )

@@ -110,6 +110,8 @@ def load():
         L.ts_quant_append.argtypes = [pp, pc, ctypes.POINTER(_CRope), vp, i64, vp, i64, vp, i64, vp, i32, vp, vp, vp]
         L.ts_quant_read.argtypes = [pp, pc, vp, i32, vp, vp, vp]
         L.ts_quant_pages_copy.argtypes = [pp, pc, vp, vp, i32, i32, vp]
+        L.ts_quant_attn_workspace_bytes.argtypes = [pp, i32, ctypes.POINTER(sz)]
+        L.ts_quant_attn.argtypes = [pp, pc, vp, vp, i32, i32, vp, i32, f32, vp, vp, vp, sz, vp]
         L.ts_tree_mask.argtypes = [pp, vp, vp, i32, vp, i32, vp, vp]
         L.ts_tree_attn.argtypes = [pp, vp, vp, i32, i32, vp, i32, f32, vp, vp, vp, sz, vp]
         L.ts_tree_keep.argtypes = [pp, pc, vp, i32, vp, vp, vp, vp]
@@ -128,7 +130,7 @@ def load():
                      "ts_soft_vote_bounds", "ts_topk_exact", "ts_debug_set_codes_path", "ts_topk_noalloc",
                      "ts_paged_qk_scores_checked", "ts_paged_qk_codes_checked", "ts_soft_vote_ranked",
                      "ts_paged_attn_workspace_bytes", "ts_paged_attn", "ts_paged_attn_rounded", "ts_rope_append", "ts_pages_copy", "ts_cache_compact",
-                     "ts_quant_append", "ts_quant_read", "ts_quant_pages_copy", "ts_tree_mask", "ts_tree_attn", "ts_tree_keep"):
+                     "ts_quant_append", "ts_quant_read", "ts_quant_attn_workspace_bytes", "ts_quant_attn", "ts_quant_pages_copy", "ts_tree_mask", "ts_tree_attn", "ts_tree_keep"):
             getattr(L, name).restype = i32
         _lib = L
     return _lib
@@ -652,3 +654,23 @@ def ts_tree_keep(p: Problem, c, path, path_stride: int, count, q_indptr, to_lens
     _ok(load().ts_tree_keep(p.ref(), None if c is None else _quant_of(p, c), _at(p, path, "path", _INT, B * int(path_stride)), int(path_stride),
                             _at(p, count, "count", _INT, B), _at(p, q_indptr, "q_indptr", _INT, B + 1), _at(p, to_lens, "to_lens", _INT, B),
                             _stream_of(p, stream)), "ts_tree_keep")
+
+
+def ts_quant_attn_workspace_bytes(p: Problem, num_rows: int) -> int:
+    out = ctypes.c_size_t(0)
+    _ok(load().ts_quant_attn_workspace_bytes(p.ref(), int(num_rows), ctypes.byref(out)), "ts_quant_attn_workspace_bytes")
+    return int(out.value)
+
+
+def ts_quant_attn(p: Problem, c: QuantCache, q, q_indptr, num_rows: int, window: int, mask, sm_scale: float, out, lse, ws, stream=None) -> None:
+    """mask: None, or what the new tokens see of each other, as for ts_tree_attn."""
+    n = int(num_rows)
+    if _STORED is None:
+        _load_types()
+    stored, quant = _STORED.get(p.dtype, ()), _quant_of(p, c)
+    if ws is not None and ws.get_device() != p.device:
+        raise ValueError("ws: on the device of the pools")
+    mask_at, words = _mask_of(p, mask, n)
+    _ok(load().ts_quant_attn(p.ref(), quant, _at(p, q, "q", stored, n * p.q_row), _at(p, q_indptr, "q_indptr", _INT, p.batch + 1), n, int(window), mask_at,
+                             words, float(sm_scale), _at(p, out, "out", stored, n * p.q_row), _at(p, lse, "lse", _FLOAT, n * p.heads), _ptr(ws), _nbytes(ws),
+                             _stream_of(p, stream)), "ts_quant_attn")

@@ -18,7 +18,7 @@ LIB = os.path.join(HERE, "libtokenselect.so")
 SOURCES = ["api.hip", "score_decode.hip", "soft_vote.hip", "topk.hip", "selcache.hip", "sparse_attn_decode.hip", "sparse_attn_stream.hip", "prefill_select.hip", "sparse_attn_chunk.hip", "sparse_attn_chunk_wide.hip",
            "chunk_mean_query.hip", "select_variants.hip", "select_compact.hip", "score_codes_mfma.hip",
            "cache_api.hip", "paged_attn.hip", "paged_attn_stream.hip", "paged_attn_tall.hip", "rope_append.hip", "cache_pages.hip",
-           "quant_api.hip", "quant_cache.hip", "draft_api.hip", "draft_tree.hip"]
+           "quant_api.hip", "quant_cache.hip", "quant_attn.hip", "draft_api.hip", "draft_tree.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -26,9 +26,9 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=o
 
 # Flags of single files.  sparse_attn_chunk_wide: its kernel runs one wave per SIMD and needs both halves of the register file; the
 # results of its matrix products are read by vector instructions, which see the first half only, and without this option the
-# compiler keeps all of them in the second half and moves every score over (2113 moves in the kernel, with it 182).  paged_attn_*: built the same way, for the same reason.
+# compiler keeps all of them in the second half and moves every score over (2113 moves in the kernel, with it 182).  paged_attn_*, quant_attn: built the same way, for the same reason.
 FILE_FLAGS = {"sparse_attn_chunk_wide.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "paged_attn_tall.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-              "paged_attn_stream.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+              "paged_attn_stream.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"], "quant_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 
 def _deps():

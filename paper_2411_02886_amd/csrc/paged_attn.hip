@@ -179,6 +179,11 @@ static hipError_t merge(const PagedAttnArgs& a, const ShareArgs& sh, int rows, l
   return hipGetLastError();
 }
 
+hipError_t launch_paged_merge(int dtype, int D, const PagedAttnArgs& a, const ShareArgs& sh, int rows, long tiles, hipStream_t s) {
+  if (dtype == TS_BF16) return D == 64 ? merge<2, 64>(a, sh, rows, tiles, s) : merge<2, 128>(a, sh, rows, tiles, s);
+  return D == 64 ? merge<4, 64>(a, sh, rows, tiles, s) : merge<4, 128>(a, sh, rows, tiles, s);
+}
+
 // bytes that tiles of `rows` rows leave pieces in
 static size_t piece_bytes(int rows, int D) {
   return align_up((size_t)kShareWgs * 32, 256) + align_up((size_t)kShareWgs * 2 * rows * 2 * 4, 256) + (size_t)kShareWgs * 2 * rows * D * 4;
@@ -242,8 +247,7 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
     at += piece_bytes(rows, D);
     const hipError_t e = tall ? launch_paged_tall(D, a, sh, s) : launch_paged_stream(dtype, D, rows / 16, a, sh, s);
     if (e != hipSuccess || whole) return e;
-    if (dtype == TS_BF16) return D == 64 ? merge<2, 64>(a, sh, rows, tiles_of(sh.tpt, beside), s) : merge<2, 128>(a, sh, rows, tiles_of(sh.tpt, beside), s);
-    return D == 64 ? merge<4, 64>(a, sh, rows, tiles_of(sh.tpt, beside), s) : merge<4, 128>(a, sh, rows, tiles_of(sh.tpt, beside), s);
+    return launch_paged_merge(dtype, D, a, sh, rows, tiles_of(sh.tpt, beside), s);
   };
   // A workgroup per tile, and no merge, where tiles are short, or where there are enough of them that are not long.  (200 keys: 8.2 us, in shares 10.3; 64
   // sequences of 250 to 500 keys, 512 tiles: 22.8 and 29; but 16 fp32 sequences of 1000 to 2000 keys, 32 tiles, 42 us instead of 17.)  Beside large

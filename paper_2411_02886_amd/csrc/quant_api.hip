@@ -47,6 +47,38 @@ int32_t ts_quant_read(const ts_problem* p, const ts_quant* c, const int32_t* q_i
   return launch_quant_read(p->dtype, a, pools, (hipStream_t)stream) == hipSuccess ? TS_OK : TS_ERR_HIP;
 }
 
+int32_t ts_quant_attn_workspace_bytes(const ts_problem* p, int32_t num_rows, size_t* bytes) {
+  if (bytes == nullptr || num_rows < 0) return TS_ERR_INVALID_ARG;
+  const int32_t st = check_problem(p);
+  if (st != TS_OK) return st;
+  *bytes = quant_attn_workspace(p->dtype, p->head_dim, p->num_q_heads / p->num_kv_heads, p->chunk);
+  return TS_OK;
+}
+
+int32_t ts_quant_attn(const ts_problem* p, const ts_quant* c, const void* q, const int32_t* q_indptr, int32_t num_rows, int32_t window, const uint32_t* mask,
+                      int32_t mask_words, float sm_scale, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  QuantPools pools;
+  int32_t st = check_quant(p, c, &pools);
+  if (st != TS_OK) return st;
+  if ((st = check_rows(p, q_indptr, num_rows)) != TS_OK) return st;
+  if (window < 0 || !(fabsf(sm_scale) < INFINITY)) return TS_ERR_INVALID_ARG;
+  if (mask != nullptr && (mask_words < 1 || ((uintptr_t)mask & 3) != 0)) return TS_ERR_INVALID_ARG;
+  if (num_rows == 0) return TS_OK;
+  if (q == nullptr || out == nullptr || !aligned16(q) || !aligned16(out)) return TS_ERR_INVALID_ARG;
+  const size_t es = p->dtype == TS_BF16 ? 2 : 4, bytes = (size_t)num_rows * p->num_q_heads * p->head_dim * es;
+  if (overlap(q, bytes, out, bytes)) return TS_ERR_INVALID_ARG;
+  const size_t need = quant_attn_workspace(p->dtype, p->head_dim, p->num_q_heads / p->num_kv_heads, p->chunk);
+  if (ws == nullptr || ((uintptr_t)ws & 255) != 0 || ws_bytes < need) return TS_ERR_WORKSPACE;
+  PagedAttnArgs a{};
+  a.q = (const uint8_t*)q;
+  a.page_indptr = p->page_indptr; a.page_indices = p->page_indices; a.seq_lens = p->seq_lens; a.q_indptr = q_indptr;
+  a.out = (uint8_t*)out; a.lse = lse;
+  a.B = p->batch; a.C = p->chunk; a.T = num_rows; a.H = p->num_q_heads; a.H_kv = p->num_kv_heads;
+  a.P = p->page_size; a.p_shift = ilog2(p->page_size); a.max_seq_len = p->max_seq_len; a.window = window < p->max_seq_len ? window : 0;   // one that reaches every token is none
+  a.sm_scale = sm_scale; a.mask = mask; a.mask_words = mask_words;
+  return launch_quant_attn(p->dtype, p->head_dim, a, pools, ws, (hipStream_t)stream) == hipSuccess ? TS_OK : TS_ERR_HIP;
+}
+
 int32_t ts_quant_pages_copy(const ts_problem* p, const ts_quant* c, const int32_t* src, const int32_t* dst, int32_t n, int32_t num_pages, void* stream) {
   QuantPools pools;
   const int32_t st = check_quant(p, c, &pools);

@@ -298,6 +298,9 @@ struct QuantReadArgs {
 hipError_t launch_quant_read(int dtype, const QuantReadArgs& a, const QuantPools& c, hipStream_t s);
 hipError_t launch_quant_pages_copy(const QuantPools& c, const int32_t* src, const int32_t* dst, int n, int num_pages, int P, int H_kv, int D, hipStream_t s);
 
+size_t quant_attn_workspace(int dtype, int D, int G, int chunk);
+hipError_t launch_quant_attn(int dtype, int D, const PagedAttnArgs& a, const QuantPools& c, void* ws, hipStream_t s);   // (a's pools are not used)
+
 // drafted trees (draft_api.hip)
 struct TreeMaskArgs {
   const int32_t* parents;

@@ -78,6 +78,45 @@ def test_pages_copy_refusals():
     assert call(n=0, src=None, dst=None) == OK
 
 
+def attn(p=None, c=None, q=A, ind=None, rows=2, window=0, mask=None, words=0, sm=0.1, out=0x900000, lse=None, ws=0x2000000, ws_bytes=BIG, quant=True):
+    return ts.load().ts_quant_attn(p or cproblem(), (c or cquant()) if quant else None, q, ind, rows, window, mask, words, sm, out, lse, ws, ws_bytes, None)
+
+
+def test_attn_refusals():
+    for kw in (dict(q=None), dict(out=None), dict(rows=3), dict(rows=-1), dict(window=-1), dict(sm=float("nan")), dict(sm=float("inf")), dict(quant=False),
+               dict(mask=0x500000), dict(mask=0x500000, words=-1), dict(mask=0x500002, words=1), dict(q=A + 8), dict(out=0x900004), dict(out=A),
+               dict(out=A + 2 * 8 * 64 * 2 - 16), dict(p=cproblem(seq_lens=None)), dict(p=cproblem(num_q_heads=7))):
+        assert attn(**kw) == BAD, kw
+    for c in BAD_QUANT[1:]:
+        assert attn(c=c) == BAD
+    assert attn(p=cproblem(head_dim=96)) == UNSUP and attn(p=cproblem(page_size=12)) == UNSUP
+    for kw in (dict(ws=None), dict(ws=0x2000010), dict(ws_bytes=16)):
+        assert attn(**kw) == WS, kw
+    assert attn(rows=0, q=None, out=None, ws=None, ws_bytes=0) == OK
+
+
+def test_attn_workspace():
+    L, out = ts.load(), ctypes.c_size_t(0)
+    get = lambda rows, **kw: (L.ts_quant_attn_workspace_bytes(cproblem(**kw), rows, ctypes.byref(out)), out.value)
+    assert get(-1)[0] == BAD and L.ts_quant_attn_workspace_bytes(None, 1, ctypes.byref(out)) == BAD
+    assert get(1, head_dim=80)[0] == UNSUP
+    for dtype in (ts.TS_BF16, ts.TS_F32):                     # one workspace serves every call with fewer rows, shorter chunks and sequences, fewer sequences
+        for H, H_kv, D in ((8, 2, 64), (32, 8, 128), (28, 4, 128), (3, 1, 64), (128, 32, 128)):
+            shape = dict(num_q_heads=H, num_kv_heads=H_kv, head_dim=D, dtype=dtype)
+            for axis, values in (("rows", [0, 1, 2, 31, 33, 64, 500, 5000, 100000]), ("chunk", [1, 2, 3, 4, 8, 9, 16, 17, 64, 500, 9000]),
+                                 ("batch", [1, 2, 7, 64, 300, 5000]), ("max_seq_len", [1, 100, 1000, 5000, 100000, 1 << 20])):
+                last = 0
+                for x in values:
+                    rows, kw = 64, dict(chunk=20, batch=3, max_seq_len=20000)
+                    if axis == "rows":
+                        rows = x
+                    else:
+                        kw[axis] = x
+                    st, n = get(rows, **kw, **shape)
+                    assert st == OK and n >= last and n % 256 == 0, (axis, x)
+                    last = n
+
+
 def tree_mask(p=None, parents=A, ind=None, rows=2, mask=0x200000, words=3, pos=0x300000):
     return ts.load().ts_tree_mask(p or cproblem(), parents, ind, rows, mask, words, pos, None)
 
@@ -172,6 +211,12 @@ def b_copy(p, c, **kw):
     ts.ts_quant_pages_copy(p, c, a["src"], a["dst"], 2, 3)
 
 
+def b_attn(p, c, **kw):
+    a = dict(q=torch.zeros(3, 4, 64), ind=ints(2), mask=ints(3, 1), out=torch.zeros(3, 4, 64), lse=torch.zeros(3, 4))
+    a.update(kw)
+    ts.ts_quant_attn(p, c, a["q"], a["ind"], 3, 0, a["mask"], 0.1, a["out"], a["lse"], torch.zeros(64))
+
+
 def b_mask(p, c, **kw):
     a = dict(parents=ints(3), ind=ints(2), mask=ints(3, 1), positions=ints(3))
     a.update(kw)
@@ -190,9 +235,9 @@ def b_keep(p, c, **kw):
     ts.ts_tree_keep(p, c, a["path"], 4, a["count"], a["ind"], a["to_lens"])
 
 
-SHAPED = ("b_append", "b_read", "b_copy", "b_keep")          # calls that compare the cache with the problem
+SHAPED = ("b_append", "b_read", "b_copy", "b_keep", "b_attn")          # calls that compare the cache with the problem
 CALLS = [(b_mask, n) for n in ("parents", "ind", "mask", "positions")] + [(b_tree, n) for n in ("q", "ind", "mask", "out", "lse")] + \
-    [(b_keep, n) for n in ("path", "count", "ind", "to_lens")] + [(b_append, n) for n in ("q", "k", "v", "ind", "pos", "q_out")] + [(b_read, n) for n in ("ind", "k_out", "v_out")] + [(b_copy, n) for n in ("src", "dst")]
+    [(b_attn, n) for n in ("q", "ind", "mask", "out", "lse")] + [(b_keep, n) for n in ("path", "count", "ind", "to_lens")] + [(b_append, n) for n in ("q", "k", "v", "ind", "pos", "q_out")] + [(b_read, n) for n in ("ind", "k_out", "v_out")] + [(b_copy, n) for n in ("src", "dst")]
 
 
 @pytest.mark.parametrize("call,name", CALLS, ids=lambda x: getattr(x, "__name__", x))

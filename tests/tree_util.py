@@ -28,9 +28,10 @@ def words_of(sees, words):
     return (bits[:, :words * 32].reshape(n, words, 32) << np.arange(32, dtype=np.uint64)).sum(axis=-1).astype(np.uint32)
 
 
-def attention(cache, q, new, window, sm, sees=None, more=0):
+def attention(cache, q, new, window, sm, sees=None, more=0, tiny=0.0):
     """q [T][H][D] stored; sees: per sequence bool [n][n], or None: causal.  (out, lse, bound on out, bound on lse), rows in order; `cache` holds k, v in 64
-    bits.  Bounds as in cache_util.attention, with `more` roundings of a logit and of a weight (scales)."""
+    bits.  Bounds as in cache_util.attention, with `more` roundings of a logit and of a weight (scales), and `tiny` of output for each key that a row sees: what is
+    lost where weights leave the range of float."""
     q64 = W.as_f32(q, cache.dtype).astype(np.float64)
     T, H, D = q64.shape
     G, u, row = H // cache.H_kv, 2.0 ** -24, 0
@@ -54,6 +55,8 @@ def attention(cache, q, new, window, sm, sees=None, more=0):
             k, v = cache.k[at, kv], cache.v[at, kv]
             used = seen.any(axis=0)                          # (what nobody sees may be anything)
             k, v = np.where(used[:, None], k, 0.0), np.where(used[:, None], v, 0.0)
+            lost = (seen & np.isnan(v).any(axis=1)).any(axis=1)          # rows that see a value which is no number; it is nothing to the others
+            v = np.where(np.isnan(v).any(axis=1, keepdims=True), 0.0, v)
             for g in range(G):
                 h = kv * G + g
                 qq = q64[row:row + n, h]
@@ -68,10 +71,10 @@ def attention(cache, q, new, window, sm, sees=None, more=0):
                 d = np.where(l > 0, l, 1.0)
                 o, A, M = p @ v / d, p @ np.abs(v) / d, seen.sum(axis=1)
                 rel = (np.expm1(2 * e) + (2 * M + 32 + more) * u)[:, None]
-                out[row:row + n, h] = o
+                out[row:row + n, h] = np.where(lost[:, None], np.nan, o)
                 with np.errstate(divide="ignore"):
                     lse[row:row + n, h] = np.where(some, np.where(some, m[:, 0], 0.0) + np.log(l[:, 0]), -np.inf)
-                tol_o[row:row + n, h] = A * rel + HALF[cache.dtype] * (np.abs(o) + A * rel) + 1e-38
+                tol_o[row:row + n, h] = A * rel + HALF[cache.dtype] * (np.abs(o) + A * rel) + 1e-38 + tiny * M[:, None]
                 tol_l[row:row + n, h] = e + (M + 16) * u + 4 * u * np.abs(np.where(some, lse[row:row + n, h], 0.0))
         row += n
     return out, lse, tol_o, tol_l
