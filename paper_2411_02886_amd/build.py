@@ -18,7 +18,7 @@ LIB = os.path.join(HERE, "libtokenselect.so")
 SOURCES = ["api.hip", "score_decode.hip", "soft_vote.hip", "topk.hip", "selcache.hip", "sparse_attn_decode.hip", "sparse_attn_stream.hip", "prefill_select.hip", "sparse_attn_chunk.hip", "sparse_attn_chunk_wide.hip",
            "chunk_mean_query.hip", "select_variants.hip", "select_compact.hip", "score_codes_mfma.hip",
            "cache_api.hip", "paged_attn.hip", "paged_attn_stream.hip", "paged_attn_tall.hip", "rope_append.hip", "cache_pages.hip",
-           "quant_api.hip", "quant_cache.hip", "quant_attn.hip", "draft_api.hip", "draft_tree.hip"]
+           "quant_api.hip", "quant_cache.hip", "quant_attn.hip", "paged_wide.hip", "draft_api.hip", "draft_tree.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

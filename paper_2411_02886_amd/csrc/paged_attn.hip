@@ -9,11 +9,6 @@ namespace ts {
 hipError_t launch_paged_stream(int dtype, int D, int blocks, const PagedAttnArgs& a, const ShareArgs& sh, hipStream_t s);
 hipError_t launch_paged_tall(int D, const PagedAttnArgs& a, const ShareArgs& sh, hipStream_t s);
 
-constexpr int kTallRows = 256;
-// Workgroups that cut the line into shares: one per CU (128 / 192 / 256 / 512 of the stream kernel: a bf16 token over 131072 keys 129, 98, 91, 95 us, over
-// 1000 keys 10.9, 11.0, 11.1, 13.5, 16 drafts of 8 over 3000 keys 66, 51, 46, 49: fewer start, and fewer pieces are joined).
-constexpr int kShareWgs = 256;
-
 // Pieces of the tile that workgroup w's share began: its own and those of workgroups w + 1 .. w + count - 1, up to the one that ends the tile; a
 // share in between may hold no unit of it.  The states of the first 64 are loaded beside w's own.
 struct Pieces {
@@ -112,10 +107,10 @@ __global__ __launch_bounds__(THREADS) void paged_merge_kernel(PagedAttnArgs a, S
   }
 }
 
-// The same for the tall kernel, whose pieces lie as in its registers: of each block of 32 rows 16 bytes of the output [D / 8][64 lanes], the
+// The same for the tall kernel and the wide one, whose pieces lie as in its registers: of each block of 32 rows 16 bytes of the output [D / 8][64 lanes], the
 // lane's row lane % 32, its elements 8 i + 4 (lane / 32) .. + 3.  A wave of a workgroup (blockIdx.x: block of rows, then i / 4) has one i.
 template <int D>
-__global__ __launch_bounds__(256) void paged_merge_tall_kernel(PagedAttnArgs a, ShareArgs sh) {
+__global__ __launch_bounds__(256) void paged_merge_tall_kernel(PagedAttnArgs a, ShareArgs sh, int rows) {
   constexpr int PB = D / 32, US = 6;                    // workgroups per block of rows; partial results in flight
   const int w = blockIdx.y, G = a.H / a.H_kv;
   const int32_t* d1 = sh.desc + (size_t)w * 8 + 4;
@@ -138,8 +133,8 @@ __global__ __launch_bounds__(256) void paged_merge_tall_kernel(PagedAttnArgs a, 
       v[u] = make_float2(-INFINITY, 0.f);
       x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (p >= pieces || !pc.there(sh, w, p)) continue;
-      v[u] = *reinterpret_cast<const float2*>(sh.part_ml + (slot * kTallRows + j) * 2);
-      x[u] = reinterpret_cast<const float4*>(sh.part_o + slot * kTallRows * D)[(block * (D / 8) + i) * 64 + lane];
+      v[u] = *reinterpret_cast<const float2*>(sh.part_ml + (slot * rows + j) * 2);
+      x[u] = reinterpret_cast<const float4*>(sh.part_o + slot * rows * D)[(block * (D / 8) + i) * 64 + lane];
     }
     float m = M;
 #pragma unroll
@@ -164,9 +159,9 @@ __global__ __launch_bounds__(256) void paged_merge_tall_kernel(PagedAttnArgs a, 
 }
 
 template <int ES, int D>
-static hipError_t merge(const PagedAttnArgs& a, const ShareArgs& sh, int rows, long tiles, hipStream_t s) {
-  if (rows == kTallRows) {                       // (tiles are short only where their sequence is)
-    hipLaunchKernelGGL(paged_merge_tall_kernel<D>, dim3(kTallRows / 32 * (D / 32), sh.wgs), dim3(256), 0, s, a, sh);
+static hipError_t merge(const PagedAttnArgs& a, const ShareArgs& sh, int rows, bool by_blocks, long tiles, hipStream_t s) {
+  if (by_blocks) {                  // (tiles are short only where their sequence is)
+    hipLaunchKernelGGL(paged_merge_tall_kernel<D>, dim3(rows / 32 * (D / 32), sh.wgs), dim3(256), 0, s, a, sh, rows);
     return hipGetLastError();
   }
   // A workgroup per row that a tile may have; where only the sequences with few rows are meant, as many as one token has (12 mixed ones, 28 heads: 4 us
@@ -179,9 +174,10 @@ static hipError_t merge(const PagedAttnArgs& a, const ShareArgs& sh, int rows, l
   return hipGetLastError();
 }
 
-hipError_t launch_paged_merge(int dtype, int D, const PagedAttnArgs& a, const ShareArgs& sh, int rows, long tiles, hipStream_t s) {
-  if (dtype == TS_BF16) return D == 64 ? merge<2, 64>(a, sh, rows, tiles, s) : merge<2, 128>(a, sh, rows, tiles, s);
-  return D == 64 ? merge<4, 64>(a, sh, rows, tiles, s) : merge<4, 128>(a, sh, rows, tiles, s);
+// by_blocks: the pieces lie as the tall and the wide kernel leave them
+hipError_t launch_paged_merge(int dtype, int D, const PagedAttnArgs& a, const ShareArgs& sh, int rows, bool by_blocks, long tiles, hipStream_t s) {
+  if (dtype == TS_BF16) return D == 64 ? merge<2, 64>(a, sh, rows, by_blocks, tiles, s) : merge<2, 128>(a, sh, rows, by_blocks, tiles, s);
+  return D == 64 ? merge<4, 64>(a, sh, rows, by_blocks, tiles, s) : merge<4, 128>(a, sh, rows, by_blocks, tiles, s);
 }
 
 // bytes that tiles of `rows` rows leave pieces in
@@ -198,18 +194,20 @@ static size_t piece_bytes(int rows, int D) {
 // Rounded weights, for which the tall kernel needs half the time: up to 64 rows by the stream kernel (16 tokens over 2000 keys 18.6 us, by the tall kernel 27.7, 8
 // times 4000 47 and 53; with 96 rows it would be 75 and 52), twice that where a packed batch's sequences are
 // shorter than the bound (loose: less than three quarters of it on average; 8 of 1 to 30 tokens over up to 4000 keys 42 us, else 76; but 8 of 24 each 73 and 57).
+// A mask among the new tokens: up to 64 rows by the stream kernel as well, more by the wide one (8 trees of 16 tokens over 2000 keys 33 us, by the wide one
+// 34, over 8000 78 and 90; of 24 tokens 49 and 36, 133 and 88).
 struct PagedPlan { int few_rows, many_rows; };   // rows of the tiles of sequences with few rows, and of those with more (0: there are none)
-static PagedPlan paged_plan(int dtype, int G, int chunk, bool packed, bool loose, bool rounded) {
+static PagedPlan paged_plan(int dtype, int G, int chunk, bool packed, bool loose, bool rounded, bool tree) {
   const long rows = (long)chunk * G;
   if (rows <= 16) return PagedPlan{16, 0};
-  if (rows <= (dtype == TS_F32 ? (packed ? 64 : 32) : rounded && !loose ? 64 : 128)) return PagedPlan{32, 0};
-  return dtype == TS_BF16 ? PagedPlan{32, kTallRows} : PagedPlan{16, 64};
+  if (rows <= (dtype == TS_F32 ? (packed || tree ? 64 : 32) : tree || (rounded && !loose) ? 64 : 128)) return PagedPlan{32, 0};
+  return dtype == TS_BF16 ? PagedPlan{32, tree ? kWideRows : kTallRows} : PagedPlan{16, 64};
 }
 
 size_t paged_attn_workspace(int dtype, int D, int G, int chunk) {
   size_t most = 0;
-  for (int form = 0; form < 4; ++form) {
-    const PagedPlan pl = paged_plan(dtype, G, chunk, (form & 1) != 0, (form & 1) != 0, (form & 2) != 0);
+  for (int form = 0; form < 8; ++form) {
+    const PagedPlan pl = paged_plan(dtype, G, chunk, (form & 1) != 0, (form & 1) != 0, (form & 2) != 0, (form & 4) != 0);
     most = std::max(most, align_up(piece_bytes(pl.few_rows, D) + (pl.many_rows ? piece_bytes(pl.many_rows, D) : 0), 256));
   }
   return most;
@@ -217,7 +215,7 @@ size_t paged_attn_workspace(int dtype, int D, int G, int chunk) {
 
 hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws, hipStream_t s) {
   const int G = a.H / a.H_kv;
-  const PagedPlan pl = paged_plan(dtype, G, a.C, a.q_indptr != nullptr, (long)a.T * 4 <= (long)a.B * a.C * 3, a.round_weights != 0);
+  const PagedPlan pl = paged_plan(dtype, G, a.C, a.q_indptr != nullptr, (long)a.T * 4 <= (long)a.B * a.C * 3, a.round_weights != 0, a.mask != nullptr);
   uint8_t* at = (uint8_t*)ws;
   // tiles of every sequence (0: not as many), and bounds on all tiles and on the keys of one.  A tile of few rows beside large ones is its whole sequence.
   auto each_of = [&](int tpt, bool beside) -> int { return beside ? 1 : a.q_indptr != nullptr ? 0 : (a.C + tpt - 1) / tpt; };
@@ -227,7 +225,7 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
   };
   auto keys_of = [&](int tpt) -> long { return std::min((long)a.max_seq_len, a.window > 0 ? (long)a.window + tpt : LONG_MAX); };
   auto run = [&](int rows, int more_rows, int most_rows, bool whole) -> hipError_t {
-    const bool tall = rows == kTallRows;
+    const bool wide = rows == kWideRows && a.mask != nullptr, tall = rows == kTallRows || wide;
     const int kt = tall || dtype == TS_F32 ? 64 : 128;
     ShareArgs sh{};
     sh.tpt = rows / G;
@@ -245,9 +243,9 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
     sh.part_ml = (float*)(at + align_up((size_t)kShareWgs * 32, 256));
     sh.part_o = (float*)((uint8_t*)sh.part_ml + align_up((size_t)kShareWgs * 2 * rows * 2 * 4, 256));
     at += piece_bytes(rows, D);
-    const hipError_t e = tall ? launch_paged_tall(D, a, sh, s) : launch_paged_stream(dtype, D, rows / 16, a, sh, s);
+    const hipError_t e = wide ? launch_paged_wide(D, a, nullptr, sh, s) : tall ? launch_paged_tall(D, a, sh, s) : launch_paged_stream(dtype, D, rows / 16, a, sh, s);
     if (e != hipSuccess || whole) return e;
-    return launch_paged_merge(dtype, D, a, sh, rows, tiles_of(sh.tpt, beside), s);
+    return launch_paged_merge(dtype, D, a, sh, rows, tall, tiles_of(sh.tpt, beside), s);
   };
   // A workgroup per tile, and no merge, where tiles are short, or where there are enough of them that are not long.  (200 keys: 8.2 us, in shares 10.3; 64
   // sequences of 250 to 500 keys, 512 tiles: 22.8 and 29; but 16 fp32 sequences of 1000 to 2000 keys, 32 tiles, 42 us instead of 17.)  Beside large
@@ -262,7 +260,7 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
   // tile 20.7, 512 tokens 17 and 29, with rounded weights 20.8; 768, more tiles than that, 33 and 38, rounded 27, and 4 of 256 25 and 22.  fp32: 256 tokens 20.5, by 64 rows a tile 33, 400 39 and 48.)
   // (fp32, whose larger tiles save less, also with more tiles of few keys: 16 sequences of 64 tokens 33 and 45, 4 of 256 60 and 60.)
   const long small = tiles_of(32 / G, false), small_keys = keys_of(32 / G);
-  if (small_keys <= 1024 && (small <= 2 * kShareWgs || (dtype == TS_F32 && small * small_keys <= 1l << 18))) return run(32, 0, INT_MAX, true);
+  if (small_keys <= (a.mask != nullptr ? 512 : 1024) && (small <= 2 * kShareWgs || (dtype == TS_F32 && small * small_keys <= 1l << 18))) return run(32, 0, INT_MAX, true);
   if (a.q_indptr != nullptr) {                             // (without, every sequence has as many)
     const hipError_t e = run(pl.few_rows, 0, pl.few_rows, few_whole(pl.few_rows, true));
     if (e != hipSuccess) return e;

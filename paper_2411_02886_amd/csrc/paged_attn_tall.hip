@@ -50,7 +50,7 @@ template <int D> __device__ __forceinline__ int pt_swz(int key) {
   return D == 128 ? (((key & 3) << 2) | ((key >> 2) & 3)) : ((((key >> 1) & 1) << 2) | (((key >> 2) & 1) << 1) | ((key >> 3) & 1));
 }
 
-template <int D, bool FULL, bool TREE>        // FULL: weights of 24 bits, else rounded to bf16; TREE: a mask among the new tokens
+template <int D, bool FULL>                   // FULL: weights of 24 bits, else rounded to bf16
 __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, ShareArgs sh) {
   constexpr int KS = D / 16;                  // k-steps of Q K^T
   constexpr int NBO = D / 32;                 // 32-row blocks of the transposed output
@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
   const int wg = share_of(blockIdx.x, sh.wgs);
   SharePlace from, to;
   SeqShape first;
-  find_share<kPtTile>(a, sh, G, wg, s_share, &from, &to, &first, TREE);
+  find_share<kPtTile>(a, sh, G, wg, s_share, &from, &to, &first);
   int32_t* desc = sh.desc + (size_t)wg * 8;
   if (!sh.whole && threadIdx.x == 0) { desc[3] = kPieceNone; desc[7] = kPieceNone; }
 
@@ -98,8 +98,7 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
 
   walk_share<kPtTile>(a, sh, G, from, to, first, [&](int kvh, const SeqShape& sq, int r, const TileKeys& keys, int ua, int ub, bool again) __attribute__((always_inline)) -> bool {
     const int c0 = r * sh.tpt, ntok = min(sh.tpt, sq.n - c0), nrows = ntok * G;
-    const int row0 = sq.row0 + c0, base = sq.N - sq.n;
-    const int x0 = TREE ? base - 1 : base + c0, x1 = TREE ? base + sq.n - 1 : x0 + ntok - 1;   // places of the first and last token (TREE: that all rows see, that some row may)
+    const int row0 = sq.row0 + c0, x0 = sq.N - sq.n + c0, x1 = x0 + ntok - 1;   // first row; places of the first and last token
     const bool whole = ua == 0 && ub == keys.units;
     const int tmax = keys.end - 1;
     auto token_of = [&](uint32_t j) -> uint32_t { return __umul24(j, g_inv) >> 16; };   // j / G
@@ -180,8 +179,7 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
 #pragma unroll
     for (int rb = 0; rb < 2; ++rb) {
       const int j = wave * 64 + rb * 32 + col;
-      if constexpr (TREE) low[rb] = (uint32_t)tree_low(a, row0 + min((int)token_of(j), ntok - 1), sq.n, base);
-      else low[rb] = (uint32_t)(j < nrows ? x0 + token_of(j) : x1) - (reach - 1u);
+      low[rb] = (uint32_t)(j < nrows ? x0 + token_of(j) : x1) - (reach - 1u);
     }
     asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NLQ) : "memory");    // page ids
     rows_of(0);
@@ -211,19 +209,6 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
 #pragma unroll
         for (int e = 0; e < 16; ++e) oacc[rb][nb][e] = 0.f;
 
-
-    // TREE: hides what the lane's row does not see of a block of 32 keys; j0: the key of element 0
-    auto bits_of = [&](int rb, int j0) __attribute__((always_inline)) -> uint32_t {
-      return tree_bits(a, row0 + min((int)token_of(wave * 64 + rb * 32 + col), ntok - 1), sq.n, base, (int)low[rb], j0 - 4 * half) >> (4 * half);
-    };
-    auto hide = [&](f32x16_t (&x)[2], int j0) __attribute__((always_inline)) {
-#pragma unroll
-      for (int rb = 0; rb < 2; ++rb) {
-        const uint32_t bits = bits_of(rb, j0);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[rb][e] = (bits >> (8 * (e >> 2) + (e & 3)) & 1u) != 0u ? x[rb][e] : hidden;
-      }
-    };
 
     // ---- blocks of 32 keys, two to a tile.  While the vector ALU forms the weights of block j, the matrix cores form the scores of
     // block j + 1 and add the output of block j - 1.
@@ -268,8 +253,6 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
       f32x16_t (&x)[2] = s[CUR];
       const int j0 = key0 + it * kPtTile + CUR * 32 + 4 * half;    // key of element 0
       if constexpr (MASKED) {
-        if constexpr (TREE) hide(x, j0);
-        else
 #pragma unroll
         for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
@@ -447,13 +430,11 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
       for (int g = G0; g < G1 && g < G0 + AHEAD; ++g) { if (CIN) frag[g] = carry[g - G0]; else fetch(g); }
       constexpr int FORM = 16 / VS, SPLIT = 8 / NBO, LATE = 8 / KS;   // pairs formed per output step, split per output step of k-step 1, split per score step
       if constexpr (MASKED) {
-        if constexpr (TREE) hide(x, j0);
-        else
 #pragma unroll
         for (int rb = 0; rb < 2; ++rb)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const uint32_t key = (uint32_t)(j0 + 8 * (e >> 2) + (e & 3)) - low[rb];   // counted from the first that the row sees
+            const uint32_t key = (uint32_t)(j0 + 8 * (e >> 2) + (e & 3)) - low[rb];
             x[rb][e] = key < reach ? x[rb][e] : hidden;
           }
         if (__builtin_expect(f1 == INT_MIN, 0)) round_logits(x);
@@ -559,11 +540,6 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
 #pragma unroll
     for (int rb = 0; rb < 2; ++rb) {
       float m = -INFINITY;
-      if constexpr (TREE) {
-        const uint32_t bits = bits_of(rb, key0 + 4 * half);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) m = fmaxf(m, (bits >> (8 * (e >> 2) + (e & 3)) & 1u) != 0u ? c2 * s[0][rb][e] : -INFINITY);
-      } else
 #pragma unroll
       for (int e = 0; e < 16; ++e) m = fmaxf(m, (uint32_t)(key0 + 4 * half + 8 * (e >> 2) + (e & 3)) - low[rb] < reach ? c2 * s[0][rb][e] : -INFINITY);
       m = fmaxf(m, __shfl_xor(m, 32)) + kPtHead;
@@ -677,24 +653,23 @@ __global__ __launch_bounds__(256, 1) void paged_tall_kernel(PagedAttnArgs a, Sha
       }
     }
     return false;
-  }, TREE);
+  });
 }
 
-template <int D, bool FULL, bool TREE>
+template <int D, bool FULL>
 static hipError_t tall_one(const PagedAttnArgs& a, const ShareArgs& sh, hipStream_t s) {
   constexpr int lds = 2 * kPtBuf * kPtTile * D * 2 + 4 * kPtRing * 256 + sizeof(ShareScratch) + 16;
   if (lds > 65536) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_tall_kernel<D, FULL, TREE>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_tall_kernel<D, FULL>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((paged_tall_kernel<D, FULL, TREE>), dim3(sh.wgs), dim3(256), lds, s, a, sh);
+  hipLaunchKernelGGL((paged_tall_kernel<D, FULL>), dim3(sh.wgs), dim3(256), lds, s, a, sh);
   return hipGetLastError();
 }
 
 hipError_t launch_paged_tall(int D, const PagedAttnArgs& a, const ShareArgs& sh, hipStream_t s) {
-  if (a.mask != nullptr) return D == 64 ? tall_one<64, true, true>(a, sh, s) : tall_one<128, true, true>(a, sh, s);
-  if (a.round_weights) return D == 64 ? tall_one<64, false, false>(a, sh, s) : tall_one<128, false, false>(a, sh, s);
-  return D == 64 ? tall_one<64, true, false>(a, sh, s) : tall_one<128, true, false>(a, sh, s);
+  if (a.round_weights) return D == 64 ? tall_one<64, false>(a, sh, s) : tall_one<128, false>(a, sh, s);
+  return D == 64 ? tall_one<64, true>(a, sh, s) : tall_one<128, true>(a, sh, s);
 }
 
 }  // namespace ts

@@ -26,6 +26,8 @@ struct ShareArgs {
   int min_keys;     // smallest share
   int tile_cost;    // keys that a tile's start and end cost
   int wgs;          // workgroups of the launch
+  int heads_shift;  // 8-bit caches: log2 of the KV heads that a workgroup has side by side
+  int together;     // a cut has a multiple of together + 1 units (a power of two) in front of it
   int32_t* desc;    // [wgs][2][4]: first row, KV head and number of tokens of the tile, kPiece*; [0]: the piece goes on from the workgroup before, [1]: it begins the tile
   float* part_o;    // [wgs][2][rows][D] not normalised
   float* part_ml;   // [wgs][2][rows][2] (reference, sum)
@@ -105,15 +107,15 @@ __device__ __forceinline__ void find_unit(const PagedAttnArgs& a, const ShareArg
   }
   const double begin = line_room(a, sh, q, lo, tree), room = line_room(a, sh, q, lo + 1, tree) - begin;
   const TileKeys k = tile_keys<KT>(a, sh, q, tile_at(q, lo), tree);
-  const int u = max((int)fmin(floor_div((y - begin) * k.units, room), (double)k.units), 0);
+  const int u = max((int)fmin(floor_div((y - begin) * k.units, room), (double)k.units), 0) & ~sh.together;
   const int near = (int)fmin(share * (1. / (KT * 24)), (double)k.units);   // a cut so near an end would cost more than it evens out
   *tile = lo;
   *unit = u < near ? 0 : k.units - u < near ? k.units : u;
 }
 
-// Begin and end of this workgroup's share, in scalar registers, and the sequence that it begins in.  Called by all threads of the workgroup (256).
+// Begin and end of this workgroup's share, in scalar registers, and the sequence that it begins in.  Called by all threads of the workgroup (256 or more).
 struct ShareScratch { double sums[4], y[2]; int kvh[2]; SeqShape shape[2]; SharePlace place[2]; };
-template <int KT>
+template <int KT, int THREADS = 256>
 __device__ __forceinline__ void find_share(const PagedAttnArgs& a, const ShareArgs& sh, int G, int wg, ShareScratch* lds, SharePlace* from,
                                            SharePlace* to, SeqShape* first, bool tree = false) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -186,7 +188,7 @@ __device__ __forceinline__ void find_share(const PagedAttnArgs& a, const ShareAr
   double upto = mine;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) { const double x = __shfl_up(upto, d); if (lane >= d) upto += x; }
-  if (lane == 63) lds->sums[wave] = upto;
+  if (lane == 63 && (THREADS == 256 || wave < 4)) lds->sums[wave] = upto;     // (those of later waves have no sequences)
   if (tid < 2) lds->kvh[tid] = a.H_kv;         // the end of the line; also where lengths that change under the call lead nowhere
   __syncthreads();
   double before = upto - mine, line = 0.;

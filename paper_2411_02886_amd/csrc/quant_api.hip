@@ -51,7 +51,7 @@ int32_t ts_quant_attn_workspace_bytes(const ts_problem* p, int32_t num_rows, siz
   if (bytes == nullptr || num_rows < 0) return TS_ERR_INVALID_ARG;
   const int32_t st = check_problem(p);
   if (st != TS_OK) return st;
-  *bytes = quant_attn_workspace(p->dtype, p->head_dim, p->num_q_heads / p->num_kv_heads, p->chunk);
+  *bytes = quant_attn_workspace(p->dtype, p->head_dim, p->num_q_heads / p->num_kv_heads, p->num_kv_heads, p->chunk);
   return TS_OK;
 }
 
@@ -67,7 +67,7 @@ int32_t ts_quant_attn(const ts_problem* p, const ts_quant* c, const void* q, con
   if (q == nullptr || out == nullptr || !aligned16(q) || !aligned16(out)) return TS_ERR_INVALID_ARG;
   const size_t es = p->dtype == TS_BF16 ? 2 : 4, bytes = (size_t)num_rows * p->num_q_heads * p->head_dim * es;
   if (overlap(q, bytes, out, bytes)) return TS_ERR_INVALID_ARG;
-  const size_t need = quant_attn_workspace(p->dtype, p->head_dim, p->num_q_heads / p->num_kv_heads, p->chunk);
+  const size_t need = quant_attn_workspace(p->dtype, p->head_dim, p->num_q_heads / p->num_kv_heads, p->num_kv_heads, p->chunk);
   if (ws == nullptr || ((uintptr_t)ws & 255) != 0 || ws_bytes < need) return TS_ERR_WORKSPACE;
   PagedAttnArgs a{};
   a.q = (const uint8_t*)q;

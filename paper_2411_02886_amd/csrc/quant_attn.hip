@@ -4,40 +4,29 @@
 // numbers that bf16 holds exactly, so scores are bf16 products of queries and codes, summed in float, times the key's scale; a weight is multiplied
 // with the value's scale and cut into three bf16 numbers that add up to it, each of which multiplies the codes of V: nothing is rounded that float
 // arithmetic would not round.  fp32 queries are three bf16 numbers as well.
-// Four waves walk wave tiles of 32 keys of their own without barriers, rows in registers: K as the matrix product wants it (a lane has a key's 16 bytes), V as rows too (a
+// This is the kernel of few rows, bound by the bytes it reads: a workgroup's four waves have four KV heads side by side, or share the keys of one.  Many rows: paged_wide.hip.
+// The waves walk wave tiles of 32 keys of their own without barriers, rows in registers: K as the matrix product wants it (a lane has a key's 16 bytes), V as rows too (a
 // lane has the same bytes of its eight keys), whose bytes are transposed in the lane by byte permutations before they are widened.  A tile's rows, scales and page ids
 // are requested a tile ahead.
+// Eight sequences of 16384 to 65536 keys, 8 KV heads of 128, int8, a token each: 148 us, 5.4 TB/s with the joining of the pieces; the same read pattern without arithmetic
+// reaches 5.8 to 6.1 TB/s, one head per workgroup 5.35.
 #include "paged_shares.h"
 #include "ts_codes.h"
 #include <algorithm>
 
 namespace ts {
 
-hipError_t launch_paged_merge(int dtype, int D, const PagedAttnArgs& a, const ShareArgs& sh, int rows, long tiles, hipStream_t s);
+hipError_t launch_paged_merge(int dtype, int D, const PagedAttnArgs& a, const ShareArgs& sh, int rows, bool by_blocks, long tiles, hipStream_t s);
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
 typedef __attribute__((ext_vector_type(4))) float f32x4_t;
 
-constexpr int kQaWgs = 256;                   // workgroups that cut the line into shares
 constexpr int kQaTile = 32;                   // keys of a wave tile
 constexpr float kQaUnset = -3.40282347e38f;   // reference exponent before the first key: no finite one lies below it
 constexpr float kQaHead = 6.f;                // a raised reference lies this far above the largest exponent so far ...
 constexpr float kQaRaise = 2.f;               // ... and is raised again when a lane's weights of a tile exceed this together
 
-// four codes as two pairs of bf16 numbers
-template <int CODE>
-__device__ __forceinline__ uint2 widen(uint32_t w) {
-  if constexpr (CODE == TS_E4M3) {
-    return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.f, false)),
-                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.f, true)));
-  } else {                                     // a whole number of seven bits is the high half of its float
-    float x[4];
-    codes_to_f32<CODE>(w, x);
-    return make_uint2(__builtin_amdgcn_perm(__float_as_uint(x[1]), __float_as_uint(x[0]), 0x07060302u),
-                      __builtin_amdgcn_perm(__float_as_uint(x[3]), __float_as_uint(x[2]), 0x07060302u));
-  }
-}
 // byte c of each of four words, as word c
 __device__ __forceinline__ void transpose4(uint32_t (&v)[4]) {
   const uint32_t lo01 = __builtin_amdgcn_perm(v[1], v[0], 0x05010400u), hi01 = __builtin_amdgcn_perm(v[1], v[0], 0x07030602u);
@@ -53,7 +42,7 @@ __device__ __forceinline__ float low_part(float y) { return y - __uint_as_float(
 
 template <int CODE, int ES, int D, int CB>    // ES: bytes of a query's and an output's element; CB: blocks of 16 rows
 __global__ __launch_bounds__(256, CB == 1 ? 2 : 1) void quant_attn_kernel(PagedAttnArgs a, QuantPools c, ShareArgs sh) {
-  constexpr int TK = kQaTile, KT = 4 * TK;
+  constexpr int TK = kQaTile;
   constexpr int QP = ES == 2 ? 1 : 3;         // bf16 numbers that a query element is the sum of
   constexpr int NP = D / 64;                  // 16-byte pieces of a key per lane
   constexpr int VB = D / 16;                  // bytes of a value per lane, and 16-row blocks of the transposed output
@@ -65,29 +54,39 @@ __global__ __launch_bounds__(256, CB == 1 ? 2 : 1) void quant_attn_kernel(PagedA
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, kgrp = lane >> 4;
-  const int H = a.H, G = a.H / a.H_kv;
+  // The waves have one, two or four KV heads side by side, and share the keys of a head if it is fewer than four.  To the shares and the merge the heads of a
+  // workgroup are one with all of their query heads (`line`).
+  const int heads_shift = sh.heads_shift, heads = 1 << heads_shift, parts = 4 >> heads_shift;
+  const int my_head = wave & (heads - 1), my_part = wave >> heads_shift;
+  const int H = a.H, G = a.H / a.H_kv, GW = G << heads_shift;
+  PagedAttnArgs line = a;
+  line.H_kv = a.H_kv >> heads_shift;
   const bool tree = a.mask != nullptr;
   const int wg = share_of(blockIdx.x, sh.wgs);
   SharePlace from, to;
   SeqShape first;
-  find_share<KT>(a, sh, G, wg, &s_share, &from, &to, &first, tree);
+  find_share<TK>(line, sh, G, wg, &s_share, &from, &to, &first, tree);
   int32_t* desc = sh.desc + (size_t)wg * 8;
   if (!sh.whole && threadIdx.x == 0) { desc[3] = kPieceNone; desc[7] = kPieceNone; }
   const uint32_t g_inv = 65536u / (uint32_t)G + 1u;             // exact for rows below 256
   const float c2 = a.sm_scale * 1.44269504088896340736f;        // logits are exponents of two here
   const int row_shift = 31 - __builtin_clz((uint32_t)(a.H_kv * D));   // H_kv is a power of two
 
-  walk_share<KT>(a, sh, G, from, to, first, [&](int kvh, const SeqShape& sq, int r, const TileKeys& keys, int ua, int ub, bool) -> bool {
+  walk_share<TK>(line, sh, G, from, to, first, [&](int group, const SeqShape& sq, int r, const TileKeys& keys, int ua, int ub, bool) -> bool {
     const int c0 = r * sh.tpt, ntok = min(sh.tpt, sq.n - c0), nrows = ntok * G;
     const int row0 = sq.row0 + c0, base = sq.N - sq.n;
     const bool whole = ua == 0 && ub == keys.units;
     const int tmax = keys.end - 1;
     auto token_of = [&](uint32_t j) -> int { return (int)min(__umul24(j, g_inv) >> 16, (uint32_t)(ntok - 1)); };   // j / G; rows past the last stand for it
-    const size_t tile_row = (size_t)row0 * H + kvh * G;
-    auto row_at = [&](uint32_t j) -> uint32_t { return __umul24(__umul24(j, g_inv) >> 16, (uint32_t)(H - G)) + j; };
+    const int kvh = (group << heads_shift) + my_head;
+    // row j of a wave's head in q, out and lse, and in a piece: its token's rows, the workgroup's heads side by side
+    const size_t tile_row = (size_t)row0 * H + group * GW;
+    auto row_at = [&](uint32_t j, int h) -> uint32_t { return __umul24(__umul24(j, g_inv) >> 16, (uint32_t)(H - G)) + j + (uint32_t)(h * G); };
+    auto piece_at = [&](uint32_t j, int h) -> uint32_t { return __umul24(__umul24(j, g_inv) >> 16, (uint32_t)(GW - G)) + j + (uint32_t)(h * G); };
     if (keys.end <= keys.first) {                                  // no row sees a token (one unit: the tile is not cut)
-      for (int i = threadIdx.x; i < nrows * D; i += 256) {
-        const size_t o = tile_row + row_at((uint32_t)(i / D));
+      for (int i = threadIdx.x; i < (nrows << heads_shift) * D; i += 256) {
+        const int j = i / D;
+        const size_t o = tile_row + row_at((uint32_t)(j >> heads_shift), j & (heads - 1));
         if (ES == 2) reinterpret_cast<uint16_t*>(a.out)[o * D + i % D] = 0; else reinterpret_cast<float*>(a.out)[o * D + i % D] = 0.f;
         if (i % D == 0 && a.lse != nullptr) a.lse[o] = -INFINITY;
       }
@@ -96,13 +95,11 @@ __global__ __launch_bounds__(256, CB == 1 ? 2 : 1) void quant_attn_kernel(PagedA
     const int slot = ua > 0 ? 0 : 1;
     if (!whole && threadIdx.x == 0) {
       int32_t* d = desc + slot * 4;
-      d[0] = row0; d[1] = kvh; d[2] = ntok; d[3] = ub == keys.units ? kPieceEnds : kPieceGoesOn;
+      d[0] = row0; d[1] = group; d[2] = ntok; d[3] = ub == keys.units ? kPieceEnds : kPieceGoesOn;
     }
     const int32_t* pages = a.page_indices + sq.page0;
-    // the wave's tiles: tile i holds keys key0 + i * KT .. + TK; a last one without a key is left out
-    const int key0 = (keys.u0 + ua) * KT + wave * TK;
-    int nt = ub - ua;
-    if (key0 + (nt - 1) * KT > tmax) --nt;
+    // the wave's tiles: tile i holds keys key0 + i * KT .. + TK
+    const int KT = TK * parts, key0 = (keys.u0 + ua) * TK + my_part * TK, nt = (ub - ua - my_part + parts - 1) >> (2 - heads_shift);
     // (keys past the end or in front of the tile's first window stand for the nearest that some row sees: no other place of the cache is read)
     const int my_key = lane & (TK - 1);
     auto key_of = [&](int i) -> int { return min(max(key0 + i * KT + my_key, keys.first), tmax); };
@@ -117,7 +114,7 @@ __global__ __launch_bounds__(256, CB == 1 ? 2 : 1) void quant_attn_kernel(PagedA
       const bool there = (int)j < nrows;
       place[cb] = base + c0 + token_of(j);
       low[cb] = tree ? tree_low(a, row0 + token_of(j), sq.n, base) : a.window > 0 ? place[cb] - a.window + 1 : 0;
-      const uint8_t* q = a.q + (tile_row + (there ? row_at(j) : 0u)) * (size_t)(D * ES);
+      const uint8_t* q = a.q + (tile_row + (there ? row_at(j, my_head) : 0u)) * (size_t)(D * ES);
 #pragma unroll
       for (int x = 0; x < 2 * NP; ++x) {
         const int d = 64 * (x >> 1) + 16 * kgrp + 8 * (x & 1);
@@ -143,7 +140,7 @@ __global__ __launch_bounds__(256, CB == 1 ? 2 : 1) void quant_attn_kernel(PagedA
       }
     }
 
-    uint4 kr[2][NP];                                               // the next tile's keys 16 kb + col
+    u32x4_t kr[2][NP];                                             // the next tile's keys 16 kb + col
     uint32_t vr[8][VB / 4];                                        // its values of keys 16 (j / 4) + 4 kgrp + j % 4, bytes VB col ..
     float scale;                                                   // of key my_key: K's in lanes 0 .. 31, V's in the others
     const uint8_t* const k_head = c.k_codes + kvh * D + kgrp * 16;
@@ -159,7 +156,7 @@ __global__ __launch_bounds__(256, CB == 1 ? 2 : 1) void quant_attn_kernel(PagedA
       for (int kb = 0; kb < 2; ++kb) {
         const uint8_t* row = k_head + ((uint64_t)s_slot[wave][kb * 16 + col] << row_shift);
 #pragma unroll
-        for (int x = 0; x < NP; ++x) kr[kb][x] = *reinterpret_cast<const uint4*>(row + x * 64);
+        for (int x = 0; x < NP; ++x) kr[kb][x] = *reinterpret_cast<const u32x4_t*>(row + x * 64);
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -187,7 +184,7 @@ __global__ __launch_bounds__(256, CB == 1 ? 2 : 1) void quant_attn_kernel(PagedA
     }
     for (int i = 0; i < nt; ++i) {
       const int k0 = key0 + i * KT;
-      uint4 k_now[2][NP];
+      u32x4_t k_now[2][NP];
       uint32_t v_now[8][VB / 4];
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
@@ -213,8 +210,8 @@ __global__ __launch_bounds__(256, CB == 1 ? 2 : 1) void quant_attn_kernel(PagedA
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int x = 0; x < 2 * NP; ++x) {
-          const uint4 w = k_now[kb][x >> 1];
-          const bf16x8_t kf = (x & 1) == 0 ? frag_of(widen<CODE>(w.x), widen<CODE>(w.y)) : frag_of(widen<CODE>(w.z), widen<CODE>(w.w));
+          const u32x4_t w = k_now[kb][x >> 1];
+          const bf16x8_t kf = frag_of(widen<CODE>(w[2 * (x & 1)]), widen<CODE>(w[2 * (x & 1) + 1]));
 #pragma unroll
           for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
@@ -293,9 +290,10 @@ __global__ __launch_bounds__(256, CB == 1 ? 2 : 1) void quant_attn_kernel(PagedA
       }
     }
 
-    // ---- the four waves meet, sixteen rows at a time
-    float* part_o = sh.part_o + ((size_t)wg * 2 + slot) * (16 * CB) * D;
-    float* part_ml = sh.part_ml + ((size_t)wg * 2 + slot) * (16 * CB) * 2;
+    // ---- the waves of a head meet, sixteen rows of each head at a time
+    const int rows = 16 * CB << heads_shift;
+    float* part_o = sh.part_o + ((size_t)wg * 2 + slot) * rows * D;
+    float* part_ml = sh.part_ml + ((size_t)wg * 2 + slot) * rows * 2;
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
       if (cb * 16 >= nrows) break;
@@ -310,23 +308,25 @@ __global__ __launch_bounds__(256, CB == 1 ? 2 : 1) void quant_attn_kernel(PagedA
           *reinterpret_cast<float4*>(&s_o[wave][col][VB * (4 * kgrp + e) + x]) = make_float4(o[cb][x][e], o[cb][x + 1][e], o[cb][x + 2][e], o[cb][x + 3][e]);
       if (kgrp == 0) { s_ml[wave][col][0] = ref[cb]; s_ml[wave][col][1] = l; }
       __syncthreads();
-#pragma unroll
-      for (int it = 0; it < 16 * D / 4 / 256; ++it) {
-        const int i = it * 256 + threadIdx.x, jj = i / (D / 4), d = i % (D / 4) * 4, j = cb * 16 + jj;
+      for (int i = threadIdx.x; i < (16 * D / 4) << heads_shift; i += 256) {
+        const int jw = i / (D / 4), h = jw >> 4, jj = jw & 15, d = i % (D / 4) * 4, j = cb * 16 + jj;
         if (j >= nrows) continue;
-        const float m = fmaxf(fmaxf(s_ml[0][jj][0], s_ml[1][jj][0]), fmaxf(s_ml[2][jj][0], s_ml[3][jj][0]));
+        float m = kQaUnset;
+#pragma unroll
+        for (int w4 = 0; w4 < 4; ++w4) m = fmaxf(m, (w4 & (heads - 1)) == h ? s_ml[w4][jj][0] : kQaUnset);
         float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
         float L = 0.f;
 #pragma unroll
         for (int w4 = 0; w4 < 4; ++w4) {
-          const float f = __builtin_amdgcn_exp2f(s_ml[w4][jj][0] - m);       // a wave without keys of the row: its sums are 0
           const float4 z = *reinterpret_cast<const float4*>(&s_o[w4][jj][d]);
+          const float l = s_ml[w4][jj][1], f = __builtin_amdgcn_exp2f(s_ml[w4][jj][0] - m);       // a wave without keys of the row: its sums are 0
+          if ((w4 & (heads - 1)) != h) continue;
           y.x = fmaf(f, z.x, y.x); y.y = fmaf(f, z.y, y.y); y.z = fmaf(f, z.z, y.z); y.w = fmaf(f, z.w, y.w);
-          L = fmaf(f, s_ml[w4][jj][1], L);
+          L = fmaf(f, l, L);
         }
         constexpr float kLn2 = 0.69314718055994530942f;
         if (whole) {
-          const size_t hb = tile_row + row_at((uint32_t)j);
+          const size_t hb = tile_row + row_at((uint32_t)j, h);
           const float inv = L == 0.f ? 0.f : 1.f / L;                        // (a sum that is no number stays one)
           y = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
           if (ES == 2) {
@@ -335,8 +335,9 @@ __global__ __launch_bounds__(256, CB == 1 ? 2 : 1) void quant_attn_kernel(PagedA
           } else *reinterpret_cast<float4*>(a.out + (hb * D + d) * 4) = y;
           if (d == 0 && a.lse != nullptr) a.lse[hb] = L == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(L)) * kLn2;
         } else {
-          *reinterpret_cast<float4*>(part_o + j * D + d) = y;
-          if (d == 0) { part_ml[2 * j] = L == 0.f ? -INFINITY : m * kLn2; part_ml[2 * j + 1] = L; }   // in units of the logits
+          const uint32_t pr = piece_at((uint32_t)j, h);
+          *reinterpret_cast<float4*>(part_o + (size_t)pr * D + d) = y;
+          if (d == 0) { part_ml[2 * pr] = L == 0.f ? -INFINITY : m * kLn2; part_ml[2 * pr + 1] = L; }   // in units of the logits
         }
       }
     }
@@ -352,54 +353,81 @@ static hipError_t quant_one(const PagedAttnArgs& a, const QuantPools& c, const S
 template <int CODE, int D>
 static hipError_t quant_some(int dtype, int blocks, const PagedAttnArgs& a, const QuantPools& c, const ShareArgs& sh, hipStream_t s) {
   if (dtype == TS_F32) return blocks == 1 ? quant_one<CODE, 4, D, 1>(a, c, sh, s) : quant_one<CODE, 4, D, 2>(a, c, sh, s);
-  return blocks == 1 ? quant_one<CODE, 2, D, 1>(a, c, sh, s) : blocks == 2 ? quant_one<CODE, 2, D, 2>(a, c, sh, s) : quant_one<CODE, 2, D, 4>(a, c, sh, s);
+  return blocks == 1 ? quant_one<CODE, 2, D, 1>(a, c, sh, s) : quant_one<CODE, 2, D, 2>(a, c, sh, s);
+}
+
+// KV heads that a workgroup may have side by side
+static int most_beside(int H_kv) { return H_kv < 4 ? H_kv : 4; }
+// Heads side by side read four times as many bytes of a token at once, one head has its keys divided among four waves.  A call with much to read for
+// every workgroup is bound by the bytes (int8, 8 KV heads of 128, one token each; side by side against one: 64 sequences of 6000 keys 147 against 165 us, 8 of up
+// to 65536 147 against 165, 32 of 8000 with D 64 45 against 51), others by the way through the keys (one of 8000 22.9 against 17.4, 8 of 4000 26.5 against
+// 20.8, 64 of 500 24.7 against 17.6, drafts of four tokens over 16 of 8000 79 against 58).
+static int heads_beside(const PagedAttnArgs& a, int D) {
+  const long keys = std::min((long)a.max_seq_len, a.window > 0 ? (long)a.window + a.C : LONG_MAX);
+  return (double)a.B * keys * a.H_kv / kShareWgs >= 48. * D ? most_beside(a.H_kv) : 1;
 }
 
 // bytes that tiles of `rows` rows leave pieces in
-static size_t quant_piece_bytes(int rows, int D) {
-  return align_up((size_t)kQaWgs * 32, 256) + align_up((size_t)kQaWgs * 2 * rows * 2 * 4, 256) + (size_t)kQaWgs * 2 * rows * D * 4;
+static size_t quant_piece_bytes(int wgs, int rows, int D) {
+  return align_up((size_t)wgs * 32, 256) + align_up((size_t)wgs * 2 * rows * 2 * 4, 256) + (size_t)wgs * 2 * rows * D * 4;
 }
 
+// A sequence's rows n * G decide.  Up to 32 are a tile of the stream kernel, up to 64 two (28/4 heads: over 2000 keys 18 us, by the wide
+// kernel 24, 8 times 8000 keys 97 and 89); more are tiles of the wide kernel in bf16, which reads and widens a key once for 256, of 32 rows in fp32, whose products
+// are three times as many and need the registers.
 struct QuantPlan { int few_rows, many_rows; };   // rows of the tiles of sequences with few rows, and of those with more (0: there are none)
 static QuantPlan quant_plan(int dtype, int G, int chunk) {
   const long rows = (long)chunk * G;
   if (rows <= 16) return QuantPlan{16, 0};
-  if (rows <= 32) return QuantPlan{32, 0};
-  return QuantPlan{16, dtype == TS_F32 ? 32 : 64};
+  if (rows <= 64) return QuantPlan{32, 0};
+  return dtype == TS_F32 ? QuantPlan{16, 32} : QuantPlan{32, kWideRows};
 }
 
-size_t quant_attn_workspace(int dtype, int D, int G, int chunk) {
+size_t quant_attn_workspace(int dtype, int D, int G, int H_kv, int chunk) {
   const QuantPlan pl = quant_plan(dtype, G, chunk);
-  return align_up(quant_piece_bytes(pl.few_rows, D) + (pl.many_rows ? quant_piece_bytes(pl.many_rows, D) : 0), 256);
+  size_t bytes = quant_piece_bytes(kShareWgs, pl.few_rows * most_beside(H_kv), D);
+  if (pl.many_rows == kWideRows) bytes += quant_piece_bytes(kShareWgs, kWideRows, D);
+  else if (pl.many_rows) bytes += quant_piece_bytes(kShareWgs, pl.many_rows * most_beside(H_kv), D);
+  return align_up(bytes, 256);
 }
 
 hipError_t launch_quant_attn(int dtype, int D, const PagedAttnArgs& a, const QuantPools& c, void* ws, hipStream_t s) {
-  const int G = a.H / a.H_kv;
+  const int G = a.H / a.H_kv, heads = heads_beside(a, D);
   const QuantPlan pl = quant_plan(dtype, G, a.C);
   uint8_t* at = (uint8_t*)ws;
   auto run = [&](int rows, int more_rows, int most_rows) -> hipError_t {
+    const bool wide = rows == kWideRows;
+    PagedAttnArgs line = a;                                // what the merge sees: the heads that a workgroup has side by side are one
+    if (!wide) line.H_kv = a.H_kv / heads;
+    const int held = wide ? rows : rows * heads, wgs = kShareWgs;
     ShareArgs sh{};
+    sh.heads_shift = wide ? 0 : ilog2(heads);
+    sh.together = wide ? 0 : 4 / heads - 1;                // a unit for each wave (else the cuts fall so that one workgroup has two short pieces, one after the other: 4095 keys 13.1 us instead of 10.2)
     sh.tpt = rows / G;
     sh.more_rows = more_rows;
     sh.most_rows = most_rows;
     const bool beside = most_rows < INT_MAX;
     // tiles of every sequence (0: not as many), and bounds on all tiles and on the keys of one
     sh.each = beside ? 1 : a.q_indptr != nullptr ? 0 : (a.C + sh.tpt - 1) / sh.tpt;
-    const long tiles = (sh.each > 0 ? (long)a.B * sh.each : (long)a.T / sh.tpt + a.B) * a.H_kv;
+    const long tiles = (sh.each > 0 ? (long)a.B * sh.each : (long)a.T / sh.tpt + a.B) * line.H_kv;
     const long keys = std::min((long)a.max_seq_len, a.window > 0 ? (long)a.window + a.C : LONG_MAX);
-    sh.whole = tiles < (1l << 23) && (keys <= 512 || (tiles >= kQaWgs && keys <= 16 * 4 * kQaTile)) ? 1 : 0;
-    sh.min_keys = 4 * kQaTile;
-    sh.tile_cost = 64;
-    sh.wgs = sh.whole ? (int)tiles : kQaWgs;
+    // A workgroup per tile and no merge where that is no longer a way than the pieces' and their joining (one bf16 token, D 128, 8 KV heads: 400 keys 9.2 us, cut
+    // 13.8; 1000 keys 14.0 and 13.9; 2000 keys 23.3 and 14.0; fp32 over 500 keys 7.0 and 12.7)
+    sh.whole = wide ? tiles <= wgs * (a.q_indptr != nullptr ? 2 : 1) && keys <= 1024
+                    : tiles < (1l << 23) && (keys <= 512 || (tiles >= kShareWgs && keys <= 2048));
+    sh.min_keys = wide ? 128 : kQaTile * 4 / heads;
+    sh.tile_cost = wide ? 256 : 64;
+    sh.wgs = sh.whole ? (int)tiles : wgs;
     sh.desc = (int32_t*)at;
-    sh.part_ml = (float*)(at + align_up((size_t)kQaWgs * 32, 256));
-    sh.part_o = (float*)((uint8_t*)sh.part_ml + align_up((size_t)kQaWgs * 2 * rows * 2 * 4, 256));
-    at += quant_piece_bytes(rows, D);
+    sh.part_ml = (float*)(at + align_up((size_t)wgs * 32, 256));
+    sh.part_o = (float*)((uint8_t*)sh.part_ml + align_up((size_t)wgs * 2 * held * 2 * 4, 256));
+    at += quant_piece_bytes(wgs, held, D);
     hipError_t e;
-    if (c.code == TS_INT8) e = D == 64 ? quant_some<TS_INT8, 64>(dtype, rows / 16, a, c, sh, s) : quant_some<TS_INT8, 128>(dtype, rows / 16, a, c, sh, s);
+    if (wide) e = launch_paged_wide(D, a, &c, sh, s);
+    else if (c.code == TS_INT8) e = D == 64 ? quant_some<TS_INT8, 64>(dtype, rows / 16, a, c, sh, s) : quant_some<TS_INT8, 128>(dtype, rows / 16, a, c, sh, s);
     else e = D == 64 ? quant_some<TS_E4M3, 64>(dtype, rows / 16, a, c, sh, s) : quant_some<TS_E4M3, 128>(dtype, rows / 16, a, c, sh, s);
     if (e != hipSuccess || sh.whole) return e;
-    return launch_paged_merge(dtype, D, a, sh, rows, tiles, s);
+    return launch_paged_merge(dtype, D, line, sh, held, wide, tiles, s);
   };
   if (!pl.many_rows) return run(pl.few_rows, 0, INT_MAX);
   if (a.q_indptr != nullptr) {                             // (without, every sequence has as many)

@@ -19,5 +19,18 @@ __device__ __forceinline__ void codes_to_f32(uint32_t w, float (&x)[4]) {
   }
 }
 
+// four codes as two pairs of bf16 numbers
+template <int CODE>
+__device__ __forceinline__ uint2 widen(uint32_t w) {
+  if constexpr (CODE == TS_E4M3) {
+    return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.f, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.f, true)));
+  } else {                                     // a whole number of seven bits is the high half of its float
+    float x[4];
+    codes_to_f32<CODE>(w, x);
+    return make_uint2(__builtin_amdgcn_perm(__float_as_uint(x[1]), __float_as_uint(x[0]), 0x07060302u),
+                      __builtin_amdgcn_perm(__float_as_uint(x[3]), __float_as_uint(x[2]), 0x07060302u));
+  }
+}
 }  // namespace ts
 #endif

@@ -298,7 +298,13 @@ struct QuantReadArgs {
 hipError_t launch_quant_read(int dtype, const QuantReadArgs& a, const QuantPools& c, hipStream_t s);
 hipError_t launch_quant_pages_copy(const QuantPools& c, const int32_t* src, const int32_t* dst, int n, int num_pages, int P, int H_kv, int D, hipStream_t s);
 
-size_t quant_attn_workspace(int dtype, int D, int G, int chunk);
+struct ShareArgs;
+constexpr int kTallRows = 256, kWideRows = 256;   // rows of a tile of the tall kernel, and of the wide one
+// Workgroups that cut the line into shares: one per CU (128 / 192 / 256 / 512 of the stream kernel: a bf16 token over 131072 keys 129, 98, 91, 95 us, over
+// 1000 keys 10.9, 11.0, 11.1, 13.5, 16 drafts of 8 over 3000 keys 66, 51, 46, 49: fewer start, and fewer pieces are joined).
+constexpr int kShareWgs = 256;
+hipError_t launch_paged_wide(int D, const PagedAttnArgs& a, const QuantPools* c, const ShareArgs& sh, hipStream_t s);
+size_t quant_attn_workspace(int dtype, int D, int G, int H_kv, int chunk);
 hipError_t launch_quant_attn(int dtype, int D, const PagedAttnArgs& a, const QuantPools& c, void* ws, hipStream_t s);   // (a's pools are not used)
 
 // drafted trees (draft_api.hip)

@@ -31,7 +31,8 @@ def words_of(sees, words):
 def attention(cache, q, new, window, sm, sees=None, more=0, tiny=0.0):
     """q [T][H][D] stored; sees: per sequence bool [n][n], or None: causal.  (out, lse, bound on out, bound on lse), rows in order; `cache` holds k, v in 64
     bits.  Bounds as in cache_util.attention, with `more` roundings of a logit and of a weight (scales), and `tiny` of output for each key that a row sees: what is
-    lost where weights leave the range of float."""
+    lost where weights leave the range of float.  bf16: a weight may be multiplied as two bf16 numbers, each rounded to nearest.  With 2^e <= w < 2^(e+1) the first's
+    half step is 2^(e-8); what it leaves is that (a bf16 number) or has an exponent of e - 9 at most, and the second's half step is 2^(e-17) <= 2^-17 w."""
     q64 = W.as_f32(q, cache.dtype).astype(np.float64)
     T, H, D = q64.shape
     G, u, row = H // cache.H_kv, 2.0 ** -24, 0
@@ -70,7 +71,7 @@ def attention(cache, q, new, window, sm, sees=None, more=0, tiny=0.0):
                 l = p.sum(axis=1, keepdims=True)
                 d = np.where(l > 0, l, 1.0)
                 o, A, M = p @ v / d, p @ np.abs(v) / d, seen.sum(axis=1)
-                rel = (np.expm1(2 * e) + (2 * M + 32 + more) * u)[:, None]
+                rel = (np.expm1(2 * e) + (2 * M + 32 + more) * u + (2.0 ** -17 if cache.dtype == W.BF16 else 0.0))[:, None]
                 out[row:row + n, h] = np.where(lost[:, None], np.nan, o)
                 with np.errstate(divide="ignore"):
                     lse[row:row + n, h] = np.where(some, np.where(some, m[:, 0], 0.0) + np.log(l[:, 0]), -np.inf)
