@@ -364,7 +364,7 @@ static int most_beside(int H_kv) { return H_kv < 4 ? H_kv : 4; }
 // 20.8, 64 of 500 24.7 against 17.6, drafts of four tokens over 16 of 8000 79 against 58).
 static int heads_beside(const PagedAttnArgs& a, int D) {
   const long keys = std::min((long)a.max_seq_len, a.window > 0 ? (long)a.window + a.C : LONG_MAX);
-  return (double)a.B * keys * a.H_kv / kShareWgs >= 48. * D ? most_beside(a.H_kv) : 1;
+  return (double)a.B * keys * a.H_kv / kShareWgs >= 50. * D ? most_beside(a.H_kv) : 1;
 }
 
 // bytes that tiles of `rows` rows leave pieces in

@@ -98,6 +98,14 @@ class PagePool:
         self._lens[seq] = n + int(tokens)
         return copies
 
+    def cut(self, seq, tokens: int) -> None:
+        """The sequence ends behind its first `tokens` tokens, such as the accepted ones of a draft; pages behind them are given back."""
+        pages, need = self._pages[seq], -(-int(tokens) // self.page_size)
+        if not 0 <= tokens <= self._lens[seq]:
+            raise ValueError("%d tokens of a sequence of %d" % (tokens, self._lens[seq]))
+        self._release(pages[need:])
+        self._pages[seq], self._lens[seq] = pages[:need], int(tokens)
+
     def fork(self, seq, child) -> None:
         """`child` begins as `seq` is now and shares its pages."""
         if child in self._pages:

@@ -25,24 +25,50 @@ def to_host(t: torch.Tensor, bits16: bool = False) -> np.ndarray:
     return a.view(np.uint16) if bits16 else a
 
 
-def copy_pages(problem, copies, num_pages, device=None):
-    """Makes the page copies [(src, dst)] that a PagePool asks for, in the pools of `problem` (one call per layer).  The lists of several of its methods
+def copy_pages(problem, copies, num_pages, device=None, cache=None):
+    """Makes the page copies [(src, dst)] that a PagePool asks for, in the pools of `problem` or in a QuantCache (one call per layer).  The lists of several of its methods
     may be joined: what an earlier pair concerns is copied before a later one reads or overwrites it.  device: where the list goes; the pools' by default."""
     if copies:
-        pairs = torch.tensor(copies, dtype=torch.int32, device=problem._keep[0].device if device is None else device).t().contiguous()
+        if device is None:
+            device = (problem if cache is None else cache)._keep[0].device
+        pairs = torch.tensor(copies, dtype=torch.int32, device=device).t().contiguous()
         for a, b in copy_runs(copies):
-            ts.ts_pages_copy(problem, pairs[0, a:b], pairs[1, a:b], b - a, num_pages)
+            if cache is None:
+                ts.ts_pages_copy(problem, pairs[0, a:b], pairs[1, a:b], b - a, num_pages)
+            else:
+                ts.ts_quant_pages_copy(problem, cache, pairs[0, a:b], pairs[1, a:b], b - a, num_pages)
 
 
 class _NewTokens:
     """The calls on new tokens that both layers have.  seq_lens count them; they are rows [B * C] without q_indptr, any
-    number per sequence with it."""
+    number per sequence with it.  cache: a QuantCache that the layer's page table leads into, in place of its pools."""
 
-    def append(self, k, v, q=None, q_out=None, rope=None, positions=None, q_indptr=None):
+    def append(self, k, v, q=None, q_out=None, rope=None, positions=None, q_indptr=None, cache=None):
         """Writes the new tokens' K and V rows into their pages, keys turned by `rope`, and the turned queries into q_out (either
-        alone: k and v, or q and q_out, None).  Rows [rows][heads][D] or [rows][heads * D], or as a step or chunk has them, [B][C][heads][D]."""
+        alone: k and v, or q and q_out, None; with `cache` k and v are needed).  Rows [rows][heads][D] or [rows][heads * D], or as a step or chunk has them, [B][C][heads][D]."""
         q, k, v = (t.flatten(0, 1) if t is not None and t.dim() == 4 else t for t in (q, k, v))
-        ts.ts_rope_append(self.problem, rope, q, k, v, q_indptr, (q if k is None else k).shape[0], positions, q_out)
+        rows = (q if k is None else k).shape[0]
+        if cache is None:
+            ts.ts_rope_append(self.problem, rope, q, k, v, q_indptr, rows, positions, q_out)
+        else:
+            ts.ts_quant_append(self.problem, cache, rope, q, k, v, q_indptr, rows, positions, q_out)
+
+    def read_back(self, cache, k_out, v_out, q_indptr=None):
+        """K and V of the new tokens from an 8-bit cache, as rows of the layer's type (either may be None); q_indptr of whole sequences reads all of them."""
+        ts.ts_quant_read(self.problem, cache, q_indptr, self._rows(k_out if v_out is None else v_out, q_indptr), k_out, v_out)
+
+    def tree_mask(self, parents, mask, positions=None, q_indptr=None):
+        """What the new tokens, drafted trees, see of each other (for attend_all), and their places (for append), from their parents."""
+        ts.ts_tree_mask(self.problem, parents, q_indptr, self._rows(parents, q_indptr), mask, positions)
+
+    def keep(self, path, count, to_lens, q_indptr=None, cache=None):
+        """Closes up the rows of the accepted paths: path [B][..], count [B]; to_lens [B] gets the new lengths, which the caller copies to seq_lens
+        when every layer is done."""
+        ts.ts_tree_keep(self.problem, cache, path, path.shape[-1], count, q_indptr, to_lens)
+
+    def _rows(self, t, q_indptr):
+        """New tokens of the call: the rows that t has with q_indptr."""
+        return self.B * self.problem.c.chunk if q_indptr is None else t.shape[0]
 
     def _with_chunk(self, chunk):
         """The layer's problem with another number of new tokens per sequence."""
@@ -53,27 +79,35 @@ class _NewTokens:
             kept[1][chunk] = self.problem.with_chunk(chunk)
         return kept[1][chunk]
 
-    def attend_all(self, q, sm_scale=None, window=0, q_indptr=None, out=None, lse=None, round_weights=False, ws=None, most_new=None):
+    def attend_all(self, q, sm_scale=None, window=0, q_indptr=None, out=None, lse=None, round_weights=False, ws=None, most_new=None,
+                   mask=None, cache=None):
         """Attention of the new tokens over their whole sequence: no selection.  Without q_indptr q is the step's or chunk's
         query and the result is in self.out / self.lse; packed rows bring their own `out` (and `lse`).
         round_weights: bf16 prompts in half the time, their weights rounded to bf16 (ts_paged_attn_rounded).
         ws: the workspace; by default one that the layer keeps for the current stream.  Calls that may run at once need one each: graphs that are
         replayed on different streams and were captured on one bring their own.
         most_new: packed rows: the most that a sequence has, which the choice of a kernel goes by (any number is computed).  The layer's chunk by
-        default, 1 in a DecodeLayer: prompts among the rows want it said."""
+        default, 1 in a DecodeLayer: prompts among the rows want it said.
+        mask: which new tokens a row sees (tree_mask), instead of those before it."""
+        if round_weights and (mask is not None or cache is not None):
+            raise ValueError("round_weights: not with a mask or an 8-bit cache")
         sm = sm_scale if sm_scale is not None else 1.0 / float(np.sqrt(self.D))
-        rows = self.B * self.problem.c.chunk if q_indptr is None else q.shape[0]
+        rows = self._rows(q, q_indptr)
         if q_indptr is None:
             out, lse = self.out if out is None else out, self.lse if lse is None else lse
         problem = self.problem if q_indptr is None or most_new is None else self._with_chunk(int(most_new))
-        nbytes = ts.ts_paged_attn_workspace_bytes(problem, rows)
+        nbytes = (ts.ts_paged_attn_workspace_bytes if cache is None else ts.ts_quant_attn_workspace_bytes)(problem, rows)
         if ws is None:
             kept, key = self.__dict__.setdefault("_all_ws", {}), (ts._current_stream(), nbytes)
             if key not in kept:                   # (none is ever replaced: a graph may hold it)
                 kept[key] = torch.empty((nbytes + 255) // 256 * 64, dtype=torch.int32, device=self.k_pool.device)
             ws = kept[key]
-        attend = ts.ts_paged_attn_rounded if round_weights else ts.ts_paged_attn
-        attend(problem, q, q_indptr, rows, window, sm, out, lse, ws)
+        if cache is not None:
+            ts.ts_quant_attn(problem, cache, q, q_indptr, rows, window, mask, sm, out, lse, ws)
+        elif mask is not None:
+            ts.ts_tree_attn(problem, q, q_indptr, rows, window, mask, sm, out, lse, ws)
+        else:
+            (ts.ts_paged_attn_rounded if round_weights else ts.ts_paged_attn)(problem, q, q_indptr, rows, window, sm, out, lse, ws)
 
 
 class DecodeLayer(_NewTokens):

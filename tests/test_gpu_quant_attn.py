@@ -158,6 +158,27 @@ def test_long_caches_are_cut_into_shares(gpu, dtype, H, H_kv, D, new, old, code,
     check_attention(*run(gpu, c, H, new, seed=H, max_seq_len=300000 if loose else None, chunk=40 if loose else None), old)
 
 
+# A bound that promises long sequences gives a workgroup several KV heads at once; what the sequences have is another matter.
+@DTYPES
+@CODES
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("H,H_kv", HEADS)
+@pytest.mark.parametrize("new", [[1] * 5, [2, 1, 0, 9, 4]], ids=["tokens", "drafts"])
+def test_heads_side_by_side(gpu, dtype, code, D, H, H_kv, new):
+    c = QuantPages(dtype, code, H_kv, D, 16, [1, 300, 33, 2500, 700], seed=H + D)
+    check_attention(*run(gpu, c, H, new, max_seq_len=1 << 24, seed=H), (H, H_kv))
+
+
+@DTYPES
+@CODES
+@pytest.mark.parametrize("H,H_kv", [(8, 8), (6, 2), (28, 4), (4, 1)])
+@pytest.mark.parametrize("window", [0, 1 << 23])
+def test_trees_with_heads_side_by_side(gpu, dtype, code, H, H_kv, window):
+    new = [13, 1, 70, 5, 0, 33]
+    c = QuantPages(dtype, code, H_kv, 64, 16, [13, 400, 2000, 90, 11, 20], seed=H)     # the last has fewer tokens than new ones: rows that see nothing
+    check_attention(*run(gpu, c, H, new, window=window, max_seq_len=1 << 24, sees=trees(new, H), seed=H, behind=3), (H, H_kv))
+
+
 def test_many_sequences(gpu):
     rng = np.random.Generator(np.random.PCG64(4))
     lens = rng.integers(0, 60, size=700).tolist()

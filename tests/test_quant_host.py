@@ -260,3 +260,80 @@ def test_wrong_types_lengths_and_devices_are_refused(call, name):
 def test_more_pages_than_the_cache_holds_are_refused():
     with pytest.raises(ValueError, match="holds 3"):
         ts.ts_quant_pages_copy(problem(), ts.QuantCache(**parts()), ints(1), ints(1), 1, 4)
+
+
+def test_a_sequence_is_cut():
+    from paper_2411_02886_amd.pages import PagePool
+    pool = PagePool(10, 4)
+    pool.add("a", 18)                                    # five pages
+    pool.fork("a", "b")
+    with pytest.raises(ValueError):
+        pool.cut("a", 19)
+    with pytest.raises(ValueError):
+        pool.cut("a", -1)
+    pool.cut("a", 18)
+    assert pool.pages("a") == [0, 1, 2, 3, 4] and pool.free_pages == 5
+    pool.cut("a", 9)
+    assert pool.pages("a") == [0, 1, 2] and pool.length("a") == 9 and pool.free_pages == 5 and pool.pages("b") == [0, 1, 2, 3, 4]
+    assert pool.grow("a", 1) == [(2, 5)]                 # the page behind the cut is still b's
+    pool.cut("b", 0)
+    assert pool.pages("b") == [] and pool.free_pages == 10 - 3 and pool.length("b") == 0
+    assert pool.grow("b", 2) == [] and pool.pages("b") == [2]
+
+
+class Layer:
+    """A layer whose calls are written down instead of launched."""
+
+    def __init__(self, monkeypatch):
+        from paper_2411_02886_amd import runtime
+        self.calls, fake, z = [], self, torch.zeros(9, dtype=torch.int32)
+        for name in ("ts_rope_append", "ts_quant_append", "ts_quant_read", "ts_tree_mask", "ts_tree_keep", "ts_paged_attn", "ts_paged_attn_rounded", "ts_tree_attn", "ts_quant_attn",
+                     "ts_pages_copy", "ts_quant_pages_copy"):
+            monkeypatch.setattr(runtime.ts, name, lambda *a, name=name: fake.calls.append((name,) + a))
+        for name in ("ts_paged_attn_workspace_bytes", "ts_quant_attn_workspace_bytes"):
+            monkeypatch.setattr(runtime.ts, name, lambda p, rows, name=name: 256 if name == "ts_paged_attn_workspace_bytes" else 512)
+        monkeypatch.setattr(runtime.ts, "_current_stream", lambda: 7)
+
+        class New(runtime._NewTokens):
+            k_pool, B, D = torch.zeros(4, 16, 2, 64), 2, 64
+            problem = ts.Problem(batch=2, chunk=3, num_q_heads=4, num_kv_heads=2, head_dim=64, page_size=16, max_seq_len=64, dtype=ts.TS_F32, k_pool=k_pool, v_pool=k_pool,
+                                 page_indptr=z, page_indices=z, seq_lens=z)
+            out, lse = torch.zeros(2, 3, 4, 64), torch.zeros(2, 3, 4)
+
+        self.layer, self.copy_pages = New(), runtime.copy_pages
+
+
+def test_a_layer_calls_what_its_arguments_say(monkeypatch):
+    f = Layer(monkeypatch)
+    lay, cache, ind = f.layer, ts.QuantCache.empty(4, 16, 2, 64, ts.TS_INT8, device="cpu"), torch.zeros(3, dtype=torch.int32)
+    q, kv, mask = torch.zeros(2, 3, 4, 64), torch.zeros(2, 3, 2, 64), torch.zeros((6, 1), dtype=torch.int32)
+    for kw, name in (({}, "ts_paged_attn"), (dict(round_weights=True), "ts_paged_attn_rounded"), (dict(mask=mask), "ts_tree_attn"), (dict(cache=cache), "ts_quant_attn"),
+                     (dict(cache=cache, mask=mask), "ts_quant_attn")):
+        lay.attend_all(q, window=5, **kw)
+        call = f.calls[-1]
+        at = 2 if "cache" in kw else 1
+        assert call[0] == name and call[at + 1:at + 5] == (q, None, 6, 5) and ("cache" not in kw or call[2] is cache)
+        assert call[-1].numel() * 4 == (512 if "cache" in kw else 256) and call[-3] is lay.out and call[-2] is lay.lse
+        assert name not in ("ts_tree_attn", "ts_quant_attn") or call[at + 5] is kw.get("mask")
+    for kw in (dict(mask=mask), dict(cache=cache)):
+        with pytest.raises(ValueError, match="round_weights"):
+            lay.attend_all(q, round_weights=True, **kw)
+    lay.append(kv, kv, q=q, q_out=q, cache=cache)
+    assert f.calls[-1][0] == "ts_quant_append" and f.calls[-1][2] is cache and f.calls[-1][8] == 6 and f.calls[-1][10] is q
+    lay.append(kv, kv)
+    assert f.calls[-1][0] == "ts_rope_append" and f.calls[-1][7] == 6
+    rows = torch.zeros(11, 2, 64)
+    lay.read_back(cache, rows, None, q_indptr=ind)
+    assert f.calls[-1][:1] + f.calls[-1][2:] == ("ts_quant_read", cache, ind, 11, rows, None)
+    lay.read_back(cache, None, rows)
+    assert f.calls[-1][4] == 6
+    parents = torch.zeros(11, dtype=torch.int32)
+    lay.tree_mask(parents, mask, q_indptr=ind)
+    assert f.calls[-1][:1] + f.calls[-1][2:] == ("ts_tree_mask", parents, ind, 11, mask, None)
+    path = torch.zeros((2, 5), dtype=torch.int32)
+    lay.keep(path, ind, ind, q_indptr=ind, cache=cache)
+    assert f.calls[-1][:1] + f.calls[-1][2:] == ("ts_tree_keep", cache, path, 5, ind, ind, ind)
+    f.copy_pages(lay.problem, [(0, 1), (1, 2)], 4, cache=cache)
+    assert [c[0] for c in f.calls[-2:]] == ["ts_quant_pages_copy"] * 2 and f.calls[-1][2] is cache
+    f.copy_pages(lay.problem, [(0, 1)], 4)
+    assert f.calls[-1][0] == "ts_pages_copy"
