@@ -226,6 +226,7 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
   auto keys_of = [&](int tpt) -> long { return std::min((long)a.max_seq_len, a.window > 0 ? (long)a.window + tpt : LONG_MAX); };
   auto run = [&](int rows, int more_rows, int most_rows, bool whole) -> hipError_t {
     const bool wide = rows == kWideRows && a.mask != nullptr, tall = rows == kTallRows || wide;
+    if (wide) rows = wide_rows(a);
     const int kt = tall || dtype == TS_F32 ? 64 : 128;
     ShareArgs sh{};
     sh.tpt = rows / G;
@@ -243,7 +244,7 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
     sh.part_ml = (float*)(at + align_up((size_t)kShareWgs * 32, 256));
     sh.part_o = (float*)((uint8_t*)sh.part_ml + align_up((size_t)kShareWgs * 2 * rows * 2 * 4, 256));
     at += piece_bytes(rows, D);
-    const hipError_t e = wide ? launch_paged_wide(D, a, nullptr, sh, s) : tall ? launch_paged_tall(D, a, sh, s) : launch_paged_stream(dtype, D, rows / 16, a, sh, s);
+    const hipError_t e = wide ? launch_paged_wide(D, rows, a, nullptr, sh, s) : tall ? launch_paged_tall(D, a, sh, s) : launch_paged_stream(dtype, D, rows / 16, a, sh, s);
     if (e != hipSuccess || whole) return e;
     return launch_paged_merge(dtype, D, a, sh, rows, tall, tiles_of(sh.tpt, beside), s);
   };

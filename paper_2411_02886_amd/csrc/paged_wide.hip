@@ -1,6 +1,6 @@
 // Dense attention of many new tokens, bf16 queries, over a cache in 8 bits, and of drafted trees over one in bf16: on the matrix cores.
 //
-// A tile is 256 rows (256 / G tokens times the G heads of a KV head) in eight waves of 32, two to a SIMD: while one of them forms weights on the vector
+// A tile is 256 rows (256 / G tokens times the G heads of a KV head) in eight waves of 32, two to a SIMD (or 128 rows, see below): while one of them forms weights on the vector
 // ALU the other one's matrix products run.  All walk the same tiles of 64 keys, which the workgroup widens to bf16 (codes are small numbers that bf16
 // holds) and puts into LDS, a tile ahead of their use and requested another one ahead; one barrier a tile.  Scores get their key's scale, weights their
 // value's.  A weight is multiplied with V as the sum of two bf16 numbers, each rounded to nearest (8 bits): what the first leaves is at most half its last bit, 2^-8 of the weight,
@@ -20,7 +20,6 @@ typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 
 constexpr int kPwTile = 64;                   // keys per tile
-constexpr int kPwRows = 256;                  // rows per tile of the share
 constexpr int kPwThreads = 512;
 constexpr int kPwRing = 4;                    // tiles whose scales are in LDS
 constexpr float kPwUnset = -3.40282347e38f;   // reference exponent before the first key: no finite one lies below it
@@ -33,8 +32,12 @@ template <int D> __device__ __forceinline__ int pw_swz(int key) {
   return D == 128 ? (((key & 3) << 2) | ((key >> 2) & 3)) : ((((key >> 1) & 1) << 2) | (((key >> 2) & 1) << 1) | ((key >> 3) & 1));
 }
 
-template <int KIND, int D>
+// BLOCKS: blocks of 32 keys of a tile that a wave has.  2: waves of 32 rows each, 256 in all.  1: 128 rows, the second four waves have the rows of the first four and the other half of
+// each tile's keys; the two halves of a row are joined in LDS behind the last tile.  (With up to 128 rows in tiles of 256 half of the waves would only stage, and the matrix cores rest while the
+// other half forms its weights.)
+template <int KIND, int D, int BLOCKS>
 __global__ __launch_bounds__(kPwThreads, 2) void paged_wide_kernel(PagedAttnArgs a, QuantPools c, ShareArgs sh) {
+  constexpr int ROWS = 128 * BLOCKS;
   constexpr int KS = D / 16, NB = D / 32;     // k-steps of K Q^T, 32-row blocks of the transposed output
   constexpr int RB = D * 2, TILE_B = kPwTile * RB;
   constexpr int SB = KIND == kRows16 ? RB : D;        // bytes of a row in the cache
@@ -94,8 +97,9 @@ __global__ __launch_bounds__(kPwThreads, 2) void paged_wide_kernel(PagedAttnArgs
     }
     const int32_t* pages = a.page_indices + sq.page0;
     const int key0 = (keys.u0 + ua) * kPwTile, nt = ub - ua;       // first key and number of tiles
-    const int j = wave * 32 + col;                                 // the lane's row
-    const bool there = j < nrows, busy = wave * 32 < nrows;        // (a wave without rows only stages)
+    const int late = wave >> 2, row_block = BLOCKS == 2 ? wave : wave & 3, key_block = BLOCKS == 2 ? 0 : late;   // (first block of the tile's keys)
+    const int j = row_block * 32 + col;                            // the lane's row
+    const bool there = j < nrows, busy = row_block * 32 < nrows;   // (a wave without rows only stages)
 
     // ---- a tile's keys from memory to LDS
     // (keys past the end or in front of the tile's first window stand for the nearest that some row sees: no other place of the cache is read)
@@ -181,9 +185,8 @@ __global__ __launch_bounds__(kPwThreads, 2) void paged_wide_kernel(PagedAttnArgs
     // barriers a wave either adds the output of tile it - 1 and forms the scores of tile `it` (the matrix cores), its part of the staging between the products, or forms
     // the weights of tile `it` (the vector ALU); the second four do what the first did a turn before.  K tile `it` and V tile it - 1 are read in turns 2 it and
     // 2 it + 1, and those that follow staged in the same turns into the places of those before, which have been read by then.
-    const int late = wave >> 2;
-    f32x16_t s[2];                                                 // S^T of the tile's two blocks of 32 keys: key 8 (e / 4) + 4 half + e % 4
-    uint32_t w[2][2][8];                                           // [block][part] their weights; k-step k2 takes elements 8 k2 ..
+    f32x16_t s[BLOCKS];                                            // S^T of the wave's blocks of 32 keys: key 8 (e / 4) + 4 half + e % 4
+    uint32_t w[BLOCKS][2][8];                                      // [block][part] their weights; k-step k2 takes elements 8 k2 ..
     // weights 2 i and 2 i + 1 of a block, as the sums of two bf16 numbers each
     auto split = [&](int kb, int i) __attribute__((always_inline)) {
       const float y0 = s[kb][2 * i], y1 = s[kb][2 * i + 1];
@@ -193,9 +196,9 @@ __global__ __launch_bounds__(kPwThreads, 2) void paged_wide_kernel(PagedAttnArgs
     };
     // O^T += V^T P^T of a tile, by pairs of blocks (the two products of a block stand a block apart: the second waits for the first), fragments a pair ahead
     auto output = [&](int it, auto stages) __attribute__((always_inline)) {
-      const uint32_t vt = fresh(va0 + (uint32_t)((it & 1) * TILE_B));
+      const uint32_t vt = fresh(va0 + (uint32_t)((it & 1) * TILE_B + key_block * 32 * RB));
       bf16x8_t vf[2][2];
-      auto fetch = [&](int t) __attribute__((always_inline)) {      // pair t: keys 16 (2 t / NB) .. of the tile, blocks 2 t % NB and the next
+      auto fetch = [&](int t) __attribute__((always_inline)) {      // pair t: keys 16 (2 t / NB) .. of the wave's, blocks 2 t % NB and the next
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const int k4 = 2 * t / NB, nb = 2 * t % NB + u;
@@ -209,8 +212,8 @@ __global__ __launch_bounds__(kPwThreads, 2) void paged_wide_kernel(PagedAttnArgs
       };
       fetch(0);
 #pragma unroll
-      for (int t = 0; t < 2 * NB; ++t) {
-        if (t + 1 < 2 * NB) fetch(t + 1);
+      for (int t = 0; t < BLOCKS * NB; ++t) {
+        if (t + 1 < BLOCKS * NB) fetch(t + 1);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int part = 0; part < 2; ++part)
@@ -222,23 +225,23 @@ __global__ __launch_bounds__(kPwThreads, 2) void paged_wide_kernel(PagedAttnArgs
           }
         __builtin_amdgcn_sched_barrier(0);
         if (decltype(stages)::value) {
-          constexpr int EACH = NB == 4 ? 1 : 2;
+          constexpr int EACH = 8 / (BLOCKS * NB);
 #pragma unroll
           for (int i = t * EACH; i < (t + 1) * EACH; ++i) staging(it + 1, i);
         }
-        if (t < NB) {                                              // the second block's weights, while the first one's are multiplied
+        if (BLOCKS == 2 && t < NB) {                               // the second block's weights, while the first one's are multiplied
 #pragma unroll
-          for (int i = t * (8 / NB); i < (t + 1) * (8 / NB); ++i) split(1, i);
+          for (int i = t * (8 / NB); i < (t + 1) * (8 / NB); ++i) split(BLOCKS - 1, i);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
     };
     auto scores = [&](int it) __attribute__((always_inline)) {
-      const uint32_t kt = fresh(ka0 + (uint32_t)((it & 1) * TILE_B));
-      bf16x8_t kf[KS][2];
+      const uint32_t kt = fresh(ka0 + (uint32_t)((it & 1) * TILE_B + key_block * 32 * RB));
+      bf16x8_t kf[KS][BLOCKS];
       auto fetch = [&](int ks) __attribute__((always_inline)) {
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) kf[ks][kb] = *(lds_bf16x8*)((kt ^ (uint32_t)(ks * 32)) + (uint32_t)(kb * 32 * RB));
+        for (int kb = 0; kb < BLOCKS; ++kb) kf[ks][kb] = *(lds_bf16x8*)((kt ^ (uint32_t)(ks * 32)) + (uint32_t)(kb * 32 * RB));
       };
       fetch(0);
       fetch(1);
@@ -247,16 +250,16 @@ __global__ __launch_bounds__(kPwThreads, 2) void paged_wide_kernel(PagedAttnArgs
         if (ks + 2 < KS) fetch(ks + 2);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks][kb], qf[ks], ks == 0 ? (f32x16_t){} : s[kb], 0, 0, 0);
+        for (int kb = 0; kb < BLOCKS; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks][kb], qf[ks], ks == 0 ? (f32x16_t){} : s[kb], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
     };
     auto weights = [&](int it) __attribute__((always_inline)) {
-      const float* const scales = s_scale + (it & (kPwRing - 1)) * 2 * kPwTile;
-      const int k0 = key0 + it * kPwTile;
-      const bool masked = k0 + kPwTile - 1 > (tree ? base - 1 : base + c0) || (a.window > 0 && k0 <= (tree ? base + sq.n - 1 : base + c0 + ntok - 1) - a.window);
+      const float* const scales = s_scale + (it & (kPwRing - 1)) * 2 * kPwTile + key_block * 32;
+      const int k0 = key0 + it * kPwTile + key_block * 32;
+      const bool masked = k0 + 32 * BLOCKS - 1 > (tree ? base - 1 : base + c0) || (a.window > 0 && k0 <= (tree ? base + sq.n - 1 : base + c0 + ntok - 1) - a.window);
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
+      for (int kb = 0; kb < BLOCKS; ++kb) {
         f32x16_t& x = s[kb];
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) {                           // (rounded before the reference is taken off: a fused product of large logits would be off by more than a weight)
@@ -264,10 +267,12 @@ __global__ __launch_bounds__(kPwThreads, 2) void paged_wide_kernel(PagedAttnArgs
           x[4 * q4] *= k4.x; x[4 * q4 + 1] *= k4.y; x[4 * q4 + 2] *= k4.z; x[4 * q4 + 3] *= k4.w;
         }
       }
-      uint32_t bits[2] = {~0u, ~0u};                               // the keys that the row sees
+      uint32_t bits[BLOCKS];                                // the keys that the row sees
+#pragma unroll
+      for (int kb = 0; kb < BLOCKS; ++kb) bits[kb] = ~0u;
       if (__builtin_expect(masked, 0)) {
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
+        for (int kb = 0; kb < BLOCKS; ++kb) {
           const int b0 = k0 + kb * 32;
           if (tree) bits[kb] = tree_bits(a, row0 + token_of((uint32_t)j), sq.n, base, low, b0);
           else {
@@ -289,7 +294,7 @@ __global__ __launch_bounds__(kPwThreads, 2) void paged_wide_kernel(PagedAttnArgs
         return sum + more;
       };
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
+      for (int kb = 0; kb < BLOCKS; ++kb) {
         f32x16_t p;
         float sum = sum_of(p, s[kb]);
         if (__builtin_amdgcn_ballot_w64(!(sum <= kPwRaise)) != 0) {            // a key far above the reference, such as a row's first
@@ -316,7 +321,7 @@ __global__ __launch_bounds__(kPwThreads, 2) void paged_wide_kernel(PagedAttnArgs
       }
       if constexpr (KIND != kRows16) {
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+        for (int kb = 0; kb < BLOCKS; ++kb)
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4) {
             float4 v4 = *reinterpret_cast<const float4*>(scales + kPwTile + kb * 32 + 8 * q4 + 4 * half);
@@ -365,7 +370,33 @@ __global__ __launch_bounds__(kPwThreads, 2) void paged_wide_kernel(PagedAttnArgs
     if (!late) __syncthreads();
 
     // ---- results: whole tiles are written, pieces left as they lie in the registers (the merge knows)
-    if (!busy) return false;
+    if (!busy && BLOCKS == 2) return false;
+    if constexpr (BLOCKS == 1) {                                   // the second four waves' sums to the first, in the place of the tiles and scales
+      float4* const half_o = reinterpret_cast<float4*>(smem) + row_block * (NB * 4 * 64) + lane;
+      float2* const half_ml = reinterpret_cast<float2*>(s_scale) + row_block * 64 + lane;
+      __syncthreads();                                             // which have been read
+      if (busy && late) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4) half_o[(nb * 4 + q4) * 64] = make_float4(o[nb][q4 * 4], o[nb][q4 * 4 + 1], o[nb][q4 * 4 + 2], o[nb][q4 * 4 + 3]);
+        *half_ml = make_float2(ref, lsum);
+      }
+      __syncthreads();
+      if (!busy || late) return false;
+      const float2 ml = *half_ml;
+      const float m = fmaxf(ref, ml.x), f = __builtin_amdgcn_exp2f(ref - m), g = __builtin_amdgcn_exp2f(ml.x - m);   // (a half without keys of the row: its sums are 0)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const float4 x = half_o[(nb * 4 + q4) * 64];
+          o[nb][q4 * 4] = fmaf(f, o[nb][q4 * 4], g * x.x); o[nb][q4 * 4 + 1] = fmaf(f, o[nb][q4 * 4 + 1], g * x.y);
+          o[nb][q4 * 4 + 2] = fmaf(f, o[nb][q4 * 4 + 2], g * x.z); o[nb][q4 * 4 + 3] = fmaf(f, o[nb][q4 * 4 + 3], g * x.w);
+        }
+      lsum = fmaf(f, lsum, g * ml.y);
+      ref = m;
+    }
     const float l = lsum + __shfl_xor(lsum, 32);
     constexpr float kLn2 = 0.69314718055994530942f;
     if (whole) {
@@ -382,13 +413,13 @@ __global__ __launch_bounds__(kPwThreads, 2) void paged_wide_kernel(PagedAttnArgs
         if (half == 0 && a.lse != nullptr) a.lse[hb] = l == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(l)) * kLn2;
       }
     } else {
-      float4* po = reinterpret_cast<float4*>(sh.part_o + ((size_t)wg * 2 + slot) * kPwRows * D) + wave * (NB * 4 * 64) + lane;
+      float4* po = reinterpret_cast<float4*>(sh.part_o + ((size_t)wg * 2 + slot) * ROWS * D) + row_block * (NB * 4 * 64) + lane;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) po[(nb * 4 + q4) * 64] = make_float4(o[nb][q4 * 4], o[nb][q4 * 4 + 1], o[nb][q4 * 4 + 2], o[nb][q4 * 4 + 3]);
       if (half == 0) {
-        float* pm = sh.part_ml + (((size_t)wg * 2 + slot) * kPwRows + j) * 2;
+        float* pm = sh.part_ml + (((size_t)wg * 2 + slot) * ROWS + j) * 2;
         pm[0] = l == 0.f ? -INFINITY : ref * kLn2; pm[1] = l;      // in units of the logits
       }
     }
@@ -396,22 +427,35 @@ __global__ __launch_bounds__(kPwThreads, 2) void paged_wide_kernel(PagedAttnArgs
   }, tree);
 }
 
-template <int KIND, int D>
+template <int KIND, int D, int BLOCKS>
 static hipError_t wide_one(const PagedAttnArgs& a, const QuantPools& c, const ShareArgs& sh, hipStream_t s) {
   constexpr int lds = 4 * kPwTile * D * 2 + kPwRing * 2 * kPwTile * 4 + sizeof(ShareScratch);
+  static_assert(4 * D / 8 * 64 * 16 <= 4 * kPwTile * D * 2 && 4 * 64 * 8 <= kPwRing * 2 * kPwTile * 4, "the halves' sums");
   if (lds > 65536) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_wide_kernel<KIND, D>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&paged_wide_kernel<KIND, D, BLOCKS>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((paged_wide_kernel<KIND, D>), dim3(sh.wgs), dim3(kPwThreads), lds, s, a, c, sh);
+  hipLaunchKernelGGL((paged_wide_kernel<KIND, D, BLOCKS>), dim3(sh.wgs), dim3(kPwThreads), lds, s, a, c, sh);
   return hipGetLastError();
 }
+template <int KIND>
+static hipError_t wide_some(int D, int rows, const PagedAttnArgs& a, const QuantPools& c, const ShareArgs& sh, hipStream_t s) {
+  if (rows == 128) return D == 64 ? wide_one<KIND, 64, 1>(a, c, sh, s) : wide_one<KIND, 128, 1>(a, c, sh, s);
+  return D == 64 ? wide_one<KIND, 64, 2>(a, c, sh, s) : wide_one<KIND, 128, 2>(a, c, sh, s);
+}
 
-// c null: the pools of `a`, rows of bf16
-hipError_t launch_paged_wide(int D, const PagedAttnArgs& a, const QuantPools* c, const ShareArgs& sh, hipStream_t s) {
-  if (c == nullptr) return D == 64 ? wide_one<kRows16, 64>(a, QuantPools{}, sh, s) : wide_one<kRows16, 128>(a, QuantPools{}, sh, s);
-  if (c->code == TS_INT8) return D == 64 ? wide_one<TS_INT8, 64>(a, *c, sh, s) : wide_one<TS_INT8, 128>(a, *c, sh, s);
-  return D == 64 ? wide_one<TS_E4M3, 64>(a, *c, sh, s) : wide_one<TS_E4M3, 128>(a, *c, sh, s);
+// Tiles of 128 rows where a sequence has no more of them on average (trees, 28/4 heads, int8, 24 sequences over 3000 keys: 84 rows 59 us, by tiles of 256 69, 119 rows 65 and 74; 32 over
+// 700: 33 and 37; a single sequence, whose keys are few for every workgroup, 40 and 40 to 42).  More rows: their keys would be staged twice (320 and 384 rows, 24 sequences over 3000 keys, 32/8 heads, bf16: 262 and 280 us
+// instead of 222 and 239, 512 tokens over 65536 keys 820 instead of 710).
+int wide_rows(const PagedAttnArgs& a) {
+  const long tokens = a.q_indptr != nullptr ? ((long)a.T + a.B - 1) / a.B : a.C;
+  return tokens * (a.H / a.H_kv) <= 128 ? 128 : kWideRows;
+}
+
+// rows: of a tile, 128 or 256; c null: the pools of `a`, rows of bf16
+hipError_t launch_paged_wide(int D, int rows, const PagedAttnArgs& a, const QuantPools* c, const ShareArgs& sh, hipStream_t s) {
+  if (c == nullptr) return wide_some<kRows16>(D, rows, a, QuantPools{}, sh, s);
+  return c->code == TS_INT8 ? wide_some<TS_INT8>(D, rows, a, *c, sh, s) : wide_some<TS_E4M3>(D, rows, a, *c, sh, s);
 }
 
 }  // namespace ts

@@ -399,6 +399,7 @@ hipError_t launch_quant_attn(int dtype, int D, const PagedAttnArgs& a, const Qua
     const bool wide = rows == kWideRows;
     PagedAttnArgs line = a;                                // what the merge sees: the heads that a workgroup has side by side are one
     if (!wide) line.H_kv = a.H_kv / heads;
+    if (wide) rows = wide_rows(a);
     const int held = wide ? rows : rows * heads, wgs = kShareWgs;
     ShareArgs sh{};
     sh.heads_shift = wide ? 0 : ilog2(heads);
@@ -423,7 +424,7 @@ hipError_t launch_quant_attn(int dtype, int D, const PagedAttnArgs& a, const Qua
     sh.part_o = (float*)((uint8_t*)sh.part_ml + align_up((size_t)wgs * 2 * held * 2 * 4, 256));
     at += quant_piece_bytes(wgs, held, D);
     hipError_t e;
-    if (wide) e = launch_paged_wide(D, a, &c, sh, s);
+    if (wide) e = launch_paged_wide(D, rows, a, &c, sh, s);
     else if (c.code == TS_INT8) e = D == 64 ? quant_some<TS_INT8, 64>(dtype, rows / 16, a, c, sh, s) : quant_some<TS_INT8, 128>(dtype, rows / 16, a, c, sh, s);
     else e = D == 64 ? quant_some<TS_E4M3, 64>(dtype, rows / 16, a, c, sh, s) : quant_some<TS_E4M3, 128>(dtype, rows / 16, a, c, sh, s);
     if (e != hipSuccess || sh.whole) return e;
