@@ -3,8 +3,8 @@
 //
 // Writing: one, two or four waves take a token, as in rotation and append of a plain cache.  D / 8 lanes hold a row of eight elements each, so that
 // a row's largest absolute value is three or four steps of the lanes' network away.  Rows are
-// requested a turn ahead, the first before the token's place is known; cosines and sines stay in LDS (in registers they cost two waves of seven on a SIMD): 16661 bf16 tokens of
-// 32/8 heads of 128, all of it turned, into e4m3 102 us instead of 116, into int8 100 instead of 106; nothing turned 78 and 76 (4.8 TB/s).  All arithmetic is in double, which this machine does at the rate of float: a
+// requested a turn ahead, the first before the token's place is known; cosines and sines stay in LDS (in registers they leave a SIMD four or five waves instead of seven): 16661 bf16 tokens of
+// 32/8 heads of 128, all of it turned, into e4m3 102 us instead of 116, into int8 100 instead of 106; nothing turned 78 and 76 (4.8 TB/s).  All arithmetic is in double: a
 // turned key next to the middle of two stored values, or a quotient next to the middle of two codes, falls as the definition says.  A quotient x Q / m is
 // formed by the row's reciprocal and one correction with the exact remainder (Markstein's division): a quotient that is a double -- every tie
 // between two codes is -- comes out exactly.
