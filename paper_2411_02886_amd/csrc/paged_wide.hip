@@ -38,6 +38,7 @@ template <int D> __device__ __forceinline__ int pw_swz(int key) {
 template <int KIND, int D, int BLOCKS>
 __global__ __launch_bounds__(kPwThreads, 2) void paged_wide_kernel(PagedAttnArgs a, QuantPools c, ShareArgs sh) {
   constexpr int ROWS = 128 * BLOCKS;
+  constexpr int AHEAD = BLOCKS == 1 ? 2 : 1;  // tiles that loads are ahead of their way to LDS (those of 128 rows take hardly more time than a load: 24 sequences over 3000 bf16 keys, 32/8 heads, 96 rows 94 us, one ahead 102)
   constexpr int KS = D / 16, NB = D / 32;     // k-steps of K Q^T, 32-row blocks of the transposed output
   constexpr int RB = D * 2, TILE_B = kPwTile * RB;
   constexpr int SB = KIND == kRows16 ? RB : D;        // bytes of a row in the cache
@@ -106,9 +107,9 @@ __global__ __launch_bounds__(kPwThreads, 2) void paged_wide_kernel(PagedAttnArgs
     auto key_of = [&](int it) -> int { return min(max(key0 + it * kPwTile + st_key, keys.first), tmax); };
     auto page_of = [&](int it) -> int { return pages[key_of(it) >> a.p_shift]; };
     typedef typename std::conditional<LB == 16, u32x4_t, u32x2_t>::type load_t;   // (vectors: structs that are written under a condition would go by way of memory)
-    load_t kr[NL], vr[NL];                                         // requested: a tile of K, and the one before of V
-    float scale = 0.f;                                             // of the tile of K
-    uint64_t at = 0;                                               // the place of the tile of K in the pools
+    load_t kr[AHEAD][NL], vr[AHEAD][NL];                           // requested: tiles of K, and the ones before of V (tile t in t % AHEAD)
+    float scale[AHEAD] = {};                                       // of the tiles of K
+    uint64_t at = 0;                                               // the place of the last tile of K in the pools
     const uint8_t* const k_head = (KIND == kRows16 ? a.k_pool : c.k_codes) + kvh * SB;
     const uint8_t* const v_head = (KIND == kRows16 ? a.v_pool : c.v_codes) + kvh * SB;
     // (formed anew in each turn: the compiler would keep dozens of addresses, and spill)
@@ -120,16 +121,16 @@ __global__ __launch_bounds__(kPwThreads, 2) void paged_wide_kernel(PagedAttnArgs
       before = at;
       at = ((uint64_t)(((uint32_t)page << a.p_shift) + (uint32_t)in_page) << row_shift) + (uint32_t)(st_part * LB);
     };
-    auto request_k = [&]() __attribute__((always_inline)) {
+    auto request_k = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
-      for (int l = 0; l < NL; ++l) kr[l] = *reinterpret_cast<const load_t*>(k_head + at + l * 8 * LB);
+      for (int l = 0; l < NL; ++l) kr[i][l] = *reinterpret_cast<const load_t*>(k_head + at + l * 8 * LB);
     };
-    auto request_v = [&]() __attribute__((always_inline)) {
+    auto request_v = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
-      for (int l = 0; l < NL; ++l) vr[l] = *reinterpret_cast<const load_t*>(v_head + before + l * 8 * LB);
+      for (int l = 0; l < NL; ++l) vr[i][l] = *reinterpret_cast<const load_t*>(v_head + before + l * 8 * LB);
     };
-    auto request_scale = [&](int page) __attribute__((always_inline)) {
-      if (KIND != kRows16 && st_part < 2) scale = (st_part == 0 ? c.k_scale : c.v_scale)[(((int64_t)page * a.H_kv + kvh) << a.p_shift) + in_page];
+    auto request_scale = [&](int page, int i) __attribute__((always_inline)) {
+      if (KIND != kRows16 && st_part < 2) scale[i] = (st_part == 0 ? c.k_scale : c.v_scale)[(((int64_t)page * a.H_kv + kvh) << a.p_shift) + in_page];
     };
     typedef __attribute__((address_space(3))) u32x4_t lds_u32x4;
     auto put = [&](uint32_t tile, const load_t (&x)[NL]) {
@@ -145,20 +146,21 @@ __global__ __launch_bounds__(kPwThreads, 2) void paged_wide_kernel(PagedAttnArgs
         }
       }
     };
-    auto put_k = [&](int it) __attribute__((always_inline)) { put((uint32_t)((it & 1) * TILE_B), kr); };
-    auto put_v = [&](int it) __attribute__((always_inline)) { put((uint32_t)((2 + (it & 1)) * TILE_B), vr); };
-    auto put_scale = [&](int it) __attribute__((always_inline)) {
-      if (KIND != kRows16 && st_part < 2) s_scale[((it & (kPwRing - 1)) * 2 + st_part) * kPwTile + st_key] = st_part == 0 ? scale * c2 : scale;
+    auto put_k = [&](int it, int i) __attribute__((always_inline)) { put((uint32_t)((it & 1) * TILE_B), kr[i]); };
+    auto put_v = [&](int it, int i) __attribute__((always_inline)) { put((uint32_t)((2 + (it & 1)) * TILE_B), vr[i]); };
+    auto put_scale = [&](int it, int i) __attribute__((always_inline)) {
+      if (KIND != kRows16 && st_part < 2) s_scale[((it & (kPwRing - 1)) * 2 + st_part) * kPwTile + st_key] = st_part == 0 ? scale[i] * c2 : scale[i];
     };
     int page = 0, page_then = 0;                                   // of the tile of K that is requested next, and the one after it
-    // K tile it + 1 and V tile `it` to LDS, K tile it + 2 and V tile it + 1 requested: in steps, which stand between matrix products
-    auto staging = [&](int it, int part) __attribute__((always_inline)) {
-      if (part == 0) put_k(it + 1);
-      if (part == 1) put_v(it);
-      if (part == 2) { put_scale(it + 1); page_then = page_of(it + 3); locate(it + 2, page); }
-      if (part == 3) request_k();
-      if (part == 4) request_v();
-      if (part == 5) { request_scale(page); page = page_then; }
+    // K tile it + 1 and V tile `it` to LDS, K tile it + 1 + AHEAD and V tile it + AHEAD requested: in steps, which stand between matrix products (parity: it % AHEAD)
+    auto staging = [&](int it, auto parity, int part) __attribute__((always_inline)) {
+      constexpr int v = decltype(parity)::value, k = AHEAD - 1 - v;
+      if (part == 0) put_k(it + 1, k);
+      if (part == 1) put_v(it, v);
+      if (part == 2) { put_scale(it + 1, k); page_then = page_of(it + 2 + AHEAD); locate(it + 1 + AHEAD, page); }
+      if (part == 3) request_k(k);
+      if (part == 4) request_v(v);
+      if (part == 5) { request_scale(page, k); page = page_then; }
     };
 
     // ---- queries: lane holds row col, elements 16 ks + 8 half ..
@@ -195,7 +197,7 @@ __global__ __launch_bounds__(kPwThreads, 2) void paged_wide_kernel(PagedAttnArgs
       w[kb][1][i] = __builtin_bit_cast(uint32_t, (bf16x2_t){(__bf16)(y0 - bf16_lo(hi)), (__bf16)(y1 - bf16_hi(hi))});
     };
     // O^T += V^T P^T of a tile, by pairs of blocks (the two products of a block stand a block apart: the second waits for the first), fragments a pair ahead
-    auto output = [&](int it, auto stages) __attribute__((always_inline)) {
+    auto output = [&](int it, auto stages, auto parity) __attribute__((always_inline)) {
       const uint32_t vt = fresh(va0 + (uint32_t)((it & 1) * TILE_B + key_block * 32 * RB));
       bf16x8_t vf[2][2];
       auto fetch = [&](int t) __attribute__((always_inline)) {      // pair t: keys 16 (2 t / NB) .. of the wave's, blocks 2 t % NB and the next
@@ -227,7 +229,7 @@ __global__ __launch_bounds__(kPwThreads, 2) void paged_wide_kernel(PagedAttnArgs
         if (decltype(stages)::value) {
           constexpr int EACH = 8 / (BLOCKS * NB);
 #pragma unroll
-          for (int i = t * EACH; i < (t + 1) * EACH; ++i) staging(it + 1, i);
+          for (int i = t * EACH; i < (t + 1) * EACH; ++i) staging(it + 1, parity, i);
         }
         if (BLOCKS == 2 && t < NB) {                               // the second block's weights, while the first one's are multiplied
 #pragma unroll
@@ -337,36 +339,49 @@ __global__ __launch_bounds__(kPwThreads, 2) void paged_wide_kernel(PagedAttnArgs
     };
     using Yes = std::true_type;
     using No = std::false_type;
+    using Even = std::integral_constant<int, 0>;
+    using Odd = std::integral_constant<int, AHEAD - 1>;
     __syncthreads();                                               // the tiles of the piece before have been read
     {
-      const int p0 = page_of(0), p1 = page_of(1);
-      page = page_of(2);
+      const int p0 = page_of(0), p1 = page_of(1), p2 = page_of(2);
+      page = AHEAD == 2 ? page_of(3) : p2;
       locate(0, p0);
-      request_k();
-      request_scale(p0);
-      put_k(0);
-      put_scale(0);
+      request_k(0);
+      request_scale(p0, 0);
+      if (AHEAD == 1) { put_k(0, 0); put_scale(0, 0); }
       locate(1, p1);
-      request_k();
-      request_v();
-      request_scale(p1);
+      request_k(AHEAD - 1);
+      request_v(0);
+      request_scale(p1, AHEAD - 1);
+      if (AHEAD == 2) {
+        put_k(0, 0);
+        put_scale(0, 0);
+        locate(2, p2);
+        request_k(0);
+        request_v(AHEAD - 1);
+        request_scale(p2, 0);
+      }
     }
     __syncthreads();
     if (late) __syncthreads();
-    for (int it = 0; it < nt; ++it) {
+    auto turn = [&](int it, auto parity) __attribute__((always_inline)) {
       __builtin_amdgcn_s_setprio(1);
-      if (busy && it > 0) output(it - 1, Yes{});
+      if (busy && it > 0) output(it - 1, Yes{}, parity);
       else {
 #pragma unroll
-        for (int i = 0; i < 6; ++i) staging(it, i);
+        for (int i = 0; i < 6; ++i) staging(it, parity, i);
       }
       if (busy) scores(it);
       __builtin_amdgcn_s_setprio(0);
       __syncthreads();
       if (busy) weights(it);
       __syncthreads();
+    };
+    for (int it = 0; it < nt; it += AHEAD) {
+      turn(it, Even{});
+      if (AHEAD == 2 && it + 1 < nt) turn(it + 1, Odd{});
     }
-    if (busy) output(nt - 1, No{});
+    if (busy) output(nt - 1, No{}, Even{});
     if (!late) __syncthreads();
 
     // ---- results: whole tiles are written, pieces left as they lie in the registers (the merge knows)
