@@ -109,9 +109,9 @@ __global__ __launch_bounds__(THREADS) void paged_merge_kernel(PagedAttnArgs a, S
 
 // The same for the tall kernel and the wide one, whose pieces lie as in its registers: of each block of 32 rows 16 bytes of the output [D / 8][64 lanes], the
 // lane's row lane % 32, its elements 8 i + 4 (lane / 32) .. + 3.  A wave of a workgroup (blockIdx.x: block of rows, then i / 4) has one i.
-template <int D>
+template <int D, int US>                                // US: partial results in flight
 __global__ __launch_bounds__(256) void paged_merge_tall_kernel(PagedAttnArgs a, ShareArgs sh, int rows) {
-  constexpr int PB = D / 32, US = 6;                    // workgroups per block of rows; partial results in flight
+  constexpr int PB = D / 32;                            // workgroups per block of rows
   const int w = blockIdx.y, G = a.H / a.H_kv;
   const int32_t* d1 = sh.desc + (size_t)w * 8 + 4;
   const int lane = threadIdx.x & 63, next = next_piece(sh, w, lane);
@@ -159,9 +159,12 @@ __global__ __launch_bounds__(256) void paged_merge_tall_kernel(PagedAttnArgs a, 
 }
 
 template <int ES, int D>
-static hipError_t merge(const PagedAttnArgs& a, const ShareArgs& sh, int rows, bool by_blocks, long tiles, hipStream_t s) {
-  if (by_blocks) {                  // (tiles are short only where their sequence is)
-    hipLaunchKernelGGL(paged_merge_tall_kernel<D>, dim3(rows / 32 * (D / 32), sh.wgs), dim3(256), 0, s, a, sh, rows);
+static hipError_t merge(const PagedAttnArgs& a, const ShareArgs& sh, int rows, PieceOrder order, long tiles, hipStream_t s) {
+  if (order != kRowByRow) {         // (tiles are short only where their sequence is)
+    const dim3 grid(rows / 32 * (D / 32), sh.wgs);
+    // few tiles have many pieces: 2 heads of 64, 17 tokens over 30000 keys, 128 pieces a tile, 42.3 us, with six in flight 49.6; 4 of 128 over 8000 38.4 and 41.1
+    if (order == kWideBlocks && tiles * 8 <= sh.wgs) hipLaunchKernelGGL((paged_merge_tall_kernel<D, 16>), grid, dim3(256), 0, s, a, sh, rows);
+    else hipLaunchKernelGGL((paged_merge_tall_kernel<D, 6>), grid, dim3(256), 0, s, a, sh, rows);
     return hipGetLastError();
   }
   // A workgroup per row that a tile may have; where only the sequences with few rows are meant, as many as one token has (12 mixed ones, 28 heads: 4 us
@@ -174,10 +177,9 @@ static hipError_t merge(const PagedAttnArgs& a, const ShareArgs& sh, int rows, b
   return hipGetLastError();
 }
 
-// by_blocks: the pieces lie as the tall and the wide kernel leave them
-hipError_t launch_paged_merge(int dtype, int D, const PagedAttnArgs& a, const ShareArgs& sh, int rows, bool by_blocks, long tiles, hipStream_t s) {
-  if (dtype == TS_BF16) return D == 64 ? merge<2, 64>(a, sh, rows, by_blocks, tiles, s) : merge<2, 128>(a, sh, rows, by_blocks, tiles, s);
-  return D == 64 ? merge<4, 64>(a, sh, rows, by_blocks, tiles, s) : merge<4, 128>(a, sh, rows, by_blocks, tiles, s);
+hipError_t launch_paged_merge(int dtype, int D, const PagedAttnArgs& a, const ShareArgs& sh, int rows, PieceOrder order, long tiles, hipStream_t s) {
+  if (dtype == TS_BF16) return D == 64 ? merge<2, 64>(a, sh, rows, order, tiles, s) : merge<2, 128>(a, sh, rows, order, tiles, s);
+  return D == 64 ? merge<4, 64>(a, sh, rows, order, tiles, s) : merge<4, 128>(a, sh, rows, order, tiles, s);
 }
 
 // bytes that tiles of `rows` rows leave pieces in
@@ -246,7 +248,7 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
     at += piece_bytes(rows, D);
     const hipError_t e = wide ? launch_paged_wide(D, rows, a, nullptr, sh, s) : tall ? launch_paged_tall(D, a, sh, s) : launch_paged_stream(dtype, D, rows / 16, a, sh, s);
     if (e != hipSuccess || whole) return e;
-    return launch_paged_merge(dtype, D, a, sh, rows, tall, tiles_of(sh.tpt, beside), s);
+    return launch_paged_merge(dtype, D, a, sh, rows, wide ? kWideBlocks : tall ? kTallBlocks : kRowByRow, tiles_of(sh.tpt, beside), s);
   };
   // A workgroup per tile, and no merge, where tiles are short, or where there are enough of them that are not long.  (200 keys: 8.2 us, in shares 10.3; 64
   // sequences of 250 to 500 keys, 512 tiles: 22.8 and 29; but 16 fp32 sequences of 1000 to 2000 keys, 32 tiles, 42 us instead of 17.)  Beside large

@@ -16,7 +16,7 @@
 
 namespace ts {
 
-hipError_t launch_paged_merge(int dtype, int D, const PagedAttnArgs& a, const ShareArgs& sh, int rows, bool by_blocks, long tiles, hipStream_t s);
+hipError_t launch_paged_merge(int dtype, int D, const PagedAttnArgs& a, const ShareArgs& sh, int rows, PieceOrder order, long tiles, hipStream_t s);
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_t;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_t;
@@ -428,7 +428,7 @@ hipError_t launch_quant_attn(int dtype, int D, const PagedAttnArgs& a, const Qua
     else if (c.code == TS_INT8) e = D == 64 ? quant_some<TS_INT8, 64>(dtype, rows / 16, a, c, sh, s) : quant_some<TS_INT8, 128>(dtype, rows / 16, a, c, sh, s);
     else e = D == 64 ? quant_some<TS_E4M3, 64>(dtype, rows / 16, a, c, sh, s) : quant_some<TS_E4M3, 128>(dtype, rows / 16, a, c, sh, s);
     if (e != hipSuccess || sh.whole) return e;
-    return launch_paged_merge(dtype, D, line, sh, held, wide, tiles, s);
+    return launch_paged_merge(dtype, D, line, sh, held, wide ? kWideBlocks : kRowByRow, tiles, s);
   };
   if (!pl.many_rows) return run(pl.few_rows, 0, INT_MAX);
   if (a.q_indptr != nullptr) {                             // (without, every sequence has as many)

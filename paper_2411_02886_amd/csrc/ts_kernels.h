@@ -299,6 +299,7 @@ hipError_t launch_quant_read(int dtype, const QuantReadArgs& a, const QuantPools
 hipError_t launch_quant_pages_copy(const QuantPools& c, const int32_t* src, const int32_t* dst, int n, int num_pages, int P, int H_kv, int D, hipStream_t s);
 
 struct ShareArgs;
+enum PieceOrder { kRowByRow, kTallBlocks, kWideBlocks };   // how partial results lie: the tall kernel's and the wide one's as in their registers
 constexpr int kTallRows = 256, kWideRows = 256;   // rows of a tile of the tall kernel, and of the wide one
 // Workgroups that cut the line into shares: one per CU (128 / 192 / 256 / 512 of the stream kernel: a bf16 token over 131072 keys 129, 98, 91, 95 us, over
 // 1000 keys 10.9, 11.0, 11.1, 13.5, 16 drafts of 8 over 3000 keys 66, 51, 46, 49: fewer start, and fewer pieces are joined).
