@@ -1,7 +1,7 @@
 // A cache in 8 bits: new tokens turned, quantised and written into their pages, tokens read back, pages copied.  Bound by memory: every
 // row is read and written once.
 //
-// Writing: one, two or four waves take a token, as in rotation and append of a plain cache.  D / 8 lanes hold a row of eight elements each, so that
+// Writing: up to sixteen waves take a token.  D / 8 lanes hold a row of eight elements each, so that
 // a row's largest absolute value is three or four steps of the lanes' network away.  Rows are
 // requested a turn ahead, the first before the token's place is known; cosines and sines stay in LDS (in registers they leave a SIMD four or five waves instead of seven): 16661 bf16 tokens of
 // 32/8 heads of 128, all of it turned, into e4m3 102 us instead of 116, into int8 100 instead of 106; nothing turned 78 and 76 (4.8 TB/s).  All arithmetic is in double: a
@@ -59,8 +59,9 @@ template <typename T, int CODE, int D>
 __global__ __launch_bounds__(256) void quant_append_kernel(RopeAppendArgs a, QuantPools c) {
   constexpr int LPR = D / 8, RPW = 64 / LPR, ES = sizeof(T), RB = D * ES;   // lanes of a row, rows side by side in a wave, bytes of a row
   __shared__ __attribute__((aligned(16))) double s_turn[4][8 * 9][2];       // pair p at p + p / 8: lanes read eight pairs each, 144 bytes apart
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), share = 1 << a.share_shift;
-  const int part = wave & (share - 1), row = (int)((((uint64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + wave) >> a.share_shift);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint64_t turn = ((uint64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + wave;
+  const int part = (int)turn & ((1 << a.share_shift) - 1), row = (int)(turn >> a.share_shift);
   if (row >= a.T) return;
   const int half = a.rotary >> 1, nq = a.q != nullptr ? a.H : 0, nk = a.H_kv;
   const uint8_t* q_row = a.q + row * a.q_stride;
@@ -180,10 +181,22 @@ __global__ __launch_bounds__(256) void quant_append_kernel(RopeAppendArgs a, Qua
   }
 }
 
+// log2 of the waves that share a token (a row that is read): no more than have a turn.  Few tokens are bound by one turn after the other, many by what each wave does before its first one.
+// Device times of appending with 2, 4, 8 and 16 waves a token, int8 and 32/8 heads of 128: 64 tokens 8.1, 5.9, 5.2, 4.4 us; 256 8.3, 6.3, 6.1, 6.6; 512 8.8, 7.4, 8.2, 10.2; 4096 26, 29, 41, 62.  Reading
+// with 1, 2, 4 and 8: 64 3.6, 3.0, 2.8, 2.8; 1024 4.2, 3.7, 3.8, 5.0; 4096 7.7, 7.3, 9.5, 16.
+static int most_shared(int turns) { return turns <= 1 ? 0 : turns <= 2 ? 1 : turns <= 4 ? 2 : turns <= 8 ? 3 : 4; }
+static int append_share(const RopeAppendArgs& a) {
+  const int heads = (a.q != nullptr ? a.H : 0) + 2 * a.H_kv, side = 512 / a.D;      // rows side by side in a wave
+  return std::min(most_shared((heads + side - 1) / side), a.T <= 128 ? 4 : a.T <= 256 ? 3 : a.T <= 1024 ? 2 : 1);
+}
+static int read_share(const QuantReadArgs& a) {
+  return std::min(most_shared(2 * a.H_kv * a.D / 512), a.T <= 1024 ? 2 : a.T <= 8192 ? 1 : 0);
+}
+
 template <typename T, int CODE>
 static hipError_t append_one(const RopeAppendArgs& b, const QuantPools& c, hipStream_t s) {
   RopeAppendArgs a = b;
-  a.share_shift = a.T <= 1024 ? 2 : 1;
+  a.share_shift = append_share(a);
   const long wgs = (((long)a.T << a.share_shift) + 3) / 4, wide = 1 << 20;      // (a grid has less than 2^32 threads in a dimension)
   const dim3 grid((unsigned)std::min(wgs, wide), (unsigned)((wgs + wide - 1) / wide));
   if (a.D == 64) hipLaunchKernelGGL((quant_append_kernel<T, CODE, 64>), grid, dim3(256), 0, s, a, c);
@@ -196,11 +209,12 @@ hipError_t launch_quant_append(int dtype, const RopeAppendArgs& a, const QuantPo
   return c.code == TS_INT8 ? append_one<float, TS_INT8>(a, c, s) : append_one<float, TS_E4M3>(a, c, s);
 }
 
-// A wave per row: pieces of eight codes, K's, then V's.
+// One, two or four waves per row: pieces of eight codes, K's, then V's.
 template <typename T, int CODE>
 __global__ __launch_bounds__(256) void quant_read_kernel(QuantReadArgs a, QuantPools c) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row = (int)(((uint64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + wave);
+  const uint64_t turn = ((uint64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + wave;
+  const int part = (int)turn & ((1 << a.share_shift) - 1), row = (int)(turn >> a.share_shift);
   if (row >= a.T) return;
   const RowPlace at = row_place(a.q_indptr, a.B, a.C, a.T, row);
   if (at.b < 0) return;
@@ -210,7 +224,7 @@ __global__ __launch_bounds__(256) void quant_read_kernel(QuantReadArgs a, QuantP
   if (there) page = a.page_indices[a.page_indptr[at.b] + (place >> a.p_shift)];
   const int in_page = place & (a.P - 1), d_shift = a.D == 64 ? 3 : 4, each = a.H_kv << d_shift;   // pieces of K, and of V
   const int64_t slot = (page << a.p_shift) + in_page;
-  for (int i = lane; i < 2 * each; i += 64) {
+  for (int i = part * 64 + lane; i < 2 * each; i += 64 << a.share_shift) {
     const bool is_v = i >= each;
     const int j = is_v ? i - each : i, kv = j >> d_shift;
     uint8_t* out = is_v ? a.v_out : a.k_out;
@@ -229,8 +243,10 @@ __global__ __launch_bounds__(256) void quant_read_kernel(QuantReadArgs a, QuantP
   }
 }
 
-hipError_t launch_quant_read(int dtype, const QuantReadArgs& a, const QuantPools& c, hipStream_t s) {
-  const long wgs = ((long)a.T + 3) / 4, wide = 1 << 20;
+hipError_t launch_quant_read(int dtype, const QuantReadArgs& b, const QuantPools& c, hipStream_t s) {
+  QuantReadArgs a = b;
+  a.share_shift = read_share(a);
+  const long wgs = (((long)a.T << a.share_shift) + 3) / 4, wide = 1 << 20;
   const dim3 grid((unsigned)std::min(wgs, wide), (unsigned)((wgs + wide - 1) / wide));
   if (dtype == TS_BF16) {
     if (c.code == TS_INT8) hipLaunchKernelGGL((quant_read_kernel<uint16_t, TS_INT8>), grid, dim3(256), 0, s, a, c);

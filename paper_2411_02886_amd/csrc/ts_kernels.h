@@ -294,6 +294,7 @@ struct QuantReadArgs {
   uint8_t* k_out;              // null: not wanted
   uint8_t* v_out;
   int B, C, T, H_kv, D, P, p_shift, max_seq_len;
+  int share_shift;             // log2 of the waves that share a row (set by the launch)
 };
 hipError_t launch_quant_read(int dtype, const QuantReadArgs& a, const QuantPools& c, hipStream_t s);
 hipError_t launch_quant_pages_copy(const QuantPools& c, const int32_t* src, const int32_t* dst, int n, int num_pages, int P, int H_kv, int D, hipStream_t s);
