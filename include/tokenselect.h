@@ -412,7 +412,7 @@ int32_t ts_quant_append(const ts_problem* p, const ts_quant* c, const ts_rope* r
 int32_t ts_quant_read(const ts_problem* p, const ts_quant* c, const int32_t* q_indptr, int32_t num_rows, void* k_out, void* v_out, void* stream);
 
 /* ts_paged_attn over an 8-bit cache: K and V are what the codes and scales stand for.  The same rows, window, results, rows that see nothing; weights and sums in
- * float (the products of q and codes are summed before the scale is applied; bf16 sequences of many new tokens, n_b * G > 32: a weight that multiplies V may be off by up to
+ * float (the products of q and codes are summed before the scale is applied; bf16 calls with chunk * G > 64: a weight that multiplies V may be off by up to
  * 2^-17 of itself).  mask NULL: causal, as there; else a mask among the new tokens [num_rows][mask_words], see ts_tree_mask.
  * Codes are finite numbers, so that no key or value that a row does not see can disturb it (e4m3: the two codes of NaN, 127 and 255, do not come from ts_quant_append; where they
  * stand in a cache, rows that share a tile with one that sees them may be NaN too).
@@ -440,7 +440,7 @@ int32_t ts_tree_mask(const ts_problem* p, const int32_t* parents, const int32_t*
                      int32_t* positions, void* stream);
 
 /* ts_paged_attn with a mask among the new tokens: rows, results, rows that see nothing, sums, workspace (ts_paged_attn_workspace_bytes) as there.  A new
- * token's V has to be finite, seen or not; its K may be anything where it is not seen.  bf16 sequences of many new tokens, n_b * G > 64: a weight that multiplies V may be
+ * token's V has to be finite, seen or not; its K may be anything where it is not seen.  bf16 calls with chunk * G > 64: a weight that multiplies V may be
  * off by up to 2^-17 of itself. */
 int32_t ts_tree_attn(const ts_problem* p, const void* q, const int32_t* q_indptr, int32_t num_rows, int32_t window, const uint32_t* mask, int32_t mask_words,
                      float sm_scale, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);

@@ -264,7 +264,8 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
   // (fp32, whose larger tiles save less, also with more tiles of few keys: 16 sequences of 64 tokens 33 and 45, 4 of 256 60 and 60.)
   const long small = tiles_of(32 / G, false), small_keys = keys_of(32 / G);
   if (small_keys <= (a.mask != nullptr ? 512 : 1024) && (small <= 2 * kShareWgs || (dtype == TS_F32 && small * small_keys <= 1l << 18))) return run(32, 0, INT_MAX, true);
-  if (a.q_indptr != nullptr) {                             // (without, every sequence has as many)
+  const bool alone = pl.many_rows == kWideRows && a.mask != nullptr ? wide_alone(a) : a.q_indptr == nullptr;   // (without q_indptr every sequence has as many)
+  if (!alone) {
     const hipError_t e = run(pl.few_rows, 0, pl.few_rows, few_whole(pl.few_rows, true));
     if (e != hipSuccess) return e;
   }
@@ -272,7 +273,7 @@ hipError_t launch_paged_attn(int dtype, int D, const PagedAttnArgs& a, void* ws,
   // 1024 tokens take 33.4 us, in shares 35.7, 2048 59 and 54.  A packed batch's bound counts up to a tile per sequence too many: there twice the tiles, 24 of 1
   // to 100 tokens 36 us, in shares 41, 8 of 1 to 600 68 and 75; four times would cost 64 of 64 tokens over 900 119 instead of 98 (rounded).)
   const long tiles = tiles_of(pl.many_rows / G, false);
-  return run(pl.many_rows, a.q_indptr != nullptr ? pl.few_rows : 0, INT_MAX,
+  return run(pl.many_rows, alone ? 0 : pl.few_rows, INT_MAX,
              tiles <= kShareWgs * (a.q_indptr != nullptr ? 2 : 1) && keys_of(pl.many_rows / G) <= (a.round_weights ? 1024 : 768));
 }
 

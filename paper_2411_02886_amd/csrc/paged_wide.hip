@@ -467,6 +467,13 @@ int wide_rows(const PagedAttnArgs& a) {
   return tokens * (a.H / a.H_kv) <= 128 ? 128 : kWideRows;
 }
 
+// A packed batch whose sequences all fit a tile and have half of the most on average: those with few rows take the wide kernel too.  A launch of their own and its merge cost 5 to 10 us where there
+// are none, 10 to 20 where there are some (28/4 heads, int8, drafts of 18 tokens and of one or two: 24 sequences of up to 500 keys 27 us, with a launch for the few 42, of 4000 62 and 83, of 16000 169 and
+// 175), and save at most a twentieth of a long call (64 sequences of up to 4000 bf16 keys, 32/8 heads, a third of them with few rows: 242 us instead of 228).
+bool wide_alone(const PagedAttnArgs& a) {
+  return a.q_indptr == nullptr || ((long)a.C * (a.H / a.H_kv) <= kWideRows && 2l * a.T >= (long)a.B * a.C);
+}
+
 // rows: of a tile, 128 or 256; c null: the pools of `a`, rows of bf16
 hipError_t launch_paged_wide(int D, int rows, const PagedAttnArgs& a, const QuantPools* c, const ShareArgs& sh, hipStream_t s) {
   if (c == nullptr) return wide_some<kRows16>(D, rows, a, QuantPools{}, sh, s);

@@ -431,11 +431,12 @@ hipError_t launch_quant_attn(int dtype, int D, const PagedAttnArgs& a, const Qua
     return launch_paged_merge(dtype, D, line, sh, held, wide ? kWideBlocks : kRowByRow, tiles, s);
   };
   if (!pl.many_rows) return run(pl.few_rows, 0, INT_MAX);
-  if (a.q_indptr != nullptr) {                             // (without, every sequence has as many)
+  const bool alone = pl.many_rows == kWideRows ? wide_alone(a) : a.q_indptr == nullptr;   // (without q_indptr every sequence has as many)
+  if (!alone) {
     const hipError_t e = run(pl.few_rows, 0, pl.few_rows);
     if (e != hipSuccess) return e;
   }
-  return run(pl.many_rows, a.q_indptr != nullptr ? pl.few_rows : 0, INT_MAX);
+  return run(pl.many_rows, alone ? 0 : pl.few_rows, INT_MAX);
 }
 
 }  // namespace ts

@@ -306,6 +306,7 @@ constexpr int kTallRows = 256, kWideRows = 256;   // rows of a tile of the tall 
 // 1000 keys 10.9, 11.0, 11.1, 13.5, 16 drafts of 8 over 3000 keys 66, 51, 46, 49: fewer start, and fewer pieces are joined).
 constexpr int kShareWgs = 256;
 int wide_rows(const PagedAttnArgs& a);            // of the tiles that suit a call, 128 or kWideRows
+bool wide_alone(const PagedAttnArgs& a);          // no other kernel beside it
 hipError_t launch_paged_wide(int D, int rows, const PagedAttnArgs& a, const QuantPools* c, const ShareArgs& sh, hipStream_t s);
 size_t quant_attn_workspace(int dtype, int D, int G, int H_kv, int chunk);
 hipError_t launch_quant_attn(int dtype, int D, const PagedAttnArgs& a, const QuantPools& c, void* ws, hipStream_t s);   // (a's pools are not used)
