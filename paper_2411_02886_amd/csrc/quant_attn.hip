@@ -238,9 +238,10 @@ __global__ __launch_bounds__(256, CB == 1 ? 2 : 1) void quant_attn_kernel(PagedA
           }
           bits >>= 4 * kgrp;
         }
+        auto sees = [&](int e) -> bool { return (bits >> (16 * (e >> 2) + (e & 3)) & 1u) != 0u; };
         float y[8], p[8], sum = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = (bits >> (16 * (e >> 2) + (e & 3)) & 1u) != 0u ? s[cb][e >> 2][e & 3] * ks[e] : -INFINITY;
+        for (int e = 0; e < 8; ++e) y[e] = sees(e) ? s[cb][e >> 2][e & 3] * ks[e] : -INFINITY;
         for (int tries = 0; tries < 2; ++tries) {
           sum = 0.f;
 #pragma unroll
@@ -262,8 +263,8 @@ __global__ __launch_bounds__(256, CB == 1 ? 2 : 1) void quant_attn_kernel(PagedA
         lsum[cb] += sum;
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
-          // (a weight of 0 stays 0 beside a scale that is no number: the row does not see the key, or it is too far below the others)
-          float y0 = p[e] == 0.f ? 0.f : p[e] * vs[e], y1 = p[e + 1] == 0.f ? 0.f : p[e + 1] * vs[e + 1];
+          // (a scale may be no number: it concerns the rows that see the key, those too whose weight for it is 0)
+          float y0 = sees(e) ? p[e] * vs[e] : 0.f, y1 = sees(e + 1) ? p[e + 1] * vs[e + 1] : 0.f;
 #pragma unroll
           for (int part = 0; part < 3; ++part) {
             w[cb][part][e >> 1] = high_halves(y1, y0);
