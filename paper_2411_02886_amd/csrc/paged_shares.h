@@ -61,7 +61,7 @@ __device__ __forceinline__ SeqShape seq_shape(const PagedAttnArgs& a, const Shar
 // room of a sequence's first r tiles (tree: the mask among the new tokens may let every row see all of them)
 __device__ __forceinline__ double tiles_room(const PagedAttnArgs& a, const ShareArgs& sh, const SeqShape& s, int tiles, bool tree) {
   const double r = tiles;
-  if (tree) return r * ((double)(a.window > 0 ? min(s.N, a.window + s.n) : s.N) + sh.tile_cost);
+  if (tree) return r * ((a.window > 0 ? fmin((double)s.N, (double)a.window + s.n) : (double)s.N) + sh.tile_cost);   // (window and new tokens together may pass an int)
   const double first = max(s.N - s.n, 0) + sh.tile_cost, tpt = sh.tpt;
   if (a.window == 0) return fma(r, first, tpt * (r * (r + 1.) * 0.5));
   const double cap = (double)a.window + tpt + sh.tile_cost;                     // where the window cuts a tile's keys
@@ -290,7 +290,7 @@ __device__ __forceinline__ int tree_low(const PagedAttnArgs& a, int row, int n, 
   const uint32_t* words = a.mask + (size_t)row * a.mask_words;
   int seen = 0;
   for (int w = 0; w < a.mask_words && w * 32 < n; ++w) seen += __builtin_popcount(n - w * 32 < 32 ? words[w] & ((1u << (n - w * 32)) - 1u) : words[w]);
-  return max(base + seen - a.window, 0);
+  return (int)max((long)base + seen - a.window, 0l);
 }
 
 // which piece a workgroup stands for: those of an XCD (workgroup L runs on XCD L % 8) follow each other
