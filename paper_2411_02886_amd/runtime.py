@@ -25,10 +25,19 @@ def to_host(t: torch.Tensor, bits16: bool = False) -> np.ndarray:
     return a.view(np.uint16) if bits16 else a
 
 
+def _pools(k_pool, v_pool, device):
+    """A layer's pools as it holds them; both None: it has none, its tokens are in a QuantCache."""
+    if (k_pool is None) != (v_pool is None):
+        raise ValueError("k_pool and v_pool: both or neither")
+    return [t if t is None or torch.is_tensor(t) else to_device(t, device) for t in (k_pool, v_pool)]
+
+
 def copy_pages(problem, copies, num_pages, device=None, cache=None):
     """Makes the page copies [(src, dst)] that a PagePool asks for, in the pools of `problem` or in a QuantCache (one call per layer).  The lists of several of its methods
     may be joined: what an earlier pair concerns is copied before a later one reads or overwrites it.  device: where the list goes; the pools' by default."""
     if copies:
+        if cache is None and problem._keep[0] is None:
+            raise ValueError("copy_pages: the problem has no pools, and no cache is given")
         if device is None:
             device = (problem if cache is None else cache)._keep[0].device
         pairs = torch.tensor(copies, dtype=torch.int32, device=device).t().contiguous()
@@ -41,7 +50,12 @@ def copy_pages(problem, copies, num_pages, device=None, cache=None):
 
 class _NewTokens:
     """The calls on new tokens that both layers have.  seq_lens count them; they are rows [B * C] without q_indptr, any
-    number per sequence with it.  cache: a QuantCache that the layer's page table leads into, in place of its pools."""
+    number per sequence with it.  cache: a QuantCache that the layer's page table leads into, in place of its pools: a layer
+    all of whose calls get one is made with k_pool=None, v_pool=None, and what reads or writes pools raises ValueError there."""
+
+    def _need_pools(self, call):
+        if self.k_pool is None:
+            raise ValueError("%s: the layer has no pools" % call)
 
     def append(self, k, v, q=None, q_out=None, rope=None, positions=None, q_indptr=None, cache=None):
         """Writes the new tokens' K and V rows into their pages, keys turned by `rope`, and the turned queries into q_out (either
@@ -49,6 +63,8 @@ class _NewTokens:
         q, k, v = (t.flatten(0, 1) if t is not None and t.dim() == 4 else t for t in (q, k, v))
         rows = (q if k is None else k).shape[0]
         if cache is None:
+            if k is not None:
+                self._need_pools("append without a cache")
             ts.ts_rope_append(self.problem, rope, q, k, v, q_indptr, rows, positions, q_out)
         else:
             ts.ts_quant_append(self.problem, cache, rope, q, k, v, q_indptr, rows, positions, q_out)
@@ -64,6 +80,8 @@ class _NewTokens:
     def keep(self, path, count, to_lens, q_indptr=None, cache=None):
         """Closes up the rows of the accepted paths: path [B][..], count [B]; to_lens [B] gets the new lengths, which the caller copies to seq_lens
         when every layer is done."""
+        if cache is None:
+            self._need_pools("keep without a cache")
         ts.ts_tree_keep(self.problem, cache, path, path.shape[-1], count, q_indptr, to_lens)
 
     def _rows(self, t, q_indptr):
@@ -91,6 +109,8 @@ class _NewTokens:
         mask: which new tokens a row sees (tree_mask), instead of those before it."""
         if round_weights and (mask is not None or cache is not None):
             raise ValueError("round_weights: not with a mask or an 8-bit cache")
+        if cache is None:
+            self._need_pools("attend_all without a cache")
         sm = sm_scale if sm_scale is not None else 1.0 / float(np.sqrt(self.D))
         rows = self._rows(q, q_indptr)
         if q_indptr is None:
@@ -100,7 +120,7 @@ class _NewTokens:
         if ws is None:
             kept, key = self.__dict__.setdefault("_all_ws", {}), (ts._current_stream(), nbytes)
             if key not in kept:                   # (none is ever replaced: a graph may hold it)
-                kept[key] = torch.empty((nbytes + 255) // 256 * 64, dtype=torch.int32, device=self.k_pool.device)
+                kept[key] = torch.empty((nbytes + 255) // 256 * 64, dtype=torch.int32, device=self.seq_lens.device)
             ws = kept[key]
         if cache is not None:
             ts.ts_quant_attn(problem, cache, q, q_indptr, rows, window, mask, sm, out, lse, ws)
@@ -111,7 +131,8 @@ class _NewTokens:
 
 
 class DecodeLayer(_NewTokens):
-    """Paged KV pool of B sequences on the GPU plus every buffer the decode step needs."""
+    """Paged KV pool of B sequences on the GPU plus every buffer the decode step needs.  k_pool, v_pool None: the sequences' tokens are in
+    8-bit caches, which the calls on new tokens are given; nothing is selected."""
 
     def __init__(self, *, dtype, H, H_kv, D, P, k, k_pool, v_pool, page_indptr, page_indices, seq_lens,
                  max_seq_len=None, device="cuda:0", num_initial=0, num_local=0):
@@ -119,8 +140,7 @@ class DecodeLayer(_NewTokens):
         self.dtype, self.H, self.H_kv, self.D, self.P, self.k = dtype, H, H_kv, D, P, k
         self.num_initial, self.num_local = int(num_initial), int(num_local)   # forced tokens (Sec. 6.1)
         self.B = int(len(seq_lens))
-        self.k_pool = k_pool if torch.is_tensor(k_pool) else to_device(k_pool, device)
-        self.v_pool = v_pool if torch.is_tensor(v_pool) else to_device(v_pool, device)
+        self.k_pool, self.v_pool = _pools(k_pool, v_pool, device)
         self.page_indptr = to_device(np.asarray(page_indptr, dtype=np.int32), device)
         self.page_indices = to_device(np.asarray(page_indices, dtype=np.int32), device)
         self.seq_lens = to_device(np.asarray(seq_lens, dtype=np.int32), device)
@@ -160,7 +180,7 @@ class DecodeLayer(_NewTokens):
 
     def swap_pool(self, k_pool: torch.Tensor, v_pool: torch.Tensor, page_indices: torch.Tensor = None):
         """Points the layer at another resident pool of the same shape (benchmark cache rotation)."""
-        self.k_pool, self.v_pool = k_pool, v_pool
+        self.k_pool, self.v_pool = _pools(k_pool, v_pool, self.device)
         if page_indices is not None:
             self.page_indices = page_indices
         self._make_problem()
@@ -178,6 +198,7 @@ class DecodeLayer(_NewTokens):
         check_theta: run Algorithm 1's test inside the score launch (skip is then self.reuse).
         ranked_vote (Eq. 5 only): the vote launch also builds the first histogram of the TopK
         (ts_soft_vote_ranked + TS_TOPK_VOTE_HIST)."""
+        self._need_pools("select")
         if check_theta is not None:
             ts.ts_paged_qk_scores_checked(self.problem, q, self.cached_q, self.cached_q_next, self.first, self.first_next,
                                           self.reuse, check_theta, self.scores, score_scale, self.ws)
@@ -205,6 +226,7 @@ class DecodeLayer(_NewTokens):
     def select_compact(self, q, score_scale=1.0, skip=None, check_theta=None, lower_bounds=True):
         """Eq. 5 selection without the score matrix in memory: one byte per score, vote bounds, exact votes of
         the candidates.  Same idx / count as select(kind="soft")."""
+        self._need_pools("select_compact")
         if getattr(self, "codes", None) is None:
             B, M = self.B, self.max_seq_len
             self.codes = torch.empty((B, M, self.H), dtype=torch.uint8, device=self.device)
@@ -225,11 +247,13 @@ class DecodeLayer(_NewTokens):
                          self.ws, sel_votes=getattr(self, "sel_votes", None))
 
     def attend(self, q, sm_scale):
+        self._need_pools("attend")
         ts.ts_sparse_paged_attn(self.problem, q, self.idx, self.k, self.count, sm_scale, self.out, self.lse, self.ws)
 
     def compact(self, to_indptr, to_indices, to_lens, skip=None):
         """Copies what attend() reads of every sequence (initial block, selection, recent block) densely into other pages;
         to_lens gets the new lengths (not self.seq_lens: copy them there afterwards).  Attending all of the new pages then gives what attend() gives."""
+        self._need_pools("compact")
         ts.ts_cache_compact(self.problem, self.idx, self.k, self.count, skip, to_indptr, to_indices, to_lens)
 
     def compact_form_pays(self) -> bool:
@@ -252,6 +276,7 @@ class DecodeLayer(_NewTokens):
         attention.  No host synchronisation.  compact: the form of the selection (None = by the size of the score
         matrices, see compact_form_pays).  fused_check: the check runs inside the score launch (one launch
         less; self.cached_q / self.first are swapped with their second copies after the step)."""
+        self._need_pools("step")
         sm = sm_scale if sm_scale is not None else 1.0 / float(np.sqrt(self.D))
         if compact is None:
             compact = self.compact_form_pays()
@@ -271,15 +296,14 @@ class DecodeLayer(_NewTokens):
 
 class ChunkSelector(_NewTokens):
     """Chunked-prefill selection for one layer: the C queries of a chunk are the last C tokens of
-    their sequences; two MFMA sweeps give the votes, ts_topk the shared index set."""
+    their sequences; two MFMA sweeps give the votes, ts_topk the shared index set.  Without pools as DecodeLayer."""
 
     def __init__(self, *, C, H, H_kv, D, P, k, k_pool, v_pool, page_indptr, page_indices, seq_lens, max_seq_len=None,
                  device="cuda:0", num_initial=0, num_local=0):
         self.C, self.H, self.H_kv, self.D, self.P, self.k = C, H, H_kv, D, P, k
         self.num_initial, self.num_local = int(num_initial), int(num_local)   # forced cached tokens (Sec. 6.1)
         self.B = int(len(seq_lens))
-        self.k_pool = k_pool if torch.is_tensor(k_pool) else to_device(k_pool, device)
-        self.v_pool = v_pool if torch.is_tensor(v_pool) else to_device(v_pool, device)
+        self.k_pool, self.v_pool = _pools(k_pool, v_pool, device)
         self.page_indptr = to_device(np.asarray(page_indptr, dtype=np.int32), device)
         self.page_indices = to_device(np.asarray(page_indices, dtype=np.int32), device)
         self.seq_lens = to_device(np.asarray(seq_lens, dtype=np.int32), device)
@@ -306,18 +330,20 @@ class ChunkSelector(_NewTokens):
                    num_initial=num_initial, num_local=num_local)
 
     def select(self, q, score_scale=1.0):
+        self._need_pools("select")
         ts.ts_chunk_row_stats(self.problem, q, score_scale, self.row_stats, self.ws)
         ts.ts_chunk_soft_vote(self.problem, q, self.row_stats, score_scale, self.votes, self.ws)
         ts.ts_topk(self.problem, self.votes, self.k, self.idx, self.count, None, self.ws)
 
     def attend(self, q, sm_scale=None):
+        self._need_pools("attend")
         sm = sm_scale if sm_scale is not None else 1.0 / float(np.sqrt(self.D))
         ts.ts_sparse_paged_attn(self.problem, q, self.idx, self.k, self.count, sm, self.out, self.lse, self.ws)
 
     # ---- Sec. 5.2 as printed: one selection per chunk with the mean query, through the decode calls
     def _mean_query_state(self):
         if getattr(self, "_mq", None) is None:
-            dev = self.k_pool.device
+            dev = self.seq_lens.device
             B, M = self.B, self.max_seq_len
             cached = torch.clamp(self.seq_lens - self.C, min=0).to(torch.int32)
             prob = ts.Problem(batch=B, chunk=1, num_q_heads=self.H, num_kv_heads=self.H_kv, head_dim=self.D,
@@ -336,6 +362,7 @@ class ChunkSelector(_NewTokens):
     def select_mean_query(self, q, score_scale=1.0):
         """Mean of the chunk's queries -> decode score pass, soft vote and top-k over the cached tokens.
         Fills self.votes / self.idx / self.count like select()."""
+        self._need_pools("select_mean_query")
         m = self._mean_query_state()
         ts.ts_chunk_mean_query(self.problem, q, m["q_mean"])
         ts.ts_paged_qk_scores(m["problem"], m["q_mean"], m["scores"], score_scale, None, m["ws"])
