@@ -434,8 +434,8 @@ int32_t ts_quant_pages_copy(const ts_problem* p, const ts_quant* c, const int32_
 
 /* The mask of trees.  parents [device] int32 [num_rows]: for new token c of a sequence the new token that it follows, in [0, c); anything else makes it a root.
  *   mask[r] = the bits of c and of all that lead to it,  positions[r] = N_b - n_b + (their number) - 1
- * positions [device] int32 [num_rows] (what ts_rope_append takes), or NULL.  mask_words >= 1; bits of new tokens beyond are dropped.  Rows that belong to no sequence are left as they
- * are.  Uses batch, chunk and seq_lens of p; its pools may be NULL. */
+ * positions [device] int32 [num_rows] (what ts_rope_append takes), or NULL.  mask_words >= 1; bits of new tokens beyond are dropped.  Neither mask nor positions may
+ * overlap another array of the call.  Rows that belong to no sequence are left as they are.  Uses batch, chunk and seq_lens of p; its pools may be NULL. */
 int32_t ts_tree_mask(const ts_problem* p, const int32_t* parents, const int32_t* q_indptr, int32_t num_rows, uint32_t* mask, int32_t mask_words,
                      int32_t* positions, void* stream);
 

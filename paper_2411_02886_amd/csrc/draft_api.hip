@@ -14,9 +14,12 @@ int32_t ts_tree_mask(const ts_problem* p, const int32_t* parents, const int32_t*
   if (num_rows == 0) return TS_OK;
   if (parents == nullptr || mask == nullptr) return TS_ERR_INVALID_ARG;
   const size_t rows = (size_t)num_rows * 4, words = rows * mask_words;
-  if (overlap(mask, words, parents, rows) || overlap(mask, words, p->seq_lens, (size_t)p->batch * 4)) return TS_ERR_INVALID_ARG;
-  if (positions != nullptr && (overlap(positions, rows, parents, rows) || overlap(positions, rows, mask, words) || overlap(positions, rows, p->seq_lens, (size_t)p->batch * 4)))
-    return TS_ERR_INVALID_ARG;
+  // a sequence's workgroups write while others still read what tells them their rows
+  const size_t lens = (size_t)p->batch * 4;
+  auto taken = [&](const void* x, size_t n) {
+    return overlap(x, n, parents, rows) || overlap(x, n, p->seq_lens, lens) || (q_indptr != nullptr && overlap(x, n, q_indptr, lens + 4));
+  };
+  if (taken(mask, words) || (positions != nullptr && (taken(positions, rows) || overlap(positions, rows, mask, words)))) return TS_ERR_INVALID_ARG;
   TreeMaskArgs a{};
   a.parents = parents; a.q_indptr = q_indptr; a.seq_lens = p->seq_lens; a.mask = mask; a.positions = positions;
   a.C = p->chunk; a.T = num_rows; a.words = mask_words;
