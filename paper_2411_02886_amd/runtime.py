@@ -120,7 +120,7 @@ class _NewTokens:
         if ws is None:
             kept, key = self.__dict__.setdefault("_all_ws", {}), (ts._current_stream(), nbytes)
             if key not in kept:                   # (none is ever replaced: a graph may hold it)
-                kept[key] = torch.empty((nbytes + 255) // 256 * 64, dtype=torch.int32, device=self.seq_lens.device)
+                kept[key] = torch.empty((nbytes + 255) // 256 * 64, dtype=torch.int32, device=(self.seq_lens if self.k_pool is None else self.k_pool).device)
             ws = kept[key]
         if cache is not None:
             ts.ts_quant_attn(problem, cache, q, q_indptr, rows, window, mask, sm, out, lse, ws)
