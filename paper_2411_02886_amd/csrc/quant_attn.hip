@@ -229,19 +229,21 @@ __global__ __launch_bounds__(256, CB == 1 ? 2 : 1) void quant_attn_kernel(PagedA
       uint32_t w[CB][3][4];
 #pragma unroll
       for (int cb = 0; cb < CB; ++cb) {
-        uint32_t bits = ~0u;                                                 // the keys that the row sees
-        if (masked) {
+        float y[8], p[8], sum = 0.f, seen_vs[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { y[e] = s[cb][e >> 2][e & 3] * ks[e]; seen_vs[e] = vs[e]; }
+        if (masked) {                                                        // (a scale may be no number: it concerns the rows that see the key, those too whose weight for it is 0)
+          uint32_t bits;                                                     // the keys that the row sees
           if (tree) bits = tree_bits(a, row0 + token_of((uint32_t)(cb * 16 + col)), sq.n, base, low[cb], k0);
           else {
             const int many = min(max(place[cb] + 1 - k0, 0), 32), cut = min(max(low[cb] - k0, 0), 32);
             bits = (uint32_t)(((1ull << many) - 1ull) & ~((1ull << cut) - 1ull));
           }
           bits >>= 4 * kgrp;
-        }
-        auto sees = [&](int e) -> bool { return (bits >> (16 * (e >> 2) + (e & 3)) & 1u) != 0u; };
-        float y[8], p[8], sum = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = sees(e) ? s[cb][e >> 2][e & 3] * ks[e] : -INFINITY;
+          for (int e = 0; e < 8; ++e)
+            if ((bits >> (16 * (e >> 2) + (e & 3)) & 1u) == 0u) { y[e] = -INFINITY; seen_vs[e] = 0.f; }
+        }
         for (int tries = 0; tries < 2; ++tries) {
           sum = 0.f;
 #pragma unroll
@@ -263,8 +265,7 @@ __global__ __launch_bounds__(256, CB == 1 ? 2 : 1) void quant_attn_kernel(PagedA
         lsum[cb] += sum;
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
-          // (a scale may be no number: it concerns the rows that see the key, those too whose weight for it is 0)
-          float y0 = sees(e) ? p[e] * vs[e] : 0.f, y1 = sees(e + 1) ? p[e + 1] * vs[e + 1] : 0.f;
+          float y0 = p[e] * seen_vs[e], y1 = p[e + 1] * seen_vs[e + 1];
 #pragma unroll
           for (int part = 0; part < 3; ++part) {
             w[cb][part][e >> 1] = high_halves(y1, y0);
