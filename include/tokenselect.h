@@ -414,7 +414,8 @@ int32_t ts_quant_read(const ts_problem* p, const ts_quant* c, const int32_t* q_i
 /* ts_paged_attn over an 8-bit cache: K and V are what the codes and scales stand for.  The same rows, window, results, rows that see nothing; weights and sums in
  * float (the products of q and codes are summed before the scale is applied; bf16 calls with chunk * G > 64: a weight that multiplies V may be off by up to
  * 2^-17 of itself).  mask NULL: causal, as there; else a mask among the new tokens [num_rows][mask_words], see ts_tree_mask.
- * Codes are finite numbers, so that no key or value that a row does not see can disturb it (e4m3: the two codes of NaN, 127 and 255, do not come from ts_quant_append; where they
+ * A row that sees a key or value whose scale is NaN comes out NaN, however small its weight for it (a value's: not its lse).  Codes are finite numbers, so that no key or
+ * value that a row does not see can disturb it (e4m3: the two codes of NaN, 127 and 255, do not come from ts_quant_append; where they
  * stand in a cache, rows that share a tile with one that sees them may be NaN too).
  * ws: ts_quant_attn_workspace_bytes() bytes, 256-byte aligned, contents irrelevant on entry and exit; one for num_rows, chunk, batch and max_seq_len
  * serves every call with fewer or smaller ones and the same heads and dtype.  sm_scale finite, window >= 0. */

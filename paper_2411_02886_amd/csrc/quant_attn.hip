@@ -363,7 +363,8 @@ static int most_beside(int H_kv) { return H_kv < 4 ? H_kv : 4; }
 // Heads side by side read four times as many bytes of a token at once, one head has its keys divided among four waves.  A call with much to read for
 // every workgroup is bound by the bytes (int8, 8 KV heads of 128, one token each; side by side against one: 64 sequences of 6000 keys 147 against 165 us, 8 of up
 // to 65536 147 against 165, 32 of 8000 with D 64 45 against 51), others by the way through the keys (one of 8000 22.9 against 17.4, 8 of 4000 26.5 against
-// 20.8, 64 of 500 24.7 against 17.6, drafts of four tokens over 16 of 8000 79 against 58).
+// 20.8, 64 of 500 24.7 against 17.6, drafts of four tokens over 16 of 8000 79 against 58).  The host knows the bound, not the lengths: a bound far above them chooses heads side by side where
+// one would be quicker, at these costs.
 static int heads_beside(const PagedAttnArgs& a, int D) {
   const long keys = std::min((long)a.max_seq_len, a.window > 0 ? (long)a.window + a.C : LONG_MAX);
   return (double)a.B * keys * a.H_kv / kShareWgs >= 50. * D ? most_beside(a.H_kv) : 1;

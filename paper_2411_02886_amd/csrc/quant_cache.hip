@@ -4,7 +4,7 @@
 // Writing: up to sixteen waves take a token.  D / 8 lanes hold a row of eight elements each, so that
 // a row's largest absolute value is three or four steps of the lanes' network away.  Rows are
 // requested a turn ahead, the first before the token's place is known; cosines and sines stay in LDS (in registers they leave a SIMD four or five waves instead of seven): 16661 bf16 tokens of
-// 32/8 heads of 128, all of it turned, into e4m3 102 us instead of 116, into int8 100 instead of 106; nothing turned 78 and 76 (4.8 TB/s).  All arithmetic is in double: a
+// 32/8 heads of 128, all of it turned, into e4m3 102 us instead of 116, into int8 100 instead of 106 (97 and 89 on another card); nothing turned 78 and 76 (4.8 TB/s); fp32 153 us (4.7 TB/s).  All arithmetic is in double: a
 // turned key next to the middle of two stored values, or a quotient next to the middle of two codes, falls as the definition says.  A quotient x Q / m is
 // formed by the row's reciprocal and one correction with the exact remainder (Markstein's division): a quotient that is a double -- every tie
 // between two codes is -- comes out exactly.
@@ -182,7 +182,7 @@ __global__ __launch_bounds__(256) void quant_append_kernel(RopeAppendArgs a, Qua
 }
 
 // log2 of the waves that share a token (a row that is read): no more than have a turn.  Few tokens are bound by one turn after the other, many by what each wave does before its first one.
-// Device times of appending with 2, 4, 8 and 16 waves a token, int8 and 32/8 heads of 128: 64 tokens 8.1, 5.9, 5.2, 4.4 us; 256 8.3, 6.3, 6.1, 6.6; 512 8.8, 7.4, 8.2, 10.2; 4096 26, 29, 41, 62.  Reading
+// Times of a call in a captured graph of twenty (alone, with its start and end, a microsecond more), appending with 2, 4, 8 and 16 waves a token, int8 and 32/8 heads of 128: 64 tokens 8.1, 5.9, 5.2, 4.4 us; 256 8.3, 6.3, 6.1, 6.6; 512 8.8, 7.4, 8.2, 10.2; 4096 26, 29, 41, 62.  Reading
 // with 1, 2, 4 and 8: 64 3.6, 3.0, 2.8, 2.8; 1024 4.2, 3.7, 3.8, 5.0; 4096 7.7, 7.3, 9.5, 16.
 static int most_shared(int turns) { return turns <= 1 ? 0 : turns <= 2 ? 1 : turns <= 4 ? 2 : turns <= 8 ? 3 : 4; }
 static int append_share(const RopeAppendArgs& a) {
